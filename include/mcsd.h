@@ -23,6 +23,14 @@
  *   mcsd_kv_commit      The step after: the accepted path's keys and values join
  *                       the prefix cache, prefix_len grows, the endpoint becomes
  *                       the next root.
+ *   mcsd_tree_attn_fourbit, mcsd_kv_commit_fourbit, mcsd_kv_store_fourbit,
+ *   mcsd_kv_load_fourbit
+ *                       The same attention and commit over a paged prefix cache
+ *                       held in 4 bits, and rows into such a cache and back.
+ *   mcsd_page_assign    Block tables, slot map and free list of a paged cache,
+ *                       from the lengths the requests are to have.
+ *   mcsd_logits_rules   Penalties, biases and grammar masks on the logits of the
+ *                       candidate trees, ahead of sampling and verification.
  *
  * Conventions
  *   - Plain C, plain-old-data structs; the first field of every struct is its
@@ -102,7 +110,10 @@ enum {
     MCSD_FLAG_BAD_TREE = 64,          /* a row with children has no valid q_row entry: handled as a leaf; or the walk
                                          reached gamma_max on a row that accepted a child (tree deeper than gamma_max) */
     MCSD_FLAG_NEAR_TIE_DRAW = 128,    /* mcsd_draft_sample: u_draw within near_tie_eps of an edge of the chosen CDF interval */
-    MCSD_FLAG_CACHE_FULL = 256        /* mcsd_kv_commit: prefix_len + n_accepted > L_stride, nothing committed for this sequence */
+    MCSD_FLAG_CACHE_FULL = 256,       /* mcsd_kv_commit: prefix_len + n_accepted > L_stride, nothing committed for this sequence;
+                                         mcsd_page_assign: no pages for it, nothing assigned to this sequence */
+    MCSD_FLAG_BAD_PAGES = 512,        /* mcsd_page_assign: a negative length, or counts that do not fit the table or the pool */
+    MCSD_FLAG_SLOTS_FULL = 1024       /* mcsd_page_assign: the slot map ends before this sequence's last slot */
 };
 
 const char *mcsd_last_error(void);
@@ -389,6 +400,163 @@ int32_t mcsd_kv_commit(const mcsd_commit_desc *desc, const mcsd_commit_bufs *buf
  * MCSD_FLAG_BAD_TREE; nothing outside the pools is written. */
 int32_t mcsd_kv_commit_paged(const mcsd_commit_desc *desc, const mcsd_commit_bufs *bufs, const mcsd_paged_kv *paged,
                              void *stream);
+
+/* ---------------------------------------------------- prefix cache in 4 bits
+ * A paged prefix cache (as for mcsd_tree_attn_paged) at 4.25 bits a value: a row of d values (d a
+ * multiple of 32) is d / 32 blocks of 32 consecutive ones, each with one scale.
+ *   code   sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives
+ *   scale  one byte s, the factor 2^(s - 127); s = 255: the whole block reads as NaN
+ * A block x is held as s = 127 + e with e the smallest integer for which max|x| <= 7 2^e, within
+ * -119..125, and the codes nearest to x 2^-e (ties to the even code, magnitudes above 6 as 6).  A value is off by at most
+ * a fifth of itself, or by 2^e / 4 where that is more (7 2^e, a seventh above 6 2^e, is no farther off than others are, which
+ * is why the finer scale is taken up to there); only magnitudes above 7 2^125 saturate.  A block that holds a NaN or an
+ * infinity gets s = 255.  All of it is exact arithmetic, so that codes and scales are defined to the bit.
+ * Layout (uint8, 16-byte aligned), in tiles of 16 rows:
+ *   codes  [n_pages][H_kv][page_size / 16][d / 32][16 rows][16 bytes]   value 2i of a block in the low half of byte i
+ *   scales [n_pages][H_kv][page_size / 16][d / 32][16 rows]
+ * Pools of several layers lie back to back.  A slot is page * page_size + row in the page.  A cache that is not
+ * paged is one page per sequence.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t page_size;              /* tokens per page, multiple of 32 */
+    int32_t n_pages;                /* pages in the pools; n_pages * page_size < 2^31 */
+    int32_t max_pages_per_seq;      /* row length of block_table */
+    const int32_t *block_table;     /* [B][max_pages_per_seq] device; not read by mcsd_kv_store_fourbit / mcsd_kv_load_fourbit (may be NULL there) */
+    void *k_codes, *v_codes;
+    void *k_scales, *v_scales;
+} mcsd_fourbit_kv;
+
+/* mcsd_tree_attn over a prefix held in 4 bits: q, k_tree, v_tree and out as there, the prefix as written by the
+ * calls below; bufs->k_prefix and bufs->v_prefix are ignored.  bf16 only (MCSD_E_UNSUPPORTED otherwise),
+ * d a multiple of 32.  A lone token per sequence is a tree of one node.  Prefix keys and values enter the
+ * products exactly as what they stand for, accumulation is fp32, and the softmax weights enter PV as bf16.  Only the
+ * pages that hold rows below prefix_len[b] are read, and rows at or past it do not count, whatever
+ * they hold.  A table entry outside [0, n_pages) is a data error: its rows read as zeros.  The
+ * results do not depend on what other sequences of the batch hold beyond the rounding of a split. */
+size_t mcsd_attn_fourbit_workspace_bytes(const mcsd_attn_desc *desc);
+int32_t mcsd_tree_attn_fourbit(const mcsd_attn_desc *desc, const mcsd_attn_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream);
+
+/* mcsd_kv_commit_paged into a cache held in 4 bits: bufs->k_prefix and bufs->v_prefix are ignored, the pools of
+ * n_layers layers lie back to back, everything else (counts, flags, prefix_len, next_root) is as there.
+ * d must be a multiple of 32. */
+int32_t mcsd_kv_commit_fourbit(const mcsd_commit_desc *desc, const mcsd_commit_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream);
+
+/* Rows of tokens into the cache (a prompt's keys and values) and back (exactly what they stand for; bf16 holds every one of these values).
+ * Row t of the packed arrays goes to, or comes from, slot slot_map[t], all KV heads and layers.  A slot outside [0, n_pages * page_size) is
+ * passed over: nothing is stored, a row of the destination is left as it was.  The slots of one store have
+ * to differ from each other (two rows for one slot leave a mixture of both). */
+typedef struct {
+    uint32_t struct_size;
+    int32_t T;              /* tokens, >= 0 */
+    int32_t H_kv;
+    int32_t d;              /* multiple of 32, <= MCSD_MAX_HEAD_DIM */
+    int32_t dtype;          /* MCSD_DTYPE_* of k and v */
+    int32_t n_layers;       /* >= 1 */
+    int64_t k_stride, v_stride;               /* elements from a token's row [H_kv][d] to the next one's, >= H_kv * d; times the element size a multiple of 16 bytes */
+    int64_t k_layer_stride, v_layer_stride;   /* elements from one layer's rows to the next one's (not used with one layer) */
+} mcsd_rows_desc;
+
+typedef struct {
+    uint32_t struct_size;
+    void *k, *v;                    /* [n_layers][T][H_kv][d] with the strides above, 16-byte aligned: read by the store, written by the load */
+    const int32_t *slot_map;        /* [T] */
+} mcsd_rows_bufs;
+
+int32_t mcsd_kv_store_fourbit(const mcsd_rows_desc *desc, const mcsd_rows_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream);
+int32_t mcsd_kv_load_fourbit(const mcsd_rows_desc *desc, const mcsd_rows_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream);
+
+/* ------------------------------------------------------- pages from lengths
+ * mcsd_page_assign brings the block table of every sequence to the pages that want_len[b] tokens
+ * need, ceil(want_len[b] / page_size), on the device.  The pool's free pages are a stack:
+ * free_pages[0 .. n_free-1], taken from the top.
+ *   1. Pages that a sequence holds beyond its need go back (want_len = 0 gives all of them back), and their
+ *      table entries become -1.  They are stacked so that the first page given back by the first such sequence is on top:
+ *      giving back what one call has assigned restores the stack.
+ *   2. Then the sequences take the pages that they lack, in order of b.  A sequence is served if
+ *      what it and all sequences before it lack is there; otherwise (MCSD_FLAG_CACHE_FULL, also where
+ *      want_len needs more than max_pages_per_seq pages) it keeps what it holds and gets no slots.  A sequence that does not
+ *      fit its table does not count for those behind it.
+ *   3. slot_map lists the slots (page * page_size + row) of the new tokens, positions
+ *      prefix_len[b] .. want_len[b]-1 of every sequence that was served, one sequence behind the other:
+ *      those of b at slot_start[b] .. slot_start[b+1]-1.  Entries behind the last one are -1, so that a
+ *      captured mcsd_kv_store_fourbit over max_slots rows stores the new rows alone.  Where max_slots is too few the
+ *      map ends there and slot_start with it (MCSD_FLAG_SLOTS_FULL for the sequences that lose slots).
+ * Page ids are moved, never followed; a table entry outside [0, n_pages) gives the slot -1.  Data errors (MCSD_FLAG_BAD_PAGES): a
+ * sequence with a negative length or n_held outside [0, max_pages_per_seq] is left alone and gets no slots; n_free is
+ * taken within [0, n_pages], and a page that would be pushed past n_pages is lost and flags its sequence.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t B;                      /* sequences */
+    int32_t page_size;              /* tokens per page, >= 1 */
+    int32_t n_pages;                /* pages in the pool, n_pages * page_size < 2^31 */
+    int32_t max_pages_per_seq;      /* row length of block_table */
+    int32_t max_slots;              /* length of slot_map (0 with slot_map = NULL) */
+} mcsd_page_desc;
+
+typedef struct {
+    uint32_t struct_size;
+    const int32_t *prefix_len;      /* [B] tokens in the cache */
+    const int32_t *want_len;        /* [B] tokens there is to be room for */
+    int32_t *n_held;                /* [B] in/out: pages assigned */
+    int32_t *block_table;           /* [B][max_pages_per_seq] in/out */
+    int32_t *free_pages;            /* [n_pages] in/out; entries at and above n_free mean nothing */
+    int32_t *n_free;                /* [1] in/out */
+    int32_t *slot_start;            /* [B+1] out; NULL exactly when slot_map is */
+    int32_t *slot_map;              /* [max_slots] out, nullable */
+    uint32_t *flags;                /* [B] out */
+} mcsd_page_bufs;
+
+int32_t mcsd_page_assign(const mcsd_page_desc *desc, const mcsd_page_bufs *bufs, void *stream);
+
+/* ------------------------------------------------------------ rules on logits
+ * What a request asks of its next token besides the temperature, applied to the logit rows of its
+ * candidate tree before they are sampled from (mcsd_draft_sample) or verified (mcsd_verify_sample).  The row of tree row r
+ * (0 = root, 1 + i = node i) of sequence b continues the tokens
+ *   history[b][0 .. hist_len[b]-1], then cand_tok[b] of the node's ancestors and of the node itself,
+ * of which the first prompt_len[b] are the prompt.  With count(x) = how often x stands behind the
+ * prompt, seen(x) = x stands anywhere, and per sequence a repetition penalty R > 0, a presence
+ * penalty P and a frequency penalty F:
+ *   z(x) = logits;   if seen(x): z > 0 ? z / R : z R;   z -= F count(x) + P [count(x) > 0];
+ *   z += bias(x)  (of several entries of the list for one token the last one counts);   mask bit 0: z = -infinity
+ * out is fp32, whatever the logits are; with fp32 logits it may be the logits themselves (in place: what no rule touches
+ * is then neither read nor written).  Token ids outside [0, V) are passed over.  A row whose mask
+ * leaves nothing becomes -infinity throughout (mcsd_verify_sample flags such a row MCSD_FLAG_NONFINITE).
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t B;
+    int32_t N;              /* tree nodes per sequence, 0..MCSD_MAX_NODES (0: the root's row alone) */
+    int32_t V;              /* vocabulary, >= 1 */
+    int32_t R;              /* logit rows per sequence */
+    int32_t dtype;          /* MCSD_DTYPE_* of logits */
+    int32_t parent_per_seq; /* 0: one tree for the batch; 1: parent[B][N], row_map[B][1+N] */
+    int32_t row_begin, row_end; /* tree rows dealt with, 0 <= row_begin <= row_end <= 1 + N (a level of the tree, say) */
+    int32_t hist_stride;    /* row length of history */
+    int32_t n_bias;         /* row length of bias_tok and bias_val */
+} mcsd_logits_desc;
+
+typedef struct {
+    uint32_t struct_size;
+    const void *logits;             /* [B][R][V] */
+    float *out;                     /* [B][R][V] */
+    const int32_t *row_map;         /* [1+N] or [B][1+N]: logit row of every tree row, no row twice, outside [0, R) = none (q_row of the
+                                       draft logits); NULL: tree row r is row r, R = 1 + N */
+    const int32_t *parent;          /* [N] or [B][N]; may be NULL with N = 0 */
+    const int32_t *cand_tok;        /* [B][N]; may be NULL with N = 0 */
+    const int32_t *history;         /* [B][hist_stride], NULL with hist_stride = 0 */
+    const int32_t *hist_len;        /* [B] (taken within [0, hist_stride]), NULL with hist_stride = 0 */
+    const int32_t *prompt_len;      /* [B], nullable (0) */
+    const float *repetition;        /* [B], nullable (1) */
+    const float *presence;          /* [B], nullable (0) */
+    const float *frequency;         /* [B], nullable (0) */
+    const int32_t *bias_tok;        /* [B][n_bias], ids outside [0, V) = no entry; NULL with n_bias = 0 */
+    const float *bias_val;          /* [B][n_bias] */
+    const uint32_t *mask;           /* [B][R][ceil(V / 32)], nullable: bit x % 32 of word x / 32 set = token x is allowed */
+} mcsd_logits_bufs;
+
+int32_t mcsd_logits_rules(const mcsd_logits_desc *desc, const mcsd_logits_bufs *bufs, void *stream);
 
 /* ------------------------------------------------------------ profiling aid
  * Not part of the verification step.  mcsd_kernel_timing(1) makes every kernel launch of the

@@ -23,10 +23,13 @@ MAX_NODES, MAX_VOCAB = 128, 65536
 
 FLAG_NEAR_TIE_ACCEPT, FLAG_NEAR_TIE_ENDPOINT, FLAG_BAD_TOKEN = 1, 2, 4
 FLAG_ZERO_DRAFT_PROB, FLAG_ZERO_RESIDUAL, FLAG_NONFINITE, FLAG_BAD_TREE = 8, 16, 32, 64
+FLAG_CACHE_FULL, FLAG_BAD_PAGES, FLAG_SLOTS_FULL = 256, 512, 1024
 
 EXPORTS = ["mcsd_last_error", "mcsd_version", "mcsd_tree_validate", "mcsd_attn_workspace_bytes",
            "mcsd_tree_attn", "mcsd_tree_attn_static", "mcsd_attn_plan_override", "mcsd_tree_attn_paged", "mcsd_verify_workspace_bytes", "mcsd_verify_sample", "mcsd_verify_step",
            "mcsd_draft_sample", "mcsd_tree_size", "mcsd_tree_build", "mcsd_kv_commit", "mcsd_kv_commit_paged",
+           "mcsd_tree_attn_fourbit", "mcsd_attn_fourbit_workspace_bytes", "mcsd_kv_commit_fourbit",
+           "mcsd_kv_store_fourbit", "mcsd_kv_load_fourbit", "mcsd_page_assign", "mcsd_logits_rules",
            "mcsd_kernel_timing", "mcsd_kernel_count", "mcsd_kernel_name", "mcsd_kernel_timing_read"]
 
 
@@ -90,6 +93,43 @@ class CommitBufs(C.Structure):
         "prefix_len", "next_root", "flags")]
 
 
+class FourbitKV(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("page_size", C.c_int32), ("n_pages", C.c_int32),
+                ("max_pages_per_seq", C.c_int32)] + [(n, C.c_void_p) for n in (
+                    "block_table", "k_codes", "v_codes", "k_scales", "v_scales")]
+
+
+class RowsDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("T", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32),
+                ("dtype", C.c_int32), ("n_layers", C.c_int32), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("k_layer_stride", C.c_int64), ("v_layer_stride", C.c_int64)]
+
+
+class RowsBufs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("k", C.c_void_p), ("v", C.c_void_p), ("slot_map", C.c_void_p)]
+
+
+class PageDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("B", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32),
+                ("max_pages_per_seq", C.c_int32), ("max_slots", C.c_int32)]
+
+
+class PageBufs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_void_p) for n in (
+        "prefix_len", "want_len", "n_held", "block_table", "free_pages", "n_free", "slot_start", "slot_map", "flags")]
+
+
+class LogitsDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "B", "N", "V", "R", "dtype", "parent_per_seq", "row_begin", "row_end", "hist_stride", "n_bias")]
+
+
+class LogitsBufs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_void_p) for n in (
+        "logits", "out", "row_map", "parent", "cand_tok", "history", "hist_len", "prompt_len", "repetition",
+        "presence", "frequency", "bias_tok", "bias_val", "mask")]
+
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -133,6 +173,17 @@ def lib() -> C.CDLL:
         L.mcsd_kv_commit.restype = C.c_int32
         L.mcsd_kv_commit_paged.argtypes = [C.POINTER(CommitDesc), C.POINTER(CommitBufs), C.POINTER(PagedKV), C.c_void_p]
         L.mcsd_kv_commit_paged.restype = C.c_int32
+        L.mcsd_attn_fourbit_workspace_bytes.argtypes = [C.POINTER(AttnDesc)]
+        L.mcsd_attn_fourbit_workspace_bytes.restype = C.c_size_t
+        for name, desc, bufs, kv in (("mcsd_tree_attn_fourbit", AttnDesc, AttnBufs, FourbitKV),
+                                     ("mcsd_kv_commit_fourbit", CommitDesc, CommitBufs, FourbitKV),
+                                     ("mcsd_kv_store_fourbit", RowsDesc, RowsBufs, FourbitKV),
+                                     ("mcsd_kv_load_fourbit", RowsDesc, RowsBufs, FourbitKV),
+                                     ("mcsd_page_assign", PageDesc, PageBufs, None),
+                                     ("mcsd_logits_rules", LogitsDesc, LogitsBufs, None)):
+            f = getattr(L, name)
+            f.argtypes = [C.POINTER(t) for t in (desc, bufs, kv) if t is not None] + [C.c_void_p]
+            f.restype = C.c_int32
         L.mcsd_kernel_timing.argtypes = [C.c_int32]
         L.mcsd_kernel_timing.restype = C.c_int32
         L.mcsd_kernel_count.restype = C.c_int32
@@ -498,6 +549,270 @@ def paged_commit_args(k_pool, v_pool, block_table, k_tree, v_tree, n_accepted, a
 
 def mcsd_kv_commit_paged(args: CommitArgs, paged: PagedKV, stream=None) -> None:
     _check(lib().mcsd_kv_commit_paged(C.byref(args.desc), C.byref(args.bufs), C.byref(paged), _stream(stream)))
+
+
+# ------------------------------------------------------------ prefix cache in 4 bits
+def _dtype_of(t: torch.Tensor) -> int:
+    if t.dtype == torch.float32:
+        return DTYPE_FP32
+    if t.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    raise ValueError(f"unsupported dtype {t.dtype}")
+
+
+def _one_device(*tensors) -> int:
+    """Index of the device that all these tensors lie on."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise ValueError(f"the tensors of a call must be on one GPU, got {sorted(str(d) for d in devices)}")
+    return next(iter(devices)).index
+
+
+def _launch(f, device: int, stream, *structs) -> None:
+    """Calls f, whose tensors lie on `device`; the library enqueues on the current one."""
+    current = _current_device() if _current_device is not None else torch.cuda.current_device()
+    if current != device:
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{current}")
+    _check(f(*[C.byref(s) for s in structs], _stream(stream)))
+
+
+def fourbit_shapes(n_pages: int, H_kv: int, page_size: int, d: int, n_layers: Optional[int] = None) -> tuple:
+    """Shapes of the uint8 tensors of codes and of scales that hold n_pages pages (of n_layers layers) in 4 bits."""
+    scales = (() if n_layers is None else (n_layers,)) + (n_pages, H_kv, page_size // 16, d // 32, 16)
+    return scales + (16,), scales
+
+
+@dataclass
+class FourbitCache:
+    kv: FourbitKV
+    n_layers: int
+    H_kv: int
+    d: int
+    layered: bool     # the pools have a leading axis of layers
+    device: int
+    keep: tuple
+
+
+def fourbit_kv(k_codes, k_scales, v_codes, v_scales, block_table=None) -> FourbitCache:
+    """A paged prefix cache held in 4 bits: uint8 tensors of the shapes of fourbit_shapes (pages in units of 16 rows; a leading axis of
+    layers where they hold several) and block_table int32 [B][max_pages_per_seq] (not needed by rows in and out)."""
+    if k_codes.dim() not in (6, 7) or tuple(k_codes.shape[-2:]) != (16, 16):
+        raise ValueError("codes must be [n_pages][H_kv][page_size/16][d/32][16][16], with or without layers in front")
+    for t, shp in [(v_codes, k_codes.shape), (k_scales, k_codes.shape[:-1]), (v_scales, k_codes.shape[:-1])]:
+        if tuple(t.shape) != tuple(shp):
+            raise ValueError(f"shape mismatch: got {tuple(t.shape)}, expected {tuple(shp)}")
+    if block_table is not None and block_table.dim() != 2:
+        raise ValueError("block_table must be [B][max_pages_per_seq]")
+    layered = k_codes.dim() == 7
+    n_pages, H_kv, tiles, blocks = k_codes.shape[-6:-2]
+    u8 = torch.uint8
+    kv = FourbitKV(C.sizeof(FourbitKV), 16 * tiles, n_pages, 1 if block_table is None else block_table.shape[1],
+                   _ptr(block_table, torch.int32, "block_table"), _ptr(k_codes, u8, "k_codes"), _ptr(v_codes, u8, "v_codes"),
+                   _ptr(k_scales, u8, "k_scales"), _ptr(v_scales, u8, "v_scales"))
+    device = _one_device(k_codes, k_scales, v_codes, v_scales, block_table)
+    return FourbitCache(kv, k_codes.shape[0] if layered else 1, H_kv, 32 * blocks, layered, device,
+                        (k_codes, k_scales, v_codes, v_scales, block_table))
+
+
+@dataclass
+class FourbitAttnArgs:
+    desc: AttnDesc
+    bufs: AttnBufs
+    kv: FourbitKV
+    device: int
+    keep: tuple
+
+
+def mcsd_attn_fourbit_workspace_bytes(desc: AttnDesc) -> int:
+    return int(lib().mcsd_attn_fourbit_workspace_bytes(C.byref(desc)))
+
+
+def fourbit_attn_args(q, cache: FourbitCache, prefix_len, k_tree, v_tree, parent, out, scale, L_stride: int,
+                      workspace: Optional[torch.Tensor] = None) -> FourbitAttnArgs:
+    """Like paged_attn_args with the prefix in a FourbitCache (one layer, with a block table).  If q, out, k_tree and
+    v_tree have one row more than parent has entries, row 0 is the root."""
+    B, rows, H_q, d = q.shape
+    root_row = parent.shape[-1] == rows - 1
+    N = rows - 1 if root_row else rows
+    H_kv = cache.H_kv
+    if cache.n_layers != 1 or cache.d != d:
+        raise ValueError("the cache must hold one layer of the query's head dimension")
+    if cache.keep[4] is None or cache.keep[4].shape[0] != B:
+        raise ValueError("block_table must be [B][max_pages_per_seq]")
+    for t, shp in [(k_tree, (B, H_kv, rows, d)), (v_tree, (B, H_kv, rows, d)), (out, (B, rows, H_q, d)), (prefix_len, (B,))]:
+        if tuple(t.shape) != shp:
+            raise ValueError(f"shape mismatch: got {tuple(t.shape)}, expected {shp}")
+    if tuple(parent.shape) not in ((N,), (B, N)):
+        raise ValueError("parent must be [N] or [B][N]")
+    desc = attn_desc(B, N, H_q, H_kv, d, _dtype_of(q), L_stride, scale, parent.dim() == 2, root_row)
+    bufs = AttnBufs(C.sizeof(AttnBufs), _ptr(q, q.dtype, "q"), None, None, _ptr(prefix_len, torch.int32, "prefix_len"),
+                    _ptr(k_tree, q.dtype, "k_tree"), _ptr(v_tree, q.dtype, "v_tree"), _ptr(parent, torch.int32, "parent"),
+                    _ptr(out, q.dtype, "out"), _ptr(workspace, None, "workspace"),
+                    0 if workspace is None else workspace.numel() * workspace.element_size())
+    device = _one_device(q, cache.keep[0], prefix_len, k_tree, v_tree, parent, out, workspace)
+    return FourbitAttnArgs(desc, bufs, cache.kv, device, (q, cache, prefix_len, k_tree, v_tree, parent, out, workspace))
+
+
+def mcsd_tree_attn_fourbit(args: FourbitAttnArgs, stream=None) -> None:
+    _launch(lib().mcsd_tree_attn_fourbit, args.device, stream, args.desc, args.bufs, args.kv)
+
+
+@dataclass
+class FourbitCommitArgs:
+    desc: CommitDesc
+    bufs: CommitBufs
+    kv: FourbitKV
+    device: int
+    keep: tuple
+
+
+def fourbit_commit_args(cache: FourbitCache, k_tree, v_tree, n_accepted, accepted_path, out_tokens, prefix_len,
+                        next_root, flags, L_stride: int, root_row: bool = False) -> FourbitCommitArgs:
+    """Like paged_commit_args with the destination a FourbitCache (with a block table); k/v_tree fp32 or bf16."""
+    lead = (cache.n_layers,) if cache.layered else ()
+    B, N = k_tree.shape[-4], k_tree.shape[-2] - (1 if root_row else 0)
+    gamma_max = accepted_path.shape[1]
+    tree_shape = lead + (B, cache.H_kv, N + (1 if root_row else 0), cache.d)
+    if cache.keep[4] is None or cache.keep[4].shape[0] != B:
+        raise ValueError("block_table must be [B][max_pages_per_seq]")
+    for t, shp in [(k_tree, tree_shape), (v_tree, tree_shape), (n_accepted, (B,)), (accepted_path, (B, gamma_max)),
+                   (out_tokens, (B, gamma_max + 1)), (prefix_len, (B,)), (next_root, (B,)), (flags, (B,))]:
+        if tuple(t.shape) != shp:
+            raise ValueError(f"shape mismatch: got {tuple(t.shape)}, expected {shp}")
+    i32 = torch.int32
+    desc = CommitDesc(C.sizeof(CommitDesc), B, N, cache.H_kv, cache.d, _dtype_of(k_tree), L_stride, gamma_max, cache.n_layers,
+                      1 if root_row else 0)
+    bufs = CommitBufs(C.sizeof(CommitBufs), None, None, _ptr(k_tree, k_tree.dtype, "k_tree"), _ptr(v_tree, k_tree.dtype, "v_tree"),
+                      _ptr(n_accepted, i32, "n_accepted"), _ptr(accepted_path, i32, "accepted_path"),
+                      _ptr(out_tokens, i32, "out_tokens"), _ptr(prefix_len, i32, "prefix_len"),
+                      _ptr(next_root, i32, "next_root"), _ptr(flags, i32, "flags"))
+    keep = (cache, k_tree, v_tree, n_accepted, accepted_path, out_tokens, prefix_len, next_root, flags)
+    return FourbitCommitArgs(desc, bufs, cache.kv, _one_device(cache.keep[0], *keep[1:]), keep)
+
+
+def mcsd_kv_commit_fourbit(args: FourbitCommitArgs, stream=None) -> None:
+    _launch(lib().mcsd_kv_commit_fourbit, args.device, stream, args.desc, args.bufs, args.kv)
+
+
+@dataclass
+class RowsArgs:
+    desc: RowsDesc
+    bufs: RowsBufs
+    kv: FourbitKV
+    device: int
+    keep: tuple
+
+
+def _rows_ptr(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    H_kv, d = t.shape[-2:]
+    if t.numel() and (t.stride(-1) != 1 or (H_kv > 1 and t.stride(-2) != d)):
+        raise ValueError(f"{name}: a token's row [H_kv][d] must be contiguous")
+    return t.data_ptr()
+
+
+def fourbit_rows_args(k, v, slot_map, cache: FourbitCache) -> RowsArgs:
+    """Rows of tokens for a store into, or a load from, the cache: k, v [T][H_kv][d] ([n_layers][T][H_kv][d] where the
+    cache has layers), a token's row contiguous, any stride from row to row; slot_map int32 [T]."""
+    T = slot_map.shape[0]
+    shape = ((cache.n_layers,) if cache.layered else ()) + (T, cache.H_kv, cache.d)
+    if slot_map.dim() != 1 or tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != v.dtype:
+        raise ValueError(f"k and v must be {shape} of one dtype, slot_map [T]")
+    row = cache.H_kv * cache.d
+    stride = lambda t: t.stride(-3) if T > 1 else row
+    layer = lambda t: t.stride(0) if cache.n_layers > 1 else 0
+    desc = RowsDesc(C.sizeof(RowsDesc), T, cache.H_kv, cache.d, _dtype_of(k), cache.n_layers, stride(k), stride(v), layer(k), layer(v))
+    bufs = RowsBufs(C.sizeof(RowsBufs), _rows_ptr(k, "k"), _rows_ptr(v, "v"), _ptr(slot_map, torch.int32, "slot_map"))
+    return RowsArgs(desc, bufs, cache.kv, _one_device(k, v, slot_map, cache.keep[0]), (k, v, slot_map, cache))
+
+
+def mcsd_kv_store_fourbit(args: RowsArgs, stream=None) -> None:
+    _launch(lib().mcsd_kv_store_fourbit, args.device, stream, args.desc, args.bufs, args.kv)
+
+
+def mcsd_kv_load_fourbit(args: RowsArgs, stream=None) -> None:
+    _launch(lib().mcsd_kv_load_fourbit, args.device, stream, args.desc, args.bufs, args.kv)
+
+
+# ------------------------------------------------------------------ pages from lengths
+@dataclass
+class PageArgs:
+    desc: PageDesc
+    bufs: PageBufs
+    device: int
+    keep: tuple
+
+
+def page_args(prefix_len, want_len, n_held, block_table, free_pages, n_free, flags, page_size: int,
+              slot_start=None, slot_map=None) -> PageArgs:
+    """int32 tensors: prefix_len, want_len, n_held, flags [B]; block_table [B][max_pages_per_seq]; free_pages [n_pages];
+    n_free [1]; slot_start [B+1] and slot_map [max_slots] (both or neither)."""
+    B, width = block_table.shape
+    if (slot_start is None) != (slot_map is None):
+        raise ValueError("slot_start and slot_map come together")
+    shapes = [(t, (B,)) for t in (prefix_len, want_len, n_held, flags)] + [(n_free, (1,))]
+    if slot_map is not None:
+        shapes += [(slot_start, (B + 1,))]
+    for t, shp in shapes:
+        if tuple(t.shape) != shp:
+            raise ValueError(f"shape mismatch: got {tuple(t.shape)}, expected {shp}")
+    if free_pages.dim() != 1 or (slot_map is not None and slot_map.dim() != 1):
+        raise ValueError("free_pages and slot_map must be vectors")
+    i32 = torch.int32
+    desc = PageDesc(C.sizeof(PageDesc), B, int(page_size), free_pages.shape[0], width, 0 if slot_map is None else slot_map.shape[0])
+    keep = (prefix_len, want_len, n_held, block_table, free_pages, n_free, slot_start, slot_map, flags)
+    names = ("prefix_len", "want_len", "n_held", "block_table", "free_pages", "n_free", "slot_start", "slot_map", "flags")
+    bufs = PageBufs(C.sizeof(PageBufs), *[_ptr(t, i32, n) for t, n in zip(keep, names)])
+    return PageArgs(desc, bufs, _one_device(*keep), keep)
+
+
+def mcsd_page_assign(args: PageArgs, stream=None) -> None:
+    _launch(lib().mcsd_page_assign, args.device, stream, args.desc, args.bufs)
+
+
+# --------------------------------------------------------------------- rules on logits
+@dataclass
+class LogitsArgs:
+    desc: LogitsDesc
+    bufs: LogitsBufs
+    device: int
+    keep: tuple
+
+
+def logits_args(logits, out, parent=None, cand_tok=None, history=None, hist_len=None, prompt_len=None, repetition=None,
+                presence=None, frequency=None, bias_tok=None, bias_val=None, mask=None, row_map=None, rows=None) -> LogitsArgs:
+    """logits [B][R][V] fp32 or bf16, out [B][R][V] fp32 (the logits themselves: in place); parent int32 [N] or [B][N], cand_tok int32
+    [B][N] (neither: the root's row alone); history int32 [B][S] with hist_len, prompt_len int32 [B]; repetition, presence,
+    frequency fp32 [B]; bias_tok int32 and bias_val fp32 [B][n]; mask int32 [B][R][ceil(V/32)] (32 tokens a word);
+    row_map int32 [1+N] or [B][1+N] (as parent); rows: (begin, end) of the tree rows dealt with, all by default."""
+    B, R, V = logits.shape
+    N = 0 if parent is None else parent.shape[-1]
+    per_seq = parent is not None and parent.dim() == 2
+    if (parent is None) != (cand_tok is None) or (history is None) != (hist_len is None) or (bias_tok is None) != (bias_val is None):
+        raise ValueError("parent and cand_tok, history and hist_len, bias_tok and bias_val come together")
+    if row_map is not None and parent is None:
+        per_seq = row_map.dim() == 2
+    f32, i32 = torch.float32, torch.int32
+    S = 0 if history is None else history.shape[1]
+    n_bias = 0 if bias_tok is None else bias_tok.shape[1]
+    shapes = [(out, (B, R, V)), (parent, (B, N) if per_seq else (N,)), (cand_tok, (B, N)), (history, (B, S)),
+              (row_map, (B, 1 + N) if per_seq else (1 + N,)), (bias_tok, (B, n_bias)), (bias_val, (B, n_bias)), (mask, (B, R, (V + 31) // 32))]
+    shapes += [(t, (B,)) for t in (hist_len, prompt_len, repetition, presence, frequency)]
+    for t, shp in shapes:
+        if t is not None and tuple(t.shape) != shp:
+            raise ValueError(f"shape mismatch: got {tuple(t.shape)}, expected {shp}")
+    begin, end = (0, 1 + N) if rows is None else rows
+    desc = LogitsDesc(C.sizeof(LogitsDesc), B, N, V, R, _dtype_of(logits), 1 if per_seq else 0, int(begin), int(end), S, n_bias)
+    keep = (logits, out, row_map, parent, cand_tok, history, hist_len, prompt_len, repetition, presence, frequency, bias_tok, bias_val, mask)
+    types = (logits.dtype, f32, i32, i32, i32, i32, i32, i32, f32, f32, f32, i32, f32, i32)
+    names = [n for n, _ in LogitsBufs._fields_[1:]]
+    bufs = LogitsBufs(C.sizeof(LogitsBufs), *[None if t is None or t.numel() == 0 else _ptr(t, ty, n) for t, ty, n in zip(keep, types, names)])
+    return LogitsArgs(desc, bufs, _one_device(*keep), keep)
+
+
+def mcsd_logits_rules(args: LogitsArgs, stream=None) -> None:
+    _launch(lib().mcsd_logits_rules, args.device, stream, args.desc, args.bufs)
 
 
 # ------------------------------------------------------------------- profiling aid

@@ -1,5 +1,5 @@
 // C ABI of libmcsd: argument validation, error reporting, optional per-kernel
-// event timing.  All compute happens in tree_attn.hip, verify_sample.hip, draft_sample.hip and tree_commit.hip.
+// event timing.  All compute happens in the other .hip files.
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -32,7 +32,9 @@ std::vector<EventPair> g_pending;
 double g_total_ms[K_COUNT];
 long long g_count[K_COUNT];
 const char *const g_names[K_COUNT] = {"tree_attn_mfma", "tree_attn_generic", "tree_attn_combine",
-                                      "verify_rows", "walk", "draft_rows", "tree_build", "kv_copy", "kv_finish"};
+                                      "verify_rows", "walk", "draft_rows", "tree_build", "kv_copy", "kv_finish",
+                                      "kv_store_fourbit", "kv_load_fourbit", "attn_fourbit", "attn_fourbit_combine",
+                                      "page_assign", "page_slots", "logits_rules"};
 }  // namespace
 
 bool timing_new_events(hipEvent_t *start, hipEvent_t *stop)
@@ -320,7 +322,7 @@ int32_t mcsd_tree_build(const int32_t *kconfig, int32_t gamma, int32_t B, const 
     return launch_tree_build(kconfig, gamma, n, B, prefix_len, parent, depth, q_row, position_ids, root_row, (hipStream_t)stream);
 }
 
-static int32_t check_commit(const mcsd_commit_desc *d, const mcsd_commit_bufs *b)
+static int32_t check_commit(const mcsd_commit_desc *d, const mcsd_commit_bufs *b, bool prefix_in_bufs = true)
 {
     if (!d) { set_error("commit desc is NULL"); return MCSD_E_NULL; }
     if (d->struct_size != sizeof(mcsd_commit_desc)) { set_error("commit desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_commit_desc)); return MCSD_E_SHAPE; }
@@ -333,9 +335,10 @@ static int32_t check_commit(const mcsd_commit_desc *d, const mcsd_commit_bufs *b
     if (d->B > 65535 || d->gamma_max > 65535 || d->n_layers > 65535) { set_error("commit: grid too large"); return MCSD_E_UNSUPPORTED; }
     if (!b) { set_error("commit bufs is NULL"); return MCSD_E_NULL; }
     if (b->struct_size != sizeof(mcsd_commit_bufs)) { set_error("commit bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_commit_bufs)); return MCSD_E_SHAPE; }
-    if (!b->k_prefix || !b->v_prefix || !b->k_tree || !b->v_tree || !b->n_accepted || !b->accepted_path ||
+    if ((prefix_in_bufs && (!b->k_prefix || !b->v_prefix)) || !b->k_tree || !b->v_tree || !b->n_accepted || !b->accepted_path ||
         !b->out_tokens || !b->prefix_len || !b->next_root || !b->flags) { set_error("commit: NULL buffer"); return MCSD_E_NULL; }
-    if (((uintptr_t)b->k_prefix | (uintptr_t)b->v_prefix | (uintptr_t)b->k_tree | (uintptr_t)b->v_tree) & 15u) {
+    const uintptr_t prefix = prefix_in_bufs ? (uintptr_t)b->k_prefix | (uintptr_t)b->v_prefix : 0;
+    if ((prefix | (uintptr_t)b->k_tree | (uintptr_t)b->v_tree) & 15u) {
         set_error("commit: caches must be 16-byte aligned");
         return MCSD_E_SHAPE;
     }
@@ -360,6 +363,147 @@ int32_t mcsd_kv_commit_paged(const mcsd_commit_desc *d, const mcsd_commit_bufs *
     if (paged->n_pages < 1 || paged->max_pages_per_seq < 1) { set_error("paged: non-positive size"); return MCSD_E_SHAPE; }
     if ((long)paged->max_pages_per_seq * paged->page_size < (long)d->L_stride) { set_error("paged: L_stride %d exceeds max_pages_per_seq * page_size", d->L_stride); return MCSD_E_SHAPE; }
     return launch_kv_commit(*d, *b, (hipStream_t)stream, paged);
+}
+
+// ------------------------------------------------------------ prefix cache in 4 bits
+// L_stride >= 0: the logical capacity that the block table has to hold (rows in and out by slot have none: -1)
+static int32_t check_fourbit(const mcsd_fourbit_kv *kv, int d, long L_stride)
+{
+    if (!kv) { set_error("fourbit: cache descriptor is NULL"); return MCSD_E_NULL; }
+    if (kv->struct_size != sizeof(mcsd_fourbit_kv)) { set_error("fourbit: struct_size %u != %zu", kv->struct_size, sizeof(mcsd_fourbit_kv)); return MCSD_E_SHAPE; }
+    if (d < 32 || d % 32 != 0 || d > MCSD_MAX_HEAD_DIM) { set_error("fourbit: head dim %d is not a multiple of 32 up to %d", d, MCSD_MAX_HEAD_DIM); return MCSD_E_UNSUPPORTED; }
+    if (kv->page_size < 32 || kv->page_size % 32 != 0) { set_error("fourbit: page_size %d is not a positive multiple of 32", kv->page_size); return MCSD_E_SHAPE; }
+    if (kv->n_pages < 1 || (L_stride >= 0 && kv->max_pages_per_seq < 1)) { set_error("fourbit: non-positive size"); return MCSD_E_SHAPE; }
+    if ((long)kv->n_pages * kv->page_size > 0x7fffffffL) { set_error("fourbit: n_pages * page_size does not fit a slot"); return MCSD_E_UNSUPPORTED; }
+    if (L_stride >= 0 && (long)kv->max_pages_per_seq * kv->page_size < L_stride) { set_error("fourbit: L_stride %ld exceeds max_pages_per_seq * page_size", L_stride); return MCSD_E_SHAPE; }
+    if (!kv->k_codes || !kv->v_codes || !kv->k_scales || !kv->v_scales) { set_error("fourbit: NULL pool"); return MCSD_E_NULL; }
+    if (L_stride >= 0 && !kv->block_table) { set_error("fourbit: block_table is NULL"); return MCSD_E_NULL; }
+    if (((uintptr_t)kv->k_codes | (uintptr_t)kv->v_codes | (uintptr_t)kv->k_scales | (uintptr_t)kv->v_scales) & 15u) {
+        set_error("fourbit: pools must be 16-byte aligned");
+        return MCSD_E_SHAPE;
+    }
+    return MCSD_OK;
+}
+
+static int32_t check_attn_fourbit(const mcsd_attn_desc *d, const mcsd_attn_bufs *b, FourbitPlan *plan)
+{
+    AttnPlan unused;
+    int32_t rc = check_attn(d, nullptr, &unused);
+    if (rc != MCSD_OK) return rc;
+    if (d->dtype != MCSD_DTYPE_BF16) { set_error("attn(fourbit): bf16 queries only"); return MCSD_E_UNSUPPORTED; }
+    if (d->d % 32 != 0) { set_error("attn(fourbit): head dim %d is not a multiple of 32", d->d); return MCSD_E_UNSUPPORTED; }
+    if (d->B > 65535) { set_error("attn(fourbit): B %d > 65535", d->B); return MCSD_E_UNSUPPORTED; }
+    if (!make_fourbit_plan(*d, plan)) { set_error("attn(fourbit): no kernel for this shape"); return MCSD_E_UNSUPPORTED; }
+    if (!b) return MCSD_OK;
+    if (b->struct_size != sizeof(mcsd_attn_bufs)) { set_error("attn bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_attn_bufs)); return MCSD_E_SHAPE; }
+    if (!b->q || !b->k_tree || !b->v_tree || !b->prefix_len || !b->parent || !b->out) { set_error("attn(fourbit): NULL buffer"); return MCSD_E_NULL; }
+    if (plan->ws_bytes > 0) {
+        if (!b->workspace) { set_error("attn(fourbit): workspace is NULL, %zu bytes needed", plan->ws_bytes); return MCSD_E_WORKSPACE; }
+        if (b->workspace_bytes < plan->ws_bytes) { set_error("attn(fourbit): workspace %zu < %zu bytes", b->workspace_bytes, plan->ws_bytes); return MCSD_E_WORKSPACE; }
+        if (((uintptr_t)b->workspace & 255u) != 0) { set_error("attn(fourbit): workspace not 256-byte aligned"); return MCSD_E_WORKSPACE; }
+    }
+    if (((uintptr_t)b->q | (uintptr_t)b->k_tree | (uintptr_t)b->v_tree | (uintptr_t)b->out) & 15u) { set_error("attn(fourbit): tensors must be 16-byte aligned"); return MCSD_E_SHAPE; }
+    return MCSD_OK;
+}
+
+size_t mcsd_attn_fourbit_workspace_bytes(const mcsd_attn_desc *desc)
+{
+    FourbitPlan plan;
+    return check_attn_fourbit(desc, nullptr, &plan) == MCSD_OK ? plan.ws_bytes : 0;
+}
+
+int32_t mcsd_tree_attn_fourbit(const mcsd_attn_desc *desc, const mcsd_attn_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream)
+{
+    FourbitPlan plan;
+    if (!bufs) { set_error("attn bufs is NULL"); return MCSD_E_NULL; }
+    int32_t rc = check_attn_fourbit(desc, bufs, &plan);
+    if (rc != MCSD_OK) return rc;
+    rc = check_fourbit(kv, desc->d, desc->L_stride);
+    if (rc != MCSD_OK) return rc;
+    return launch_attn_fourbit(*desc, *bufs, *kv, plan, (hipStream_t)stream);
+}
+
+int32_t mcsd_kv_commit_fourbit(const mcsd_commit_desc *d, const mcsd_commit_bufs *b, const mcsd_fourbit_kv *kv, void *stream)
+{
+    int32_t rc = check_commit(d, b, false);
+    if (rc != MCSD_OK) return rc;
+    rc = check_fourbit(kv, d->d, d->L_stride);
+    if (rc != MCSD_OK) return rc;
+    return launch_kv_commit(*d, *b, (hipStream_t)stream, nullptr, kv);
+}
+
+static int32_t check_rows(const mcsd_rows_desc *d, const mcsd_rows_bufs *b, const mcsd_fourbit_kv *kv)
+{
+    if (!d) { set_error("rows desc is NULL"); return MCSD_E_NULL; }
+    if (d->struct_size != sizeof(mcsd_rows_desc)) { set_error("rows desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_rows_desc)); return MCSD_E_SHAPE; }
+    if (d->T < 0 || d->H_kv < 1 || d->n_layers < 1) { set_error("rows: non-positive size"); return MCSD_E_SHAPE; }
+    if (d->dtype != MCSD_DTYPE_FP32 && d->dtype != MCSD_DTYPE_BF16) { set_error("rows: unknown dtype %d", d->dtype); return MCSD_E_UNSUPPORTED; }
+    const int32_t rc = check_fourbit(kv, d->d, -1);
+    if (rc != MCSD_OK) return rc;
+    if (d->n_layers > 65535 || d->T > (1 << 30) || d->H_kv > 65535 || ((long)d->T + 3) / 4 * d->H_kv * (d->d / 32) > 0x7fffffffL * 16) { set_error("rows: grid too large"); return MCSD_E_UNSUPPORTED; }
+    const int64_t row = (int64_t)d->H_kv * d->d, per16 = d->dtype == MCSD_DTYPE_FP32 ? 4 : 8;
+    if (d->k_stride < row || d->v_stride < row) { set_error("rows: a stride is less than a row"); return MCSD_E_SHAPE; }
+    if (d->k_stride % per16 != 0 || d->v_stride % per16 != 0) { set_error("rows: strides must be multiples of 16 bytes"); return MCSD_E_SHAPE; }
+    if (d->n_layers > 1 && (d->k_layer_stride % per16 != 0 || d->v_layer_stride % per16 != 0 || d->k_layer_stride < 0 || d->v_layer_stride < 0)) {
+        set_error("rows: layer strides must be multiples of 16 bytes");
+        return MCSD_E_SHAPE;
+    }
+    if (!b) { set_error("rows bufs is NULL"); return MCSD_E_NULL; }
+    if (b->struct_size != sizeof(mcsd_rows_bufs)) { set_error("rows bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_rows_bufs)); return MCSD_E_SHAPE; }
+    if (d->T == 0) return MCSD_OK;
+    if (!b->k || !b->v || !b->slot_map) { set_error("rows: NULL buffer"); return MCSD_E_NULL; }
+    if (((uintptr_t)b->k | (uintptr_t)b->v) & 15u) { set_error("rows: k and v must be 16-byte aligned"); return MCSD_E_SHAPE; }
+    return MCSD_OK;
+}
+
+int32_t mcsd_kv_store_fourbit(const mcsd_rows_desc *d, const mcsd_rows_bufs *b, const mcsd_fourbit_kv *kv, void *stream)
+{
+    const int32_t rc = check_rows(d, b, kv);
+    return rc != MCSD_OK ? rc : launch_fourbit_rows(*d, *b, *kv, true, (hipStream_t)stream);
+}
+
+int32_t mcsd_kv_load_fourbit(const mcsd_rows_desc *d, const mcsd_rows_bufs *b, const mcsd_fourbit_kv *kv, void *stream)
+{
+    const int32_t rc = check_rows(d, b, kv);
+    return rc != MCSD_OK ? rc : launch_fourbit_rows(*d, *b, *kv, false, (hipStream_t)stream);
+}
+
+// ------------------------------------------------------- pages from lengths, rules on logits
+int32_t mcsd_page_assign(const mcsd_page_desc *d, const mcsd_page_bufs *b, void *stream)
+{
+    if (!d) { set_error("page desc is NULL"); return MCSD_E_NULL; }
+    if (d->struct_size != sizeof(mcsd_page_desc)) { set_error("page desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_page_desc)); return MCSD_E_SHAPE; }
+    if (d->B < 1 || d->page_size < 1 || d->n_pages < 1 || d->max_pages_per_seq < 1 || d->max_slots < 0) { set_error("pages: non-positive size"); return MCSD_E_SHAPE; }
+    if (d->B > 65535) { set_error("pages: B %d > 65535", d->B); return MCSD_E_UNSUPPORTED; }
+    if ((long)d->n_pages * d->page_size > 0x7fffffffL) { set_error("pages: n_pages * page_size does not fit a slot"); return MCSD_E_UNSUPPORTED; }
+    if (!b) { set_error("page bufs is NULL"); return MCSD_E_NULL; }
+    if (b->struct_size != sizeof(mcsd_page_bufs)) { set_error("page bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_page_bufs)); return MCSD_E_SHAPE; }
+    if (!b->prefix_len || !b->want_len || !b->n_held || !b->block_table || !b->free_pages || !b->n_free || !b->flags) { set_error("pages: NULL buffer"); return MCSD_E_NULL; }
+    if (!b->slot_map != !b->slot_start) { set_error("pages: slot_map and slot_start come together"); return MCSD_E_NULL; }
+    if (!b->slot_map && d->max_slots > 0) { set_error("pages: max_slots without a slot_map"); return MCSD_E_NULL; }
+    return launch_page_assign(*d, *b, (hipStream_t)stream);
+}
+
+int32_t mcsd_logits_rules(const mcsd_logits_desc *d, const mcsd_logits_bufs *b, void *stream)
+{
+    if (!d) { set_error("logits desc is NULL"); return MCSD_E_NULL; }
+    if (d->struct_size != sizeof(mcsd_logits_desc)) { set_error("logits desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_logits_desc)); return MCSD_E_SHAPE; }
+    if (d->B < 1 || d->V < 1 || d->R < 1 || d->hist_stride < 0 || d->n_bias < 0) { set_error("logits: non-positive size"); return MCSD_E_SHAPE; }
+    if (d->N < 0 || d->N > MCSD_MAX_NODES) { set_error("logits: N %d outside 0..%d", d->N, MCSD_MAX_NODES); return MCSD_E_TREE; }
+    if (d->B > 65535 || d->V > (1 << 30)) { set_error("logits: B %d > 65535 or V %d > %d", d->B, d->V, 1 << 30); return MCSD_E_UNSUPPORTED; }
+    if (d->dtype != MCSD_DTYPE_FP32 && d->dtype != MCSD_DTYPE_BF16) { set_error("logits: unknown dtype %d", d->dtype); return MCSD_E_UNSUPPORTED; }
+    if (d->parent_per_seq != 0 && d->parent_per_seq != 1) { set_error("logits: parent_per_seq must be 0 or 1"); return MCSD_E_SHAPE; }
+    if (d->row_begin < 0 || d->row_begin > d->row_end || d->row_end > 1 + d->N) { set_error("logits: rows %d..%d outside the tree's 0..%d", d->row_begin, d->row_end, 1 + d->N); return MCSD_E_SHAPE; }
+    if (!b) { set_error("logits bufs is NULL"); return MCSD_E_NULL; }
+    if (b->struct_size != sizeof(mcsd_logits_bufs)) { set_error("logits bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_logits_bufs)); return MCSD_E_SHAPE; }
+    if (!b->logits || !b->out || (d->N > 0 && (!b->parent || !b->cand_tok)) || (d->hist_stride > 0 && (!b->history || !b->hist_len)) ||
+        (d->n_bias > 0 && (!b->bias_tok || !b->bias_val))) { set_error("logits: NULL buffer"); return MCSD_E_NULL; }
+    if (!b->row_map && d->R != 1 + d->N) { set_error("logits: R %d != 1 + N without a row_map", d->R); return MCSD_E_SHAPE; }
+    const uintptr_t esize = d->dtype == MCSD_DTYPE_FP32 ? 4 : 2, in = (uintptr_t)b->logits, out = (uintptr_t)b->out;
+    if (in % esize != 0 || out % 4 != 0) { set_error("logits: misaligned"); return MCSD_E_SHAPE; }
+    const uintptr_t n = (uintptr_t)d->B * d->R * d->V;
+    if (in < out + 4 * n && out < in + esize * n && !(in == out && esize == 4)) { set_error("logits: out overlaps the logits without being them"); return MCSD_E_SHAPE; }
+    return launch_logits_rules(*d, *b, (hipStream_t)stream);
 }
 
 int32_t mcsd_verify_step(const mcsd_attn_desc *ad, const mcsd_attn_bufs *ab, const mcsd_verify_desc *vd,

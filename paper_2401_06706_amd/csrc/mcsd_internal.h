@@ -10,7 +10,8 @@
 namespace mcsd {
 
 // Kernel ids for the optional per-kernel event timing.
-enum KernelId { K_ATTN_MFMA = 0, K_ATTN_GENERIC = 1, K_ATTN_COMBINE = 2, K_VERIFY_ROWS = 3, K_WALK = 4, K_DRAFT_ROWS = 5, K_TREE_BUILD = 6, K_KV_COPY = 7, K_KV_FINISH = 8, K_COUNT = 9 };
+enum KernelId { K_ATTN_MFMA = 0, K_ATTN_GENERIC = 1, K_ATTN_COMBINE = 2, K_VERIFY_ROWS = 3, K_WALK = 4, K_DRAFT_ROWS = 5, K_TREE_BUILD = 6, K_KV_COPY = 7, K_KV_FINISH = 8, K_KV_STORE = 9, K_KV_LOAD = 10,
+                K_ATTN_FOURBIT = 11, K_ATTN_FOURBIT_COMBINE = 12, K_PAGE_ASSIGN = 13, K_PAGE_SLOTS = 14, K_LOGITS_RULES = 15, K_COUNT = 16 };
 
 void set_error(const char *fmt, ...);
 
@@ -123,6 +124,22 @@ constexpr int MAX_GAMMA = 16;
 int32_t launch_tree_build(const int32_t *kconfig, int gamma, int n_nodes, int B, const int32_t *prefix_len,
                           int32_t *parent, int32_t *depth, int32_t *q_row, int32_t *position_ids, int root_row, hipStream_t stream);
 int32_t launch_kv_commit(const mcsd_commit_desc &d, const mcsd_commit_bufs &b, hipStream_t stream,
-                         const mcsd_paged_kv *paged = nullptr);
+                         const mcsd_paged_kv *paged = nullptr, const mcsd_fourbit_kv *fourbit = nullptr);
+
+// ---- prefix cache in 4 bits -------------------------------------------------
+struct FourbitPlan {
+    int rows_per_kv;      // query rows that share one KV head
+    int variant;          // instantiation of the attention kernel
+    int n_row_tiles, row_tile;
+    int n_segments_max;   // grid extent along the keys
+    size_t ws_bytes;
+};
+bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan);
+int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, const mcsd_fourbit_kv &kv, const FourbitPlan &plan, hipStream_t stream);
+int32_t launch_fourbit_rows(const mcsd_rows_desc &d, const mcsd_rows_bufs &b, const mcsd_fourbit_kv &kv, bool store, hipStream_t stream);
+
+// ---- pages from lengths, rules on logits ------------------------------------
+int32_t launch_page_assign(const mcsd_page_desc &d, const mcsd_page_bufs &b, hipStream_t stream);
+int32_t launch_logits_rules(const mcsd_logits_desc &d, const mcsd_logits_bufs &b, hipStream_t stream);
 
 }  // namespace mcsd

@@ -1,7 +1,7 @@
 // Bookkeeping around the verification step, on the device: the candidate tree of a
 // k-configuration (Sec. 3 / Sec. 4.3, generation order of Sec. 3.3) and the commit of the
 // accepted path's keys and values to the prefix cache (Sec. 3.3).  Latency-sized kernels.
-#include "mcsd_internal.h"
+#include "fourbit.h"
 
 namespace mcsd {
 namespace {
@@ -69,6 +69,9 @@ struct CommitParams {
     // paged destination (block_table != nullptr): pools [n_layers][n_pages][H_kv][page_size][d]
     const int32_t *block_table;
     int page_size, n_pages, max_pages;
+    // a paged destination in 4 bits (mcsd.h): the pools instead of k_prefix and v_prefix
+    uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
+    int n_blocks, is_f32;
 };
 
 // What sequence b commits, found by one wavefront: every lane looks at one row, so that the path and
@@ -235,6 +238,61 @@ __global__ __launch_bounds__(64 * COMMIT_WAVES) void kv_commit_kernel(CommitPara
     }
 }
 
+// The same two forms of the commit into a cache held in 4 bits.  A row (all KV heads, K and V) in units of eight
+// values, four neighbouring threads a block; `first` and `step` are multiples of four apart from the unit's quarter.
+__device__ __forceinline__ void commit_row_fourbit(const CommitParams &p, int layer, int b, int src_row, int page, int page_row, int first, int step)
+{
+    const int per_side = p.H_kv * p.n_blocks * 4;
+    const size_t lb = (size_t)layer * p.B + b;
+    for (int e = first; e < 2 * per_side; e += step) {
+        const bool is_v = e >= per_side;
+        const int u = is_v ? e - per_side : e, quarter = u & 3, hb = u >> 2, g = hb / p.n_blocks, blk = hb % p.n_blocks;
+        const size_t src = ((lb * p.H_kv + g) * (size_t)(p.N + p.root_row) + src_row) * p.row_bytes + (size_t)(blk * FB_BLOCK + 8 * quarter) * (p.is_f32 ? 4 : 2);
+        float x[8];
+        load8((is_v ? p.v_tree : p.k_tree) + src, p.is_f32, x);
+        const uint32_t s = fourbit_scale_byte(fourbit_amax_bits(x));
+        const size_t block = fourbit_block((((size_t)layer * p.n_pages + page) * p.H_kv + g) * p.page_size + page_row, p.n_blocks, blk);
+        reinterpret_cast<uint32_t *>(is_v ? p.v_codes : p.k_codes)[block * 4 + quarter] = fourbit_encode8(x, s);
+        if (quarter == 0) (is_v ? p.v_scales : p.k_scales)[block] = (uint8_t)s;
+    }
+}
+
+__global__ __launch_bounds__(256) void kv_copy_fourbit_kernel(CommitParams p)
+{
+    const int j = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
+    const CommitRows c = commit_rows(p, b, threadIdx.x & 63);
+    if (j >= c.rows) return;
+    const int src_row = (p.root_row && j == 0) ? 0 : p.root_row + p.accepted_path[(size_t)b * p.gamma_max + (j - p.root_row)];
+    const int page = p.block_table[(size_t)b * p.max_pages + (c.L + j) / p.page_size];
+    commit_row_fourbit(p, layer, b, src_row, page, (c.L + j) % p.page_size, threadIdx.x, blockDim.x);
+}
+
+__global__ __launch_bounds__(64 * COMMIT_WAVES) void kv_commit_fourbit_kernel(CommitParams p)
+{
+    __shared__ int s_src[COMMIT_ROWS], s_page[COMMIT_ROWS];
+    __shared__ int s_rows, s_L;
+    const int b = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (wave == 0) {
+        const CommitRows c = commit_rows(p, b, lane);
+        if (lane < c.rows) {
+            s_src[lane] = lane < p.root_row ? 0 : p.root_row + p.accepted_path[(size_t)b * p.gamma_max + (lane - p.root_row)];
+            s_page[lane] = p.block_table[(size_t)b * p.max_pages + (c.L + lane) / p.page_size];
+        }
+        if (lane == 0) {
+            s_rows = c.rows;
+            s_L = c.L;
+            finish_sequence(p, b, c, next_root_of(p, b, c));
+        }
+    }
+    __syncthreads();
+    const int rows = __builtin_amdgcn_readfirstlane(s_rows), L = __builtin_amdgcn_readfirstlane(s_L);
+    for (int q = wave; q < rows * p.n_layers; q += COMMIT_WAVES) {
+        const int j = q / p.n_layers, layer = q % p.n_layers;
+        commit_row_fourbit(p, layer, b, __builtin_amdgcn_readfirstlane(s_src[j]), __builtin_amdgcn_readfirstlane(s_page[j]),
+                           (L + j) % p.page_size, lane, 64);
+    }
+}
+
 }  // namespace
 
 int32_t launch_tree_build(const int32_t *kconfig, int gamma, int n_nodes, int B, const int32_t *prefix_len,
@@ -251,13 +309,20 @@ int32_t launch_tree_build(const int32_t *kconfig, int gamma, int n_nodes, int B,
 }
 
 int32_t launch_kv_commit(const mcsd_commit_desc &d, const mcsd_commit_bufs &b, hipStream_t stream,
-                         const mcsd_paged_kv *paged)
+                         const mcsd_paged_kv *paged, const mcsd_fourbit_kv *fourbit)
 {
-    CommitParams p;
+    CommitParams p = {};
     p.block_table = nullptr; p.page_size = p.n_pages = p.max_pages = 0;
     if (paged) {
         p.block_table = paged->block_table; p.page_size = paged->page_size;
         p.n_pages = paged->n_pages; p.max_pages = paged->max_pages_per_seq;
+    }
+    if (fourbit) {
+        p.block_table = fourbit->block_table; p.page_size = fourbit->page_size;
+        p.n_pages = fourbit->n_pages; p.max_pages = fourbit->max_pages_per_seq;
+        p.k_codes = static_cast<uint8_t *>(fourbit->k_codes); p.v_codes = static_cast<uint8_t *>(fourbit->v_codes);
+        p.k_scales = static_cast<uint8_t *>(fourbit->k_scales); p.v_scales = static_cast<uint8_t *>(fourbit->v_scales);
+        p.n_blocks = d.d / FB_BLOCK; p.is_f32 = d.dtype == MCSD_DTYPE_FP32;
     }
     p.B = d.B; p.N = d.N; p.H_kv = d.H_kv; p.L_stride = d.L_stride; p.gamma_max = d.gamma_max; p.n_layers = d.n_layers;
     p.root_row = d.root_row ? 1 : 0;
@@ -272,12 +337,12 @@ int32_t launch_kv_commit(const mcsd_commit_desc &d, const mcsd_commit_bufs &b, h
     // 10.2 and 7.8; 32 KV heads (256 KB) 10.2 and 10.0; 768 KB 10.1 and 21.5.
     const size_t most = (size_t)(d.gamma_max + p.root_row) * d.n_layers * d.H_kv * p.row_bytes * 2;
     if (d.gamma_max + p.root_row <= COMMIT_ROWS && most <= COMMIT_BYTES) {
-        launch_kernel(K_KV_COPY, kv_commit_kernel, dim3(d.B), dim3(64 * COMMIT_WAVES), stream, p);
+        launch_kernel(K_KV_COPY, fourbit ? kv_commit_fourbit_kernel : kv_commit_kernel, dim3(d.B), dim3(64 * COMMIT_WAVES), stream, p);
         const hipError_t e1 = hipGetLastError();
         if (e1 != hipSuccess) { set_error("kv_commit launch failed: %s", hipGetErrorString(e1)); return MCSD_E_HIP; }
         return MCSD_OK;
     }
-    launch_kernel(K_KV_COPY, kv_copy_kernel, dim3(d.gamma_max + p.root_row, d.B, d.n_layers), dim3(256), stream, p);
+    launch_kernel(K_KV_COPY, fourbit ? kv_copy_fourbit_kernel : kv_copy_kernel, dim3(d.gamma_max + p.root_row, d.B, d.n_layers), dim3(256), stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("kv_copy launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     launch_kernel(K_KV_FINISH, kv_finish_kernel, dim3(d.B), dim3(64), stream, p);

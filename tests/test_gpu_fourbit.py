@@ -1,0 +1,374 @@
+"""The prefix cache held in 4 bits on the GPU: rows in and out and commits to the bit, attention over it against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2401_06706_amd import binding as M
+from tests import fourbit_ref as F
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def to_dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return t.to(DEV) if dtype is None else t.to(dtype).to(DEV)
+
+
+def i32(a):
+    return to_dev(np.asarray(a, np.int32))
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def empty_cache(n_pages, H_kv, ps, d, block_table=None, n_layers=None, fill=None):
+    """Pools of junk that reads as NaN wherever it is used by mistake (fill: a scale byte, all codes 0)."""
+    cs, ss = M.fourbit_shapes(n_pages, H_kv, ps, d, n_layers)
+    make = lambda shape, v: torch.full(shape, v, dtype=torch.uint8, device=DEV)
+    pools = [make(cs, 0x5a if fill is None else 0), make(ss, 255 if fill is None else fill)]
+    pools += [t.clone() for t in pools]
+    return M.fourbit_kv(*pools, block_table=block_table), pools
+
+
+def hard_rows(rng, T, H, d, dtype):
+    """Rows over many magnitudes, with ties, zeros, negative zeros and blocks at the edge of a finer scale."""
+    x = rng.normal(size=(T, H, d)) * np.exp2(rng.integers(-30, 30, size=(T, H, d // 32)).repeat(32, -1).astype(np.float64))
+    grid = rng.choice(np.r_[F.MAGNITUDES, (F.MAGNITUDES[1:] + F.MAGNITUDES[:-1]) / 2, 7.0], size=(T, H, d)) * rng.choice([-1, 1], size=(T, H, d))
+    x = np.where(rng.random((T, H, 1)) < 0.5, grid, x)
+    x[rng.random((T, H)) < 0.1] = 0.0
+    return torch.from_numpy(x).to(dtype).to(DEV)
+
+
+# ------------------------------------------------------------------ rows in and out
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H,d,ps,layers,gap", [(1, 1, 32, 32, None, 0), (3, 2, 64, 32, None, 0), (33, 8, 64, 64, None, 64), (130, 5, 96, 96, None, 96 * 5),
+                                                 (257, 8, 128, 64, None, 2048), (70, 3, 256, 32, 3, 0), (9, 1, 160, 128, 2, 32)])
+def test_rows_in_and_out_to_the_bit(T, H, d, ps, layers, gap, dtype):
+    rng = np.random.default_rng(T * d + H)
+    NL = layers or 1
+    n_pages = -(-T // ps) + 3
+    wide = [torch.zeros(NL, T, H * d + gap, dtype=dtype, device=DEV) for _ in range(2)]
+    rows = []
+    for w in wide:
+        for l in range(NL):
+            w[l, :, :H * d] = hard_rows(rng, T, H, d, dtype).reshape(T, H * d)
+        rows.append(w[:, :, :H * d].unflatten(-1, (H, d)))
+    slots = rng.permutation(n_pages * ps)[:T].astype(np.int32)
+    if T > 2:
+        slots[1], slots[-1] = -1, n_pages * ps           # passed over
+    cache, pools = empty_cache(n_pages, H, ps, d, n_layers=layers)
+    before = [p.cpu().numpy().copy() for p in pools]
+    k, v = rows if layers else (rows[0][0], rows[1][0])
+    M.mcsd_kv_store_fourbit(M.fourbit_rows_args(k, v, i32(slots), cache))
+    torch.cuda.synchronize()
+    good = [t for t in range(T) if 0 <= slots[t] < n_pages * ps]
+    for i, x in ((0, rows[0]), (2, rows[1])):
+        code, s = F.encode(f64(x))                       # [NL][T][H][nb][32]
+        want_c, want_s = before[i].reshape(NL, n_pages, H, ps // 16, d // 32, 16, 16), before[i + 1].reshape(NL, n_pages, H, ps // 16, d // 32, 16)
+        for t in good:
+            pg, r = slots[t] // ps, slots[t] % ps
+            want_c[:, pg, :, r // 16, :, r % 16] = code[:, t, ..., 0::2] | code[:, t, ..., 1::2] << 4
+            want_s[:, pg, :, r // 16, :, r % 16] = s[:, t]
+        assert (pools[i].cpu().numpy() == want_c.reshape(pools[i].shape)).all()
+        assert (pools[i + 1].cpu().numpy() == want_s.reshape(pools[i + 1].shape)).all()
+    back = [torch.full((NL, T, H, d), 7.0, dtype=dtype, device=DEV) for _ in range(2)]
+    kb, vb = back if layers else (back[0][0], back[1][0])
+    M.mcsd_kv_load_fourbit(M.fourbit_rows_args(kb, vb, i32(slots), cache))
+    torch.cuda.synchronize()
+    for x, y in zip(rows, back):
+        want = F.decode(*F.encode(f64(x)))
+        bad = [t for t in range(T) if t not in good]
+        want[:, bad] = 7.0                               # left as they were
+        assert (f64(y) == want).all()
+
+
+def test_values_that_are_no_numbers_and_the_ends_of_the_range():
+    d = 64
+    x = torch.ones(6, 1, d, dtype=torch.float32, device=DEV)
+    x[0, 0, 3], x[1, 0, 40], x[2, 0, 0] = float("nan"), float("-inf"), 3.4e38
+    x[3] = 1e-40
+    x[4] = 2.0 ** -121
+    x[5, 0, :32] = 7.0
+    cache, pools = empty_cache(1, 1, 32, d)
+    M.mcsd_kv_store_fourbit(M.fourbit_rows_args(x, x, i32(range(6)), cache))
+    y = torch.zeros_like(x)
+    M.mcsd_kv_load_fourbit(M.fourbit_rows_args(y, y.clone(), i32(range(6)), cache))
+    y = f64(y)[:, 0]
+    want = F.decode(*F.encode(f64(x)))[:, 0]
+    assert np.isnan(y[0, :32]).all() and (y[0, 32:] == 1).all() and np.isnan(y[1, 32:]).all() and (y[1, :32] == 1).all()
+    assert ((y == want) | (np.isnan(y) & np.isnan(want))).all()
+    assert y[2, 0] == 6 * 2.0 ** 125 and (y[3] == 0).all()
+
+
+def test_no_rows_is_no_work():
+    cache, _ = empty_cache(1, 1, 32, 64)
+    e = torch.zeros(0, 1, 64, device=DEV)
+    M.mcsd_kv_store_fourbit(M.fourbit_rows_args(e, e, torch.zeros(0, dtype=torch.int32, device=DEV), cache))
+    torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------ commit
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,layers,H,d,N,gamma,ps,root_row", [(1, 1, 1, 32, 1, 1, 32, False), (3, 4, 8, 128, 28, 3, 64, True),
+                                                              (2, 32, 32, 128, 60, 5, 32, True), (5, 2, 3, 96, 127, 70, 96, True), (4, 3, 2, 256, 12, 6, 32, False)])
+def test_commit_is_the_paged_commit_of_the_held_values(B, layers, H, d, N, gamma, ps, root_row, dtype):
+    rng = np.random.default_rng(B * 100 + N)
+    R = 1 if root_row else 0
+    L = [0, 31, 62, 95, 40][:B]
+    capacity = 200
+    width = -(-capacity // ps)
+    n_pages = B * width + 1
+    table = rng.permutation(n_pages)[:B * width].reshape(B, width).astype(np.int32)
+    n_acc = rng.integers(0, gamma + 1, size=B).astype(np.int32)
+    n_acc[0] = min(gamma, N)
+    path = np.full((B, gamma), -1, np.int32)
+    for b in range(B):
+        n_acc[b] = min(n_acc[b], N)
+        path[b, :n_acc[b]] = np.sort(rng.permutation(N)[:n_acc[b]])
+    if B > 3:
+        path[2, 0], n_acc[2] = N, max(1, n_acc[2])         # outside the tree: nothing of the path
+        table[3, (L[3] + 0) // ps] = n_pages                 # no such page
+    tokens = rng.integers(0, 1000, size=(B, gamma + 1)).astype(np.int32)
+    trees = [torch.stack([hard_rows(rng, B * (N + R), H, d, dtype) for _ in range(layers)]).reshape(layers, B, N + R, H, d).transpose(2, 3).contiguous() for _ in range(2)]
+    cache, pools = empty_cache(n_pages, H, ps, d, i32(table), layers)
+    out = dict(prefix=i32(L), root=torch.full((B,), -5, dtype=torch.int32, device=DEV), flags=torch.full((B,), -5, dtype=torch.int32, device=DEV))
+    M.mcsd_kv_commit_fourbit(M.fourbit_commit_args(cache, *trees, i32(n_acc), i32(path), i32(tokens), out["prefix"], out["root"], out["flags"], capacity, root_row))
+    # the same through the paged commit of full precision
+    ref_pools = [torch.full((layers, n_pages, H, ps, d), float("nan"), dtype=dtype, device=DEV) for _ in range(2)]
+    ref = dict(prefix=i32(L), root=torch.full((B,), -5, dtype=torch.int32, device=DEV), flags=torch.full((B,), -5, dtype=torch.int32, device=DEV))
+    a, pg = M.paged_commit_args(*ref_pools, i32(table), *trees, i32(n_acc), i32(path), i32(tokens), ref["prefix"], ref["root"], ref["flags"], capacity, root_row)
+    M.mcsd_kv_commit_paged(a, pg)
+    torch.cuda.synchronize()
+    for n in out:
+        assert torch.equal(out[n], ref[n]), n
+    for i, rp in ((0, ref_pools[0]), (2, ref_pools[1])):
+        got = np.stack([F.pool_rows(pools[i][l].cpu().numpy(), pools[i + 1][l].cpu().numpy()) for l in range(layers)])
+        full = f64(rp)
+        written = ~np.isnan(full[..., :1])
+        want = np.where(written, F.decode(*F.encode(np.where(written, full, 0.0))), np.nan)
+        assert ((got == want) | (np.isnan(got) & np.isnan(want))).all()
+
+
+# ------------------------------------------------------------------ attention
+def chain(n):
+    return np.arange(-1, n - 1, dtype=np.int32)
+
+
+def star(n):
+    return np.full(n, -1, np.int32)
+
+
+def random_tree(n):
+    rng = np.random.default_rng(n)
+    return np.array([-1 if i == 0 else rng.integers(-1, i) for i in range(n)], np.int32)
+
+
+class AttnCase:
+    def __init__(self, B, H_q, H_kv, d, lens, N, tree, ps, root_row=False, per_seq=False, scale=None, seed=0, spare=2, capacity=None, q_scale=1.0):
+        rng = np.random.default_rng(seed + 7 * d + N)
+        rows = N + (1 if root_row else 0)
+        self.capacity = capacity or max(max(lens), 1)
+        width = -(-self.capacity // ps)
+        used = [-(-n // ps) for n in lens]
+        n_pages = sum(used) + spare
+        self.table = np.full((B, width), -1, np.int32)
+        order, at = rng.permutation(n_pages), 0
+        for b in range(B):
+            self.table[b, :used[b]] = order[at:at + used[b]]
+            at += used[b]
+        self.lens, self.ps, self.H_kv, self.d, self.n_pages = lens, ps, H_kv, d, n_pages
+        self.scale = d ** -0.5 if scale is None else scale
+        bf = lambda *s: torch.from_numpy(rng.normal(size=s).astype(np.float32)).bfloat16().to(DEV)
+        self.q, self.k_tree, self.v_tree = (q_scale * bf(B, rows, H_q, d).float()).bfloat16(), bf(B, H_kv, rows, d), bf(B, H_kv, rows, d)
+        parents = [tree(N) for _ in range(B)]
+        if per_seq:
+            parents = [random_tree(N) if b % 2 else p for b, p in enumerate(parents)]
+        self.parents, self.per_seq, self.root_row = parents, per_seq, root_row
+        # what is stored goes through the library; everything else in the pools is junk that reads as NaN
+        self.cache, self.pools = empty_cache(n_pages, H_kv, ps, d, i32(self.table))
+        slots = np.concatenate([self.table[b, np.arange(n) // ps] * ps + np.arange(n) % ps for b, n in enumerate(lens)] + [np.zeros(0, np.int64)]).astype(np.int32)
+        if len(slots):
+            M.mcsd_kv_store_fourbit(M.fourbit_rows_args(bf(len(slots), H_kv, d), bf(len(slots), H_kv, d), i32(slots), self.cache))
+        self.prefix_len, self.parent = i32(lens), i32(np.stack(parents) if per_seq else parents[0])
+        self.out = torch.full_like(self.q, 9.0)
+        self.make_args()
+
+    def make_args(self):
+        make = lambda ws: M.fourbit_attn_args(self.q, self.cache, self.prefix_len, self.k_tree, self.v_tree, self.parent, self.out, self.scale, self.capacity, ws)
+        need = M.mcsd_attn_fourbit_workspace_bytes(make(None).desc)
+        self.ws = torch.full((max(need, 1),), 0xff, dtype=torch.uint8, device=DEV) if need else None     # (NaN as floats)
+        self.args = make(self.ws)
+
+    def run(self, stream=None):
+        M.mcsd_tree_attn_fourbit(self.args, stream)
+
+    def held(self, b, bad_as_zero=False):
+        k, v = (F.pool_rows(self.pools[i].cpu().numpy(), self.pools[i + 1].cpu().numpy()) for i in (0, 2))
+        n = self.lens[b]
+        table = self.table[b, :-(-n // self.ps)]
+        pick = lambda pool: np.concatenate([np.zeros(pool.shape[1:]) if not 0 <= t < self.n_pages else pool[t] for t in table] + [np.zeros((self.H_kv, 0, self.d))], 1)[:, :n]
+        return pick(k), pick(v)
+
+    def check(self, sequences=None):
+        torch.cuda.synchronize()
+        got = f64(self.out)
+        worst = 0.0
+        for b in range(len(self.lens)) if sequences is None else sequences:
+            parent = self.parents[b]
+            if self.root_row:
+                parent = np.r_[-1, np.where(parent < 0, 0, parent + 1)]
+            k, v = self.held(b)
+            want, bound = F.attention(f64(self.q[b]), k, v, f64(self.k_tree[b]), f64(self.v_tree[b]), F.ancestors(parent), self.scale)
+            err = np.abs(got[b] - want)
+            assert np.isfinite(got[b]).all(), f"sequence {b}"
+            assert (err <= bound).all(), (b, float((err / bound).max()), np.unravel_index((err / bound).argmax(), err.shape))
+            worst = max(worst, float((err / bound).max()))
+        return worst
+
+
+CASES = [
+    dict(B=1, H_q=1, H_kv=1, d=64, lens=[0], N=1, tree=chain, ps=32),                       # itself alone
+    dict(B=1, H_q=1, H_kv=1, d=32, lens=[1], N=1, tree=chain, ps=32),
+    dict(B=4, H_q=8, H_kv=2, d=64, lens=[0, 31, 32, 33], N=3, tree=chain, ps=32),
+    dict(B=3, H_q=4, H_kv=4, d=128, lens=[63, 64, 65], N=28, tree=random_tree, ps=64),
+    dict(B=2, H_q=32, H_kv=8, d=128, lens=[517, 100], N=1, tree=chain, ps=64),
+    dict(B=2, H_q=7, H_kv=1, d=96, lens=[300, 129], N=5, tree=star, ps=96),
+    dict(B=2, H_q=6, H_kv=3, d=160, lens=[200, 31], N=17, tree=random_tree, ps=32),
+    dict(B=2, H_q=4, H_kv=2, d=256, lens=[333, 64], N=33, tree=chain, ps=64),
+    dict(B=1, H_q=2, H_kv=1, d=224, lens=[95], N=60, tree=star, ps=32),
+    dict(B=2, H_q=16, H_kv=2, d=128, lens=[1000, 700], N=84, tree=random_tree, ps=128),
+    dict(B=1, H_q=8, H_kv=1, d=128, lens=[450], N=128, tree=chain, ps=64),
+    dict(B=2, H_q=4, H_kv=2, d=128, lens=[77, 0], N=127, tree=random_tree, ps=32, root_row=True),
+    dict(B=5, H_q=4, H_kv=1, d=64, lens=[5, 64, 2000, 0, 96], N=12, tree=chain, ps=96, root_row=True, per_seq=True),
+    dict(B=1, H_q=2, H_kv=2, d=128, lens=[9000], N=4, tree=star, ps=256),                  # many segments
+    dict(B=2, H_q=40, H_kv=8, d=128, lens=[3000, 1], N=1, tree=chain, ps=64),
+    dict(B=3, H_q=2, H_kv=1, d=128, lens=[100, 4000, 33], N=9, tree=random_tree, ps=32, capacity=16000),
+    dict(B=70, H_q=2, H_kv=1, d=64, lens=[(37 * b) % 300 for b in range(70)], N=2, tree=chain, ps=32),
+    dict(B=2, H_q=2, H_kv=1, d=128, lens=[200, 150], N=8, tree=star, ps=32, scale=0.0),       # all weights alike
+    dict(B=1, H_q=4, H_kv=1, d=128, lens=[700], N=16, tree=random_tree, ps=64, q_scale=40.0),  # one key takes nearly all
+]
+
+
+@pytest.mark.parametrize("kw", CASES, ids=lambda kw: f"B{kw['B']}h{kw['H_q']}/{kw['H_kv']}d{kw['d']}L{max(kw['lens'])}N{kw['N']}")
+def test_attention_against_64_bits(kw):
+    c = AttnCase(**kw)
+    c.run()
+    print("largest share of the bound", c.check())
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_attention_random_shapes(seed):
+    rng = np.random.default_rng(1000 + seed)
+    H_kv = int(rng.integers(1, 5))
+    B = int(rng.integers(1, 6))
+    N = int(rng.integers(1, 128))
+    c = AttnCase(B, H_kv * int(rng.integers(1, 6)), H_kv, 32 * int(rng.integers(1, 9)), [int(x) for x in rng.integers(0, 900, size=B)], N,
+                 [chain, star, random_tree][seed % 3], 32 * int(rng.integers(1, 5)), root_row=bool(seed % 2), per_seq=bool(seed % 3), seed=seed)
+    c.run()
+    c.check()
+
+
+def test_rows_past_the_end_do_not_count_and_results_repeat_to_the_bit():
+    c = AttnCase(3, 8, 2, 128, [2000, 33, 700], 20, random_tree, 64)
+    c.run()
+    first = c.out.clone()
+    for i in (0, 2):                     # other junk behind the lengths, and another workspace
+        codes, scales = c.pools[i], c.pools[i + 1]
+        codes[scales == 255] = 0x77
+        scales[scales == 255] = 200
+    c.out.fill_(3.0)
+    c.ws.zero_()
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(first.view(torch.int16), c.out.view(torch.int16))
+    c.check()
+
+
+def test_pages_outside_the_pool_read_as_zeros():
+    c = AttnCase(2, 4, 2, 128, [200, 100], 6, chain, 32)
+    c.table[0, 2], c.table[0, 6], c.table[1, 0] = -1, c.n_pages, 2 ** 31 - 1
+    c.cache.keep[4].copy_(i32(c.table))
+    c.run()
+    c.check()
+
+
+def test_a_block_that_is_no_number_reaches_its_head_alone():
+    c = AttnCase(2, 4, 2, 128, [200, 100], 6, chain, 32)
+    pg, r = c.table[0, 50 // 32], 50 % 32
+    c.pools[1][pg, 1, r // 16, 2, r % 16] = 255           # a key block of KV head 1
+    c.run()
+    torch.cuda.synchronize()
+    got = f64(c.out)
+    assert np.isnan(got[0, :, 2:]).all() and np.isfinite(got[0, :, :2]).all() and np.isfinite(got[1]).all()
+
+
+def test_short_sequences_do_not_depend_on_the_capacity_named():
+    a = AttnCase(2, 8, 2, 64, [90, 33], 10, random_tree, 32, capacity=96)
+    b = AttnCase(2, 8, 2, 64, [90, 33], 10, random_tree, 32, capacity=30000)
+    a.run(); b.run()
+    a.check(); b.check()
+
+
+def test_attention_in_a_graph_on_another_stream_beside_eager_calls():
+    c, other = AttnCase(2, 8, 2, 128, [3000, 513], 12, random_tree, 64), AttnCase(1, 8, 2, 128, [2500], 9, chain, 64, seed=5)
+    c.run()
+    torch.cuda.synchronize()
+    want = c.out.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        c.run()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run()
+    for _ in range(3):
+        c.out.fill_(5.0)
+        graph.replay()
+        other.run()
+        torch.cuda.synchronize()
+        assert torch.equal(c.out.view(torch.int16), want.view(torch.int16))
+    other.check()
+
+
+def test_pools_of_more_than_four_gib():
+    H, ps, d = 8, 256, 128
+    n_pages = 36000                                       # 4.7 GB of codes each for K and V
+    cs, ss = M.fourbit_shapes(n_pages, H, ps, d)
+    pools = [torch.empty(s, dtype=torch.uint8, device=DEV) for s in (cs, ss, cs, ss)]
+    table = np.array([[n_pages - 1, 3, n_pages - 2]], np.int32)
+    cache = M.fourbit_kv(*pools, block_table=i32(table))
+    rng = np.random.default_rng(3)
+    L = 600
+    bf = lambda *s: torch.from_numpy(rng.normal(size=s).astype(np.float32)).bfloat16().to(DEV)
+    slots = table[0, np.arange(L) // ps] * ps + np.arange(L) % ps
+    k, v = bf(L, H, d), bf(L, H, d)
+    M.mcsd_kv_store_fourbit(M.fourbit_rows_args(k, v, i32(slots), cache))
+    kb, vb = torch.zeros_like(k), torch.zeros_like(v)
+    M.mcsd_kv_load_fourbit(M.fourbit_rows_args(kb, vb, i32(slots), cache))
+    held = [F.decode(*F.encode(f64(x))) for x in (k, v)]
+    assert (f64(kb) == held[0]).all() and (f64(vb) == held[1]).all()
+    q, kt, vt = bf(1, 2, 16, d), bf(1, H, 2, d), bf(1, H, 2, d)
+    out = torch.empty_like(q)
+    parent = i32([-1, 0])
+    make = lambda ws: M.fourbit_attn_args(q, cache, i32([L]), kt, vt, parent, out, d ** -0.5, L, ws)
+    ws = torch.empty(max(M.mcsd_attn_fourbit_workspace_bytes(make(None).desc), 256), dtype=torch.uint8, device=DEV)
+    M.mcsd_tree_attn_fourbit(make(ws))
+    want, bound = F.attention(f64(q[0]), held[0].transpose(1, 0, 2), held[1].transpose(1, 0, 2), f64(kt[0]), f64(vt[0]), F.ancestors([-1, 0]), d ** -0.5)
+    assert (np.abs(f64(out[0]) - want) <= bound).all()
+
+
+def test_python_refusals():
+    c = AttnCase(1, 4, 2, 64, [40], 4, chain, 32)
+    with pytest.raises(M.McsdError) as e:                 # fp32 queries
+        f = lambda t: t.float()
+        M.mcsd_tree_attn_fourbit(M.fourbit_attn_args(f(c.q), c.cache, c.prefix_len, f(c.k_tree), f(c.v_tree), c.parent, f(c.out), 1.0, 40))
+    assert e.value.code == -3
+    with pytest.raises(ValueError):
+        M.fourbit_attn_args(c.q[..., :32].contiguous(), c.cache, c.prefix_len, c.k_tree, c.v_tree, c.parent, c.out, 1.0, 40)
+    with pytest.raises(ValueError):
+        M.fourbit_rows_args(c.k_tree[0].transpose(1, 2), c.v_tree[0], c.prefix_len, c.cache)
+    with pytest.raises(ValueError):
+        M.fourbit_rows_args(torch.zeros(1, 2, 64), torch.zeros(1, 2, 64), c.prefix_len, c.cache)
