@@ -52,6 +52,15 @@ __device__ __forceinline__ long total_tiles(const FourbitParams &p, int lane)
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef v4i16 __attribute__((address_space(3))) *lds_v4i16_ptr;
 
+// Eight codes of a block -> eight bf16.
+__device__ __forceinline__ u32x4 decode8(uint32_t c, float s)
+{
+    return (u32x4){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3))};
+}
+
 // DP: d padded to 64, 128 or 256.  RT: 16-row tiles of query rows per wavefront; all four wavefronts have the same rows
 // and every fourth tile.
 template <int DP, int RT>
@@ -63,6 +72,7 @@ void attn_fourbit_kernel(FourbitParams p)
     constexpr int RUN = DP / 4 / NR;                // columns per run: 16, 32, 32
     constexpr int NKK = DP / 32, NNT = DP / 16;
     constexpr int W = RUN / 8;                      // words of codes per run
+    typedef uint32_t u32xW __attribute__((ext_vector_type(W)));
     constexpr int PV = DP / 2 + 8;                  // row pitch of V in LDS, words
     constexpr int PO = DP + 4;                      // row pitch of the epilogue
     constexpr int TILE_WORDS = KT * PV;
@@ -120,70 +130,10 @@ void attn_fourbit_kernel(FourbitParams p)
     const float c2 = p.scale_log2;
     uint32_t *const vt = s_big + ks * AREA;
 
-    for (int t = t_begin + ks; t < t_end; t += KS) {
-        const bool tree = t >= tiles_prefix;
-        const int key0 = t * KT, node0 = key0 - tiles_prefix * KT;
-        const int nvalid = tree ? p.N - node0 : L - key0;
-        bf16x8 kop[2][NKK];
-        if (!tree) {
-            int blk = p.block_table[(size_t)b * p.max_pages + key0 / p.page_size];
-            blk = __builtin_amdgcn_readfirstlane(blk);
-            const bool bad = (unsigned)blk >= (unsigned)p.n_pages;
-            const size_t tile0 = (((size_t)(bad ? 0 : blk) * p.H_kv + g) * p.page_size + key0 % p.page_size) / FB_TILE;
-#pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                const bool off = bad || 16 * sub + lc >= nvalid;
-#pragma unroll
-                for (int run = 0; run < NR; ++run) {
-                    // the lane's block (d = 64: half of one); a column past d reads the last block: Q is zero there, and V's columns are not written
-                    const int blk_of = min(DP == 64 ? lj >> 1 : 4 * run + lj, p.n_blocks - 1);
-                    const size_t block = ((tile0 + sub) * p.n_blocks + blk_of) * FB_TILE + lc;
-                    const size_t at = block * 16 + (DP == 64 ? 8 * (lj & 1) : 0);
-                    uint32_t kw[W], vw[W];
-                    if constexpr (W == 4) {
-                        *reinterpret_cast<u32x4 *>(kw) = *reinterpret_cast<const u32x4 *>(p.k_codes + at);
-                        *reinterpret_cast<u32x4 *>(vw) = *reinterpret_cast<const u32x4 *>(p.v_codes + at);
-                    } else {
-                        *reinterpret_cast<u32x2 *>(kw) = *reinterpret_cast<const u32x2 *>(p.k_codes + at);
-                        *reinterpret_cast<u32x2 *>(vw) = *reinterpret_cast<const u32x2 *>(p.v_codes + at);
-                    }
-                    // rows past the end hold anything: they take part as zeros
-                    const float sk = fourbit_scale(off ? 127u : p.k_scales[block]), sv = fourbit_scale(off ? 127u : p.v_scales[block]);
-#pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        const uint32_t kc = off ? 0u : kw[w], vc = off ? 0u : vw[w];
-                        u32x4 ko, vo;
-#define MCSD_CVT(o, c, s) \
-                        o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0)); \
-                        o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1)); \
-                        o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2)); \
-                        o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
-                        MCSD_CVT(ko, kc, sk)
-                        MCSD_CVT(vo, vc, sv)
-#undef MCSD_CVT
-                        kop[sub][run * 4 + w] = __builtin_bit_cast(bf16x8, ko);
-                        *reinterpret_cast<u32x4 *>(vt + (16 * sub + lc) * PV + col0(run * 4 + w) / 2) = vo;
-                    }
-                }
-            }
-        } else {
-            const size_t head = ((size_t)b * p.H_kv + g) * p.N;
-#pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                const int node = node0 + 16 * sub + lc;
-                const size_t at = (head + min(node, p.N - 1)) * p.d;
-#pragma unroll
-                for (int kk = 0; kk < NKK; ++kk) {
-                    u32x4 ko = {0u, 0u, 0u, 0u}, vo = {0u, 0u, 0u, 0u};
-                    if (node < p.N && col0(kk) < p.d) {
-                        ko = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p.k_tree) + at + col0(kk));
-                        vo = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p.v_tree) + at + col0(kk));
-                    }
-                    kop[sub][kk] = __builtin_bit_cast(bf16x8, ko);
-                    *reinterpret_cast<u32x4 *>(vt + (16 * sub + lc) * PV + col0(kk) / 2) = vo;
-                }
-            }
-        }
+    // One tile whose operands are there: K in kop, V as rows in LDS.  vis_of(mt): the keys of the tile that count for the lane's row of
+    // row tile mt, where `masked`.
+    bf16x8 kop[2][NKK];
+    auto tile_step = [&](const bool masked, auto vis_of) __attribute__((always_inline)) {
         f32x4 sacc[2][RT];
 #pragma unroll
         for (int mt = 0; mt < RT; ++mt)
@@ -194,7 +144,6 @@ void attn_fourbit_kernel(FourbitParams p)
                 for (int kk = 0; kk < NKK; ++kk)
                     sacc[sub][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[sub][kk], qreg[mt][kk], sacc[sub][mt], 0, 0, 0);
             }
-        const bool masked = tree || nvalid < KT;
         uint32_t vis[RT];
         float lmax[RT];
         bool raise = false;
@@ -202,9 +151,7 @@ void attn_fourbit_kernel(FourbitParams p)
         for (int mt = 0; mt < RT; ++mt) {
             settle_scores(sacc[0][mt], sacc[1][mt]);
             if (masked) {
-                vis[mt] = (1u << (nvalid & 31)) - 1u;
-                if (tree) vis[mt] = s_anc[min(row0 + 16 * mt + lc, p.M - 1) / p.G][t - tiles_prefix];
-                vis[mt] >>= 4 * lj;
+                vis[mt] = vis_of(mt) >> (4 * lj);
 #pragma unroll
                 for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
@@ -256,6 +203,101 @@ void attn_fourbit_kernel(FourbitParams p)
 #pragma unroll
             for (int mt = 0; mt < RT; ++mt) oacc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, pop[mt], oacc[nt][mt], 0, 0, 0);
         }
+    };
+
+    // ---- the prefix.  The codes of a wavefront's next tile are asked for before its present one is worked on, and the
+    // block-table entry of the one behind that; page and row of it advance without a division.
+    int t = t_begin + ks;
+    const int t_prefix = min(t_end, tiles_prefix);
+    if (t < t_prefix) {
+        const int32_t *table = p.block_table + (size_t)b * p.max_pages;
+        int page = (t * KT) / p.page_size, page_row = (t * KT) % p.page_size;
+        const int page_step = KS * KT / p.page_size, row_step = KS * KT % p.page_size;
+        auto entry = [&]() __attribute__((always_inline)) { return table[page]; };
+        // codes and scales of the tile that starts at row page_row of page blk; a column past d reads the last block (Q is zero
+        // there, and V's columns are not written)
+        u32xW kraw[2][NR], vraw[2][NR];
+        uint32_t ksc[2][NR], vsc[2][NR];
+        uint32_t block_of[NR];
+#pragma unroll
+        for (int run = 0; run < NR; ++run) block_of[run] = min(DP == 64 ? lj >> 1 : 4 * run + lj, p.n_blocks - 1) * FB_TILE + lc;
+        auto request = [&](int blk, int row) __attribute__((always_inline)) {
+            const size_t tile0 = (((size_t)((unsigned)blk < (unsigned)p.n_pages ? blk : 0) * p.H_kv + g) * p.page_size + row) / FB_TILE;
+            const size_t at = tile0 * p.n_blocks * FB_TILE;
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                for (int run = 0; run < NR; ++run) {
+                    const uint32_t block = block_of[run] + sub * p.n_blocks * FB_TILE, byte = block * 16 + (DP == 64 ? 8 * (lj & 1) : 0);
+                    kraw[sub][run] = *reinterpret_cast<const u32xW *>(p.k_codes + at * 16 + byte);
+                    ksc[sub][run] = (p.k_scales + at)[block];
+                    vraw[sub][run] = *reinterpret_cast<const u32xW *>(p.v_codes + at * 16 + byte);
+                    vsc[sub][run] = (p.v_scales + at)[block];
+                }
+        };
+        int blk = __builtin_amdgcn_readfirstlane(entry());
+        request(blk, page_row);
+        int next = 0, next_row = 0;
+        auto look_up = [&](int t_next) __attribute__((always_inline)) {
+            page += page_step;
+            page_row += row_step;
+            if (page_row >= p.page_size) { page_row -= p.page_size; ++page; }
+            if (t_next < t_prefix) next = entry();
+            next_row = page_row;
+        };
+        look_up(t + KS);
+        for (; t < t_prefix; t += KS) {
+            const int nvalid = L - t * KT;
+            if (nvalid < KT || (unsigned)blk >= (unsigned)p.n_pages) {
+                // rows past the end hold anything, and those of a page that is none were read from another: they take part as zeros
+                const int keep = (unsigned)blk < (unsigned)p.n_pages ? nvalid : 0;
+#pragma unroll
+                for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                    for (int run = 0; run < NR; ++run)
+                        if (16 * sub + lc >= keep) {
+                            kraw[sub][run] = (u32xW)(0u);
+                            vraw[sub][run] = (u32xW)(0u);
+                            ksc[sub][run] = vsc[sub][run] = 127u;
+                        }
+            }
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                for (int run = 0; run < NR; ++run)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        kop[sub][run * 4 + w] = __builtin_bit_cast(bf16x8, decode8(kraw[sub][run][w], fourbit_scale(ksc[sub][run])));
+                        *reinterpret_cast<u32x4 *>(vt + (16 * sub + lc) * PV + col0(run * 4 + w) / 2) = decode8(vraw[sub][run][w], fourbit_scale(vsc[sub][run]));
+                    }
+            if (t + KS < t_prefix) {
+                blk = __builtin_amdgcn_readfirstlane(next);
+                request(blk, next_row);
+                look_up(t + 2 * KS);
+            }
+            tile_step(nvalid < KT, [&](int) __attribute__((always_inline)) { return (1u << (nvalid & 31)) - 1u; });
+        }
+    }
+    // ---- the tree block, bf16
+    for (; t < t_end; t += KS) {
+        const int node0 = (t - tiles_prefix) * KT;
+        const size_t head = ((size_t)b * p.H_kv + g) * p.N;
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            const int node = node0 + 16 * sub + lc;
+            const size_t at = (head + min(node, p.N - 1)) * p.d;
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) {
+                u32x4 ko = {0u, 0u, 0u, 0u}, vo = {0u, 0u, 0u, 0u};
+                if (node < p.N && col0(kk) < p.d) {
+                    ko = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p.k_tree) + at + col0(kk));
+                    vo = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p.v_tree) + at + col0(kk));
+                }
+                kop[sub][kk] = __builtin_bit_cast(bf16x8, ko);
+                *reinterpret_cast<u32x4 *>(vt + (16 * sub + lc) * PV + col0(kk) / 2) = vo;
+            }
+        }
+        tile_step(true, [&](int mt) __attribute__((always_inline)) { return s_anc[min(row0 + 16 * mt + lc, p.M - 1) / p.G][t - tiles_prefix]; });
     }
 
     // ---- epilogue, 16 rows at a time: the wavefronts leave (m, l) and O in LDS and are added up behind a barrier
