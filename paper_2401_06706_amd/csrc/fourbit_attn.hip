@@ -12,6 +12,7 @@
 // matrix cores through the converters alone, without LDS.  V has to be transposed: converted, stored to
 // LDS as rows and read back with the transposing load.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_common.h"
 #include "fourbit.h"
@@ -23,30 +24,88 @@ struct FourbitParams : AttnParams {
     const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
     int n_blocks;           // d / 32
     int n_seg_max;
-    int units;              // row tiles x KV heads
-    int target;             // workgroups aimed at
+    int min_seg;            // tiles of a segment at least
+    int units;              // row tiles x KV heads: workgroups of a segment
+    float units_per_target, bias;   // units / workgroups aimed at; see find_segment
+    uint32_t G_magic;       // r / G = r G_magic >> 32 for the rows there are
 };
 
-constexpr int MIN_SEG = 8;      // tiles of a segment at least: two steps of four wavefronts
+// How the tiles of all sequences are cut: a sequence of T tiles into max(1, T / chunk + bias) segments, with chunk so that there are
+// as many workgroups as aimed at, by the real lengths (a cache's capacity says little about them).  Where they are more than one per
+// CU they are numbered longest first, and if all of them fit the chip at once (two per CU) the second 256 shortest first: the
+// hardware deals them out one per CU in order, so that a long one shares its CU with a short one.
+// A wavefront finds, for itself, the segment of number `index`, or (by_sequence) the segments of sequence `index`: its lanes take a
+// sequence each.  Numbers past the last segment: none.
+struct Segment { int b, L, n, first, i; };       // sequence, its length, its segments, the number of its first one, which of them
 
-// Segments of a sequence of T tiles where all sequences have `total`: as many workgroups as aimed at, each a whole number
-// of steps of the four wavefronts.
-__device__ __forceinline__ void fourbit_segments(const FourbitParams &p, int T, long total, int *n, int *seg)
+__device__ __forceinline__ int lane_sum(int v, int lane, int *all)
 {
-    const long chunk = max((long)MIN_SEG, (total * p.units + p.target - 1) / p.target);
-    const int want = (int)min((long)p.n_seg_max, max(1L, (T + chunk / 2) / chunk));
-    *seg = ((T + want - 1) / want + 3) & ~3;
-    *n = (T + *seg - 1) / *seg;
+    const int x = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(v, o);
+        if (lane >= o) v += u;
+    }
+    *all = __builtin_amdgcn_readlane(v, 63);
+    return v - x;
 }
 
-// Tiles of all sequences, by every wavefront for itself.
-__device__ __forceinline__ long total_tiles(const FourbitParams &p, int lane)
+__device__ __forceinline__ Segment find_segment(const FourbitParams &p, int index, bool by_sequence, int lane)
 {
-    long t = 0;
-    for (int b = lane; b < p.B; b += 64) t += (max(0, min(p.prefix_len[b], p.L_stride)) + KT - 1) / KT + p.tiles_tree;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) t += __shfl_xor(t, o);
-    return t;
+    Segment s = {-1, 0, 0, 0, 0};
+    auto length = [&](int b) __attribute__((always_inline)) { return b < p.B ? max(0, min(p.prefix_len[b], p.L_stride)) : 0; };
+    auto tiles = [&](int b, int L) __attribute__((always_inline)) { return b < p.B ? (L + KT - 1) / KT + p.tiles_tree : 0; };
+    if (p.n_seg_max == 1 && (p.B > 64 || p.bias != 0.f || p.B * p.units <= 256)) {
+        s.b = index; s.L = length(index); s.n = 1; s.first = index;
+        return s;
+    }
+    int L = length(lane), total = 0, all;
+    lane_sum(tiles(lane, L), lane, &total);
+    for (int b0 = 64; b0 < p.B; b0 += 64) {
+        lane_sum(tiles(b0 + lane, length(b0 + lane)), lane, &all);
+        total += all;
+    }
+    // (in floating point: a rounding moves a cut by a tile)
+    const int chunk = max(p.min_seg, (int)ceilf((float)total * p.units_per_target));
+    const float per_chunk = 1.0f / (float)chunk;
+    int before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        if (b0 > 0) L = length(b0 + lane);
+        const int T = tiles(b0 + lane, L);
+        const int n = b0 + lane < p.B ? max(1, min(p.n_seg_max, (int)((float)T * per_chunk + p.bias))) : 0;
+        int at = before + lane_sum(n, lane, &all);
+        int wanted = index;
+        if (p.B <= 64 && p.bias == 0.f && all * p.units > 256) {
+            // tiles of a segment and the lane, as one number: the segments of all sequences with a larger one come before this one's
+            const int key = (T / max(n, 1) << 6) | (63 - lane);
+            at = 0;
+            for (int j = 0; j < p.B; ++j) at += __builtin_amdgcn_readlane(key, j) > key ? __builtin_amdgcn_readlane(n, j) : 0;
+            const int half = 256 / p.units;
+            if (all * p.units <= 512 && index >= half) wanted = all - 1 - (index - half);
+            if (index >= all) wanted = -1;
+        }
+        const unsigned long long hit = __ballot(by_sequence ? b0 + lane == index : n > 0 && wanted >= at && wanted < at + n);
+        if (hit) {
+            const int l = __ffsll((long long)hit) - 1;
+            s.b = b0 + l;
+            s.L = __builtin_amdgcn_readlane(L, l);
+            s.n = __builtin_amdgcn_readlane(n, l);
+            s.first = __builtin_amdgcn_readlane(at, l);
+            s.i = wanted - s.first;
+            return s;
+        }
+        before += all;
+    }
+    return s;
+}
+
+// Node of query row r of a KV head, and where that row's output lies.
+__device__ __forceinline__ int row_node(const FourbitParams &p, int r) { return p.G == 1 ? r : (int)__umulhi((uint32_t)r, p.G_magic); }
+
+__device__ __forceinline__ uint16_t *row_out(const FourbitParams &p, int b, int g, int r)
+{
+    const int node = row_node(p, r);
+    return static_cast<uint16_t *>(p.out) + (((size_t)b * p.N + node) * p.H_q + (size_t)g * p.G + (r - node * p.G)) * (size_t)p.d;
 }
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
@@ -61,57 +120,187 @@ __device__ __forceinline__ u32x4 decode8(uint32_t c, float s)
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3))};
 }
 
-// DP: d padded to 64, 128 or 256.  RT: 16-row tiles of query rows per wavefront; all four wavefronts have the same rows
-// and every fourth tile.
+// All bits set, or none, as bit i of `keys` is (a comparison per key would be a mask in two scalar registers, and there are none left).
+__device__ __forceinline__ uint32_t all_of(uint32_t keys, int i) { return (uint32_t)((int)(keys << (31 - i)) >> 31); }
+
+// Weights of NS parts of 16 keys with the running maximum as it stands, tested by their sum: only where that is large (or the first
+// scores come) the maximum is looked for and raised.  keys_of(mt, s): the keys of part s that count for the lane's row, the
+// lowest four bits (MASKED; a masked score can not be told by its value where scale is 0).  Weights enter PV as bf16, at most 2^-8 of each
+// off, as the framework's kernels for d = 128 have it; their sum is of the unrounded ones.
+template <int DP, int RT, int NS, bool MASKED, typename KeysOf>
+__device__ __forceinline__ void fourbit_softmax(float c2, const f32x4 (&sacc)[NS][RT], u32x2 (&pw)[NS][RT], f32x4 (&oacc)[DP / 16][RT], float (&m_used)[RT],
+                                                float (&l_part)[RT], KeysOf keys_of)
+{
+    float sum[RT];
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int mt = 0; mt < RT; ++mt) {
+            sum[mt] = 0.f;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                float pv[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pv[i] = fast_exp2(fmaf(sacc[s][mt][i], c2, -m_used[mt]));
+                if (MASKED) {
+                    const uint32_t keys = keys_of(mt, s);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pv[i] = __uint_as_float(__float_as_uint(pv[i]) & all_of(keys, i));
+                }
+                sum[mt] += (pv[0] + pv[1]) + (pv[2] + pv[3]);
+                pw[s][mt] = (u32x2){pack_bf16(pv[0], pv[1]), pack_bf16(pv[2], pv[3])};
+            }
+        }
+    };
+    weights();
+    bool raise = false;
+#pragma unroll
+    for (int mt = 0; mt < RT; ++mt) raise |= sum[mt] > 4096.f;
+    if (__any(raise)) {
+#pragma unroll
+        for (int mt = 0; mt < RT; ++mt) {
+            float rm = -INFINITY;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const uint32_t keys = MASKED ? keys_of(mt, s) : 15u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t of = MASKED ? all_of(keys, i) : ~0u;
+                    rm = fmaxf(rm, __uint_as_float((__float_as_uint(sacc[s][mt][i]) & of) | (0xff800000u & ~of)));
+                }
+            }
+            rm = rm == -INFINITY ? rm : rm * c2;
+            rm = fmaxf(rm, __shfl_xor(rm, 16));
+            rm = fmaxf(rm, __shfl_xor(rm, 32));
+            const float m_new = fmaxf(m_used[mt], rm);
+            const float alpha = fast_exp2(m_used[mt] - m_new);
+            m_used[mt] = m_new;
+            l_part[mt] *= alpha;
+#pragma unroll
+            for (int nt = 0; nt < DP / 16; ++nt) oacc[nt][mt] *= alpha;
+        }
+        weights();
+    }
+#pragma unroll
+    for (int mt = 0; mt < RT; ++mt) l_part[mt] += sum[mt];
+}
+
+// O^T += V^T P^T of a tile: V as rows in LDS, read back transposed; w0, w1 the weights of its two parts.
+template <int DP, int RT>
+__device__ __forceinline__ void fourbit_values(const uint32_t *v, int lj, int lc, const u32x2 (&w0)[RT], const u32x2 (&w1)[RT], f32x4 (&oacc)[DP / 16][RT])
+{
+    constexpr int PV = DP / 2 + 8;
+    const uint32_t *vl = v + (4 * lj + (lc >> 2)) * PV + (lc & 3) * 2;
+#pragma unroll
+    for (int nt = 0; nt < DP / 16; ++nt) {
+        const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(vl + nt * 8));
+        const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(vl + 16 * PV + nt * 8));
+        const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int mt = 0; mt < RT; ++mt) {
+            const u32x4 w = {w0[mt][0], w0[mt][1], w1[mt][0], w1[mt][1]};
+            oacc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, __builtin_bit_cast(bf16x8, w), oacc[nt][mt], 0, 0, 0);
+        }
+    }
+}
+
+// The end of both kernels, 16 rows of every row group at a time: the key streams leave (m, l) and O in LDS (4 x 16 rows) and are added up
+// behind a barrier; a sequence in one segment is written out, others leave their partials in the workspace.
+template <int DP, int RT, int RG>
+__device__ __forceinline__ void finish(const FourbitParams &p, const Segment &my, int g, int row_tile0, int tid, uint32_t *words, float (*s_m)[16], float (*s_l)[16],
+                                       const f32x4 (&oacc)[DP / 16][RT], const float (&m_used)[RT], const float (&l_part)[RT])
+{
+    constexpr int KS = 4 / RG, NNT = DP / 16, PO = DP + 4;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lj = lane >> 4, lc = lane & 15, b = my.b;
+    float *area = reinterpret_cast<float *>(words);
+#pragma unroll
+    for (int mt = 0; mt < RT; ++mt) {
+        float lt = l_part[mt];
+        lt += __shfl_xor(lt, 16);
+        lt += __shfl_xor(lt, 32);
+        __syncthreads();
+        if (lj == 0) { s_m[wave][lc] = m_used[mt]; s_l[wave][lc] = lt; }
+#pragma unroll
+        for (int nt = 0; nt < NNT; ++nt) *reinterpret_cast<f32x4 *>(area + (wave * 16 + lc) * PO + 16 * nt + 4 * lj) = oacc[nt][mt];
+        __syncthreads();
+        // (a thread has the same four columns of several rows)
+        constexpr int D4 = DP / 4, RSTEP = 256 / D4;
+        const int d4 = tid % D4;
+#pragma unroll 2
+        for (int r0 = 0; r0 < 16 * RG; r0 += RSTEP) {
+            const int r16 = r0 + tid / D4, grp = r16 >> 4, r = r16 & 15;
+            const int gr = row_tile0 + 16 * RT * grp + 16 * mt + r;
+            if (gr >= p.M || 4 * d4 >= p.d) continue;
+            float ms = s_m[grp][r], ls = 0.f;
+#pragma unroll
+            for (int k = 1; k < KS; ++k) ms = fmaxf(ms, s_m[k * RG + grp][r]);
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int w = k * RG + grp;
+                const float f = fast_exp2(s_m[w][r] - ms);
+                ls += f * s_l[w][r];
+                acc += f * *reinterpret_cast<const f32x4 *>(area + (w * 16 + r) * PO + 4 * d4);
+            }
+            if (my.n == 1) {
+                const float inv = 1.0f / ls;
+                __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(row_out(p, b, g, gr) + 4 * d4));
+            } else {
+                const size_t u = ((size_t)(my.first + my.i) * p.H_kv + g) * (size_t)p.R + gr;
+                __builtin_nontemporal_store(acc, reinterpret_cast<f32x4 *>(p.part_o + u * p.d + 4 * d4));
+                if (d4 == 0) { p.part_m[u] = ms; p.part_l[u] = ls; }
+            }
+        }
+    }
+}
+
+// DP: d padded to 64, 128 or 256.  Up to 16 RT query rows, all of them by every wavefront, which takes every fourth tile and needs no
+// barrier in its loop.
 template <int DP, int RT>
 __global__ __launch_bounds__(256, 2)
 void attn_fourbit_kernel(FourbitParams p)
 {
-    constexpr int ROWS = 16 * RT, KS = 4;
+    constexpr int KS = 4, STEP = KS;                // key streams, tiles per step
+    constexpr int NST = DP == 256 ? 1 : 2;          // steps asked for ahead
     constexpr int NR = DP == 256 ? 2 : 1;           // runs of columns a lane holds of a key's row
     constexpr int RUN = DP / 4 / NR;                // columns per run: 16, 32, 32
     constexpr int NKK = DP / 32, NNT = DP / 16;
     constexpr int W = RUN / 8;                      // words of codes per run
     typedef uint32_t u32xW __attribute__((ext_vector_type(W)));
     constexpr int PV = DP / 2 + 8;                  // row pitch of V in LDS, words
-    constexpr int PO = DP + 4;                      // row pitch of the epilogue
-    constexpr int TILE_WORDS = KT * PV;
-    constexpr int AREA = TILE_WORDS > 16 * PO ? TILE_WORDS : 16 * PO;
+    constexpr int TILE_WORDS = KT * PV, OUT_WORDS = 4 * 16 * (DP + 4);
 
-    __shared__ __attribute__((aligned(16))) uint32_t s_big[KS * AREA];
+    __shared__ __attribute__((aligned(16))) uint32_t s_big[KS * TILE_WORDS > OUT_WORDS ? KS * TILE_WORDS : OUT_WORDS];
     __shared__ uint32_t s_anc[MCSD_MAX_NODES][4];
     __shared__ int s_parent[MCSD_MAX_NODES];
-    __shared__ float s_m[KS][16], s_l[KS][16];
+    __shared__ float s_m[4][16], s_l[4][16];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lj = lane >> 4, lc = lane & 15;
-    const int g = blockIdx.x, b = blockIdx.z;
-    const int segment = blockIdx.y / p.n_row_tiles, row0 = blockIdx.y % p.n_row_tiles * ROWS;
-
-    const int L = max(0, min(p.prefix_len[b], p.L_stride));
+    const int g = blockIdx.x;
+    const Segment my = find_segment(p, blockIdx.z, false, lane);
+    const int b = my.b, L = my.L;
+    if (b < 0) return;
     const int tiles_prefix = (L + KT - 1) / KT, T = tiles_prefix + p.tiles_tree;
-    int n_seg = 1, seg = T;
-    if (p.n_seg_max > 1) fourbit_segments(p, T, total_tiles(p, lane), &n_seg, &seg);
-    n_seg = __builtin_amdgcn_readfirstlane(n_seg);
-    seg = __builtin_amdgcn_readfirstlane(seg);
-    if (segment >= n_seg) return;
-    const int t_begin = segment * seg, t_end = min(T, t_begin + seg);
+    // whole steps where that leaves no segment empty
+    const int seg = (int)(((uint32_t)(T + my.n - 1) / (uint32_t)my.n + STEP - 1) / STEP * STEP);
+    const int t_begin = min(T, my.i * seg), t_end = min(T, t_begin + seg);
 
     const int my_parent = parent_of_thread(p, b);
 
-    // column of word-run element (kk, i): lane lj holds runs [RUN lj, RUN lj + RUN) (DP = 256: of each half of the row)
-    auto col0 = [&](int kk) __attribute__((always_inline)) { return NR == 2 ? 128 * (kk / 4) + 32 * lj + 8 * (kk % 4) : RUN * lj + 8 * kk; };
+    // First of the eight columns that a lane holds in part kk of the contraction: its runs are [RUN lj, RUN lj + RUN) (DP = 256:
+    // of each half of the row).
+    auto run_col = [&](int kk) __attribute__((always_inline)) { return NR == 2 ? 128 * (kk / 4) + 32 * lj + 8 * (kk % 4) : RUN * lj + 8 * kk; };
     bf16x8 qreg[RT][NKK];
 #pragma unroll
     for (int mt = 0; mt < RT; ++mt) {
-        const int r = row0 + 16 * mt + lc;
-        const int rr = min(r, p.M - 1), node = rr / p.G, hh = rr % p.G;
+        const int r = 16 * mt + lc;
+        const int rr = min(r, p.M - 1), node = row_node(p, rr), hh = rr - node * p.G;
         const uint16_t *src = static_cast<const uint16_t *>(p.q) + (((size_t)b * p.N + node) * p.H_q + (size_t)g * p.G + hh) * (size_t)p.d;
 #pragma unroll
         for (int kk = 0; kk < NKK; ++kk) {
             u32x4 v = {0u, 0u, 0u, 0u};
-            if (r < p.M && col0(kk) < p.d) v = *reinterpret_cast<const u32x4 *>(src + col0(kk));
+            if (r < p.M && run_col(kk & ~3) < p.d) v = *reinterpret_cast<const u32x4 *>(src + run_col(kk));     // (d ends with a run)
             qreg[mt][kk] = __builtin_bit_cast(bf16x8, v);
         }
     }
@@ -128,248 +317,495 @@ void attn_fourbit_kernel(FourbitParams p)
         for (int nt = 0; nt < NNT; ++nt) oacc[nt][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     const float c2 = p.scale_log2;
-    uint32_t *const vt = s_big + ks * AREA;
 
-    // One tile whose operands are there: K in kop, V as rows in LDS.  vis_of(mt): the keys of the tile that count for the lane's row of
-    // row tile mt, where `masked`.
-    bf16x8 kop[2][NKK];
-    auto tile_step = [&](const bool masked, auto vis_of) __attribute__((always_inline)) {
-        f32x4 sacc[2][RT];
+    u32x2 pw[2][RT];
+    f32x4 sacc[2][RT];
+    uint32_t *const vt = s_big + ks * TILE_WORDS;
+    auto scores = [&](int s, auto k_of) __attribute__((always_inline)) {
 #pragma unroll
-        for (int mt = 0; mt < RT; ++mt)
+        for (int mt = 0; mt < RT; ++mt) sacc[s][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                sacc[sub][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        for (int kk = 0; kk < NKK; ++kk) {
+            const bf16x8 k = k_of(kk);
 #pragma unroll
-                for (int kk = 0; kk < NKK; ++kk)
-                    sacc[sub][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[sub][kk], qreg[mt][kk], sacc[sub][mt], 0, 0, 0);
-            }
-        uint32_t vis[RT];
-        float lmax[RT];
-        bool raise = false;
-#pragma unroll
-        for (int mt = 0; mt < RT; ++mt) {
-            settle_scores(sacc[0][mt], sacc[1][mt]);
-            if (masked) {
-                vis[mt] = vis_of(mt) >> (4 * lj);
-#pragma unroll
-                for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!((vis[mt] >> (16 * sub + i)) & 1u)) sacc[sub][mt][i] = -INFINITY;
-            }
-            const float mr = max_of_scores(sacc[0][mt], sacc[1][mt]);
-            lmax[mt] = (mr == -INFINITY) ? -INFINITY : mr * c2;
-            raise |= lmax[mt] > m_used[mt] + RESCALE_GAP;
-        }
-        if (__any(raise)) {
-#pragma unroll
-            for (int mt = 0; mt < RT; ++mt) {
-                float rm = lmax[mt];
-                rm = fmaxf(rm, __shfl_xor(rm, 16));
-                rm = fmaxf(rm, __shfl_xor(rm, 32));
-                const float m_new = fmaxf(m_used[mt], rm);
-                const float alpha = fast_exp2(m_used[mt] - m_new);
-                m_used[mt] = m_new;
-                l_part[mt] *= alpha;
-#pragma unroll
-                for (int nt = 0; nt < NNT; ++nt) oacc[nt][mt] *= alpha;
-            }
-        }
-        bf16x8 pop[RT];
-#pragma unroll
-        for (int mt = 0; mt < RT; ++mt) {
-            float pv[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) pv[e] = fast_exp2(fmaf(sacc[e >> 2][mt][e & 3], c2, -m_used[mt]));
-            if (masked) {
-                // (with scale == 0 a masked score can not be told apart by its value)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (!((vis[mt] >> (16 * (e >> 2) + (e & 3))) & 1u)) pv[e] = 0.f;
-            }
-            l_part[mt] += ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
-            u32x4 ph;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ph[j] = pack_bf16(pv[2 * j], pv[2 * j + 1]);
-            pop[mt] = __builtin_bit_cast(bf16x8, ph);
-        }
-        const uint32_t *vl = vt + (4 * lj + (lc >> 2)) * PV + (lc & 3) * 2;
-#pragma unroll
-        for (int nt = 0; nt < NNT; ++nt) {
-            const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(vl + nt * 8));
-            const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(vl + 16 * PV + nt * 8));
-            const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int mt = 0; mt < RT; ++mt) oacc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, pop[mt], oacc[nt][mt], 0, 0, 0);
+            for (int mt = 0; mt < RT; ++mt) sacc[s][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qreg[mt][kk], sacc[s][mt], 0, 0, 0);
         }
     };
+    auto softmax = [&](auto masked, auto keys_of) __attribute__((always_inline)) {
+        fourbit_softmax<DP, RT, 2, decltype(masked)::value>(c2, sacc, pw, oacc, m_used, l_part, keys_of);
+    };
+    auto values = [&]() __attribute__((always_inline)) { fourbit_values<DP, RT>(vt, lj, lc, pw[0], pw[1], oacc); };
 
-    // ---- the prefix.  The codes of a wavefront's next tile are asked for before its present one is worked on, and the
-    // block-table entry of the one behind that; page and row of it advance without a division.
-    int t = t_begin + ks;
+    // Codes and scales of a wavefront's tiles of the next NST steps are on their way while it works on the present one.  The
+    // block-table entries of 64 of them are read at once, a lane each (an entry read by itself ahead of its use was
+    // sunk down to it, a trip to memory per step).  A column past d reads the last block (Q is zero there, and V's
+    // columns are not written).
+    const int32_t *table = p.block_table + (size_t)b * p.max_pages;
+    u32xW kraw[NST][2][NR], vraw[NST][2][NR];
+    uint32_t ksc[NST][2][NR], vsc[NST][2][NR];
+    int blk[NST];
+    uint32_t block_of[NR];
+#pragma unroll
+    for (int run = 0; run < NR; ++run) block_of[run] = min(DP == 64 ? lj >> 1 : 4 * run + lj, p.n_blocks - 1) * FB_TILE + lc;
     const int t_prefix = min(t_end, tiles_prefix);
-    if (t < t_prefix) {
-        const int32_t *table = p.block_table + (size_t)b * p.max_pages;
-        int page = (t * KT) / p.page_size, page_row = (t * KT) % p.page_size;
-        const int page_step = KS * KT / p.page_size, row_step = KS * KT % p.page_size;
-        auto entry = [&]() __attribute__((always_inline)) { return table[page]; };
-        // codes and scales of the tile that starts at row page_row of page blk; a column past d reads the last block (Q is zero
-        // there, and V's columns are not written)
-        u32xW kraw[2][NR], vraw[2][NR];
-        uint32_t ksc[2][NR], vsc[2][NR];
-        uint32_t block_of[NR];
+    int t = t_begin + ks, t_ask = t;                // the tile worked on next, and the one asked for next
+    int row_ask = t_ask * KT % p.page_size;
+    const int row_step = STEP * KT % p.page_size;
+    auto look_up = [&]() __attribute__((always_inline)) { return table[min((t_ask + lane * STEP) * KT / p.page_size, p.max_pages - 1)]; };
+    int entries = look_up(), n_asked = 0;
+    // (Unconditional: behind a branch the compiler would wait for everything that is on its way.  Past the end, and for a page that
+    // is none, page 0 is read and not used.)
+    auto request = [&](auto stage) __attribute__((always_inline)) {
+        constexpr int S = decltype(stage)::value;
+        const int e = __builtin_amdgcn_readlane(entries, n_asked);
+        blk[S] = e;
+        const size_t first = (((size_t)(t_ask < t_prefix && (unsigned)e < (unsigned)p.n_pages ? e : 0) * p.H_kv + g) * p.page_size + row_ask) * p.n_blocks;
 #pragma unroll
-        for (int run = 0; run < NR; ++run) block_of[run] = min(DP == 64 ? lj >> 1 : 4 * run + lj, p.n_blocks - 1) * FB_TILE + lc;
-        auto request = [&](int blk, int row) __attribute__((always_inline)) {
-            const size_t tile0 = (((size_t)((unsigned)blk < (unsigned)p.n_pages ? blk : 0) * p.H_kv + g) * p.page_size + row) / FB_TILE;
-            const size_t at = tile0 * p.n_blocks * FB_TILE;
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
+            for (int run = 0; run < NR; ++run) {
+                const uint32_t block = block_of[run] + s * p.n_blocks * FB_TILE, byte = block * 16 + (DP == 64 ? 8 * (lj & 1) : 0);
+                kraw[S][s][run] = *reinterpret_cast<const u32xW *>(p.k_codes + first * 16 + byte);
+                ksc[S][s][run] = (p.k_scales + first)[block];
+                vraw[S][s][run] = *reinterpret_cast<const u32xW *>(p.v_codes + first * 16 + byte);
+                vsc[S][s][run] = (p.v_scales + first)[block];
+            }
+        t_ask += STEP;
+        row_ask += row_step;
+        if (row_ask >= p.page_size) row_ask -= p.page_size;
+        if (++n_asked == 64) {
+            n_asked = 0;
+            entries = look_up();
+            asm volatile("s_waitcnt vmcnt(0)" : "+v"(entries));
+        }
+    };
+    // rows from `keep` on hold anything, and those of a page that is none were read from another: they take part as zeros
+    auto zero_from = [&](int keep, auto stage) __attribute__((always_inline)) {
+        constexpr int S = decltype(stage)::value;
 #pragma unroll
-                for (int run = 0; run < NR; ++run) {
-                    const uint32_t block = block_of[run] + sub * p.n_blocks * FB_TILE, byte = block * 16 + (DP == 64 ? 8 * (lj & 1) : 0);
-                    kraw[sub][run] = *reinterpret_cast<const u32xW *>(p.k_codes + at * 16 + byte);
-                    ksc[sub][run] = (p.k_scales + at)[block];
-                    vraw[sub][run] = *reinterpret_cast<const u32xW *>(p.v_codes + at * 16 + byte);
-                    vsc[sub][run] = (p.v_scales + at)[block];
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int run = 0; run < NR; ++run)
+                if (16 * s + lc >= keep) {
+                    kraw[S][s][run] = (u32xW)(0u);
+                    vraw[S][s][run] = (u32xW)(0u);
+                    ksc[S][s][run] = vsc[S][s][run] = 127u;
                 }
-        };
-        int blk = __builtin_amdgcn_readfirstlane(entry());
-        request(blk, page_row);
-        int next = 0, next_row = 0;
-        auto look_up = [&](int t_next) __attribute__((always_inline)) {
-            page += page_step;
-            page_row += row_step;
-            if (page_row >= p.page_size) { page_row -= p.page_size; ++page; }
-            if (t_next < t_prefix) next = entry();
-            next_row = page_row;
-        };
-        look_up(t + KS);
-        for (; t < t_prefix; t += KS) {
-            const int nvalid = L - t * KT;
-            if (nvalid < KT || (unsigned)blk >= (unsigned)p.n_pages) {
-                // rows past the end hold anything, and those of a page that is none were read from another: they take part as zeros
-                const int keep = (unsigned)blk < (unsigned)p.n_pages ? nvalid : 0;
+    };
+    // K into the products, V as rows into LDS
+    auto convert = [&](auto stage) __attribute__((always_inline)) {
+        constexpr int S = decltype(stage)::value;
 #pragma unroll
-                for (int sub = 0; sub < 2; ++sub)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int run = 0; run < NR; ++run)
-                        if (16 * sub + lc >= keep) {
-                            kraw[sub][run] = (u32xW)(0u);
-                            vraw[sub][run] = (u32xW)(0u);
-                            ksc[sub][run] = vsc[sub][run] = 127u;
-                        }
+            for (int run = 0; run < NR; ++run)
+#pragma unroll
+                for (int w = 0; w < W; ++w)
+                    *reinterpret_cast<u32x4 *>(vt + (16 * s + lc) * PV + run_col(run * 4 + w) / 2) = decode8(vraw[S][s][run][w], fourbit_scale(vsc[S][s][run]));
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            scores(s, [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, decode8(kraw[S][s][kk / 4][kk % 4], fourbit_scale(ksc[S][s][kk / 4]))); });
+    };
+    // ---- whole prefix tiles
+    const int t_plain = min(t_end, L / KT);
+    auto plain = [&](auto stage) __attribute__((always_inline)) {
+        if ((unsigned)blk[decltype(stage)::value] >= (unsigned)p.n_pages) zero_from(0, stage);
+        convert(stage);
+        request(stage);
+        softmax(std::false_type(), [](int, int) __attribute__((always_inline)) { return 15u; });
+        values();
+        t += STEP;
+    };
+    // ---- the others: the end of the prefix and the tree block, bf16
+    auto any = [&](auto stage) __attribute__((always_inline)) {
+        const int left = L - t * KT;
+        uint32_t vis[RT];               // keys that count for the lane's rows
+        if (t < t_prefix) {
+            zero_from((unsigned)blk[decltype(stage)::value] < (unsigned)p.n_pages ? left : 0, stage);
+            convert(stage);
+            request(stage);
+#pragma unroll
+            for (int mt = 0; mt < RT; ++mt) vis[mt] = left >= KT ? ~0u : (1u << (left & 31)) - 1u;
+        } else {
+            const size_t head = ((size_t)b * p.H_kv + g) * p.N;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int node = (t - tiles_prefix) * KT + 16 * s + lc;
+                auto of_tree = [&](const void *from, int kk) __attribute__((always_inline)) {
+                    u32x4 x = {0u, 0u, 0u, 0u};
+                    if (node < p.N && run_col(kk & ~3) < p.d) x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(from) + (head + node) * p.d + run_col(kk));
+                    return x;
+                };
+#pragma unroll
+                for (int kk = 0; kk < NKK; ++kk) *reinterpret_cast<u32x4 *>(vt + (16 * s + lc) * PV + run_col(kk) / 2) = of_tree(p.v_tree, kk);
+                scores(s, [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, of_tree(p.k_tree, kk)); });
             }
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                for (int run = 0; run < NR; ++run)
-#pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        kop[sub][run * 4 + w] = __builtin_bit_cast(bf16x8, decode8(kraw[sub][run][w], fourbit_scale(ksc[sub][run])));
-                        *reinterpret_cast<u32x4 *>(vt + (16 * sub + lc) * PV + col0(run * 4 + w) / 2) = decode8(vraw[sub][run][w], fourbit_scale(vsc[sub][run]));
-                    }
-            if (t + KS < t_prefix) {
-                blk = __builtin_amdgcn_readfirstlane(next);
-                request(blk, next_row);
-                look_up(t + 2 * KS);
-            }
-            tile_step(nvalid < KT, [&](int) __attribute__((always_inline)) { return (1u << (nvalid & 31)) - 1u; });
+            for (int mt = 0; mt < RT; ++mt) vis[mt] = s_anc[row_node(p, min(16 * mt + lc, p.M - 1))][t - tiles_prefix];
         }
+        softmax(std::true_type(), [&](int mt, int s) __attribute__((always_inline)) { return vis[mt] >> (16 * s + 4 * lj); });
+        values();
+        t += STEP;
+    };
+    typedef std::integral_constant<int, 0> stage0;
+    typedef std::integral_constant<int, NST - 1> stage1;
+    request(stage0());
+    __builtin_amdgcn_sched_barrier(0);          // (the order in which they are waited for)
+    if (NST > 1) request(stage1());
+    __builtin_amdgcn_sched_barrier(0);
+    while (t + (NST - 1) * STEP < t_plain) {
+        plain(stage0());
+        if (NST > 1) plain(stage1());
     }
-    // ---- the tree block, bf16
-    for (; t < t_end; t += KS) {
-        const int node0 = (t - tiles_prefix) * KT;
-        const size_t head = ((size_t)b * p.H_kv + g) * p.N;
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            const int node = node0 + 16 * sub + lc;
-            const size_t at = (head + min(node, p.N - 1)) * p.d;
-#pragma unroll
-            for (int kk = 0; kk < NKK; ++kk) {
-                u32x4 ko = {0u, 0u, 0u, 0u}, vo = {0u, 0u, 0u, 0u};
-                if (node < p.N && col0(kk) < p.d) {
-                    ko = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p.k_tree) + at + col0(kk));
-                    vo = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p.v_tree) + at + col0(kk));
-                }
-                kop[sub][kk] = __builtin_bit_cast(bf16x8, ko);
-                *reinterpret_cast<u32x4 *>(vt + (16 * sub + lc) * PV + col0(kk) / 2) = vo;
-            }
-        }
-        tile_step(true, [&](int mt) __attribute__((always_inline)) { return s_anc[min(row0 + 16 * mt + lc, p.M - 1) / p.G][t - tiles_prefix]; });
+    while (t < t_end) {
+        any(stage0());
+        if (NST > 1 && t < t_end) any(stage1());
     }
-
-    // ---- epilogue, 16 rows at a time: the wavefronts leave (m, l) and O in LDS and are added up behind a barrier
-    float *area = reinterpret_cast<float *>(s_big);
-    const int d4n = p.d / 4;
-#pragma unroll
-    for (int mt = 0; mt < RT; ++mt) {
-        float lt = l_part[mt];
-        lt += __shfl_xor(lt, 16);
-        lt += __shfl_xor(lt, 32);
-        __syncthreads();
-        if (lj == 0) { s_m[ks][lc] = m_used[mt]; s_l[ks][lc] = lt; }
-#pragma unroll
-        for (int nt = 0; nt < NNT; ++nt) *reinterpret_cast<f32x4 *>(area + ks * AREA + lc * PO + 16 * nt + 4 * lj) = oacc[nt][mt];
-        __syncthreads();
-        const int first = row0 + 16 * mt, valid = min(16, p.M - first);
-        for (int idx = tid; idx < valid * d4n; idx += 256) {
-            const int r = idx / d4n, d4 = idx - r * d4n;
-            float ms = s_m[0][r], ls = 0.f;
-#pragma unroll
-            for (int k = 1; k < KS; ++k) ms = fmaxf(ms, s_m[k][r]);
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const float f = fast_exp2(s_m[k][r] - ms);
-                ls += f * s_l[k][r];
-                acc += f * *reinterpret_cast<const f32x4 *>(area + k * AREA + r * PO + 4 * d4);
-            }
-            const int gr = first + r;
-            if (n_seg == 1) {
-                const float inv = 1.0f / ls;
-                const int node = gr / p.G, hh = gr % p.G;
-                uint16_t *ob = static_cast<uint16_t *>(p.out) + (((size_t)b * p.N + node) * p.H_q + (size_t)g * p.G + hh) * (size_t)p.d + 4 * d4;
-                __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(ob));
-            } else {
-                const size_t u = (((size_t)b * p.H_kv + g) * p.n_seg_max + segment) * (size_t)p.R + gr;
-                __builtin_nontemporal_store(acc, reinterpret_cast<f32x4 *>(p.part_o + u * p.d + 4 * d4));
-                if (d4 == 0) { p.part_m[u] = ms; p.part_l[u] = ls; }
-            }
-        }
-    }
+    finish<DP, RT, 1>(p, my, g, 0, tid, s_big, s_m, s_l, oacc, m_used, l_part);
 }
 
-// A thread per four columns of a row.
+// 16 or 4 bytes per lane from base + offset straight into LDS, lane after lane from byte `to` on.  No register is written.  Written as text
+// because behind the builtin the compiler waits for everything on its way ahead of every read of LDS; who reads what arrives has counted
+// down vmcnt to it and passed a barrier (the counts are at begin_step).
+__device__ __forceinline__ void fetch16(uint32_t to, const uint8_t *base, uint32_t offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+
+__device__ __forceinline__ void fetch4(uint32_t to, const uint8_t *base, uint32_t offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+
+// More than 32 query rows: RG row groups of 16 RT rows share their keys.  Wavefront (rg, ks) of the four owns rows [16 RT rg, 16 RT (rg + 1)) of
+// the workgroup's and, RG = 2, key stream ks (one tile of the two of a step) or, RG = 4, both tiles.
+//   - Codes and scales go from memory straight into a ring of DEPTH steps in LDS (a wavefront asks for K or V of one of the two tiles), so
+//     that three steps are on their way without a register: with two steps in registers a launch that reads from memory took the
+//     sum of its loads and its arithmetic.
+//   - A wavefront converts the K that it multiplies by itself (conversions run beside matrix instructions), and a quarter of the step's V, as
+//     rows in LDS for the transposing load.
+//   - PV runs a step behind the scores: the one barrier of a step then stands between both the codes' arrival and their
+//     readers, and the V of the last step and its readers.
+template <int DP, int RT, int RG>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2)
+void attn_fourbit_shared_kernel(FourbitParams p)
+{
+    constexpr int ROWS = 16 * RT * RG, STEP = 2, DEPTH = 4;
+    constexpr int TPS = RG / 2, SUBK = 2 * TPS;     // tiles, and 16-key parts, that a wavefront multiplies per step
+    constexpr int NR = DP == 256 ? 2 : 1, RUN = DP / 4 / NR, W = RUN / 8;       // (as in attn_fourbit_kernel)
+    constexpr int NKK = DP / 32, NNT = DP / 16;
+    typedef uint32_t u32xW __attribute__((ext_vector_type(W)));
+    constexpr int PV = DP / 2 + 8, PO = DP + 4;     // row pitches of V in LDS and of the epilogue, words
+    constexpr int NLOAD = DP / 64;                  // 1 KB pieces of a tile's codes
+    constexpr int CODE_WORDS = KT * DP / 8, SCALE_WORDS = 64;       // of a tile's K or V in the ring
+    constexpr int SIDE_WORDS = CODE_WORDS + SCALE_WORDS, RING_WORDS = 4 * SIDE_WORDS;
+    constexpr int TILE_WORDS = KT * PV, VBUF_WORDS = STEP * TILE_WORDS;
+    constexpr int MAIN_WORDS = DEPTH * RING_WORDS + 2 * VBUF_WORDS, OUT_WORDS = 4 * 16 * PO;
+    static_assert(RG == 2 || RG == 4, "row groups");
+
+    __shared__ __attribute__((aligned(16))) uint32_t s_big[MAIN_WORDS > OUT_WORDS ? MAIN_WORDS : OUT_WORDS];
+    __shared__ uint32_t s_anc[MCSD_MAX_NODES][4];
+    __shared__ int s_parent[MCSD_MAX_NODES];
+    __shared__ float s_m[4][16], s_l[4][16];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rg = wave % RG, ks = wave / RG;
+    const int lj = lane >> 4, lc = lane & 15;
+    const int g = blockIdx.x, row_tile0 = blockIdx.y * ROWS, row0 = row_tile0 + 16 * RT * rg;
+    const Segment my = find_segment(p, blockIdx.z, false, lane);
+    const int b = my.b, L = my.L;
+    if (b < 0) return;
+    const int tiles_prefix = (L + KT - 1) / KT, T = tiles_prefix + p.tiles_tree;
+    // whole steps where that leaves no segment empty
+    const int seg = (int)(((uint32_t)(T + my.n - 1) / (uint32_t)my.n + STEP - 1) / STEP * STEP);
+    const int t_begin = min(T, my.i * seg), t_end = min(T, t_begin + seg), t_prefix = min(t_end, tiles_prefix);
+    const int my_parent = parent_of_thread(p, b);
+
+    // ---- requests.  This wavefront's: K (even) or V (odd) of tile wave / 2 of a step.  The block-table entries of 64 steps are read at once, a
+    // lane each.  Past the end, and for a page that is none, page 0 is read and not used: every step asks for as much, so that what is
+    // waited for can be counted.
+    const int32_t *table = p.block_table + (size_t)b * p.max_pages;
+    const uint8_t *const my_codes = wave & 1 ? p.v_codes : p.k_codes, *const my_scales = wave & 1 ? p.v_scales : p.k_scales;
+    int t_ask = t_begin + (wave >> 1), row_ask = t_ask * KT % p.page_size, n_asked = 0, slot_ask = 0;
+    const int row_step = STEP * KT % p.page_size;
+    auto look_up = [&]() __attribute__((always_inline)) { return table[min((t_ask + lane * STEP) * KT / p.page_size, p.max_pages - 1)]; };
+    int entries = look_up();
+    uint32_t code_off[NLOAD];
+#pragma unroll
+    for (int i = 0; i < NLOAD; ++i) code_off[i] = 16u * min(64 * i + lane, 2 * FB_TILE * p.n_blocks - 1);
+    const uint32_t scale_off = 4u * min(lane, 8 * p.n_blocks - 1);
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t *)s_big;
+    auto request = [&]() __attribute__((always_inline)) {
+        const int e = __builtin_amdgcn_readlane(entries, n_asked);
+        const size_t first = (((size_t)(t_ask < t_prefix && (unsigned)e < (unsigned)p.n_pages ? e : 0) * p.H_kv + g) * p.page_size + row_ask) * p.n_blocks;
+        const uint8_t *codes = my_codes + first * 16, *scales = my_scales + first;
+        const uint32_t to = ring_at + 4u * (slot_ask * RING_WORDS + wave * SIDE_WORDS);
+#pragma unroll
+        for (int i = 0; i < NLOAD; ++i) fetch16(to + 1024 * i, codes, code_off[i]);
+        fetch4(to + 4 * CODE_WORDS, scales, scale_off);
+        t_ask += STEP;
+        row_ask += row_step;
+        if (row_ask >= p.page_size) row_ask -= p.page_size;
+        slot_ask = (slot_ask + 1) % DEPTH;
+        if (++n_asked == 64) {
+            n_asked = 0;
+            entries = look_up();
+            asm volatile("s_waitcnt vmcnt(0)" : "+v"(entries) :: "memory");
+        }
+    };
+    // a page that is none among the segment's: all of its steps then look at every entry
+    bool bad_pages = false;
+    for (int e = t_begin * KT / p.page_size + lane; e * p.page_size < t_prefix * KT; e += 64) bad_pages |= (unsigned)table[e] >= (unsigned)p.n_pages;
+    const bool any_bad = __any(bad_pages);
+    const int t_plain = any_bad ? t_begin : min(t_end, L / KT);
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(entries) :: "memory");
+#pragma unroll
+    for (int s = 0; s < DEPTH - 1; ++s) request();
+
+    // First of the eight columns that a lane holds in part kk of the contraction (as in attn_fourbit_kernel).
+    auto run_col = [&](int kk) __attribute__((always_inline)) { return NR == 2 ? 128 * (kk / 4) + 32 * lj + 8 * (kk % 4) : RUN * lj + 8 * kk; };
+    bf16x8 qreg[RT][NKK];
+#pragma unroll
+    for (int mt = 0; mt < RT; ++mt) {
+        const int r = row0 + 16 * mt + lc;
+        const int rr = min(r, p.M - 1), node = row_node(p, rr), hh = rr - node * p.G;
+        const uint16_t *src = static_cast<const uint16_t *>(p.q) + (((size_t)b * p.N + node) * p.H_q + (size_t)g * p.G + hh) * (size_t)p.d;
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) {
+            u32x4 v = {0u, 0u, 0u, 0u};
+            if (r < p.M && run_col(kk & ~3) < p.d) v = *reinterpret_cast<const u32x4 *>(src + run_col(kk));     // (d ends with a run)
+            qreg[mt][kk] = __builtin_bit_cast(bf16x8, v);
+        }
+    }
+    build_ancestor_masks(p, my_parent, s_anc, s_parent);
+
+    f32x4 oacc[NNT][RT];
+    float m_used[RT], l_part[RT];
+#pragma unroll
+    for (int mt = 0; mt < RT; ++mt) {
+        m_used[mt] = M_INIT;
+        l_part[mt] = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < NNT; ++nt) oacc[nt][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const float c2 = p.scale_log2;
+    const bool active = row0 < p.M;
+    // where the lane's codes of part `s` (of a tile's K or V) lie in the ring, in words behind that side; its scale byte behind CODE_WORDS
+    int code_at[2][NR], scale_at[2][NR];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int run = 0; run < NR; ++run) {
+            const int block = (s * p.n_blocks + min(DP == 64 ? lj >> 1 : 4 * run + lj, p.n_blocks - 1)) * FB_TILE + lc;
+            code_at[s][run] = block * 4 + (DP == 64 ? 2 * (lj & 1) : 0);
+            scale_at[s][run] = CODE_WORDS * 4 + block;
+        }
+    auto codes_in = [&](const uint32_t *side, int s, int run) __attribute__((always_inline)) { return *reinterpret_cast<const u32xW *>(side + code_at[s][run]); };
+    auto scale_in = [&](const uint32_t *side, int s, int run) __attribute__((always_inline)) {
+        return fourbit_scale(reinterpret_cast<const uint8_t *>(side)[scale_at[s][run]]);
+    };
+    uint32_t *const vbuf = s_big + DEPTH * RING_WORDS;
+    const int my_tile = RG == 4 ? 0 : ks;                   // the wavefront's first tile of a step
+    const int v_row = 16 * (wave & 1) + lc;                 // its row of V in tile wave / 2
+
+    // (the first step has none before it: weights and V of zeros)
+    u32x2 pw[SUBK][RT];
+#pragma unroll
+    for (int s = 0; s < SUBK; ++s)
+#pragma unroll
+        for (int mt = 0; mt < RT; ++mt) pw[s][mt] = (u32x2){0u, 0u};
+    for (int i = tid; i < VBUF_WORDS / 4; i += 256) reinterpret_cast<u32x4 *>(vbuf + VBUF_WORDS)[i] = (u32x4){0u, 0u, 0u, 0u};
+    f32x4 sacc[SUBK][RT];
+    // O^T += V^T P^T of the last step
+    auto values = [&](const uint32_t *v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < TPS; ++j) fourbit_values<DP, RT>(v + (my_tile + j) * TILE_WORDS, lj, lc, pw[2 * j], pw[2 * j + 1], oacc);
+    };
+    auto scores = [&](int s, auto k_of) __attribute__((always_inline)) {
+#pragma unroll
+        for (int mt = 0; mt < RT; ++mt) sacc[s][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) {
+            const bf16x8 k = k_of(kk);
+#pragma unroll
+            for (int mt = 0; mt < RT; ++mt) sacc[s][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qreg[mt][kk], sacc[s][mt], 0, 0, 0);
+        }
+    };
+    auto softmax = [&](auto masked, auto keys_of) __attribute__((always_inline)) {
+        fourbit_softmax<DP, RT, SUBK, decltype(masked)::value>(c2, sacc, pw, oacc, m_used, l_part, keys_of);
+    };
+
+    // (Everything asked for so far is there; said through the builtin, so that the compiler knows it of its own loads and puts no wait for
+    // them, which would be one for the ring as well, into the loops.)
+    __builtin_amdgcn_s_waitcnt(0x0f70);         // vmcnt(0)
+    int t0 = t_begin, slot = 0, buf = 0;
+    // the codes of this step are there for all wavefronts, and the V rows of the last one; the ring's oldest place is free again
+    auto begin_step = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"((DEPTH - 2) * (NLOAD + 1)) : "memory");
+        __syncthreads();
+        request();
+    };
+    auto end_step = [&]() __attribute__((always_inline)) {
+        t0 += STEP;
+        slot = (slot + 1) % DEPTH;
+        buf ^= 1;
+    };
+    for (; t0 + STEP <= t_plain; end_step()) {
+        begin_step();
+        const uint32_t *ring = s_big + slot * RING_WORDS;
+        const uint32_t *vside = ring + (wave | 1) * SIDE_WORDS;
+#pragma unroll
+        for (int run = 0; run < NR; ++run) {
+            const u32xW c = codes_in(vside, wave & 1, run);
+            const float sc = scale_in(vside, wave & 1, run);
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                *reinterpret_cast<u32x4 *>(vbuf + buf * VBUF_WORDS + (wave >> 1) * TILE_WORDS + v_row * PV + run_col(run * 4 + w) / 2) = decode8(c[w], sc);
+        }
+        if (!active) continue;
+        // (one run of instructions: the products of the last step beside the conversions of this one)
+        values(vbuf + (buf ^ 1) * VBUF_WORDS);
+#pragma unroll
+        for (int s = 0; s < SUBK; ++s) {
+            const uint32_t *kside = ring + 2 * (my_tile + s / 2) * SIDE_WORDS;
+            u32xW c[NR];
+            float sc[NR];
+#pragma unroll
+            for (int run = 0; run < NR; ++run) { c[run] = codes_in(kside, s & 1, run); sc[run] = scale_in(kside, s & 1, run); }
+            scores(s, [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, decode8(c[kk / 4][kk % 4], sc[kk / 4])); });
+        }
+        softmax(std::false_type(), [](int, int) __attribute__((always_inline)) { return 15u; });
+    }
+    // ---- the other steps: the end of the prefix and the tree block, bf16
+    for (; t0 < t_end; end_step()) {
+        begin_step();
+        const uint32_t *ring = s_big + slot * RING_WORDS;
+        if (active) values(vbuf + (buf ^ 1) * VBUF_WORDS);
+        const size_t head = ((size_t)b * p.H_kv + g) * p.N;
+        auto of_tree = [&](const void *from, int node, int kk) __attribute__((always_inline)) {
+            u32x4 x = {0u, 0u, 0u, 0u};
+            if (node < p.N && run_col(kk & ~3) < p.d) x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(from) + (head + node) * p.d + run_col(kk));
+            return x;
+        };
+        // rows of a prefix tile that there are (none of a page that is none); the others hold anything and take part as zeros
+        auto rows_of = [&](int t) __attribute__((always_inline)) {
+            if (any_bad && (unsigned)__builtin_amdgcn_readfirstlane(table[t * KT / p.page_size]) >= (unsigned)p.n_pages) return 0;
+            return L - t * KT;
+        };
+        const int tv = t0 + (wave >> 1);
+        uint32_t *vrow = vbuf + buf * VBUF_WORDS + (wave >> 1) * TILE_WORDS + v_row * PV;
+        if (tv < t_prefix) {
+            const uint32_t *vside = ring + (wave | 1) * SIDE_WORDS;
+            const bool off = v_row >= rows_of(tv);
+#pragma unroll
+            for (int run = 0; run < NR; ++run) {
+                const u32xW c = codes_in(vside, wave & 1, run);
+                const float sc = scale_in(vside, wave & 1, run);
+#pragma unroll
+                for (int w = 0; w < W; ++w) *reinterpret_cast<u32x4 *>(vrow + run_col(run * 4 + w) / 2) = decode8(off ? 0u : c[w], off ? 1.f : sc);
+            }
+        } else {
+            const int node = tv < t_end ? (tv - tiles_prefix) * KT + v_row : p.N;
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) *reinterpret_cast<u32x4 *>(vrow + run_col(kk) / 2) = of_tree(p.v_tree, node, kk);
+        }
+        if (active) {
+#pragma unroll
+            for (int s = 0; s < SUBK; ++s) {
+                const int t = t0 + my_tile + s / 2;
+                bf16x8 k[NKK];
+                if (t < t_prefix) {
+                    const uint32_t *kside = ring + 2 * (my_tile + s / 2) * SIDE_WORDS;
+                    const bool off = 16 * (s & 1) + lc >= rows_of(t);
+#pragma unroll
+                    for (int kk = 0; kk < NKK; ++kk)
+                        k[kk] = __builtin_bit_cast(bf16x8, decode8(off ? 0u : codes_in(kside, s & 1, kk / 4)[kk % 4], off ? 1.f : scale_in(kside, s & 1, kk / 4)));
+                } else {
+#pragma unroll
+                    for (int kk = 0; kk < NKK; ++kk) k[kk] = __builtin_bit_cast(bf16x8, of_tree(p.k_tree, t < t_end ? (t - tiles_prefix) * KT + 16 * (s & 1) + lc : p.N, kk));
+                }
+                scores(s, [&](int kk) __attribute__((always_inline)) { return k[kk]; });
+            }
+            uint32_t vis[TPS][RT];          // keys of a tile that count for the lane's rows
+#pragma unroll
+            for (int j = 0; j < TPS; ++j)
+#pragma unroll
+                for (int mt = 0; mt < RT; ++mt) {
+                    const int t = t0 + my_tile + j, left = L - t * KT;
+                    vis[j][mt] = t >= t_end ? 0u : (t < t_prefix ? (left >= KT ? ~0u : (1u << (left & 31)) - 1u)
+                                                                 : s_anc[row_node(p, min(row0 + 16 * mt + lc, p.M - 1))][t - tiles_prefix]);
+                }
+            softmax(std::true_type(), [&](int mt, int s) __attribute__((always_inline)) { return vis[s / 2][mt] >> (16 * (s & 1) + 4 * lj); });
+        }
+    }
+    __syncthreads();
+    if (active && t_begin < t_end) values(vbuf + (buf ^ 1) * VBUF_WORDS);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (nothing may still be on its way into what follows)
+
+    finish<DP, RT, RG>(p, my, g, row_tile0, tid, s_big, s_m, s_l, oacc, m_used, l_part);
+}
+
+// A thread per four columns of a row, ROWS rows of a (sequence, KV head) per workgroup.
+template <int DP>
 __global__ __launch_bounds__(256) void attn_fourbit_combine_kernel(FourbitParams p)
 {
-    const int g = blockIdx.y, b = blockIdx.z;
-    const int L = max(0, min(p.prefix_len[b], p.L_stride));
-    int n_seg, seg;
-    fourbit_segments(p, (L + KT - 1) / KT + p.tiles_tree, total_tiles(p, threadIdx.x & 63), &n_seg, &seg);
-    if (n_seg == 1) return;
-    const int d4n = p.d / 4, idx = blockIdx.x * 256 + threadIdx.x, r = idx / d4n, d4 = idx - r * d4n;
-    if (r >= p.M) return;
-    const size_t u0 = ((size_t)b * p.H_kv + g) * p.n_seg_max * (size_t)p.R + r;
+    constexpr int D4 = DP / 4, ROWS = 256 / D4;
+    const int g = blockIdx.y;
+    const Segment my = find_segment(p, blockIdx.z, true, threadIdx.x & 63);
+    if (my.n <= 1) return;
+    const int d4 = threadIdx.x % D4, r = blockIdx.x * ROWS + threadIdx.x / D4;
+    if (r >= p.M || 4 * d4 >= p.d) return;
+    const size_t u0 = ((size_t)my.first * p.H_kv + g) * (size_t)p.R + r, step = (size_t)p.H_kv * p.R;
     float ms = M_INIT, ls = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < n_seg; ++s) {
-        const size_t u = u0 + (size_t)s * p.R;
-        const float m = p.part_m[u], m_new = fmaxf(ms, m), keep = fast_exp2(ms - m_new), f = fast_exp2(m - m_new);
-        ls = keep * ls + f * p.part_l[u];
-        acc = keep * acc + f * *reinterpret_cast<const f32x4 *>(p.part_o + u * p.d + 4 * d4);
+    // eight segments at a time, all of them requested before the first is used (those past the end are the first again, without weight)
+    for (int s0 = 0; s0 < my.n; s0 += 8) {
+        float m[8], l[8];
+        f32x4 o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool on = s0 + i < my.n;
+            const size_t u = u0 + (on ? s0 + i : 0) * step;
+            m[i] = on ? p.part_m[u] : M_INIT;
+            l[i] = on ? p.part_l[u] : 0.f;
+            o[i] = *reinterpret_cast<const f32x4 *>(p.part_o + u * p.d + 4 * d4);
+        }
+        float m_new = ms;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m_new = fmaxf(m_new, m[i]);
+        const float keep = fast_exp2(ms - m_new);
+        ls *= keep;
+        acc *= keep;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float f = s0 + i < my.n ? fast_exp2(m[i] - m_new) : 0.f;
+            ls += f * l[i];
+            acc += f * o[i];
+        }
         ms = m_new;
     }
     const float inv = 1.0f / ls;
-    const int node = r / p.G, hh = r % p.G;
-    uint16_t *ob = static_cast<uint16_t *>(p.out) + (((size_t)b * p.N + node) * p.H_q + (size_t)g * p.G + hh) * (size_t)p.d + 4 * d4;
-    __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(ob));
+    __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(row_out(p, my.b, g, r) + 4 * d4));
 }
 
 size_t round_256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
+
+// Variants of the kernel: 16-row tiles per wavefront and row groups.
+struct FourbitVariant { int rt, rg; };
+
+static FourbitVariant variant_of(int rows, int d)
+{
+    if (d > 128) return rows <= 16 ? FourbitVariant{1, 1} : (rows <= 32 ? FourbitVariant{1, 2} : FourbitVariant{1, 4});
+    if (rows <= 16) return {1, 1};
+    if (rows <= 32) return {2, 1};
+    return rows <= 64 ? FourbitVariant{2, 2} : FourbitVariant{2, 4};
+}
+
+constexpr int MIN_SEG = 8;      // tiles of a segment at least
+constexpr long TARGET = 768;    // workgroups aimed at where the sequences do not fill the chip
 
 bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
 {
@@ -377,16 +813,22 @@ bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
     const int rows = d.N + d.root_row;
     if (d.H_kv > 65535 || (long)rows * (d.H_q / d.H_kv) > (1 << 20)) return false;      // (grids and row counts)
     f.rows_per_kv = rows * (d.H_q / d.H_kv);
-    f.row_tile = f.rows_per_kv <= 16 || d.d > 128 ? 16 : 32;      // (32 rows of 256 columns do not fit the registers)
+    const FourbitVariant v = variant_of(f.rows_per_kv, d.d);
+    f.row_tile = 16 * v.rt * v.rg;
     f.n_row_tiles = (f.rows_per_kv + f.row_tile - 1) / f.row_tile;
+    if ((long)f.rows_per_kv * (d.H_q / d.H_kv) >= 0x7fffffffL || f.n_row_tiles > 65535) return false;
     const long units = (long)d.H_kv * f.n_row_tiles;
     const int tiles = (d.L_stride + KT - 1) / KT + (rows + KT - 1) / KT;
-    long n = std::max(1L, std::min((long)(tiles + MIN_SEG - 1) / MIN_SEG, 1024 / units + 1));
-    n = std::max(1L, std::min(n, 4096 / (units * d.B)));
-    f.n_segments_max = (int)n;
-    if (n * f.n_row_tiles > 65535) return false;
-    if (n > 1) {
-        const size_t partials = (size_t)d.B * d.H_kv * n * f.n_row_tiles * f.row_tile;
+    // Enough sequences for the chip: cut only what is twice as long as the average.  Fewer: finer, so that the end of the launch is short.
+    const bool enough = units * d.B >= 384;
+    f.target = (int)(enough ? 512 : TARGET);
+    f.bias = enough ? 0.f : 0.5f;
+    f.n_segments_max = (int)std::max(1L, std::min((long)tiles / MIN_SEG, f.target / units));
+    // Segments of all sequences: n = max(1, T / chunk + bias), with chunk >= all tiles units / target
+    f.n_segments = f.n_segments_max == 1 ? d.B : (int)std::min((long)d.B * f.n_segments_max, f.target / units + 1 + d.B);
+    if (f.n_segments > 65535) return false;
+    if (f.n_segments_max > 1) {
+        const size_t partials = (size_t)f.n_segments * d.H_kv * f.n_row_tiles * f.row_tile;
         f.ws_bytes = round_256(partials * d.d * 4) + 2 * round_256(partials * 4);
     }
     *plan = f;
@@ -406,24 +848,40 @@ int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, co
     p.k_scales = static_cast<const uint8_t *>(kv.k_scales); p.v_scales = static_cast<const uint8_t *>(kv.v_scales);
     p.n_blocks = d.d / FB_BLOCK;
     p.R = plan.n_row_tiles * plan.row_tile;
-    p.n_seg_max = plan.n_segments_max; p.units = d.H_kv * plan.n_row_tiles; p.target = 1024;
+    p.n_seg_max = plan.n_segments_max; p.min_seg = MIN_SEG; p.bias = plan.bias; p.units = d.H_kv * plan.n_row_tiles; p.units_per_target = (float)((double)d.H_kv * plan.n_row_tiles / plan.target);
+    p.G_magic = p.G > 1 ? (uint32_t)((0x100000000ull + p.G - 1) / p.G) : 0u;
     if (plan.ws_bytes > 0) {
-        const size_t partials = (size_t)d.B * d.H_kv * plan.n_segments_max * p.R;
+        const size_t partials = (size_t)plan.n_segments * d.H_kv * p.R;
         char *ws = static_cast<char *>(b.workspace);
         p.part_o = reinterpret_cast<float *>(ws);
         p.part_m = reinterpret_cast<float *>(ws + round_256(partials * d.d * 4));
         p.part_l = reinterpret_cast<float *>(ws + round_256(partials * d.d * 4) + round_256(partials * 4));
     }
-    const dim3 grid(d.H_kv, plan.n_segments_max * plan.n_row_tiles, d.B);
+    const dim3 grid(d.H_kv, plan.n_row_tiles, plan.n_segments);
     auto go = [&](auto kernel) { launch_kernel(K_ATTN_FOURBIT, kernel, grid, dim3(256), stream, p); };
-    const bool one = plan.row_tile == 16;
-    if (d.d <= 64) { if (one) go(attn_fourbit_kernel<64, 1>); else go(attn_fourbit_kernel<64, 2>); }
-    else if (d.d <= 128) { if (one) go(attn_fourbit_kernel<128, 1>); else go(attn_fourbit_kernel<128, 2>); }
-    else go(attn_fourbit_kernel<256, 1>);
+    const FourbitVariant v = variant_of(plan.rows_per_kv, d.d);
+    if (d.d > 128) {
+        if (v.rg == 1) go(attn_fourbit_kernel<256, 1>);
+        else if (v.rg == 2) go(attn_fourbit_shared_kernel<256, 1, 2>);
+        else go(attn_fourbit_shared_kernel<256, 1, 4>);
+    } else if (d.d > 64) {
+        if (v.rg == 4) go(attn_fourbit_shared_kernel<128, 2, 4>);
+        else if (v.rg == 2) go(attn_fourbit_shared_kernel<128, 2, 2>);
+        else if (v.rt == 2) go(attn_fourbit_kernel<128, 2>);
+        else go(attn_fourbit_kernel<128, 1>);
+    } else {
+        if (v.rg == 4) go(attn_fourbit_shared_kernel<64, 2, 4>);
+        else if (v.rg == 2) go(attn_fourbit_shared_kernel<64, 2, 2>);
+        else if (v.rt == 2) go(attn_fourbit_kernel<64, 2>);
+        else go(attn_fourbit_kernel<64, 1>);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("attn_fourbit launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     if (plan.n_segments_max == 1) return MCSD_OK;
-    launch_kernel(K_ATTN_FOURBIT_COMBINE, attn_fourbit_combine_kernel, dim3((p.M * (d.d / 4) + 255) / 256, d.H_kv, d.B), dim3(256), stream, p);
+    auto merge = [&](auto kernel, int rows) { launch_kernel(K_ATTN_FOURBIT_COMBINE, kernel, dim3((p.M + rows - 1) / rows, d.H_kv, d.B), dim3(256), stream, p); };
+    if (d.d > 128) merge(attn_fourbit_combine_kernel<256>, 4);
+    else if (d.d > 64) merge(attn_fourbit_combine_kernel<128>, 8);
+    else merge(attn_fourbit_combine_kernel<64>, 16);
     e = hipGetLastError();
     if (e != hipSuccess) { set_error("attn_fourbit_combine launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     return MCSD_OK;

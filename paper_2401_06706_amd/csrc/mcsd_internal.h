@@ -129,9 +129,11 @@ int32_t launch_kv_commit(const mcsd_commit_desc &d, const mcsd_commit_bufs &b, h
 // ---- prefix cache in 4 bits -------------------------------------------------
 struct FourbitPlan {
     int rows_per_kv;      // query rows that share one KV head
-    int variant;          // instantiation of the attention kernel
     int n_row_tiles, row_tile;
-    int n_segments_max;   // grid extent along the keys
+    int n_segments_max;   // segments of a sequence at most
+    int n_segments;       // of all sequences at most
+    int target;           // workgroups aimed at
+    float bias;           // rounding of a sequence's segments
     size_t ws_bytes;
 };
 bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan);
