@@ -24,7 +24,7 @@ struct FourbitParams : AttnParams {
     const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
     int n_blocks;           // d / 32
     int n_seg_max;
-    int min_seg;            // tiles of a segment at least
+    int min_seg, whole;     // tiles of a segment at least; of a sequence that stays whole at most
     int units;              // row tiles x KV heads: workgroups of a segment
     float units_per_target, bias;   // units / workgroups aimed at; see find_segment
     uint32_t G_magic;       // r / G = r G_magic >> 32 for the rows there are
@@ -66,13 +66,13 @@ __device__ __forceinline__ Segment find_segment(const FourbitParams &p, int inde
         total += all;
     }
     // (in floating point: a rounding moves a cut by a tile)
-    const int chunk = max(p.min_seg, (int)ceilf((float)total * p.units_per_target));
+    const int chunk = max(p.min_seg, (int)fminf(ceilf((float)total * p.units_per_target), 1e9f));
     const float per_chunk = 1.0f / (float)chunk;
     int before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         if (b0 > 0) L = length(b0 + lane);
         const int T = tiles(b0 + lane, L);
-        const int n = b0 + lane < p.B ? max(1, min(p.n_seg_max, (int)((float)T * per_chunk + p.bias))) : 0;
+        const int n = b0 + lane < p.B ? (T <= p.whole ? 1 : max(1, min(p.n_seg_max, (int)((float)T * per_chunk + p.bias)))) : 0;
         int at = before + lane_sum(n, lane, &all);
         int wanted = index;
         if (p.B <= 64 && p.bias == 0.f && all * p.units > 256) {
@@ -804,9 +804,6 @@ static FourbitVariant variant_of(int rows, int d)
     return rows <= 64 ? FourbitVariant{2, 2} : FourbitVariant{2, 4};
 }
 
-constexpr int MIN_SEG = 8;      // tiles of a segment at least
-constexpr long TARGET = 768;    // workgroups aimed at where the sequences do not fill the chip
-
 bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
 {
     FourbitPlan f = {};
@@ -819,11 +816,26 @@ bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
     if ((long)f.rows_per_kv * (d.H_q / d.H_kv) >= 0x7fffffffL || f.n_row_tiles > 65535) return false;
     const long units = (long)d.H_kv * f.n_row_tiles;
     const int tiles = (d.L_stride + KT - 1) / KT + (rows + KT - 1) / KT;
-    // Enough sequences for the chip: cut only what is twice as long as the average.  Fewer: finer, so that the end of the launch is short.
-    const bool enough = units * d.B >= 384;
-    f.target = (int)(enough ? 512 : TARGET);
+    // Workgroups aimed at.  Enough sequences for two workgroups per CU: cut only what is twice as long as the average.  Fewer: two, three or four
+    // per CU, whichever leaves the fullest CU with the fewest tiles if the sequences are alike, ceil(workgroups / 256) / segments of
+    // each (4 sequences of 16384 keys, 48 workgroups a segment: 256, 512, 768, 1024 aimed at 369, 294, 229, 233 us; one of 16000, 32 a segment:
+    // 512 39, 768 46 us with the merge).
+    const long base = units * d.B;
+    const bool enough = base >= 448;
+    f.target = 512;
     f.bias = enough ? 0.f : 0.5f;
-    f.n_segments_max = (int)std::max(1L, std::min((long)tiles / MIN_SEG, f.target / units));
+    double least = 1e30;
+    for (long k = 2; k <= 4 && !enough; ++k) {
+        const long n = std::max(1L, (256 * k + base / 2) / base);
+        const double cost = (double)((base * n + 255) / 256) / (double)n;
+        if (cost < least * 0.999) { least = cost; f.target = (int)(256 * k); }
+    }
+    // A merge is a launch of 4 us, which a sequence of few steps does not earn: 1 x 12 heads of 64, one row, whole / in two: 517 keys 5.9 / 8.9, 1000
+    // 7.7 / 9.3, 2000 11.4 / 9.1; 32 heads, 60 rows: 517 17.4 / 17.7, 1000 20.5 / 16.8.
+    f.min_seg = v.rg == 1 ? 16 : 8;
+    f.whole = v.rg == 1 ? 40 : 20;
+    if (tiles <= f.whole) f.target = 1;
+    f.n_segments_max = (int)std::max(1L, std::min((long)(tiles / f.min_seg), f.target / units));
     // Segments of all sequences: n = max(1, T / chunk + bias), with chunk >= all tiles units / target
     f.n_segments = f.n_segments_max == 1 ? d.B : (int)std::min((long)d.B * f.n_segments_max, f.target / units + 1 + d.B);
     if (f.n_segments > 65535) return false;
@@ -848,7 +860,7 @@ int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, co
     p.k_scales = static_cast<const uint8_t *>(kv.k_scales); p.v_scales = static_cast<const uint8_t *>(kv.v_scales);
     p.n_blocks = d.d / FB_BLOCK;
     p.R = plan.n_row_tiles * plan.row_tile;
-    p.n_seg_max = plan.n_segments_max; p.min_seg = MIN_SEG; p.bias = plan.bias; p.units = d.H_kv * plan.n_row_tiles; p.units_per_target = (float)((double)d.H_kv * plan.n_row_tiles / plan.target);
+    p.n_seg_max = plan.n_segments_max; p.min_seg = plan.min_seg; p.whole = plan.whole; p.bias = plan.bias; p.units = d.H_kv * plan.n_row_tiles; p.units_per_target = (float)((double)d.H_kv * plan.n_row_tiles / plan.target);
     p.G_magic = p.G > 1 ? (uint32_t)((0x100000000ull + p.G - 1) / p.G) : 0u;
     if (plan.ws_bytes > 0) {
         const size_t partials = (size_t)plan.n_segments * d.H_kv * p.R;

@@ -134,6 +134,7 @@ struct FourbitPlan {
     int n_segments;       // of all sequences at most
     int target;           // workgroups aimed at
     float bias;           // rounding of a sequence's segments
+    int min_seg, whole;   // tiles of a segment at least, of a sequence that stays whole at most
     size_t ws_bytes;
 };
 bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan);
