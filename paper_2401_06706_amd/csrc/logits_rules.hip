@@ -1,4 +1,6 @@
 // Penalties, biases and grammar masks on the logit rows of the candidate trees.
+#include <algorithm>
+
 #include "mcsd_internal.h"
 
 namespace mcsd {
@@ -6,6 +8,9 @@ namespace {
 
 constexpr int RULE_THREADS = 256, RULE_SLICE = 4 * RULE_THREADS;       // tokens per workgroup
 constexpr uint32_t IN_PROMPT = 0x80000000u;
+// Workgroups aimed at by dealing the rows out: all that the chip holds at once (eight per CU).  More of them count the history more often and leave a
+// second round half empty, fewer wait for memory: 976 rows of 32000, 512, 1024, 1536, 2048, 2560, 4096 workgroups 117, 80, 64, 56, 68, 60 us.
+constexpr long RULE_GROUPS = 2048;
 
 struct RuleParams {
     int B, N, V, R, parent_per_seq, row_begin, row_end, hist_stride, n_bias, rows_per_group, mask_words;
@@ -18,14 +23,17 @@ struct RuleParams {
     const uint32_t *mask;
 };
 
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));          // four values that start anywhere
+typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
+
 // grid (slices of the vocabulary, groups of tree rows, sequences).  A workgroup counts the sequence's history once, in
-// LDS, for the tokens of its slice, keeps what the rules ask of a token in registers and then
-// goes through its tree rows; of those the candidates on a row's path are counted on top, found by a
-// ballot over the at most 128 nodes.  VEC: rows that start 16-byte aligned, four neighbouring tokens a thread;
-// otherwise every 256th.
-template <bool BF16, bool VEC, bool INPLACE>
+// LDS, for the 1024 tokens of its slice, keeps what the rules ask of a thread's four tokens in registers and then goes through
+// its tree rows, AHEAD of them at a time: their mask words, then those logits that are not masked throughout, then the rules.  The
+// candidates on a row's path are counted on top of the history, found by a ballot over the at most 128 nodes.
+template <bool BF16, bool INPLACE>
 __global__ __launch_bounds__(RULE_THREADS) void logits_rules_kernel(RuleParams p)
 {
+    constexpr int AHEAD = 4;
     __shared__ uint32_t s_count[RULE_SLICE];
     __shared__ int s_bias[RULE_SLICE];
     __shared__ int s_parent[MCSD_MAX_NODES];
@@ -35,7 +43,6 @@ __global__ __launch_bounds__(RULE_THREADS) void logits_rules_kernel(RuleParams p
     const int s0 = blockIdx.x * RULE_SLICE;
     const int r0 = p.row_begin + blockIdx.y * p.rows_per_group, r1 = min(p.row_end, r0 + p.rows_per_group);
 
-    for (int i = tid; i < RULE_SLICE; i += RULE_THREADS) { s_count[i] = 0u; s_bias[i] = -1; }
     if (tid < p.N) s_parent[tid] = p.parent[(p.parent_per_seq ? (size_t)b * p.N : 0) + tid];
     if (tid <= p.N) {
         int row = tid;
@@ -44,8 +51,9 @@ __global__ __launch_bounds__(RULE_THREADS) void logits_rules_kernel(RuleParams p
     }
     // candidates of this lane: nodes lane and 64 + lane
     const int tok0 = lane < p.N ? p.cand_tok[(size_t)b * p.N + lane] : -1, tok1 = 64 + lane < p.N ? p.cand_tok[(size_t)b * p.N + 64 + lane] : -1;
+    for (int i = tid; i < RULE_SLICE; i += RULE_THREADS) { s_count[i] = 0u; s_bias[i] = -1; }
     __syncthreads();
-    if (tid <= p.N) {
+    if (tid >= r0 && tid < r1) {
         uint32_t m[4] = {0u, 0u, 0u, 0u};
         int a = tid - 1;
         for (int step = 0; step < MCSD_MAX_NODES && a >= 0; ++step) {
@@ -62,17 +70,24 @@ __global__ __launch_bounds__(RULE_THREADS) void logits_rules_kernel(RuleParams p
         const int n = min(max(p.hist_len[b], 0), p.hist_stride);
         const int prompt = p.prompt_len ? p.prompt_len[b] : 0;
         const int32_t *h = p.history + (size_t)b * p.hist_stride;
-        for (int i = tid; i < n; i += RULE_THREADS) {
-            const unsigned t = (unsigned)(h[i] - s0);
-            if (t < (unsigned)RULE_SLICE && (int)t < p.V - s0) {
-                if (i < prompt) atomicOr(&s_count[t], IN_PROMPT);
-                else atomicAdd(&s_count[t], 1u);
+        // eight tokens a thread at a time, all requested before the first is counted
+        for (int i0 = tid; i0 < n; i0 += 8 * RULE_THREADS) {
+            int tok[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) tok[k] = i0 + k * RULE_THREADS < n ? h[i0 + k * RULE_THREADS] : -1;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const unsigned t = (unsigned)(tok[k] - s0);
+                if (tok[k] >= 0 && t < (unsigned)RULE_SLICE && tok[k] < p.V) {
+                    if (i0 + k * RULE_THREADS < prompt) atomicOr(&s_count[t], IN_PROMPT);
+                    else atomicAdd(&s_count[t], 1u);
+                }
             }
         }
     }
     for (int i = tid; i < p.n_bias; i += RULE_THREADS) {
-        const unsigned t = (unsigned)(p.bias_tok[(size_t)b * p.n_bias + i] - s0);
-        if (t < (unsigned)RULE_SLICE) atomicMax(&s_bias[t], i);        // the last entry counts
+        const int tok = p.bias_tok[(size_t)b * p.n_bias + i];
+        if (tok >= 0 && (unsigned)(tok - s0) < (unsigned)RULE_SLICE) atomicMax(&s_bias[tok - s0], i);        // the last entry counts
     }
     __syncthreads();
 
@@ -82,85 +97,83 @@ __global__ __launch_bounds__(RULE_THREADS) void logits_rules_kernel(RuleParams p
     bool biased = false;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-        const int t = VEC ? 4 * tid + c : tid + RULE_THREADS * c;
-        count[c] = s_count[t];
-        const int e = s_bias[t];
+        count[c] = s_count[4 * tid + c];
+        const int e = s_bias[4 * tid + c];
         bias[c] = e >= 0 ? p.bias_val[(size_t)b * p.n_bias + e] : 0.f;
         biased |= e >= 0;
     }
-    for (int r = r0; r < r1; ++r) {
-        const int row = __builtin_amdgcn_readfirstlane(s_row[r]);
-        if (row < 0) continue;
-        const size_t base = ((size_t)b * p.R + row) * (size_t)p.V + s0;
-        // the candidates on this row's path, added to the counts of their tokens
-        uint32_t n[4] = {count[0], count[1], count[2], count[3]};
+    const bool counted = (count[0] | count[1]) | (count[2] | count[3]);
+    const int t = s0 + 4 * tid, left = p.V - t;         // the thread's tokens: t and on, `left` of them (more than three: all)
+    for (int rb = r0; rb < r1; rb += AHEAD) {
+        int row[AHEAD];
+        uint32_t allowed[AHEAD];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const uint32_t word = s_anc[r][2 * half + (lane >> 5)];
-            const int tok = half ? tok1 : tok0;
-            unsigned long long hits = __ballot(((word >> (lane & 31)) & 1u) && (unsigned)(tok - s0) < (unsigned)RULE_SLICE);
-            while (hits) {
-                const int l = __ffsll((long long)hits) - 1;
-                hits &= hits - 1;
-                const int t = __builtin_amdgcn_readlane(tok, l) - s0;
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if ((VEC ? 4 * tid + c : tid + RULE_THREADS * c) == t) ++n[c];
-            }
+        for (int u = 0; u < AHEAD; ++u) {
+            row[u] = rb + u < r1 ? __builtin_amdgcn_readfirstlane(s_row[rb + u]) : -1;
+            allowed[u] = 15u;
+            if (p.mask && row[u] >= 0 && left > 0) allowed[u] = p.mask[((size_t)b * p.R + row[u]) * p.mask_words + (t >> 5)] >> (t & 31) & 15u;
         }
-        uint32_t allowed = 15u;
-        if (p.mask) {
-            const uint32_t *m = p.mask + ((size_t)b * p.R + row) * p.mask_words;
-            if (VEC) {
-                const int t = s0 + 4 * tid;
-                allowed = t < p.V ? (m[t >> 5] >> (t & 31)) & 15u : 15u;
-            } else {
+        uint64_t extra[AHEAD];          // times that the thread's tokens stand on the row's path, 16 bits each
+        float z[AHEAD][4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int t = s0 + tid + RULE_THREADS * c;
-                    if (t < p.V && !((m[t >> 5] >> (t & 31)) & 1u)) allowed &= ~(1u << c);
+        for (int u = 0; u < AHEAD; ++u) {
+            extra[u] = 0;
+            if (row[u] < 0) continue;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint32_t word = s_anc[rb + u][2 * half + (lane >> 5)];
+                const int tok = half ? tok1 : tok0;
+                unsigned long long hits = __ballot(((word >> (lane & 31)) & 1u) && tok >= s0 && (unsigned)(tok - s0) < (unsigned)RULE_SLICE);
+                while (hits) {
+                    const int l = __ffsll((long long)hits) - 1;
+                    hits &= hits - 1;
+                    const int c = __builtin_amdgcn_readlane(tok, l) - t;
+                    if ((unsigned)c < 4u) extra[u] += 1ull << (16 * c);
                 }
             }
+            // what is masked throughout is not read, and in place what no rule touches
+            const size_t at = ((size_t)b * p.R + row[u]) * (size_t)p.V + t;
+            const bool want = allowed[u] != 0u && (!INPLACE || biased || counted || extra[u] != 0 || allowed[u] != 15u);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) z[u][c] = 0.f;
+            if (want && left > 3) {
+                if (BF16) {
+                    const u16x4u w = *reinterpret_cast<const u16x4u *>(static_cast<const uint16_t *>(p.logits) + at);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) z[u][c] = __uint_as_float((uint32_t)w[c] << 16);
+                } else {
+                    const f32x4u w = *reinterpret_cast<const f32x4u *>(static_cast<const float *>(p.logits) + at);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) z[u][c] = w[c];
+                }
+            } else if (want) {
+#pragma unroll
+                for (int c = 0; c < 3; ++c)
+                    if (c < left) z[u][c] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(p.logits)[at + c] << 16) : static_cast<const float *>(p.logits)[at + c];
+            }
         }
-        const bool touched = biased || allowed != 15u || ((n[0] | n[1]) | (n[2] | n[3]));
-        if (INPLACE && !touched) continue;
-        float z[4];
-        if (VEC) {
-            const int t = 4 * tid;
-            if (s0 + t >= p.V) continue;
-            if (BF16) {
-                const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.logits) + base + t);
-                z[0] = __uint_as_float(w.x << 16); z[1] = __uint_as_float(w.x & 0xffff0000u);
-                z[2] = __uint_as_float(w.y << 16); z[3] = __uint_as_float(w.y & 0xffff0000u);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (row[u] < 0 || left <= 0) continue;
+            const bool touched = biased || counted || extra[u] != 0 || allowed[u] != 15u;
+            if (INPLACE && !touched) continue;
+            if (touched) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t n = count[c] + (uint32_t)(extra[u] >> (16 * c) & 0xffffu), after = n & ~IN_PROMPT;
+                    if (n) z[u][c] = z[u][c] > 0.f ? z[u][c] / R : z[u][c] * R;
+                    if (after) z[u][c] = (z[u][c] - F * (float)after) - P;
+                    z[u][c] += bias[c];
+                    if (!((allowed[u] >> c) & 1u)) z[u][c] = -INFINITY;
+                }
+            }
+            float *to = p.out + ((size_t)b * p.R + row[u]) * (size_t)p.V + t;
+            if (left > 3) {
+                *reinterpret_cast<f32x4u *>(to) = (f32x4u){z[u][0], z[u][1], z[u][2], z[u][3]};
             } else {
-                const float4 w = *reinterpret_cast<const float4 *>(static_cast<const float *>(p.logits) + base + t);
-                z[0] = w.x; z[1] = w.y; z[2] = w.z; z[3] = w.w;
-            }
-        } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int t = tid + RULE_THREADS * c;
-                z[c] = 0.f;
-                if (s0 + t < p.V) z[c] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(p.logits)[base + t] << 16) : static_cast<const float *>(p.logits)[base + t];
-            }
-        }
-        if (touched) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint32_t after = n[c] & ~IN_PROMPT;
-                if (n[c]) z[c] = z[c] > 0.f ? z[c] / R : z[c] * R;
-                if (after) z[c] = (z[c] - F * (float)after) - P;
-                z[c] += bias[c];
-                if (!((allowed >> c) & 1u)) z[c] = -INFINITY;
-            }
-        }
-        if (VEC) {
-            *reinterpret_cast<float4 *>(p.out + base + 4 * tid) = make_float4(z[0], z[1], z[2], z[3]);
-        } else {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int t = tid + RULE_THREADS * c;
-                if (s0 + t < p.V) p.out[base + t] = z[c];
+                for (int c = 0; c < 3; ++c)
+                    if (c < left) to[c] = z[u][c];
             }
         }
     }
@@ -180,15 +193,14 @@ int32_t launch_logits_rules(const mcsd_logits_desc &d, const mcsd_logits_bufs &b
     const int rows = d.row_end - d.row_begin;
     if (rows == 0) return MCSD_OK;
     const int slices = (d.V + RULE_SLICE - 1) / RULE_SLICE;
-    p.rows_per_group = rows;
-    const dim3 grid(slices, 1, d.B);
-    const bool bf16 = d.dtype == MCSD_DTYPE_BF16;
-    const uintptr_t in = (uintptr_t)b.logits, out = (uintptr_t)b.out;
-    const bool vec = d.V % 4 == 0 && out % 16 == 0 && in % (bf16 ? 8 : 16) == 0, inplace = in == out;
+    const long base = (long)slices * d.B;
+    const int groups = (int)std::max(1L, std::min((long)rows, (RULE_GROUPS + base - 1) / base));
+    p.rows_per_group = (rows + groups - 1) / groups;
+    const dim3 grid(slices, (rows + p.rows_per_group - 1) / p.rows_per_group, d.B);
     auto go = [&](auto kernel) { launch_kernel(K_LOGITS_RULES, kernel, grid, dim3(RULE_THREADS), stream, p); };
-    if (bf16) { if (vec) go(logits_rules_kernel<true, true, false>); else go(logits_rules_kernel<true, false, false>); }
-    else if (inplace) { if (vec) go(logits_rules_kernel<false, true, true>); else go(logits_rules_kernel<false, false, true>); }
-    else { if (vec) go(logits_rules_kernel<false, true, false>); else go(logits_rules_kernel<false, false, false>); }
+    if (d.dtype == MCSD_DTYPE_BF16) go(logits_rules_kernel<true, false>);
+    else if (static_cast<const void *>(b.out) == b.logits) go(logits_rules_kernel<false, true>);
+    else go(logits_rules_kernel<false, false>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("logits_rules launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     return MCSD_OK;
