@@ -23,6 +23,10 @@ def f64(t):
     return t.detach().cpu().to(torch.float64).numpy()
 
 
+def dev_bf16(rng, *shape):
+    return torch.from_numpy(rng.normal(size=shape).astype(np.float32)).bfloat16().to(DEV)
+
+
 def empty_cache(n_pages, H_kv, ps, d, block_table=None, n_layers=None, fill=None):
     """Pools of junk that reads as NaN wherever it is used by mistake (fill: a scale byte, all codes 0)."""
     cs, ss = M.fourbit_shapes(n_pages, H_kv, ps, d, n_layers)
