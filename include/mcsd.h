@@ -432,8 +432,9 @@ typedef struct {
  * d a multiple of 32.  A lone token per sequence is a tree of one node.  Prefix keys and values enter the
  * products exactly as what they stand for, accumulation is fp32, and the softmax weights enter PV as bf16.  Only the
  * pages that hold rows below prefix_len[b] are read, and rows at or past it do not count, whatever
- * they hold.  A table entry outside [0, n_pages) is a data error: its rows read as zeros.  The
- * results do not depend on what other sequences of the batch hold beyond the rounding of a split. */
+ * they hold.  A table entry outside [0, n_pages) is a data error: its rows read as zeros.  What a node may not see
+ * does not reach it, but for values of v_tree that are no numbers: those reach every row of their sequence and KV head.  How a
+ * sequence's keys are split, and with it the last bits of its rows, follows the lengths of the whole batch. */
 size_t mcsd_attn_fourbit_workspace_bytes(const mcsd_attn_desc *desc);
 int32_t mcsd_tree_attn_fourbit(const mcsd_attn_desc *desc, const mcsd_attn_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream);
 
@@ -522,7 +523,8 @@ int32_t mcsd_page_assign(const mcsd_page_desc *desc, const mcsd_page_bufs *bufs,
  *   z += bias(x)  (of several entries of the list for one token the last one counts);   mask bit 0: z = -infinity
  * out is fp32, whatever the logits are; with fp32 logits it may be the logits themselves (in place: what no rule touches
  * is then neither read nor written).  Token ids outside [0, V) are passed over.  A row whose mask
- * leaves nothing becomes -infinity throughout (mcsd_verify_sample flags such a row MCSD_FLAG_NONFINITE).
+ * leaves nothing becomes -infinity throughout (mcsd_verify_sample flags such a row MCSD_FLAG_NONFINITE); a draft row has to keep as
+ * many tokens as are to be drawn from it without replacement.  R must be greater than 0; the arithmetic is fp32.
  */
 typedef struct {
     uint32_t struct_size;

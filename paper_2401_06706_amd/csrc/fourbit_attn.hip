@@ -655,26 +655,36 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         begin_step();
         const uint32_t *ring = s_big + slot * RING_WORDS;
         const uint32_t *vside = ring + (wave | 1) * SIDE_WORDS;
+        uint32_t *const vrow = vbuf + buf * VBUF_WORDS + (wave >> 1) * TILE_WORDS + v_row * PV;
+        // (One run of instructions, everything read from LDS ahead of what is written to it: the products of the last step beside the
+        // conversions of this one.)
+        u32xW vc[NR], kc[SUBK][NR];
+        float vsc[NR], ksc[SUBK][NR];
 #pragma unroll
-        for (int run = 0; run < NR; ++run) {
-            const u32xW c = codes_in(vside, wave & 1, run);
-            const float sc = scale_in(vside, wave & 1, run);
+        for (int run = 0; run < NR; ++run) { vc[run] = codes_in(vside, wave & 1, run); vsc[run] = scale_in(vside, wave & 1, run); }
+        auto convert_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int w = 0; w < W; ++w)
-                *reinterpret_cast<u32x4 *>(vbuf + buf * VBUF_WORDS + (wave >> 1) * TILE_WORDS + v_row * PV + run_col(run * 4 + w) / 2) = decode8(c[w], sc);
+            for (int run = 0; run < NR; ++run)
+#pragma unroll
+                for (int w = 0; w < W; ++w) *reinterpret_cast<u32x4 *>(vrow + run_col(run * 4 + w) / 2) = decode8(vc[run][w], vsc[run]);
+        };
+        if (!active) {
+            convert_v();
+            continue;
         }
-        if (!active) continue;
-        // (one run of instructions: the products of the last step beside the conversions of this one)
+#pragma unroll
+        for (int s = 0; s < SUBK; ++s)
+#pragma unroll
+            for (int run = 0; run < NR; ++run) {
+                const uint32_t *kside = ring + 2 * (my_tile + s / 2) * SIDE_WORDS;
+                kc[s][run] = codes_in(kside, s & 1, run);
+                ksc[s][run] = scale_in(kside, s & 1, run);
+            }
         values(vbuf + (buf ^ 1) * VBUF_WORDS);
+        convert_v();
 #pragma unroll
-        for (int s = 0; s < SUBK; ++s) {
-            const uint32_t *kside = ring + 2 * (my_tile + s / 2) * SIDE_WORDS;
-            u32xW c[NR];
-            float sc[NR];
-#pragma unroll
-            for (int run = 0; run < NR; ++run) { c[run] = codes_in(kside, s & 1, run); sc[run] = scale_in(kside, s & 1, run); }
-            scores(s, [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, decode8(c[kk / 4][kk % 4], sc[kk / 4])); });
-        }
+        for (int s = 0; s < SUBK; ++s)
+            scores(s, [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, decode8(kc[s][kk / 4][kk % 4], ksc[s][kk / 4])); });
         softmax(std::false_type(), [](int, int) __attribute__((always_inline)) { return 15u; });
     }
     // ---- the other steps: the end of the prefix and the tree block, bf16
@@ -834,7 +844,8 @@ bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
     // 7.7 / 9.3, 2000 11.4 / 9.1; 32 heads, 60 rows: 517 17.4 / 17.7, 1000 20.5 / 16.8.
     f.min_seg = v.rg == 1 ? 16 : 8;
     f.whole = v.rg == 1 ? 40 : 20;
-    if (tiles <= f.whole) f.target = 1;
+    // (beyond 512 sequences they fill the chip by themselves, and every workgroup would look through all lengths)
+    if (tiles <= f.whole || d.B > 512) f.target = 1;
     f.n_segments_max = (int)std::max(1L, std::min((long)(tiles / f.min_seg), f.target / units));
     // Segments of all sequences: n = max(1, T / chunk + bias), with chunk >= all tiles units / target
     f.n_segments = f.n_segments_max == 1 ? d.B : (int)std::min((long)d.B * f.n_segments_max, f.target / units + 1 + d.B);

@@ -250,6 +250,12 @@ CASES = [
     dict(B=2, H_q=40, H_kv=8, d=128, lens=[3000, 1], N=1, tree=chain, ps=64),
     dict(B=3, H_q=2, H_kv=1, d=128, lens=[100, 4000, 33], N=9, tree=random_tree, ps=32, capacity=16000),
     dict(B=70, H_q=2, H_kv=1, d=64, lens=[(37 * b) % 300 for b in range(70)], N=2, tree=chain, ps=32),
+    dict(B=600, H_q=1, H_kv=1, d=32, lens=[(b * 7) % 90 for b in range(600)], N=2, tree=chain, ps=32),       # more sequences than are cut
+    dict(B=100, H_q=16, H_kv=8, d=64, lens=[(53 * b) % 400 for b in range(100)], N=3, tree=star, ps=64),
+    dict(B=40, H_q=32, H_kv=16, d=64, lens=[3000] + [20 + b for b in range(39)], N=20, tree=random_tree, ps=32),    # one long among short ones
+    dict(B=16, H_q=32, H_kv=32, d=32, lens=[(389 * b) % 1500 + 1 for b in range(16)], N=40, tree=random_tree, ps=64),     # two workgroups per CU, dealt out by length
+    dict(B=20, H_q=32, H_kv=32, d=64, lens=[(389 * b) % 700 for b in range(20)], N=33, tree=chain, ps=64, root_row=True),  # more than the chip holds
+    dict(B=3, H_q=24, H_kv=2, d=256, lens=[700, 31, 900], N=12, tree=random_tree, ps=96),
     dict(B=2, H_q=2, H_kv=1, d=128, lens=[200, 150], N=8, tree=star, ps=32, scale=0.0),       # all weights alike
     dict(B=1, H_q=4, H_kv=1, d=128, lens=[700], N=16, tree=random_tree, ps=64, q_scale=40.0),  # one key takes nearly all
 ]
@@ -259,7 +265,8 @@ CASES = [
 def test_attention_against_64_bits(kw):
     c = AttnCase(**kw)
     c.run()
-    print("largest share of the bound", c.check())
+    B = len(c.lens)
+    print("largest share of the bound", c.check(None if B <= 20 else sorted({0, 1, 2, B // 2, B - 2, B - 1})))
 
 
 @pytest.mark.parametrize("seed", range(6))
@@ -306,6 +313,33 @@ def test_a_block_that_is_no_number_reaches_its_head_alone():
     torch.cuda.synchronize()
     got = f64(c.out)
     assert np.isnan(got[0, :, 2:]).all() and np.isfinite(got[0, :, :2]).all() and np.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("H_q", [4, 40])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -3.0e38])
+def test_keys_that_a_node_may_not_see_do_not_reach_it(value, H_q):
+    c = AttnCase(2, H_q, 2, 64, [70, 0], 6, star, 32)
+    c.run()
+    torch.cuda.synchronize()
+    want = c.out.clone()
+    c.k_tree[0, :, 3] = value
+    c.out.fill_(1.0)
+    c.run()
+    torch.cuda.synchronize()
+    others = [0, 1, 2, 4, 5]
+    assert torch.equal(c.out[0, others].view(torch.int16), want[0, others].view(torch.int16))
+    assert torch.equal(c.out[1].view(torch.int16), want[1].view(torch.int16))
+
+
+def test_lengths_outside_the_capacity_are_taken_within_it():
+    c = AttnCase(3, 4, 2, 64, [64, 0, 20], 5, chain, 32, capacity=64)
+    c.run()
+    torch.cuda.synchronize()
+    want = c.out.clone()
+    c.prefix_len.copy_(i32([2 ** 31 - 1, -(2 ** 31), 20]))
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(c.out.view(torch.int16), want.view(torch.int16))
 
 
 def test_short_sequences_do_not_depend_on_the_capacity_named():

@@ -167,6 +167,32 @@ def test_values_that_are_no_numbers_and_rows_without_a_token():
     assert (np.isnan(got) == np.isnan(want)).all() and (np.isneginf(got) == np.isneginf(want)).all()
 
 
+def test_a_row_without_a_token_is_flagged_by_the_verification():
+    """Masked logits go into the verification as they are; a row that has none left is flagged there and the others are as ever."""
+    from paper_2401_06706_amd import device as D
+    from paper_2401_06706_amd import workloads as W
+    from tests.parity import run_oracle
+    vi = W.gen_verify_inputs(W.WORKLOADS["c2"].with_(B=2, V=600, variant=W.WITH_REPLACEMENT))
+    call = D.make_verify_call(vi)
+    rows = 1 + vi.N
+    mask = np.random.default_rng(0).random((2, rows, 600)) < 0.7
+    np.put_along_axis(mask[:, 1:], vi.cand_tok[..., None].astype(np.int64), True, -1)
+    mask[1, 0] = False
+    z = call.tensors["target_logits"]
+    M.mcsd_logits_rules(M.logits_args(z, z, call.tensors["parent"], call.tensors["cand_tok"], mask=dev(pack(mask))))
+    M.mcsd_verify_sample(call.args)
+    torch.cuda.synchronize()
+    got = call.results()
+    assert got["flags"][1, 0] & M.FLAG_NONFINITE and not (got["flags"][0] & M.FLAG_NONFINITE).any() and not (got["flags"][1, 1:] & M.FLAG_NONFINITE).any()
+    vi.target_logits[:] = z.cpu().numpy()
+    orc = run_oracle(vi)
+    ok = orc.margin >= 1e-6
+    ok[1, 0] = False
+    assert (got["acc_child"] == orc.acc_child)[ok].all() and (got["endpoint"] == orc.endpoint)[ok].all()
+    emitted = got["endpoint"][0]
+    assert all(mask[0, r, t] for r, t in enumerate(emitted) if t >= 0)
+
+
 def test_last_entry_of_a_token_counts():
     V, n = 100, 1000
     tok = np.random.default_rng(1).integers(0, V, size=(1, n)).astype(np.int32)
