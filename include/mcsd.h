@@ -433,8 +433,8 @@ typedef struct {
  * products exactly as what they stand for, accumulation is fp32, and the softmax weights enter PV as bf16.  Only the
  * pages that hold rows below prefix_len[b] are read, and rows at or past it do not count, whatever
  * they hold.  A table entry outside [0, n_pages) is a data error: its rows read as zeros.  What a node may not see
- * does not reach it, but for values of v_tree that are no numbers: those reach every row of their sequence and KV head.  How a
- * sequence's keys are split, and with it the last bits of its rows, follows the lengths of the whole batch. */
+ * does not reach it, whatever it holds.  How a sequence's keys are split, and with it the last bits of its rows, follows the lengths of
+ * the whole batch. */
 size_t mcsd_attn_fourbit_workspace_bytes(const mcsd_attn_desc *desc);
 int32_t mcsd_tree_attn_fourbit(const mcsd_attn_desc *desc, const mcsd_attn_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream);
 

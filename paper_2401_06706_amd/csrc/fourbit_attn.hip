@@ -203,11 +203,34 @@ __device__ __forceinline__ void fourbit_values(const uint32_t *v, int lj, int lc
     }
 }
 
+// Values of a node that are no numbers (padding of a tree may hold them) would reach, as 0 times NaN, the rows that may not see the
+// node: they enter the products as zeros, and finish adds them to the rows that see it, whatever its weight.  Bit 16 h + 15 of `odd`: half
+// h of a word was one.  (In whole words: an exponent of all ones carries into its half's top bit.)
+__device__ __forceinline__ u32x4 finite_of(u32x4 x, uint32_t *odd)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t top = ((x[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+        x[i] &= ~(top | (top - (top >> 15)));
+        *odd |= top;
+    }
+    return x;
+}
+
+// Rows of the lanes with a bit set, a lane's row being its number % 16.
+__device__ __forceinline__ uint32_t rows_with(uint32_t bits)
+{
+    const unsigned long long b = __ballot(bits != 0u);
+    const uint32_t h = (uint32_t)b | (uint32_t)(b >> 32);
+    return (h | h >> 16) & 0xffffu;
+}
+
 // The end of both kernels, 16 rows of every row group at a time: the key streams leave (m, l) and O in LDS (4 x 16 rows) and are added up
-// behind a barrier; a sequence in one segment is written out, others leave their partials in the workspace.
+// behind a barrier; a sequence in one segment is written out, others leave their partials in the workspace.  s_odd: nodes of this
+// segment's tree tiles with values that are no numbers.
 template <int DP, int RT, int RG>
 __device__ __forceinline__ void finish(const FourbitParams &p, const Segment &my, int g, int row_tile0, int tid, uint32_t *words, float (*s_m)[16], float (*s_l)[16],
-                                       const f32x4 (&oacc)[DP / 16][RT], const float (&m_used)[RT], const float (&l_part)[RT])
+                                       const uint32_t (*s_anc)[4], const uint32_t *s_odd, const f32x4 (&oacc)[DP / 16][RT], const float (&m_used)[RT], const float (&l_part)[RT])
 {
     constexpr int KS = 4 / RG, NNT = DP / 16, PO = DP + 4;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lj = lane >> 4, lc = lane & 15, b = my.b;
@@ -222,6 +245,8 @@ __device__ __forceinline__ void finish(const FourbitParams &p, const Segment &my
 #pragma unroll
         for (int nt = 0; nt < NNT; ++nt) *reinterpret_cast<f32x4 *>(area + (wave * 16 + lc) * PO + 16 * nt + 4 * lj) = oacc[nt][mt];
         __syncthreads();
+        const uint32_t any_odd = s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3];
+        const uint16_t *v_tree = static_cast<const uint16_t *>(p.v_tree) + ((size_t)b * p.H_kv + g) * p.N * p.d;
         // (a thread has the same four columns of several rows)
         constexpr int D4 = DP / 4, RSTEP = 256 / D4;
         const int d4 = tid % D4;
@@ -241,6 +266,18 @@ __device__ __forceinline__ void finish(const FourbitParams &p, const Segment &my
                 ls += f * s_l[w][r];
                 acc += f * *reinterpret_cast<const f32x4 *>(area + (w * 16 + r) * PO + 4 * d4);
             }
+            if (__builtin_amdgcn_readfirstlane(any_odd) != 0u)
+#pragma unroll 1
+                for (int i = 0; i < MCSD_MAX_NODES / KT; ++i)
+                    for (uint32_t seen = s_odd[i] & s_anc[row_node(p, gr)][i]; seen != 0u; seen &= seen - 1u) {
+                        const int node = i * KT + __ffs((int)seen) - 1;
+                        const u32x2 v = *reinterpret_cast<const u32x2 *>(v_tree + (uint32_t)(node * p.d + 4 * d4));
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t x = c & 1 ? v[c / 2] & 0xffff0000u : v[c / 2] << 16;
+                            acc[c] += __uint_as_float(x & (uint32_t)((int)((x & 0x7f800000u) + 0x00800000u) >> 31));
+                        }
+                    }
             if (my.n == 1) {
                 const float inv = 1.0f / ls;
                 __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(row_out(p, b, g, gr) + 4 * d4));
@@ -273,6 +310,7 @@ void attn_fourbit_kernel(FourbitParams p)
     __shared__ uint32_t s_anc[MCSD_MAX_NODES][4];
     __shared__ int s_parent[MCSD_MAX_NODES];
     __shared__ float s_m[4][16], s_l[4][16];
+    __shared__ uint32_t s_odd[MCSD_MAX_NODES / KT + 1];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -304,6 +342,7 @@ void attn_fourbit_kernel(FourbitParams p)
             qreg[mt][kk] = __builtin_bit_cast(bf16x8, v);
         }
     }
+    if (tid <= MCSD_MAX_NODES / KT) s_odd[tid] = 0u;
     build_ancestor_masks(p, my_parent, s_anc, s_parent);
     __syncthreads();
 
@@ -428,6 +467,7 @@ void attn_fourbit_kernel(FourbitParams p)
             for (int mt = 0; mt < RT; ++mt) vis[mt] = left >= KT ? ~0u : (1u << (left & 31)) - 1u;
         } else {
             const size_t head = ((size_t)b * p.H_kv + g) * p.N;
+            uint32_t odd = 0u;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int node = (t - tiles_prefix) * KT + 16 * s + lc;
@@ -436,10 +476,13 @@ void attn_fourbit_kernel(FourbitParams p)
                     if (node < p.N && run_col(kk & ~3) < p.d) x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(from) + (head + node) * p.d + run_col(kk));
                     return x;
                 };
+                uint32_t bits = 0u;
 #pragma unroll
-                for (int kk = 0; kk < NKK; ++kk) *reinterpret_cast<u32x4 *>(vt + (16 * s + lc) * PV + run_col(kk) / 2) = of_tree(p.v_tree, kk);
+                for (int kk = 0; kk < NKK; ++kk) *reinterpret_cast<u32x4 *>(vt + (16 * s + lc) * PV + run_col(kk) / 2) = finite_of(of_tree(p.v_tree, kk), &bits);
+                odd |= rows_with(bits) << (16 * s);
                 scores(s, [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, of_tree(p.k_tree, kk)); });
             }
+            s_odd[t - tiles_prefix] = odd;              // (all lanes the same)
 #pragma unroll
             for (int mt = 0; mt < RT; ++mt) vis[mt] = s_anc[row_node(p, min(16 * mt + lc, p.M - 1))][t - tiles_prefix];
         }
@@ -461,7 +504,7 @@ void attn_fourbit_kernel(FourbitParams p)
         any(stage0());
         if (NST > 1 && t < t_end) any(stage1());
     }
-    finish<DP, RT, 1>(p, my, g, 0, tid, s_big, s_m, s_l, oacc, m_used, l_part);
+    finish<DP, RT, 1>(p, my, g, 0, tid, s_big, s_m, s_l, s_anc, s_odd, oacc, m_used, l_part);
 }
 
 // 16 or 4 bytes per lane from base + offset straight into LDS, lane after lane from byte `to` on.  No register is written.  Written as text
@@ -507,6 +550,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     __shared__ uint32_t s_anc[MCSD_MAX_NODES][4];
     __shared__ int s_parent[MCSD_MAX_NODES];
     __shared__ float s_m[4][16], s_l[4][16];
+    __shared__ uint32_t s_odd[MCSD_MAX_NODES / KT + 1];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -578,6 +622,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
             qreg[mt][kk] = __builtin_bit_cast(bf16x8, v);
         }
     }
+    if (tid <= MCSD_MAX_NODES / KT) s_odd[tid] = 0u;
     build_ancestor_masks(p, my_parent, s_anc, s_parent);
 
     f32x4 oacc[NNT][RT];
@@ -717,8 +762,11 @@ void attn_fourbit_shared_kernel(FourbitParams p)
             }
         } else {
             const int node = tv < t_end ? (tv - tiles_prefix) * KT + v_row : p.N;
+            uint32_t bits = 0u;
 #pragma unroll
-            for (int kk = 0; kk < NKK; ++kk) *reinterpret_cast<u32x4 *>(vrow + run_col(kk) / 2) = of_tree(p.v_tree, node, kk);
+            for (int kk = 0; kk < NKK; ++kk) *reinterpret_cast<u32x4 *>(vrow + run_col(kk) / 2) = finite_of(of_tree(p.v_tree, node, kk), &bits);
+            const uint32_t odd = rows_with(bits);
+            reinterpret_cast<uint16_t *>(s_odd)[2 * (tv - tiles_prefix) + (wave & 1)] = (uint16_t)odd;        // (all lanes the same; past t_end: one tile, zeros)
         }
         if (active) {
 #pragma unroll
@@ -753,7 +801,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     if (active && t_begin < t_end) values(vbuf + (buf ^ 1) * VBUF_WORDS);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (nothing may still be on its way into what follows)
 
-    finish<DP, RT, RG>(p, my, g, row_tile0, tid, s_big, s_m, s_l, oacc, m_used, l_part);
+    finish<DP, RT, RG>(p, my, g, row_tile0, tid, s_big, s_m, s_l, s_anc, s_odd, oacc, m_used, l_part);
 }
 
 // A thread per four columns of a row, ROWS rows of a (sequence, KV head) per workgroup.

@@ -331,6 +331,37 @@ def test_keys_that_a_node_may_not_see_do_not_reach_it(value, H_q):
     assert torch.equal(c.out[1].view(torch.int16), want[1].view(torch.int16))
 
 
+@pytest.mark.parametrize("d", [32, 128, 256])
+@pytest.mark.parametrize("H_q", [4, 10, 20, 40, 60])
+@pytest.mark.parametrize("lens", [[70, 0], [64, 3000]])
+def test_values_that_are_no_numbers_reach_the_nodes_that_see_them(d, H_q, lens):
+    def tree(n):                        # 0 <- 1 <- ... <- 5, and 6 ... 39 of the root
+        return np.array([max(i - 1, -1) if i < 6 else -1 for i in range(n)], np.int32)
+    c = AttnCase(2, H_q, 2, d, lens, 40, tree, 32, capacity=6000)
+    c.run()
+    torch.cuda.synchronize()
+    want = c.out.clone()
+    put = {(3, 0): float("nan"), (4, d - 1): float("inf"), (5, d - 1): float("-inf"), (35, 7): float("-inf"), (39, 9): float("nan")}
+    for (n, col), v in put.items():
+        c.v_tree[:, 0, n, col] = v
+    c.out.fill_(1.0)
+    c.run()
+    torch.cuda.synchronize()
+    want, got = want.float().cpu(), c.out.float().cpu()
+    of_head = slice(0, H_q // 2)
+    for n in range(3, 6):
+        want[:, n, of_head, 0] = float("nan")
+    want[:, 4, of_head, d - 1], want[:, 5, of_head, d - 1] = float("inf"), float("nan")
+    want[:, 35, of_head, 7], want[:, 39, of_head, 9] = float("-inf"), float("nan")
+    hit = ~torch.isfinite(want)
+    assert ((got == want) | (got.isnan() & want.isnan()))[hit].all()
+    # rows that see one of them lose its share in its column alone; every other row is the same to the bit
+    assert torch.isfinite(got[~hit]).all()
+    unseen = [n for n in range(40) if n not in (3, 4, 5, 35, 39)]
+    assert torch.equal(got[:, unseen], want[:, unseen]) and torch.equal(got[:, :, H_q // 2:], want[:, :, H_q // 2:])
+    assert torch.equal(got[~hit], want[~hit])
+
+
 def test_lengths_outside_the_capacity_are_taken_within_it():
     c = AttnCase(3, 4, 2, 64, [64, 0, 20], 5, chain, 32, capacity=64)
     c.run()
