@@ -305,6 +305,43 @@ def test_pages_outside_the_pool_read_as_zeros():
     c.check()
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("H_q", [10, 20, 40])              # 30, 60 and 120 rows per KV head
+def test_pages_outside_the_pool_with_more_rows(H_q, d):
+    c = AttnCase(2, H_q, 2, d, [500, 1100], 6, random_tree, 64)
+    c.table[0, 0], c.table[0, 3], c.table[0, 7] = -1, c.n_pages, 2 ** 31 - 1        # the last: 52 rows of a page
+    c.table[1, 5], c.table[1, 6] = -(2 ** 31), c.n_pages + 100
+    c.cache.keep[4].copy_(i32(c.table))
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("H, N, d, keys, ps", [(448, 1, 32, 8500, 96), (448, 20, 64, 8300, 32), (450, 40, 64, 4500, 32), (225, 70, 128, 4300, 64)])
+def test_long_sequences_that_stay_whole(H, N, d, keys, ps):
+    """More steps per workgroup than block-table entries are held at once; some of the heads against 64 bits."""
+    c = AttnCase(1, H, H, d, [keys], N, random_tree, ps)
+    c.run()
+    torch.cuda.synchronize()
+    some = [0, 1, H // 2, H - 1]
+    table = c.table[0, :-(-keys // ps)]
+    k, v = (F.pool_rows(c.pools[i][:, some].cpu().numpy(), c.pools[i + 1][:, some].cpu().numpy()) for i in (0, 2))
+    k, v = (np.concatenate([x[t] for t in table], 1)[:, :keys] for x in (k, v))
+    want, bound = F.attention(f64(c.q[0][:, some]), k, v, f64(c.k_tree[0][some]), f64(c.v_tree[0][some]), F.ancestors(c.parents[0]), c.scale)
+    assert (np.abs(f64(c.out[0][:, some]) - want) <= bound).all()
+    assert torch.isfinite(c.out).all()
+
+
+@pytest.mark.parametrize("H_q", [20, 40])
+def test_blocks_that_are_no_numbers_reach_their_head_alone(H_q):
+    c = AttnCase(2, H_q, 2, 128, [200, 100], 6, chain, 32)
+    c.pools[3][c.table[0, 3], 1, 1, 0, 5] = 255           # a value block of KV head 1: its 32 columns
+    c.run()
+    torch.cuda.synchronize()
+    got = f64(c.out)
+    assert np.isnan(got[0, :, H_q // 2:, :32]).all() and np.isfinite(got[0, :, H_q // 2:, 32:]).all()
+    assert np.isfinite(got[0, :, :H_q // 2]).all() and np.isfinite(got[1]).all()
+
+
 def test_a_block_that_is_no_number_reaches_its_head_alone():
     c = AttnCase(2, 4, 2, 128, [200, 100], 6, chain, 32)
     pg, r = c.table[0, 50 // 32], 50 % 32
