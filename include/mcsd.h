@@ -449,7 +449,7 @@ int32_t mcsd_kv_commit_fourbit(const mcsd_commit_desc *desc, const mcsd_commit_b
  * to differ from each other (two rows for one slot leave a mixture of both). */
 typedef struct {
     uint32_t struct_size;
-    int32_t T;              /* tokens, >= 0 */
+    int32_t T;              /* tokens, 0 <= T; T H_kv d < 2^35 */
     int32_t H_kv;
     int32_t d;              /* multiple of 32, <= MCSD_MAX_HEAD_DIM */
     int32_t dtype;          /* MCSD_DTYPE_* of k and v */
@@ -493,7 +493,7 @@ typedef struct {
     int32_t page_size;              /* tokens per page, >= 1 */
     int32_t n_pages;                /* pages in the pool, n_pages * page_size < 2^31 */
     int32_t max_pages_per_seq;      /* row length of block_table */
-    int32_t max_slots;              /* length of slot_map (0 with slot_map = NULL) */
+    int32_t max_slots;              /* length of slot_map, <= 2^30 (0 with slot_map = NULL) */
 } mcsd_page_desc;
 
 typedef struct {

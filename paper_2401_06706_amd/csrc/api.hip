@@ -440,7 +440,8 @@ static int32_t check_rows(const mcsd_rows_desc *d, const mcsd_rows_bufs *b, cons
     if (d->dtype != MCSD_DTYPE_FP32 && d->dtype != MCSD_DTYPE_BF16) { set_error("rows: unknown dtype %d", d->dtype); return MCSD_E_UNSUPPORTED; }
     const int32_t rc = check_fourbit(kv, d->d, -1);
     if (rc != MCSD_OK) return rc;
-    if (d->n_layers > 65535 || d->T > (1 << 30) || d->H_kv > 65535 || ((long)d->T + 3) / 4 * d->H_kv * (d->d / 32) > 0x7fffffffL * 16) { set_error("rows: grid too large"); return MCSD_E_UNSUPPORTED; }
+    // (a launch has fewer than 2^32 threads)
+    if (d->n_layers > 65535 || d->T > (1 << 30) || d->H_kv > 65535 || ((long)d->T + 3) / 4 * d->H_kv * (d->d / 32) >= 1L << 28) { set_error("rows: grid too large"); return MCSD_E_UNSUPPORTED; }
     const int64_t row = (int64_t)d->H_kv * d->d, per16 = d->dtype == MCSD_DTYPE_FP32 ? 4 : 8;
     if (d->k_stride < row || d->v_stride < row) { set_error("rows: a stride is less than a row"); return MCSD_E_SHAPE; }
     if (d->k_stride % per16 != 0 || d->v_stride % per16 != 0) { set_error("rows: strides must be multiples of 16 bytes"); return MCSD_E_SHAPE; }
@@ -474,7 +475,7 @@ int32_t mcsd_page_assign(const mcsd_page_desc *d, const mcsd_page_bufs *b, void 
     if (!d) { set_error("page desc is NULL"); return MCSD_E_NULL; }
     if (d->struct_size != sizeof(mcsd_page_desc)) { set_error("page desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_page_desc)); return MCSD_E_SHAPE; }
     if (d->B < 1 || d->page_size < 1 || d->n_pages < 1 || d->max_pages_per_seq < 1 || d->max_slots < 0) { set_error("pages: non-positive size"); return MCSD_E_SHAPE; }
-    if (d->B > 65535) { set_error("pages: B %d > 65535", d->B); return MCSD_E_UNSUPPORTED; }
+    if (d->B > 65535 || d->max_slots > (1 << 30)) { set_error("pages: B %d > 65535 or max_slots %d > %d", d->B, d->max_slots, 1 << 30); return MCSD_E_UNSUPPORTED; }
     if ((long)d->n_pages * d->page_size > 0x7fffffffL) { set_error("pages: n_pages * page_size does not fit a slot"); return MCSD_E_UNSUPPORTED; }
     if (!b) { set_error("page bufs is NULL"); return MCSD_E_NULL; }
     if (b->struct_size != sizeof(mcsd_page_bufs)) { set_error("page bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_page_bufs)); return MCSD_E_SHAPE; }

@@ -100,7 +100,7 @@ def test_rows_refusals(lib, name):
     bufs = lambda **kw: M.RowsBufs(*{**dict(size=C.sizeof(M.RowsBufs), k=4096, v=4096, slots=4096), **kw}.values())
     call = lambda d, b, k: getattr(lib, name)(None if d is None else C.byref(d), None if b is None else C.byref(b), None if k is None else C.byref(k), None)
     for kw, code in [(dict(T=-1), -2), (dict(H_kv=0), -2), (dict(n_layers=0), -2), (dict(dtype=2), -3), (dict(d=16), -3), (dict(d=288), -3), (dict(d=100), -3),
-                     (dict(ks=255), -2), (dict(vs=128), -2), (dict(ks=260), -2), (dict(dtype=0, ks=258), -2), (dict(n_layers=70000), -3), (dict(T=2 ** 30 + 1), -3),
+                     (dict(ks=255), -2), (dict(vs=128), -2), (dict(ks=260), -2), (dict(dtype=0, ks=258), -2), (dict(n_layers=70000), -3), (dict(T=2 ** 30 + 1), -3), (dict(T=2 ** 27, H_kv=2, d=128), -3), (dict(T=2 ** 20, H_kv=1024, d=32, ks=2 ** 15, vs=2 ** 15), -3),
                      (dict(n_layers=2, kl=1283), -2), (dict(n_layers=2, vl=-1280), -2)]:
         assert call(desc(**kw), bufs(), kv(table=None)) == code, kw
     for kw, code in BAD_KV:
@@ -116,7 +116,7 @@ def test_page_refusals(lib):
     names = [n for n, _ in M.PageBufs._fields_[1:]]
     bufs = lambda **kw: M.PageBufs(C.sizeof(M.PageBufs), *{**{n: 4096 for n in names}, **kw}.values())
     call = lambda d, b: lib.mcsd_page_assign(None if d is None else C.byref(d), None if b is None else C.byref(b), None)
-    for kw, code in [(dict(B=0), -2), (dict(B=65536), -3), (dict(page_size=0), -2), (dict(n_pages=0), -2), (dict(max_pages=0), -2), (dict(max_slots=-1), -2),
+    for kw, code in [(dict(B=0), -2), (dict(B=65536), -3), (dict(page_size=0), -2), (dict(n_pages=0), -2), (dict(max_pages=0), -2), (dict(max_slots=-1), -2), (dict(max_slots=2 ** 30 + 1), -3), (dict(max_slots=2 ** 31 - 1), -3),
                      (dict(n_pages=1 << 25), -3)]:
         assert call(desc(**kw), bufs()) == code, kw
     for n in names:
