@@ -441,7 +441,7 @@ static int32_t check_rows(const mcsd_rows_desc *d, const mcsd_rows_bufs *b, cons
     const int32_t rc = check_fourbit(kv, d->d, -1);
     if (rc != MCSD_OK) return rc;
     // (a launch has fewer than 2^32 threads)
-    if (d->n_layers > 65535 || d->T > (1 << 30) || d->H_kv > 65535 || ((long)d->T + 3) / 4 * d->H_kv * (d->d / 32) >= 1L << 28) { set_error("rows: grid too large"); return MCSD_E_UNSUPPORTED; }
+    if (d->n_layers > 65535 || d->T > (1 << 30) || d->H_kv > 65535 || ((long)d->T + 15) / 16 * d->H_kv * (d->d / 32) >= 1L << 26) { set_error("rows: grid too large"); return MCSD_E_UNSUPPORTED; }
     const int64_t row = (int64_t)d->H_kv * d->d, per16 = d->dtype == MCSD_DTYPE_FP32 ? 4 : 8;
     if (d->k_stride < row || d->v_stride < row) { set_error("rows: a stride is less than a row"); return MCSD_E_SHAPE; }
     if (d->k_stride % per16 != 0 || d->v_stride % per16 != 0) { set_error("rows: strides must be multiples of 16 bytes"); return MCSD_E_SHAPE; }
