@@ -16,7 +16,8 @@ struct RowsParams {
 
 // Bound by memory.  Four lanes a block, eight values each; a wavefront takes TOKENS tokens x 2 blocks of a head: 128-byte
 // pieces of a bf16 row, and 128-byte runs of codes where the tokens' slots follow each other.  16384 tokens of 8 heads of 128 (85 MB a
-// call): 4 tokens store 17.9, load 16.7 us; 8: 17.6, 14.3; 16: 17.4, 14.3 (from caches; with inputs that take turns 25 and 17.5).
+// call): 4 tokens store 17.9, load 16.7 us; 8: 17.6, 14.3; 16: 17.4, 14.3 (from caches; with inputs that take turns 25.0 and 15.4, and
+// 27.5 and 32.4 where a thread of the store takes two or four blocks, all of their loads ahead).
 // grid (units / 64 per workgroup of 256, 1, layers); unit = ((token / TOKENS) H_kv n_blocks + head n_blocks + block) TOKENS + token % TOKENS.
 constexpr int TOKENS = 8;
 

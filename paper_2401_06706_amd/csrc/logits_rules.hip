@@ -26,6 +26,8 @@ struct RuleParams {
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));          // four values that start anywhere
 typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
 
+// Bound by memory: 976 rows of 32000 in fp32, one token in 50 allowed: 61 us for 209 MB (84 read, 125 written), 3.4 TB/s; 254 MB
+// if all were read, 4.2.  One sequence, 29 rows of 50001 in bf16: 7 us, launch and the history's count.
 // grid (slices of the vocabulary, groups of tree rows, sequences).  A workgroup counts the sequence's history once, in
 // LDS, for the 1024 tokens of its slice, keeps what the rules ask of a thread's four tokens in registers and then goes through
 // its tree rows, AHEAD of them at a time: their mask words, then those logits that are not masked throughout, then the rules.  The

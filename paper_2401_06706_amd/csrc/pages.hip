@@ -125,8 +125,8 @@ __device__ __forceinline__ void take(const PageParams &p, const Request &r, bool
 
 // One workgroup: the stack's bookkeeping is running sums over the sequences.  NT threads, one sequence each where they are enough, which then costs a trip to
 // memory for the lengths, two pairs of sums, and a trip each for pages that come back and that go out (1024
-// sequences, 16 wavefronts: 14 us; a form that went over the sequences three times, a sum at a time, 18.5; 16 sequences in one
-// wavefront, no barrier).  SLOTS: the slot map too, where it is short: a launch of its own is 4 us.
+// sequences, 16 wavefronts: 11 us; a form that went over the sequences three times, a sum at a time, 15; 16 sequences in one
+// wavefront, no barrier, 4.1).  SLOTS: the slot map too, where it is short: a launch of its own is 4 us.
 template <int NT, bool SLOTS>
 __global__ __launch_bounds__(NT) void page_assign_kernel(PageParams p)
 {

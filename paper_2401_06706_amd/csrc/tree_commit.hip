@@ -238,7 +238,9 @@ __global__ __launch_bounds__(64 * COMMIT_WAVES) void kv_commit_kernel(CommitPara
     }
 }
 
-// The same two forms of the commit into a cache held in 4 bits.  A row (all KV heads, K and V) in units of eight
+// The same two forms of the commit into a cache held in 4 bits.  Bound by the launch and three dependent trips to memory (what is
+// committed, the rows, where they go): 5.7 us for one sequence, 11 us (and 3 for the
+// finish) for 16 of 8 heads and 32 layers, 24 MB.  (Several layers per workgroup: 10.2 us for 9.7.)  A row (all KV heads, K and V) in units of eight
 // values, four neighbouring threads a block; `first` and `step` are multiples of four apart from the unit's quarter.
 __device__ __forceinline__ void commit_row_fourbit(const CommitParams &p, int layer, int b, int src_row, int page, int page_row, int first, int step)
 {
