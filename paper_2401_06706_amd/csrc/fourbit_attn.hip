@@ -15,7 +15,7 @@
 //
 // Measured (inputs that take turns, d = 128): single tokens, 32 sequences of 100 to 8000 keys, 32 heads over 8: 39.4 us for 146 MB, 3.7 TB/s (32 us and
 // 4.5 TB/s where part of it is still in a cache; 6.2 per further byte), bound by memory and the launch's ends.  16 sequences of 256
-// to 4096 keys, 32 heads, 60 nodes: 75 us for 197 MB, 2.6 TB/s and 0.50 PFLOP/s.  4 sequences of 16384, 64 heads over 8, 84 nodes: 229 us, 0.79 PFLOP/s.  These
+// to 4096 keys, 32 heads, 60 nodes: 72.5 us for 197 MB, 2.7 TB/s and 0.52 PFLOP/s.  4 sequences of 16384, 64 heads over 8, 84 nodes: 229 us, 0.79 PFLOP/s.  These
 // two are bound by the instructions between the products: matrix instructions 29 and 37 % of the cycles, vector ones 49 and 48 %, and a wavefront's are not
 // free of each other (products of a step without softmax, conversions or V's reads: 47 to 50 of 53 us for 4096 keys more).
 #include <algorithm>
@@ -811,9 +811,9 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     finish<DP, RT, RG>(p, my, g, row_tile0, tid, s_big, s_m, s_l, s_anc, s_odd, oacc, m_used, l_part);
 }
 
-// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Bound by the launch and two trips to memory: 4.7 us for single tokens, 8.9 and
-// 12.8 (23 MB of partials) in the larger cases above.
-// A thread per four columns of a row, ROWS rows of a (sequence, KV head) per workgroup.
+// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Bound by the launch and two trips to memory: 4.7 us for single tokens, 4.0 to 4.7 where nothing is
+// cut and 12.8 for 45 MB of partials in the larger cases above.
+// A thread per four columns of a row, ROWS rows of a (sequence, KV head) at a time per workgroup.
 template <int DP>
 __global__ __launch_bounds__(256) void attn_fourbit_combine_kernel(FourbitParams p)
 {
@@ -821,39 +821,41 @@ __global__ __launch_bounds__(256) void attn_fourbit_combine_kernel(FourbitParams
     const int g = blockIdx.y;
     const Segment my = find_segment(p, blockIdx.z, true, threadIdx.x & 63);
     if (my.n <= 1) return;
-    const int d4 = threadIdx.x % D4, r = blockIdx.x * ROWS + threadIdx.x / D4;
-    if (r >= p.M || 4 * d4 >= p.d) return;
-    const size_t u0 = ((size_t)my.first * p.H_kv + g) * (size_t)p.R + r, step = (size_t)p.H_kv * p.R;
-    float ms = M_INIT, ls = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    // eight segments at a time, all of them requested before the first is used (those past the end are the first again, without weight)
-    for (int s0 = 0; s0 < my.n; s0 += 8) {
-        float m[8], l[8];
-        f32x4 o[8];
+    const int d4 = threadIdx.x % D4;
+    if (4 * d4 >= p.d) return;
+    for (int r = blockIdx.x * ROWS + threadIdx.x / D4; r < p.M; r += gridDim.x * ROWS) {
+        const size_t u0 = ((size_t)my.first * p.H_kv + g) * (size_t)p.R + r, step = (size_t)p.H_kv * p.R;
+        float ms = M_INIT, ls = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        // eight segments at a time, all of them requested before the first is used (those past the end are the first again, without weight)
+        for (int s0 = 0; s0 < my.n; s0 += 8) {
+            float m[8], l[8];
+            f32x4 o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool on = s0 + i < my.n;
-            const size_t u = u0 + (on ? s0 + i : 0) * step;
-            m[i] = on ? p.part_m[u] : M_INIT;
-            l[i] = on ? p.part_l[u] : 0.f;
-            o[i] = *reinterpret_cast<const f32x4 *>(p.part_o + u * p.d + 4 * d4);
+            for (int i = 0; i < 8; ++i) {
+                const bool on = s0 + i < my.n;
+                const size_t u = u0 + (on ? s0 + i : 0) * step;
+                m[i] = on ? p.part_m[u] : M_INIT;
+                l[i] = on ? p.part_l[u] : 0.f;
+                o[i] = *reinterpret_cast<const f32x4 *>(p.part_o + u * p.d + 4 * d4);
+            }
+            float m_new = ms;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m_new = fmaxf(m_new, m[i]);
+            const float keep = fast_exp2(ms - m_new);
+            ls *= keep;
+            acc *= keep;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float f = s0 + i < my.n ? fast_exp2(m[i] - m_new) : 0.f;
+                ls += f * l[i];
+                acc += f * o[i];
+            }
+            ms = m_new;
         }
-        float m_new = ms;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m_new = fmaxf(m_new, m[i]);
-        const float keep = fast_exp2(ms - m_new);
-        ls *= keep;
-        acc *= keep;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float f = s0 + i < my.n ? fast_exp2(m[i] - m_new) : 0.f;
-            ls += f * l[i];
-            acc += f * o[i];
-        }
-        ms = m_new;
+        const float inv = 1.0f / ls;
+        __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(row_out(p, my.b, g, r) + 4 * d4));
     }
-    const float inv = 1.0f / ls;
-    __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(row_out(p, my.b, g, r) + 4 * d4));
 }
 
 size_t round_256(size_t n) { return (n + 255) / 256 * 256; }
@@ -958,7 +960,14 @@ int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, co
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("attn_fourbit launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     if (plan.n_segments_max == 1) return MCSD_OK;
-    auto merge = [&](auto kernel, int rows) { launch_kernel(K_ATTN_FOURBIT_COMBINE, kernel, dim3((p.M + rows - 1) / rows, d.H_kv, d.B), dim3(256), stream, p); };
+    // (Where sequences are cut only far beyond the average most or all are whole: no more workgroups than start at once look whether there is
+    // something to merge.  16 x 32 heads of 60 rows, none cut: 4.0 us, with a workgroup per eight rows 7.6; one of 16000 keys among 15 of 300:
+    // 13.0, 9.4; 60 x 8 heads of 64 rows, 6 of 8000 among 54 of 500: 10.7, 17.6.)
+    auto merge = [&](auto kernel, int rows) {
+        int groups = (p.M + rows - 1) / rows;
+        if (plan.bias == 0.f) groups = std::max(1, std::min(groups, 1024 / (d.H_kv * d.B)));
+        launch_kernel(K_ATTN_FOURBIT_COMBINE, kernel, dim3(groups, d.H_kv, d.B), dim3(256), stream, p);
+    };
     if (d.d > 128) merge(attn_fourbit_combine_kernel<256>, 4);
     else if (d.d > 64) merge(attn_fourbit_combine_kernel<128>, 8);
     else merge(attn_fourbit_combine_kernel<64>, 16);
