@@ -430,8 +430,8 @@ typedef struct {
 /* mcsd_tree_attn over a prefix held in 4 bits: q, k_tree, v_tree and out as there, the prefix as written by the
  * calls below; bufs->k_prefix and bufs->v_prefix are ignored.  bf16 only (MCSD_E_UNSUPPORTED otherwise),
  * d a multiple of 32.  A lone token per sequence is a tree of one node.  Prefix keys and values enter the
- * products exactly as what they stand for, accumulation is fp32, and the softmax weights enter PV as bf16.  Only the
- * pages that hold rows below prefix_len[b] are read, and rows at or past it do not count, whatever
+ * products exactly as what they stand for, accumulation is fp32, and the softmax weights enter PV as in mcsd_tree_attn (bf16 for
+ * d == 128, two bf16 terms, at most 2^-17 off, for other d).  Only the pages that hold rows below prefix_len[b] are read, and rows at or past it do not count, whatever
  * they hold.  A table entry outside [0, n_pages) is a data error: its rows read as zeros.  What a node may not see
  * does not reach it, whatever it holds.  How a sequence's keys are split, and with it the last bits of its rows, follows the lengths of
  * the whole batch. */

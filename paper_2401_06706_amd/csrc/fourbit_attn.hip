@@ -132,10 +132,14 @@ __device__ __forceinline__ uint32_t all_of(uint32_t keys, int i) { return (uint3
 
 // Weights of NS parts of 16 keys with the running maximum as it stands, tested by their sum: only where that is large (or the first
 // scores come) the maximum is looked for and raised.  keys_of(mt, s): the keys of part s that count for the lane's row, the
-// lowest four bits (MASKED; a masked score can not be told by its value where scale is 0).  Weights enter PV as bf16, at most 2^-8 of each
-// off, as the framework's kernels for d = 128 have it; their sum is of the unrounded ones.
-template <int DP, int RT, int NS, bool MASKED, typename KeysOf>
-__device__ __forceinline__ void fourbit_softmax(float c2, const f32x4 (&sacc)[NS][RT], u32x2 (&pw)[NS][RT], f32x4 (&oacc)[DP / 16][RT], float (&m_used)[RT],
+// lowest four bits (MASKED; a masked score can not be told by its value where scale is 0).  Weights enter PV as TERMS bf16 terms each, their
+// sum is of the unrounded ones.  As in the framework's attention over caches of full precision: one at d = 128, at most 2^-8 of the weight off, two at
+// other d (the nearest bf16 and the nearest to what it leaves; what is not a number never meets them, see finite_of), at most 2^-17 off.  What the second
+// costs (us, one / two; 64 rows at a time where the weights have two, see variant_of): d 64, one token, 32 x 100-8000 keys 26.9 / 28.4, 16 x 8 heads of 60 rows
+// 27.8 / 30.6, 8 x 8 of 84 rows 25.8 / 25.3, 4 x 8 of 336 rows and 8000 keys 48.2 / 61.1; d 96, one token 18.7 / 19.5, 16 x 16 of 60 rows 48.1 / 57.2; d 256,
+// one token 24.2 / 25.1, 8 x 16 of 60 rows 85.4 / 91.9.  At d = 128 16 x 32 of 60 rows would be 70.5 / 87.1.
+template <int DP, int RT, int NS, int TERMS, bool MASKED, typename KeysOf>
+__device__ __forceinline__ void fourbit_softmax(float c2, const f32x4 (&sacc)[NS][RT], u32x2 (&pw)[TERMS][NS][RT], f32x4 (&oacc)[DP / 16][RT], float (&m_used)[RT],
                                                 float (&l_part)[RT], KeysOf keys_of)
 {
     float sum[RT];
@@ -154,7 +158,14 @@ __device__ __forceinline__ void fourbit_softmax(float c2, const f32x4 (&sacc)[NS
                     for (int i = 0; i < 4; ++i) pv[i] = __uint_as_float(__float_as_uint(pv[i]) & all_of(keys, i));
                 }
                 sum[mt] += (pv[0] + pv[1]) + (pv[2] + pv[3]);
-                pw[s][mt] = (u32x2){pack_bf16(pv[0], pv[1]), pack_bf16(pv[2], pv[3])};
+                const u32x2 hi = {pack_bf16(pv[0], pv[1]), pack_bf16(pv[2], pv[3])};
+                pw[0][s][mt] = hi;
+                if constexpr (TERMS == 2) {
+                    float lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) lo[i] = pv[i] - __uint_as_float(i & 1 ? hi[i / 2] & 0xffff0000u : hi[i / 2] << 16);
+                    pw[1][s][mt] = (u32x2){pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3])};
+                }
             }
         }
     };
@@ -191,9 +202,9 @@ __device__ __forceinline__ void fourbit_softmax(float c2, const f32x4 (&sacc)[NS
     for (int mt = 0; mt < RT; ++mt) l_part[mt] += sum[mt];
 }
 
-// O^T += V^T P^T of a tile: V as rows in LDS, read back transposed; w0, w1 the weights of its two parts.
-template <int DP, int RT>
-__device__ __forceinline__ void fourbit_values(const uint32_t *v, int lj, int lc, const u32x2 (&w0)[RT], const u32x2 (&w1)[RT], f32x4 (&oacc)[DP / 16][RT])
+// O^T += V^T P^T of a tile: V as rows in LDS, read back transposed; the weights of its two parts are 2 j and 2 j + 1 of pw.
+template <int DP, int RT, int NS, int TERMS>
+__device__ __forceinline__ void fourbit_values(const uint32_t *v, int lj, int lc, const u32x2 (&pw)[TERMS][NS][RT], int j, f32x4 (&oacc)[DP / 16][RT])
 {
     constexpr int PV = DP / 2 + 8;
     const uint32_t *vl = v + (4 * lj + (lc >> 2)) * PV + (lc & 3) * 2;
@@ -203,10 +214,13 @@ __device__ __forceinline__ void fourbit_values(const uint32_t *v, int lj, int lc
         const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(vl + 16 * PV + nt * 8));
         const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int mt = 0; mt < RT; ++mt) {
-            const u32x4 w = {w0[mt][0], w0[mt][1], w1[mt][0], w1[mt][1]};
-            oacc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, __builtin_bit_cast(bf16x8, w), oacc[nt][mt], 0, 0, 0);
-        }
+        for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+            for (int mt = 0; mt < RT; ++mt) {
+                const u32x2 w0 = pw[term][2 * j][mt], w1 = pw[term][2 * j + 1][mt];
+                const u32x4 w = {w0[0], w0[1], w1[0], w1[1]};
+                oacc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, __builtin_bit_cast(bf16x8, w), oacc[nt][mt], 0, 0, 0);
+            }
     }
 }
 
@@ -299,7 +313,7 @@ __device__ __forceinline__ void finish(const FourbitParams &p, const Segment &my
 
 // DP: d padded to 64, 128 or 256.  Up to 16 RT query rows, all of them by every wavefront, which takes every fourth tile and needs no
 // barrier in its loop.
-template <int DP, int RT>
+template <int DP, int RT, int TERMS>
 __global__ __launch_bounds__(256, 2)
 void attn_fourbit_kernel(FourbitParams p)
 {
@@ -364,7 +378,7 @@ void attn_fourbit_kernel(FourbitParams p)
     }
     const float c2 = p.scale_log2;
 
-    u32x2 pw[2][RT];
+    u32x2 pw[TERMS][2][RT];
     f32x4 sacc[2][RT];
     uint32_t *const vt = s_big + ks * TILE_WORDS;
     auto scores = [&](int s, auto k_of) __attribute__((always_inline)) {
@@ -378,9 +392,9 @@ void attn_fourbit_kernel(FourbitParams p)
         }
     };
     auto softmax = [&](auto masked, auto keys_of) __attribute__((always_inline)) {
-        fourbit_softmax<DP, RT, 2, decltype(masked)::value>(c2, sacc, pw, oacc, m_used, l_part, keys_of);
+        fourbit_softmax<DP, RT, 2, TERMS, decltype(masked)::value>(c2, sacc, pw, oacc, m_used, l_part, keys_of);
     };
-    auto values = [&]() __attribute__((always_inline)) { fourbit_values<DP, RT>(vt, lj, lc, pw[0], pw[1], oacc); };
+    auto values = [&]() __attribute__((always_inline)) { fourbit_values<DP, RT>(vt, lj, lc, pw, 0, oacc); };
 
     // Codes and scales of a wavefront's tiles of the next NST steps are on their way while it works on the present one.  The
     // block-table entries of 64 of them are read at once, a lane each (an entry read by itself ahead of its use was
@@ -536,7 +550,7 @@ __device__ __forceinline__ void fetch4(uint32_t to, const uint8_t *base, uint32_
 //     rows in LDS for the transposing load.
 //   - PV runs a step behind the scores: the one barrier of a step then stands between both the codes' arrival and their
 //     readers, and the V of the last step and its readers.
-template <int DP, int RT, int RG>
+template <int DP, int RT, int RG, int TERMS>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2)
 void attn_fourbit_shared_kernel(FourbitParams p)
 {
@@ -662,17 +676,19 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     const int v_row = 16 * (wave & 1) + lc;                 // its row of V in tile wave / 2
 
     // (the first step has none before it: weights and V of zeros)
-    u32x2 pw[SUBK][RT];
+    u32x2 pw[TERMS][SUBK][RT];
 #pragma unroll
-    for (int s = 0; s < SUBK; ++s)
+    for (int term = 0; term < TERMS; ++term)
 #pragma unroll
-        for (int mt = 0; mt < RT; ++mt) pw[s][mt] = (u32x2){0u, 0u};
+        for (int s = 0; s < SUBK; ++s)
+#pragma unroll
+            for (int mt = 0; mt < RT; ++mt) pw[term][s][mt] = (u32x2){0u, 0u};
     for (int i = tid; i < VBUF_WORDS / 4; i += 256) reinterpret_cast<u32x4 *>(vbuf + VBUF_WORDS)[i] = (u32x4){0u, 0u, 0u, 0u};
     f32x4 sacc[SUBK][RT];
     // O^T += V^T P^T of the last step
     auto values = [&](const uint32_t *v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < TPS; ++j) fourbit_values<DP, RT>(v + (my_tile + j) * TILE_WORDS, lj, lc, pw[2 * j], pw[2 * j + 1], oacc);
+        for (int j = 0; j < TPS; ++j) fourbit_values<DP, RT>(v + (my_tile + j) * TILE_WORDS, lj, lc, pw, j, oacc);
     };
     auto scores = [&](int s, auto k_of) __attribute__((always_inline)) {
 #pragma unroll
@@ -685,7 +701,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         }
     };
     auto softmax = [&](auto masked, auto keys_of) __attribute__((always_inline)) {
-        fourbit_softmax<DP, RT, SUBK, decltype(masked)::value>(c2, sacc, pw, oacc, m_used, l_part, keys_of);
+        fourbit_softmax<DP, RT, SUBK, TERMS, decltype(masked)::value>(c2, sacc, pw, oacc, m_used, l_part, keys_of);
     };
 
     // (Everything asked for so far is there; said through the builtin, so that the compiler knows it of its own loads and puts no wait for
@@ -742,6 +758,8 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     // ---- the other steps: the end of the prefix and the tree block, bf16
     for (; t0 < t_end; end_step()) {
         begin_step();
+        int t1 = t0;            // (hidden from the compiler: it would keep what depends on it in scalar registers from step to step, and there are none)
+        asm volatile("" : "+s"(t1));
         const uint32_t *ring = s_big + slot * RING_WORDS;
         if (active) values(vbuf + (buf ^ 1) * VBUF_WORDS);
         const size_t head = ((size_t)b * p.H_kv + g) * p.N;
@@ -755,7 +773,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
             if (any_bad && (unsigned)__builtin_amdgcn_readfirstlane(table[t * KT / p.page_size]) >= (unsigned)p.n_pages) return 0;
             return L - t * KT;
         };
-        const int tv = t0 + (wave >> 1);
+        const int tv = t1 + (wave >> 1);
         uint32_t *vrow = vbuf + buf * VBUF_WORDS + (wave >> 1) * TILE_WORDS + v_row * PV;
         if (tv < t_prefix) {
             const uint32_t *vside = ring + (wave | 1) * SIDE_WORDS;
@@ -778,7 +796,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         if (active) {
 #pragma unroll
             for (int s = 0; s < SUBK; ++s) {
-                const int t = t0 + my_tile + s / 2;
+                const int t = t1 + my_tile + s / 2;
                 bf16x8 k[NKK];
                 if (t < t_prefix) {
                     const uint32_t *kside = ring + 2 * (my_tile + s / 2) * SIDE_WORDS;
@@ -797,7 +815,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
             for (int j = 0; j < TPS; ++j)
 #pragma unroll
                 for (int mt = 0; mt < RT; ++mt) {
-                    const int t = t0 + my_tile + j, left = L - t * KT;
+                    const int t = t1 + my_tile + j, left = L - t * KT;
                     vis[j][mt] = t >= t_end ? 0u : (t < t_prefix ? (left >= KT ? ~0u : (1u << (left & 31)) - 1u)
                                                                  : s_anc[row_node(p, min(row0 + 16 * mt + lc, p.M - 1))][t - tiles_prefix]);
                 }
@@ -805,7 +823,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         }
     }
     __syncthreads();
-    if (active && t_begin < t_end) values(vbuf + (buf ^ 1) * VBUF_WORDS);
+    if (active) values(vbuf + (buf ^ 1) * VBUF_WORDS);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (nothing may still be on its way into what follows)
 
     finish<DP, RT, RG>(p, my, g, row_tile0, tid, s_big, s_m, s_l, s_anc, s_odd, oacc, m_used, l_part);
@@ -862,7 +880,9 @@ size_t round_256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
-// Variants of the kernel: 16-row tiles per wavefront and row groups.
+// Variants of the kernel: 16-row tiles per wavefront and row groups.  128 rows at a time only at d = 128: with two terms per weight the wider form leaves
+// a SIMD one wavefront fewer at d = 64 and spills at d = 96 (d 64, 128 / 64 rows at a time: 4 x 4 heads of 512 rows, 200 keys 18.3 / 13.0 us; 8 x 8 of 84,
+// 4000 keys 32.5 / 25.6; 4 x 8 of 336, 8000 keys 67.2 / 62.7).
 struct FourbitVariant { int rt, rg; };
 
 static FourbitVariant variant_of(int rows, int d)
@@ -870,7 +890,7 @@ static FourbitVariant variant_of(int rows, int d)
     if (d > 128) return rows <= 16 ? FourbitVariant{1, 1} : (rows <= 32 ? FourbitVariant{1, 2} : FourbitVariant{1, 4});
     if (rows <= 16) return {1, 1};
     if (rows <= 32) return {2, 1};
-    return rows <= 64 ? FourbitVariant{2, 2} : FourbitVariant{2, 4};
+    return rows <= 64 || d != 128 ? FourbitVariant{2, 2} : FourbitVariant{2, 4};
 }
 
 bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
@@ -943,19 +963,22 @@ int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, co
     auto go = [&](auto kernel) { launch_kernel(K_ATTN_FOURBIT, kernel, grid, dim3(256), stream, p); };
     const FourbitVariant v = variant_of(plan.rows_per_kv, d.d);
     if (d.d > 128) {
-        if (v.rg == 1) go(attn_fourbit_kernel<256, 1>);
-        else if (v.rg == 2) go(attn_fourbit_shared_kernel<256, 1, 2>);
-        else go(attn_fourbit_shared_kernel<256, 1, 4>);
+        if (v.rg == 1) go(attn_fourbit_kernel<256, 1, 2>);
+        else if (v.rg == 2) go(attn_fourbit_shared_kernel<256, 1, 2, 2>);
+        else go(attn_fourbit_shared_kernel<256, 1, 4, 2>);
+    } else if (d.d == 128) {
+        if (v.rg == 4) go(attn_fourbit_shared_kernel<128, 2, 4, 1>);
+        else if (v.rg == 2) go(attn_fourbit_shared_kernel<128, 2, 2, 1>);
+        else if (v.rt == 2) go(attn_fourbit_kernel<128, 2, 1>);
+        else go(attn_fourbit_kernel<128, 1, 1>);
     } else if (d.d > 64) {
-        if (v.rg == 4) go(attn_fourbit_shared_kernel<128, 2, 4>);
-        else if (v.rg == 2) go(attn_fourbit_shared_kernel<128, 2, 2>);
-        else if (v.rt == 2) go(attn_fourbit_kernel<128, 2>);
-        else go(attn_fourbit_kernel<128, 1>);
+        if (v.rg == 2) go(attn_fourbit_shared_kernel<128, 2, 2, 2>);
+        else if (v.rt == 2) go(attn_fourbit_kernel<128, 2, 2>);
+        else go(attn_fourbit_kernel<128, 1, 2>);
     } else {
-        if (v.rg == 4) go(attn_fourbit_shared_kernel<64, 2, 4>);
-        else if (v.rg == 2) go(attn_fourbit_shared_kernel<64, 2, 2>);
-        else if (v.rt == 2) go(attn_fourbit_kernel<64, 2>);
-        else go(attn_fourbit_kernel<64, 1>);
+        if (v.rg == 2) go(attn_fourbit_shared_kernel<64, 2, 2, 2>);
+        else if (v.rt == 2) go(attn_fourbit_kernel<64, 2, 2>);
+        else go(attn_fourbit_kernel<64, 1, 2>);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("attn_fourbit launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }

@@ -21,7 +21,8 @@ def test_every_form(d, rows, cut):
     lens = [4990, 1301] if cut else [190, 33]
     c = AttnCase(2, 2 * G, 2, d, lens, N, [chain, random_tree, star][d // 32 % 3], 32 if N < 7 else 96, root_row=N == 7, capacity=lens[0] + 90)
     plan = plan_of(c.args.desc)
-    assert form_of(c.args.desc, plan) == (64 if d <= 64 else 128 if d <= 128 else 256,) + (large if d > 128 else small)
+    form = large if d > 128 else small if d == 128 else min(small, (2, 2))
+    assert form_of(c.args.desc, plan) == (64 if d <= 64 else 128 if d <= 128 else 256,) + form
     n = segments_of(c.args.desc, plan, lens)
     assert (min(n) > 1) if cut else (max(n) == 1), n
     c.run()
@@ -35,12 +36,12 @@ def test_every_form(d, rows, cut):
     c.check()
 
 
-def test_two_row_tiles_of_the_widest_form():
-    for d, N, G in ((64, 40, 5), (128, 60, 3), (256, 50, 2)):
+def test_two_row_tiles_of_the_widest_forms():
+    for d, N, G, groups in ((64, 40, 3, 2), (96, 25, 4, 2), (128, 60, 3, 4), (256, 50, 2, 4)):
         for lens in ([300, 0], [3000, 2000]):
             c = AttnCase(2, 2 * G, 2, d, lens, N, random_tree, 64)
             plan = plan_of(c.args.desc)
-            assert plan.n_row_tiles == 2 and form_of(c.args.desc, plan)[2] == 4
+            assert plan.n_row_tiles == 2 and form_of(c.args.desc, plan)[2] == groups
             assert (max(segments_of(c.args.desc, plan, lens)) > 1) == (lens[0] == 3000)
             c.run()
             c.check()
