@@ -535,8 +535,8 @@ typedef struct {
     int32_t dtype;          /* MCSD_DTYPE_* of logits */
     int32_t parent_per_seq; /* 0: one tree for the batch; 1: parent[B][N], row_map[B][1+N] */
     int32_t row_begin, row_end; /* tree rows dealt with, 0 <= row_begin <= row_end <= 1 + N (a level of the tree, say) */
-    int32_t hist_stride;    /* row length of history */
-    int32_t n_bias;         /* row length of bias_tok and bias_val */
+    int32_t hist_stride;    /* row length of history, <= 2^30 */
+    int32_t n_bias;         /* row length of bias_tok and bias_val, <= 2^30 */
 } mcsd_logits_desc;
 
 typedef struct {

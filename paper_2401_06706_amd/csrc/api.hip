@@ -492,6 +492,8 @@ int32_t mcsd_logits_rules(const mcsd_logits_desc *d, const mcsd_logits_bufs *b, 
     if (d->B < 1 || d->V < 1 || d->R < 1 || d->hist_stride < 0 || d->n_bias < 0) { set_error("logits: non-positive size"); return MCSD_E_SHAPE; }
     if (d->N < 0 || d->N > MCSD_MAX_NODES) { set_error("logits: N %d outside 0..%d", d->N, MCSD_MAX_NODES); return MCSD_E_TREE; }
     if (d->B > 65535 || d->V > (1 << 30)) { set_error("logits: B %d > 65535 or V %d > %d", d->B, d->V, 1 << 30); return MCSD_E_UNSUPPORTED; }
+    // (a thread's place in them goes on by 2048, and a token's count has 31 bits)
+    if (d->hist_stride > (1 << 30) || d->n_bias > (1 << 30)) { set_error("logits: hist_stride %d or n_bias %d > 2^30", d->hist_stride, d->n_bias); return MCSD_E_UNSUPPORTED; }
     if (d->dtype != MCSD_DTYPE_FP32 && d->dtype != MCSD_DTYPE_BF16) { set_error("logits: unknown dtype %d", d->dtype); return MCSD_E_UNSUPPORTED; }
     if (d->parent_per_seq != 0 && d->parent_per_seq != 1) { set_error("logits: parent_per_seq must be 0 or 1"); return MCSD_E_SHAPE; }
     if (d->row_begin < 0 || d->row_begin > d->row_end || d->row_end > 1 + d->N) { set_error("logits: rows %d..%d outside the tree's 0..%d", d->row_begin, d->row_end, 1 + d->N); return MCSD_E_SHAPE; }
