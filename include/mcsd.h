@@ -492,7 +492,7 @@ typedef struct {
     int32_t B;                      /* sequences */
     int32_t page_size;              /* tokens per page, >= 1 */
     int32_t n_pages;                /* pages in the pool, n_pages * page_size < 2^31 */
-    int32_t max_pages_per_seq;      /* row length of block_table */
+    int32_t max_pages_per_seq;      /* row length of block_table, <= 2^30 */
     int32_t max_slots;              /* length of slot_map, <= 2^30 (0 with slot_map = NULL) */
 } mcsd_page_desc;
 

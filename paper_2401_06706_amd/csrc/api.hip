@@ -476,6 +476,8 @@ int32_t mcsd_page_assign(const mcsd_page_desc *d, const mcsd_page_bufs *b, void 
     if (d->struct_size != sizeof(mcsd_page_desc)) { set_error("page desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_page_desc)); return MCSD_E_SHAPE; }
     if (d->B < 1 || d->page_size < 1 || d->n_pages < 1 || d->max_pages_per_seq < 1 || d->max_slots < 0) { set_error("pages: non-positive size"); return MCSD_E_SHAPE; }
     if (d->B > 65535 || d->max_slots > (1 << 30)) { set_error("pages: B %d > 65535 or max_slots %d > %d", d->B, d->max_slots, 1 << 30); return MCSD_E_UNSUPPORTED; }
+    // (a wavefront goes through a sequence's pages 64 at a time)
+    if (d->max_pages_per_seq > (1 << 30)) { set_error("pages: max_pages_per_seq %d > 2^30", d->max_pages_per_seq); return MCSD_E_UNSUPPORTED; }
     if ((long)d->n_pages * d->page_size > 0x7fffffffL) { set_error("pages: n_pages * page_size does not fit a slot"); return MCSD_E_UNSUPPORTED; }
     if (!b) { set_error("page bufs is NULL"); return MCSD_E_NULL; }
     if (b->struct_size != sizeof(mcsd_page_bufs)) { set_error("page bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_page_bufs)); return MCSD_E_SHAPE; }

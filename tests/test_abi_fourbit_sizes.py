@@ -17,3 +17,11 @@ def test_histories_and_bias_lists(field, n):
     assert call(**{field: n}) == -3
     assert b"2^30" in M.lib().mcsd_last_error()
     assert call(**{field: 2 ** 30, "end": 0}) == 0             # (no rows, no launch)
+
+
+@pytest.mark.parametrize("n", [2 ** 30 + 1, 2 ** 31 - 1])
+def test_rows_of_a_block_table(n):
+    bufs = M.PageBufs(C.sizeof(M.PageBufs), *[4096 for _ in M.PageBufs._fields_[1:]])
+    desc = M.PageDesc(C.sizeof(M.PageDesc), 1, 1, 100, n, 8)
+    assert M.lib().mcsd_page_assign(C.byref(desc), C.byref(bufs), None) == -3
+    assert b"2^30" in M.lib().mcsd_last_error()
