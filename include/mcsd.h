@@ -516,7 +516,7 @@ int32_t mcsd_page_assign(const mcsd_page_desc *desc, const mcsd_page_bufs *bufs,
  * candidate tree before they are sampled from (mcsd_draft_sample) or verified (mcsd_verify_sample).  The row of tree row r
  * (0 = root, 1 + i = node i) of sequence b continues the tokens
  *   history[b][0 .. hist_len[b]-1], then cand_tok[b] of the node's ancestors and of the node itself,
- * of which the first prompt_len[b] are the prompt.  With count(x) = how often x stands behind the
+ * of which the first min(prompt_len[b], hist_len[b]) are the prompt (a candidate never is).  With count(x) = how often x stands behind the
  * prompt, seen(x) = x stands anywhere, and per sequence a repetition penalty R > 0, a presence
  * penalty P and a frequency penalty F:
  *   z(x) = logits;   if seen(x): z > 0 ? z / R : z R;   z -= F count(x) + P [count(x) > 0];
@@ -549,7 +549,7 @@ typedef struct {
     const int32_t *cand_tok;        /* [B][N]; may be NULL with N = 0 */
     const int32_t *history;         /* [B][hist_stride], NULL with hist_stride = 0 */
     const int32_t *hist_len;        /* [B] (taken within [0, hist_stride]), NULL with hist_stride = 0 */
-    const int32_t *prompt_len;      /* [B], nullable (0) */
+    const int32_t *prompt_len;      /* [B], nullable (0): tokens of the history that are the prompt, taken within [0, hist_len[b]] */
     const float *repetition;        /* [B], nullable (1) */
     const float *presence;          /* [B], nullable (0) */
     const float *frequency;         /* [B], nullable (0) */
