@@ -41,8 +41,7 @@ struct FourbitParams : AttnParams {
 // as many workgroups as aimed at, by the real lengths (a cache's capacity says little about them).  Where they are more than one per
 // CU they are numbered longest first, and if all of them fit the chip at once (two per CU) the second 256 shortest first: the
 // hardware deals them out one per CU in order, so that a long one shares its CU with a short one.
-// A wavefront finds, for itself, the segment of number `index`, or (by_sequence) the segments of sequence `index`: its lanes take a
-// sequence each.  Numbers past the last segment: none.
+// A wavefront works this out for itself, its lanes take a sequence each.
 struct Segment { int b, L, n, first, i; };       // sequence, its length, its segments, the number of its first one, which of them
 
 __device__ __forceinline__ int lane_sum(int v, int lane, int *all)
@@ -57,41 +56,62 @@ __device__ __forceinline__ int lane_sum(int v, int lane, int *all)
     return v - x;
 }
 
-__device__ __forceinline__ Segment find_segment(const FourbitParams &p, int index, bool by_sequence, int lane)
+__device__ __forceinline__ int length_of(const FourbitParams &p, int b) { return b < p.B ? max(0, min(p.prefix_len[b], p.L_stride)) : 0; }
+
+__device__ __forceinline__ int tiles_of(const FourbitParams &p, int b, int L) { return b < p.B ? (L + KT - 1) / KT + p.tiles_tree : 0; }
+
+// 1 / chunk; L0: the length of sequence `lane`.  (In floating point: a rounding moves a cut by a tile.)
+__device__ __forceinline__ float cuts_per_tile(const FourbitParams &p, int L0, int lane)
 {
-    Segment s = {-1, 0, 0, 0, 0};
-    auto length = [&](int b) __attribute__((always_inline)) { return b < p.B ? max(0, min(p.prefix_len[b], p.L_stride)) : 0; };
-    auto tiles = [&](int b, int L) __attribute__((always_inline)) { return b < p.B ? (L + KT - 1) / KT + p.tiles_tree : 0; };
-    if (p.n_seg_max == 1 && (p.B > 64 || p.bias != 0.f || p.B * p.units <= 256)) {
-        s.b = index; s.L = length(index); s.n = 1; s.first = index;
-        return s;
-    }
-    int L = length(lane), total = 0, all;
-    lane_sum(tiles(lane, L), lane, &total);
+    int total = 0, all;
+    lane_sum(tiles_of(p, lane, L0), lane, &total);
     for (int b0 = 64; b0 < p.B; b0 += 64) {
-        lane_sum(tiles(b0 + lane, length(b0 + lane)), lane, &all);
+        lane_sum(tiles_of(p, b0 + lane, length_of(p, b0 + lane)), lane, &all);
         total += all;
     }
-    // (in floating point: a rounding moves a cut by a tile)
     const int chunk = max(p.min_seg, (int)fminf(ceilf((float)total * p.units_per_target), 1e9f));
-    const float per_chunk = 1.0f / (float)chunk;
-    int before = 0;
+    return 1.0f / (float)chunk;
+}
+
+// Segments of sequence b, of T tiles.
+__device__ __forceinline__ int segments_of(const FourbitParams &p, int b, int T, float per_tile)
+{
+    return b < p.B ? (T <= p.whole ? 1 : max(1, min(p.n_seg_max, (int)((float)T * per_tile + p.bias)))) : 0;
+}
+
+// Where segments are numbered by length: the number of the first of this lane's n, of T tiles together.  (The condition stands where it is asked: as a
+// function's it becomes another schedule of the loops behind it, d 64 3 % slower.)
+__device__ __forceinline__ int first_by_length(const FourbitParams &p, int T, int n, int lane)
+{
+    // tiles of a segment and the lane, as one number: the segments of all sequences with a larger one come before this one's
+    const int key = (T / max(n, 1) << 6) | (63 - lane);
+    int at = 0;
+    for (int j = 0; j < p.B; ++j) at += __builtin_amdgcn_readlane(key, j) > key ? __builtin_amdgcn_readlane(n, j) : 0;
+    return at;
+}
+
+// The segment of number `index`; numbers past the last one: none.
+__device__ __forceinline__ Segment find_segment(const FourbitParams &p, int index, int lane)
+{
+    Segment s = {-1, 0, 0, 0, 0};
+    if (p.n_seg_max == 1 && (p.B > 64 || p.bias != 0.f || p.B * p.units <= 256)) {
+        s.b = index; s.L = length_of(p, index); s.n = 1; s.first = index;
+        return s;
+    }
+    int L = length_of(p, lane), before = 0, all;
+    const float per_tile = cuts_per_tile(p, L, lane);
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        if (b0 > 0) L = length(b0 + lane);
-        const int T = tiles(b0 + lane, L);
-        const int n = b0 + lane < p.B ? (T <= p.whole ? 1 : max(1, min(p.n_seg_max, (int)((float)T * per_chunk + p.bias)))) : 0;
+        if (b0 > 0) L = length_of(p, b0 + lane);
+        const int T = tiles_of(p, b0 + lane, L), n = segments_of(p, b0 + lane, T, per_tile);
         int at = before + lane_sum(n, lane, &all);
         int wanted = index;
         if (p.B <= 64 && p.bias == 0.f && all * p.units > 256) {
-            // tiles of a segment and the lane, as one number: the segments of all sequences with a larger one come before this one's
-            const int key = (T / max(n, 1) << 6) | (63 - lane);
-            at = 0;
-            for (int j = 0; j < p.B; ++j) at += __builtin_amdgcn_readlane(key, j) > key ? __builtin_amdgcn_readlane(n, j) : 0;
+            at = first_by_length(p, T, n, lane);
             const int half = 256 / p.units;
             if (all * p.units <= 512 && index >= half) wanted = all - 1 - (index - half);
             if (index >= all) wanted = -1;
         }
-        const unsigned long long hit = __ballot(by_sequence ? b0 + lane == index : n > 0 && wanted >= at && wanted < at + n);
+        const unsigned long long hit = __ballot(n > 0 && wanted >= at && wanted < at + n);
         if (hit) {
             const int l = __ffsll((long long)hit) - 1;
             s.b = b0 + l;
@@ -337,7 +357,7 @@ void attn_fourbit_kernel(FourbitParams p)
     const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lj = lane >> 4, lc = lane & 15;
     const int g = blockIdx.x;
-    const Segment my = find_segment(p, blockIdx.z, false, lane);
+    const Segment my = find_segment(p, blockIdx.z, lane);
     const int b = my.b, L = my.L;
     if (b < 0) return;
     const int tiles_prefix = (L + KT - 1) / KT, T = tiles_prefix + p.tiles_tree;
@@ -578,7 +598,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     const int rg = wave % RG, ks = wave / RG;
     const int lj = lane >> 4, lc = lane & 15;
     const int g = blockIdx.x, row_tile0 = blockIdx.y * ROWS, row0 = row_tile0 + 16 * RT * rg;
-    const Segment my = find_segment(p, blockIdx.z, false, lane);
+    const Segment my = find_segment(p, blockIdx.z, lane);
     const int b = my.b, L = my.L;
     if (b < 0) return;
     const int tiles_prefix = (L + KT - 1) / KT, T = tiles_prefix + p.tiles_tree;
@@ -829,50 +849,72 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     finish<DP, RT, RG>(p, my, g, row_tile0, tid, s_big, s_m, s_l, s_anc, s_odd, oacc, m_used, l_part);
 }
 
-// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Bound by the launch and two trips to memory: 4.7 us for single tokens, 4.0 to 4.7 where nothing is
-// cut and 12.8 for 45 MB of partials in the larger cases above.
-// A thread per four columns of a row, ROWS rows of a (sequence, KV head) at a time per workgroup.
+// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Bound by the launch and two trips to memory: 4.0 us for the single tokens above, 3.9 where nothing is
+// cut and 12.4 for 45 MB of partials.  A thread per four columns of a row, ROWS rows of a (sequence, KV head) at a time per workgroup.
 template <int DP>
+__device__ __forceinline__ void merge_row(const FourbitParams &p, int b, int n_seg, int first, int g, int r, int d4)
+{
+    const size_t u0 = ((size_t)first * p.H_kv + g) * (size_t)p.R + r, step = (size_t)p.H_kv * p.R;
+    float ms = M_INIT, ls = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    // eight segments at a time, all of them requested before the first is used (those past the end are the first again, without weight)
+    for (int s0 = 0; s0 < n_seg; s0 += 8) {
+        float m[8], l[8];
+        f32x4 o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool on = s0 + i < n_seg;
+            const size_t u = u0 + (on ? s0 + i : 0) * step;
+            m[i] = on ? p.part_m[u] : M_INIT;
+            l[i] = on ? p.part_l[u] : 0.f;
+            o[i] = *reinterpret_cast<const f32x4 *>(p.part_o + u * p.d + 4 * d4);
+        }
+        float m_new = ms;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m_new = fmaxf(m_new, m[i]);
+        const float keep = fast_exp2(ms - m_new);
+        ls *= keep;
+        acc *= keep;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float f = s0 + i < n_seg ? fast_exp2(m[i] - m_new) : 0.f;
+            ls += f * l[i];
+            acc += f * o[i];
+        }
+        ms = m_new;
+    }
+    const float inv = 1.0f / ls;
+    __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(row_out(p, b, g, r) + 4 * d4));
+}
+
+// Units of ROWS rows of a KV head of the sequences that are cut: a workgroup each or, LOOP, dealt out among fewer (the loop around it takes registers: 672 rows
+// of 8 KV heads and 4 sequences in eight parts 12.1 us, 13.0 with it).
+template <int DP, bool LOOP>
 __global__ __launch_bounds__(256) void attn_fourbit_combine_kernel(FourbitParams p)
 {
     constexpr int D4 = DP / 4, ROWS = 256 / D4;
-    const int g = blockIdx.y;
-    const Segment my = find_segment(p, blockIdx.z, true, threadIdx.x & 63);
-    if (my.n <= 1) return;
-    const int d4 = threadIdx.x % D4;
-    if (4 * d4 >= p.d) return;
-    for (int r = blockIdx.x * ROWS + threadIdx.x / D4; r < p.M; r += gridDim.x * ROWS) {
-        const size_t u0 = ((size_t)my.first * p.H_kv + g) * (size_t)p.R + r, step = (size_t)p.H_kv * p.R;
-        float ms = M_INIT, ls = 0.f;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        // eight segments at a time, all of them requested before the first is used (those past the end are the first again, without weight)
-        for (int s0 = 0; s0 < my.n; s0 += 8) {
-            float m[8], l[8];
-            f32x4 o[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool on = s0 + i < my.n;
-                const size_t u = u0 + (on ? s0 + i : 0) * step;
-                m[i] = on ? p.part_m[u] : M_INIT;
-                l[i] = on ? p.part_l[u] : 0.f;
-                o[i] = *reinterpret_cast<const f32x4 *>(p.part_o + u * p.d + 4 * d4);
-            }
-            float m_new = ms;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m_new = fmaxf(m_new, m[i]);
-            const float keep = fast_exp2(ms - m_new);
-            ls *= keep;
-            acc *= keep;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float f = s0 + i < my.n ? fast_exp2(m[i] - m_new) : 0.f;
-                ls += f * l[i];
-                acc += f * o[i];
-            }
-            ms = m_new;
+    const int lane = threadIdx.x & 63, d4 = threadIdx.x % D4;
+    const int groups = (p.M + ROWS - 1) / ROWS, per_sequence = groups * p.H_kv;
+    int unit = blockIdx.x, before = 0, all;         // unit: counted from the first cut sequence of the 64 that are looked at
+    const float per_tile = cuts_per_tile(p, length_of(p, lane), lane);
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int T = tiles_of(p, b0 + lane, length_of(p, b0 + lane)), n = segments_of(p, b0 + lane, T, per_tile);
+        int at = before + lane_sum(n, lane, &all);
+        if (p.B <= 64 && p.bias == 0.f && all * p.units > 256) at = first_by_length(p, T, n, lane);
+        before += all;
+        unsigned long long cut = __ballot(n > 1);
+        int passed = 0;                             // cut sequences ahead of the first that `cut` still holds
+        const int units = __popcll(cut) * per_sequence;
+        while (unit < units) {
+            const int k = unit / per_sequence, in = unit % per_sequence;
+            for (; passed < k; ++passed) cut &= cut - 1;
+            const int l = __ffsll((long long)cut) - 1, r = in % groups * ROWS + threadIdx.x / D4;
+            const int n_seg = __builtin_amdgcn_readlane(n, l), first = __builtin_amdgcn_readlane(at, l);
+            if (r < p.M && 4 * d4 < p.d) merge_row<DP>(p, b0 + l, n_seg, first, in / groups, r, d4);
+            if (!LOOP) return;
+            unit += gridDim.x;
         }
-        const float inv = 1.0f / ls;
-        __builtin_nontemporal_store((u32x2){pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)}, reinterpret_cast<u32x2 *>(row_out(p, my.b, g, r) + 4 * d4));
+        unit -= units;
     }
 }
 
@@ -983,17 +1025,17 @@ int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, co
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("attn_fourbit launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     if (plan.n_segments_max == 1) return MCSD_OK;
-    // (Where sequences are cut only far beyond the average most or all are whole: no more workgroups than start at once look whether there is
-    // something to merge.  16 x 32 heads of 60 rows, none cut: 4.0 us, with a workgroup per eight rows 7.6; one of 16000 keys among 15 of 300:
-    // 13.0, 9.4; 60 x 8 heads of 64 rows, 6 of 8000 among 54 of 500: 10.7, 17.6.)
-    auto merge = [&](auto kernel, int rows) {
-        int groups = (p.M + rows - 1) / rows;
-        if (plan.bias == 0.f) groups = std::max(1, std::min(groups, 1024 / (d.H_kv * d.B)));
-        launch_kernel(K_ATTN_FOURBIT_COMBINE, kernel, dim3(groups, d.H_kv, d.B), dim3(256), stream, p);
+    // (Where sequences are cut only far beyond the average most or all are whole: no more workgroups than start at once, among which the rows of those that are
+    // cut are dealt out.  16 x 32 heads of 60 rows, none cut: 3.9 us, with a workgroup per eight rows 7.6; one of 16000 keys among 15 of 300: 5.9, 9.4; 6
+    // of 8000 among 54 of 500, 8 heads of 84 rows: 8.0; with the workgroups dealt to sequences instead, whole or not, 12.9 and 13.3.)
+    auto merge = [&](auto whole, auto dealt, int rows) {
+        const long units = (long)((p.M + rows - 1) / rows) * d.H_kv * d.B;
+        const bool deal = plan.bias == 0.f && units > 1024;
+        launch_kernel(K_ATTN_FOURBIT_COMBINE, deal ? dealt : whole, dim3((unsigned)(deal ? 1024 : units)), dim3(256), stream, p);
     };
-    if (d.d > 128) merge(attn_fourbit_combine_kernel<256>, 4);
-    else if (d.d > 64) merge(attn_fourbit_combine_kernel<128>, 8);
-    else merge(attn_fourbit_combine_kernel<64>, 16);
+    if (d.d > 128) merge(attn_fourbit_combine_kernel<256, false>, attn_fourbit_combine_kernel<256, true>, 4);
+    else if (d.d > 64) merge(attn_fourbit_combine_kernel<128, false>, attn_fourbit_combine_kernel<128, true>, 8);
+    else merge(attn_fourbit_combine_kernel<64, false>, attn_fourbit_combine_kernel<64, true>, 16);
     e = hipGetLastError();
     if (e != hipSuccess) { set_error("attn_fourbit_combine launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     return MCSD_OK;
