@@ -331,8 +331,8 @@ __device__ __forceinline__ void finish(const FourbitParams &p, const Segment &my
     }
 }
 
-// DP: d padded to 64, 128 or 256.  Up to 16 RT query rows, all of them by every wavefront, which takes every fourth tile and needs no
-// barrier in its loop.
+// DP: d padded to 64, 128 or 256.  Up to 16 RT query rows (DP = 256: a row tile of as many), all of them by every wavefront, which takes every fourth tile
+// and needs no barrier in its loop.
 template <int DP, int RT, int TERMS>
 __global__ __launch_bounds__(256, 2)
 void attn_fourbit_kernel(FourbitParams p)
@@ -356,7 +356,7 @@ void attn_fourbit_kernel(FourbitParams p)
     const int tid = threadIdx.x, lane = tid & 63;
     const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lj = lane >> 4, lc = lane & 15;
-    const int g = blockIdx.x;
+    const int g = blockIdx.x, row0 = DP == 256 ? 16 * RT * (int)blockIdx.y : 0;
     const Segment my = find_segment(p, blockIdx.z, lane);
     const int b = my.b, L = my.L;
     if (b < 0) return;
@@ -373,7 +373,7 @@ void attn_fourbit_kernel(FourbitParams p)
     bf16x8 qreg[RT][NKK];
 #pragma unroll
     for (int mt = 0; mt < RT; ++mt) {
-        const int r = 16 * mt + lc;
+        const int r = row0 + 16 * mt + lc;
         const int rr = min(r, p.M - 1), node = row_node(p, rr), hh = rr - node * p.G;
         const uint16_t *src = static_cast<const uint16_t *>(p.q) + (((size_t)b * p.N + node) * p.H_q + (size_t)g * p.G + hh) * (size_t)p.d;
 #pragma unroll
@@ -525,7 +525,7 @@ void attn_fourbit_kernel(FourbitParams p)
             }
             s_odd[t - tiles_prefix] = odd;              // (all lanes the same)
 #pragma unroll
-            for (int mt = 0; mt < RT; ++mt) vis[mt] = s_anc[row_node(p, min(16 * mt + lc, p.M - 1))][t - tiles_prefix];
+            for (int mt = 0; mt < RT; ++mt) vis[mt] = s_anc[row_node(p, min(row0 + 16 * mt + lc, p.M - 1))][t - tiles_prefix];
         }
         softmax(std::true_type(), [&](int mt, int s) __attribute__((always_inline)) { return vis[mt] >> (16 * s + 4 * lj); });
         values();
@@ -545,7 +545,7 @@ void attn_fourbit_kernel(FourbitParams p)
         any(stage0());
         if (NST > 1 && t < t_end) any(stage1());
     }
-    finish<DP, RT, 1>(p, my, g, 0, tid, s_big, s_m, s_l, s_anc, s_odd, oacc, m_used, l_part);
+    finish<DP, RT, 1>(p, my, g, row0, tid, s_big, s_m, s_l, s_anc, s_odd, oacc, m_used, l_part);
 }
 
 // 16 or 4 bytes per lane from base + offset straight into LDS, lane after lane from byte `to` on.  No register is written.  Written as text
@@ -571,12 +571,12 @@ __device__ __forceinline__ void fetch4(uint32_t to, const uint8_t *base, uint32_
 //   - PV runs a step behind the scores: the one barrier of a step then stands between both the codes' arrival and their
 //     readers, and the V of the last step and its readers.
 template <int DP, int RT, int RG, int TERMS>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2)
+__global__ __launch_bounds__(256, 2)
 void attn_fourbit_shared_kernel(FourbitParams p)
 {
     constexpr int ROWS = 16 * RT * RG, STEP = 2, DEPTH = 4;
     constexpr int TPS = RG / 2, SUBK = 2 * TPS;     // tiles, and 16-key parts, that a wavefront multiplies per step
-    constexpr int NR = DP == 256 ? 2 : 1, RUN = DP / 4 / NR, W = RUN / 8;       // (as in attn_fourbit_kernel)
+    constexpr int RUN = DP / 4, W = RUN / 8;        // columns a lane holds of a key's row, words of their codes
     constexpr int NKK = DP / 32, NNT = DP / 16;
     typedef uint32_t u32xW __attribute__((ext_vector_type(W)));
     constexpr int PV = DP / 2 + 8, PO = DP + 4;     // row pitches of V in LDS and of the epilogue, words
@@ -648,8 +648,8 @@ void attn_fourbit_shared_kernel(FourbitParams p)
 #pragma unroll
     for (int s = 0; s < DEPTH - 1; ++s) request();
 
-    // First of the eight columns that a lane holds in part kk of the contraction (as in attn_fourbit_kernel).
-    auto run_col = [&](int kk) __attribute__((always_inline)) { return NR == 2 ? 128 * (kk / 4) + 32 * lj + 8 * (kk % 4) : RUN * lj + 8 * kk; };
+    // First of the eight columns that a lane holds in part kk of the contraction.
+    auto run_col = [&](int kk) __attribute__((always_inline)) { return RUN * lj + 8 * kk; };
     bf16x8 qreg[RT][NKK];
 #pragma unroll
     for (int mt = 0; mt < RT; ++mt) {
@@ -659,7 +659,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
 #pragma unroll
         for (int kk = 0; kk < NKK; ++kk) {
             u32x4 v = {0u, 0u, 0u, 0u};
-            if (r < p.M && run_col(kk & ~3) < p.d) v = *reinterpret_cast<const u32x4 *>(src + run_col(kk));     // (d ends with a run)
+            if (r < p.M && RUN * lj < p.d) v = *reinterpret_cast<const u32x4 *>(src + run_col(kk));     // (d ends with a lane's columns)
             qreg[mt][kk] = __builtin_bit_cast(bf16x8, v);
         }
     }
@@ -678,18 +678,16 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     const float c2 = p.scale_log2;
     const bool active = row0 < p.M;
     // where the lane's codes of part `s` (of a tile's K or V) lie in the ring, in words behind that side; its scale byte behind CODE_WORDS
-    int code_at[2][NR], scale_at[2][NR];
+    int code_at[2], scale_at[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int run = 0; run < NR; ++run) {
-            const int block = (s * p.n_blocks + min(DP == 64 ? lj >> 1 : 4 * run + lj, p.n_blocks - 1)) * FB_TILE + lc;
-            code_at[s][run] = block * 4 + (DP == 64 ? 2 * (lj & 1) : 0);
-            scale_at[s][run] = CODE_WORDS * 4 + block;
-        }
-    auto codes_in = [&](const uint32_t *side, int s, int run) __attribute__((always_inline)) { return *reinterpret_cast<const u32xW *>(side + code_at[s][run]); };
-    auto scale_in = [&](const uint32_t *side, int s, int run) __attribute__((always_inline)) {
-        return fourbit_scale(reinterpret_cast<const uint8_t *>(side)[scale_at[s][run]]);
+    for (int s = 0; s < 2; ++s) {
+        const int block = (s * p.n_blocks + min(DP == 64 ? lj >> 1 : lj, p.n_blocks - 1)) * FB_TILE + lc;
+        code_at[s] = block * 4 + (DP == 64 ? 2 * (lj & 1) : 0);
+        scale_at[s] = CODE_WORDS * 4 + block;
+    }
+    auto codes_in = [&](const uint32_t *side, int s) __attribute__((always_inline)) { return *reinterpret_cast<const u32xW *>(side + code_at[s]); };
+    auto scale_in = [&](const uint32_t *side, int s) __attribute__((always_inline)) {
+        return fourbit_scale(reinterpret_cast<const uint8_t *>(side)[scale_at[s]]);
     };
     uint32_t *const vbuf = s_big + DEPTH * RING_WORDS;
     const int my_tile = RG == 4 ? 0 : ks;                   // the wavefront's first tile of a step
@@ -746,33 +744,29 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         uint32_t *const vrow = vbuf + buf * VBUF_WORDS + (wave >> 1) * TILE_WORDS + v_row * PV;
         // (One run of instructions, everything read from LDS ahead of what is written to it: the products of the last step beside the
         // conversions of this one.)
-        u32xW vc[NR], kc[SUBK][NR];
-        float vsc[NR], ksc[SUBK][NR];
-#pragma unroll
-        for (int run = 0; run < NR; ++run) { vc[run] = codes_in(vside, wave & 1, run); vsc[run] = scale_in(vside, wave & 1, run); }
+        u32xW kc[SUBK];
+        float ksc[SUBK];
+        const u32xW vc = codes_in(vside, wave & 1);
+        const float vsc = scale_in(vside, wave & 1);
         auto convert_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int run = 0; run < NR; ++run)
-#pragma unroll
-                for (int w = 0; w < W; ++w) *reinterpret_cast<u32x4 *>(vrow + run_col(run * 4 + w) / 2) = decode8(vc[run][w], vsc[run]);
+            for (int w = 0; w < W; ++w) *reinterpret_cast<u32x4 *>(vrow + run_col(w) / 2) = decode8(vc[w], vsc);
         };
         if (!active) {
             convert_v();
             continue;
         }
 #pragma unroll
-        for (int s = 0; s < SUBK; ++s)
-#pragma unroll
-            for (int run = 0; run < NR; ++run) {
-                const uint32_t *kside = ring + 2 * (my_tile + s / 2) * SIDE_WORDS;
-                kc[s][run] = codes_in(kside, s & 1, run);
-                ksc[s][run] = scale_in(kside, s & 1, run);
-            }
+        for (int s = 0; s < SUBK; ++s) {
+            const uint32_t *kside = ring + 2 * (my_tile + s / 2) * SIDE_WORDS;
+            kc[s] = codes_in(kside, s & 1);
+            ksc[s] = scale_in(kside, s & 1);
+        }
         values(vbuf + (buf ^ 1) * VBUF_WORDS);
         convert_v();
 #pragma unroll
         for (int s = 0; s < SUBK; ++s)
-            scores(s, [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, decode8(kc[s][kk / 4][kk % 4], ksc[s][kk / 4])); });
+            scores(s, [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, decode8(kc[s][kk], ksc[s])); });
         softmax(std::false_type(), [](int, int) __attribute__((always_inline)) { return 15u; });
     }
     // ---- the other steps: the end of the prefix and the tree block, bf16
@@ -785,7 +779,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         const size_t head = ((size_t)b * p.H_kv + g) * p.N;
         auto of_tree = [&](const void *from, int node, int kk) __attribute__((always_inline)) {
             u32x4 x = {0u, 0u, 0u, 0u};
-            if (node < p.N && run_col(kk & ~3) < p.d) x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(from) + (head + node) * p.d + run_col(kk));
+            if (node < p.N && RUN * lj < p.d) x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(from) + (head + node) * p.d + run_col(kk));
             return x;
         };
         // rows of a prefix tile that there are (none of a page that is none); the others hold anything and take part as zeros
@@ -798,13 +792,10 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         if (tv < t_prefix) {
             const uint32_t *vside = ring + (wave | 1) * SIDE_WORDS;
             const bool off = v_row >= rows_of(tv);
+            const u32xW c = codes_in(vside, wave & 1);
+            const float sc = scale_in(vside, wave & 1);
 #pragma unroll
-            for (int run = 0; run < NR; ++run) {
-                const u32xW c = codes_in(vside, wave & 1, run);
-                const float sc = scale_in(vside, wave & 1, run);
-#pragma unroll
-                for (int w = 0; w < W; ++w) *reinterpret_cast<u32x4 *>(vrow + run_col(run * 4 + w) / 2) = decode8(off ? 0u : c[w], off ? 1.f : sc);
-            }
+            for (int w = 0; w < W; ++w) *reinterpret_cast<u32x4 *>(vrow + run_col(w) / 2) = decode8(off ? 0u : c[w], off ? 1.f : sc);
         } else {
             const int node = tv < t_end ? (tv - tiles_prefix) * KT + v_row : p.N;
             uint32_t bits = 0u;
@@ -823,7 +814,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
                     const bool off = 16 * (s & 1) + lc >= rows_of(t);
 #pragma unroll
                     for (int kk = 0; kk < NKK; ++kk)
-                        k[kk] = __builtin_bit_cast(bf16x8, decode8(off ? 0u : codes_in(kside, s & 1, kk / 4)[kk % 4], off ? 1.f : scale_in(kside, s & 1, kk / 4)));
+                        k[kk] = __builtin_bit_cast(bf16x8, decode8(off ? 0u : codes_in(kside, s & 1)[kk], off ? 1.f : scale_in(kside, s & 1)));
                 } else {
 #pragma unroll
                     for (int kk = 0; kk < NKK; ++kk) k[kk] = __builtin_bit_cast(bf16x8, of_tree(p.k_tree, t < t_end ? (t - tiles_prefix) * KT + 16 * (s & 1) + lc : p.N, kk));
@@ -924,13 +915,14 @@ size_t round_256(size_t n) { return (n + 255) / 256 * 256; }
 
 // Variants of the kernel: 16-row tiles per wavefront and row groups.  128 rows at a time only at d = 128: with two terms per weight the wider form leaves
 // a SIMD one wavefront fewer at d = 64 and spills at d = 96 (d 64, 128 / 64 rows at a time: 4 x 4 heads of 512 rows, 200 keys 18.3 / 13.0 us; 8 x 8 of 84,
-// 4000 keys 32.5 / 25.6; 4 x 8 of 336, 8000 keys 67.2 / 62.7).
+// 4000 keys 32.5 / 25.6; 4 x 8 of 336, 8000 keys 67.2 / 62.7).  d > 128 always in tiles of 16 rows, two workgroups per CU, one reading behind the other from cache;
+// rows that share their keys in LDS (32 or 64 of them, one workgroup per CU, its registers full of accumulators) took 41.4 us for 31.8 with 16 x 4 heads of 28
+// rows, 91.7 for 66.3 with 8 x 16 of 60, 59.7 for 40.5 with 8 x 4 of 112, 220 for 208 with 4 x 8 of 336 and 8000 keys, 643 for 640 with 4 x 32 of 1024.
 struct FourbitVariant { int rt, rg; };
 
 static FourbitVariant variant_of(int rows, int d)
 {
-    if (d > 128) return rows <= 16 ? FourbitVariant{1, 1} : (rows <= 32 ? FourbitVariant{1, 2} : FourbitVariant{1, 4});
-    if (rows <= 16) return {1, 1};
+    if (rows <= 16 || d > 128) return {1, 1};
     if (rows <= 32) return {2, 1};
     return rows <= 64 || d != 128 ? FourbitVariant{2, 2} : FourbitVariant{2, 4};
 }
@@ -950,7 +942,9 @@ bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
     // Workgroups aimed at.  Enough sequences for two workgroups per CU: cut only what is twice as long as the average.  Fewer: two, three or four
     // per CU, whichever leaves the fullest CU with the fewest tiles if the sequences are alike, ceil(workgroups / 256) / segments of
     // each (4 sequences of 16384 keys, 48 workgroups a segment: 256, 512, 768, 1024 aimed at 369, 294, 229, 233 us; one of 16000, 32 a segment:
-    // 512 39, 768 46 us with the merge).
+    // 512 39, 768 46 us with the merge).  The line between the two, fewer / enough: 8 heads of 60 rows, 32 sequences of 2000 keys each 61.8 / 71.0, 40 66.4 / 61.7,
+    // 55 59.6 / 63.9; of 100 to 4000 keys 32 55.7 / 49.7, 55 87 / 72, 60 86 / 74, 80 110 / 108, 128 158 / 149; one row, of 2000 each 56 31.8 / 38.1, 80 52.6 / 45.3; of
+    // 100 to 4000 32 26.5 / 29.4, 48 36.9 / 40.0, 64 46.8 / 46.7.
     const long base = units * d.B;
     const bool enough = base >= 448;
     f.target = 512;
@@ -962,9 +956,10 @@ bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
         if (cost < least * 0.999) { least = cost; f.target = (int)(256 * k); }
     }
     // A merge is a launch of 4 us, which a sequence of few steps does not earn: 1 x 12 heads of 64, one row, whole / in two: 517 keys 5.9 / 8.9, 1000
-    // 7.7 / 9.3, 2000 11.4 / 9.1; 32 heads, 60 rows: 517 17.4 / 17.7, 1000 20.5 / 16.8.
-    f.min_seg = v.rg == 1 ? 16 : 8;
-    f.whole = v.rg == 1 ? 40 : 20;
+    // 7.7 / 9.3, 2000 11.4 / 9.1; 32 heads, 60 rows: 517 17.4 / 17.7, 1000 20.5 / 16.8.  2 x 8 heads of 128, one row: 700 8.7 / 11.4, 1500 12.3 / 11.4.  A
+    // tile of d > 128 takes twice as long: 2 x 4 heads of 256, one row, 400 keys 10.8 whole; 1000 17.4 whole, 14.6 in two; 2000 16.1 in pieces of 16 tiles, 14.1 in pieces of 8.
+    f.min_seg = (v.rg == 1 ? 16 : 8) / (d.d > 128 ? 2 : 1);
+    f.whole = (v.rg == 1 ? 40 : 20) / (d.d > 128 ? 2 : 1);
     // (beyond 512 sequences they fill the chip by themselves, and every workgroup would look through all lengths)
     if (tiles <= f.whole || d.B > 512) f.target = 1;
     f.n_segments_max = (int)std::max(1L, std::min((long)(tiles / f.min_seg), f.target / units));
@@ -1005,9 +1000,7 @@ int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, co
     auto go = [&](auto kernel) { launch_kernel(K_ATTN_FOURBIT, kernel, grid, dim3(256), stream, p); };
     const FourbitVariant v = variant_of(plan.rows_per_kv, d.d);
     if (d.d > 128) {
-        if (v.rg == 1) go(attn_fourbit_kernel<256, 1, 2>);
-        else if (v.rg == 2) go(attn_fourbit_shared_kernel<256, 1, 2, 2>);
-        else go(attn_fourbit_shared_kernel<256, 1, 4, 2>);
+        go(attn_fourbit_kernel<256, 1, 2>);
     } else if (d.d == 128) {
         if (v.rg == 4) go(attn_fourbit_shared_kernel<128, 2, 4, 1>);
         else if (v.rg == 2) go(attn_fourbit_shared_kernel<128, 2, 2, 1>);

@@ -20,7 +20,7 @@ def lengths(B, long, at, short):
     (70, 8, 8, 64, 28, random_tree, [3, 66, 69], 6000, 40),              # in both of the 64 sequences that are looked at together
     (130, 8, 4, 96, 3, chain, [0, 63, 64, 127, 128, 129], 9000, 30),
     (16, 32, 32, 128, 60, random_tree, [1, 4, 5, 9, 11, 15], 3000, 60),  # 1536 units of rows for 1024 workgroups
-    (20, 24, 24, 256, 60, random_tree, [0, 7, 19], 4000, 60),
+    (30, 8, 8, 256, 30, random_tree, [0, 7, 19], 4000, 60),
     (500, 2, 2, 32, 2, chain, [499], 20000, 20),
 ])
 def test_few_cut_sequences(B, H_q, H_kv, d, N, tree, at, long, short):
