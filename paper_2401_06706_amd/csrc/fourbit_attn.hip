@@ -1,8 +1,8 @@
 // Tree attention (Sec. 3.3 of the paper) over a paged prefix cache held in 4 bits, on the matrix cores
 // of gfx950.
 //
-//   attn_fourbit_kernel          up to 32 query rows per KV head: a (sequence, KV head, segment of the keys) per workgroup
-//   attn_fourbit_shared_kernel   more rows, in tiles: a row tile of them per workgroup
+//   attn_fourbit_kernel          up to 32 query rows per KV head (16 for d > 128; more of them in tiles): a (sequence, KV head, row tile, segment of the keys) per workgroup
+//   attn_fourbit_shared_kernel   d = 128, more rows: tiles of 64 or 128 that share their keys
 //   attn_fourbit_combine_kernel  merges the segments of a sequence by log-sum-exp
 //
 // Keys in tiles of 32.  S^T = K Q^T leaves a lane with 8 scores of one query row, which is the B operand
@@ -155,9 +155,9 @@ __device__ __forceinline__ uint32_t all_of(uint32_t keys, int i) { return (uint3
 // lowest four bits (MASKED; a masked score can not be told by its value where scale is 0).  Weights enter PV as TERMS bf16 terms each, their
 // sum is of the unrounded ones.  As in the framework's attention over caches of full precision: one at d = 128, at most 2^-8 of the weight off, two at
 // other d (the nearest bf16 and the nearest to what it leaves; what is not a number never meets them, see finite_of), at most 2^-17 off.  What the second
-// costs (us, one / two; 64 rows at a time where the weights have two, see variant_of): d 64, one token, 32 x 100-8000 keys 26.9 / 28.4, 16 x 8 heads of 60 rows
-// 27.8 / 30.6, 8 x 8 of 84 rows 25.8 / 25.3, 4 x 8 of 336 rows and 8000 keys 48.2 / 61.1; d 96, one token 18.7 / 19.5, 16 x 16 of 60 rows 48.1 / 57.2; d 256,
-// one token 24.2 / 25.1, 8 x 16 of 60 rows 85.4 / 91.9.  At d = 128 16 x 32 of 60 rows would be 70.5 / 87.1.
+// costs, us with one (more than 32 rows: 128 together) / two (32 together, see variant_of): d 64, one token, 32 x 8 heads of 100-8000 keys 27.2 / 28.8; 16 x 8
+// of 28 rows 20.2 / 22.3; 16 x 32 of 60 55.5 / 59.2; 8 x 8 of 84 27.9 / 24.7; 4 x 8 of 336 rows and 8000 keys 48.2 / 58.9, 2 x 8 of 672 and 16000 73.7 / 96.0; d 96,
+// one token 18.5 / 19.5, 16 x 16 of 60 48.0 / 48.5, 4 x 8 of 336 76.0 / 92.4.  At d = 128 16 x 32 of 60 rows would be 70.5 / 87.1.
 template <int DP, int RT, int NS, int TERMS, bool MASKED, typename KeysOf>
 __device__ __forceinline__ void fourbit_softmax(float c2, const f32x4 (&sacc)[NS][RT], u32x2 (&pw)[TERMS][NS][RT], f32x4 (&oacc)[DP / 16][RT], float (&m_used)[RT],
                                                 float (&l_part)[RT], KeysOf keys_of)
@@ -331,7 +331,7 @@ __device__ __forceinline__ void finish(const FourbitParams &p, const Segment &my
     }
 }
 
-// DP: d padded to 64, 128 or 256.  Up to 16 RT query rows (DP = 256: a row tile of as many), all of them by every wavefront, which takes every fourth tile
+// DP: d padded to 64, 128 or 256.  Up to 16 RT query rows (d != 128: a row tile of as many), all of them by every wavefront, which takes every fourth tile
 // and needs no barrier in its loop.
 template <int DP, int RT, int TERMS>
 __global__ __launch_bounds__(256, 2)
@@ -356,7 +356,7 @@ void attn_fourbit_kernel(FourbitParams p)
     const int tid = threadIdx.x, lane = tid & 63;
     const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lj = lane >> 4, lc = lane & 15;
-    const int g = blockIdx.x, row0 = DP == 256 ? 16 * RT * (int)blockIdx.y : 0;
+    const int g = blockIdx.x, row0 = TERMS == 2 ? 16 * RT * (int)blockIdx.y : 0;
     const Segment my = find_segment(p, blockIdx.z, lane);
     const int b = my.b, L = my.L;
     if (b < 0) return;
@@ -561,7 +561,7 @@ __device__ __forceinline__ void fetch4(uint32_t to, const uint8_t *base, uint32_
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(to), "v"(offset), "s"(base) : "memory", "m0");
 }
 
-// More than 32 query rows: RG row groups of 16 RT rows share their keys.  Wavefront (rg, ks) of the four owns rows [16 RT rg, 16 RT (rg + 1)) of
+// d = 128, more than 32 query rows: RG row groups of 16 RT rows share their keys.  Wavefront (rg, ks) of the four owns rows [16 RT rg, 16 RT (rg + 1)) of
 // the workgroup's and, RG = 2, key stream ks (one tile of the two of a step) or, RG = 4, both tiles.
 //   - Codes and scales go from memory straight into a ring of DEPTH steps in LDS (a wavefront asks for K or V of one of the two tiles), so
 //     that three steps are on their way without a register: with two steps in registers a launch that reads from memory took the
@@ -570,14 +570,14 @@ __device__ __forceinline__ void fetch4(uint32_t to, const uint8_t *base, uint32_
 //     rows in LDS for the transposing load.
 //   - PV runs a step behind the scores: the one barrier of a step then stands between both the codes' arrival and their
 //     readers, and the V of the last step and its readers.
-template <int DP, int RT, int RG, int TERMS>
+template <int RT, int RG>
 __global__ __launch_bounds__(256, 2)
 void attn_fourbit_shared_kernel(FourbitParams p)
 {
-    constexpr int ROWS = 16 * RT * RG, STEP = 2, DEPTH = 4;
+    constexpr int DP = 128, ROWS = 16 * RT * RG, STEP = 2, DEPTH = 4;
     constexpr int TPS = RG / 2, SUBK = 2 * TPS;     // tiles, and 16-key parts, that a wavefront multiplies per step
     constexpr int RUN = DP / 4, W = RUN / 8;        // columns a lane holds of a key's row, words of their codes
-    constexpr int NKK = DP / 32, NNT = DP / 16;
+    constexpr int NB = DP / FB_BLOCK, NKK = DP / 32, NNT = DP / 16;
     typedef uint32_t u32xW __attribute__((ext_vector_type(W)));
     constexpr int PV = DP / 2 + 8, PO = DP + 4;     // row pitches of V in LDS and of the epilogue, words
     constexpr int NLOAD = DP / 64;                  // 1 KB pieces of a tile's codes
@@ -618,12 +618,12 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     int entries = look_up();
     uint32_t code_off[NLOAD];
 #pragma unroll
-    for (int i = 0; i < NLOAD; ++i) code_off[i] = 16u * min(64 * i + lane, 2 * FB_TILE * p.n_blocks - 1);
-    const uint32_t scale_off = 4u * min(lane, 8 * p.n_blocks - 1);
+    for (int i = 0; i < NLOAD; ++i) code_off[i] = 16u * (64 * i + lane);
+    const uint32_t scale_off = 4u * min(lane, 8 * NB - 1);
     const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t *)s_big;
     auto request = [&]() __attribute__((always_inline)) {
         const int e = __builtin_amdgcn_readlane(entries, n_asked);
-        const size_t first = (((size_t)(t_ask < t_prefix && (unsigned)e < (unsigned)p.n_pages ? e : 0) * p.H_kv + g) * p.page_size + row_ask) * p.n_blocks;
+        const size_t first = (((size_t)(t_ask < t_prefix && (unsigned)e < (unsigned)p.n_pages ? e : 0) * p.H_kv + g) * p.page_size + row_ask) * NB;
         const uint8_t *codes = my_codes + first * 16, *scales = my_scales + first;
         const uint32_t to = ring_at + 4u * (slot_ask * RING_WORDS + wave * SIDE_WORDS);
 #pragma unroll
@@ -655,11 +655,11 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     for (int mt = 0; mt < RT; ++mt) {
         const int r = row0 + 16 * mt + lc;
         const int rr = min(r, p.M - 1), node = row_node(p, rr), hh = rr - node * p.G;
-        const uint16_t *src = static_cast<const uint16_t *>(p.q) + (((size_t)b * p.N + node) * p.H_q + (size_t)g * p.G + hh) * (size_t)p.d;
+        const uint16_t *src = static_cast<const uint16_t *>(p.q) + (((size_t)b * p.N + node) * p.H_q + (size_t)g * p.G + hh) * (size_t)DP;
 #pragma unroll
         for (int kk = 0; kk < NKK; ++kk) {
             u32x4 v = {0u, 0u, 0u, 0u};
-            if (r < p.M && RUN * lj < p.d) v = *reinterpret_cast<const u32x4 *>(src + run_col(kk));     // (d ends with a lane's columns)
+            if (r < p.M) v = *reinterpret_cast<const u32x4 *>(src + run_col(kk));
             qreg[mt][kk] = __builtin_bit_cast(bf16x8, v);
         }
     }
@@ -681,8 +681,8 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     int code_at[2], scale_at[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const int block = (s * p.n_blocks + min(DP == 64 ? lj >> 1 : lj, p.n_blocks - 1)) * FB_TILE + lc;
-        code_at[s] = block * 4 + (DP == 64 ? 2 * (lj & 1) : 0);
+        const int block = (s * NB + lj) * FB_TILE + lc;
+        code_at[s] = block * 4;
         scale_at[s] = CODE_WORDS * 4 + block;
     }
     auto codes_in = [&](const uint32_t *side, int s) __attribute__((always_inline)) { return *reinterpret_cast<const u32xW *>(side + code_at[s]); };
@@ -694,9 +694,9 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     const int v_row = 16 * (wave & 1) + lc;                 // its row of V in tile wave / 2
 
     // (the first step has none before it: weights and V of zeros)
-    u32x2 pw[TERMS][SUBK][RT];
+    u32x2 pw[1][SUBK][RT];
 #pragma unroll
-    for (int term = 0; term < TERMS; ++term)
+    for (int term = 0; term < 1; ++term)
 #pragma unroll
         for (int s = 0; s < SUBK; ++s)
 #pragma unroll
@@ -719,7 +719,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         }
     };
     auto softmax = [&](auto masked, auto keys_of) __attribute__((always_inline)) {
-        fourbit_softmax<DP, RT, SUBK, TERMS, decltype(masked)::value>(c2, sacc, pw, oacc, m_used, l_part, keys_of);
+        fourbit_softmax<DP, RT, SUBK, 1, decltype(masked)::value>(c2, sacc, pw, oacc, m_used, l_part, keys_of);
     };
 
     // (Everything asked for so far is there; said through the builtin, so that the compiler knows it of its own loads and puts no wait for
@@ -779,7 +779,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
         const size_t head = ((size_t)b * p.H_kv + g) * p.N;
         auto of_tree = [&](const void *from, int node, int kk) __attribute__((always_inline)) {
             u32x4 x = {0u, 0u, 0u, 0u};
-            if (node < p.N && RUN * lj < p.d) x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(from) + (head + node) * p.d + run_col(kk));
+            if (node < p.N) x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(from) + (head + node) * DP + run_col(kk));
             return x;
         };
         // rows of a prefix tile that there are (none of a page that is none); the others hold anything and take part as zeros
@@ -913,18 +913,20 @@ size_t round_256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
-// Variants of the kernel: 16-row tiles per wavefront and row groups.  128 rows at a time only at d = 128: with two terms per weight the wider form leaves
-// a SIMD one wavefront fewer at d = 64 and spills at d = 96 (d 64, 128 / 64 rows at a time: 4 x 4 heads of 512 rows, 200 keys 18.3 / 13.0 us; 8 x 8 of 84,
-// 4000 keys 32.5 / 25.6; 4 x 8 of 336, 8000 keys 67.2 / 62.7).  d > 128 always in tiles of 16 rows, two workgroups per CU, one reading behind the other from cache;
-// rows that share their keys in LDS (32 or 64 of them, one workgroup per CU, its registers full of accumulators) took 41.4 us for 31.8 with 16 x 4 heads of 28
-// rows, 91.7 for 66.3 with 8 x 16 of 60, 59.7 for 40.5 with 8 x 4 of 112, 220 for 208 with 4 x 8 of 336 and 8000 keys, 643 for 640 with 4 x 32 of 1024.
+// Variants of the kernel: 16-row tiles per wavefront and row groups (1: rows do not share keys in LDS).
+// d = 128: 32 rows together / shared: 16 x 32 heads of 60 rows 77.8 / 71.4 us, 64 x 32 of 60 243 / 188, 4 x 8 of 672 rows and 16384 keys 249 / 222 and with 64 rows
+// together 251, 4 x 32 of 1024 221 / 171; not so where there are few workgroups: 32 x 8 of 60 46.4 / 56.9, 16 x 8 of 128 43.8 / 66.9, short ones of 60 12.4 / 15.9.
+// Other d, with two terms per weight: the shared forms have no registers for them (128 rows together: a wavefront per SIMD fewer at d = 64, spills at d = 96;
+// one workgroup per CU at d > 128) and were behind tiles of 32 (16 for d > 128) whose workgroups read one behind the other from cache, d 64, 64 rows together / 32: 8 x 8 of 60
+// rows 30.6 / 29.1, 16 x 32 of 60 64.5 / 59.2, 4 x 8 of 336 and 8000 keys 60.4 / 58.9, 4 x 32 of 1024 148 / 153; d 96, 16 x 16 of 60 57.3 / 48.5; d 256, 64 rows together /
+// 16: 8 x 16 of 60 91.7 / 66.3, 8 x 4 of 112 59.7 / 40.5, 4 x 8 of 336 220 / 208, 4 x 32 of 1024 643 / 640; 32 rows together / 16: 16 x 4 of 28 41.4 / 31.8.
 struct FourbitVariant { int rt, rg; };
 
 static FourbitVariant variant_of(int rows, int d)
 {
     if (rows <= 16 || d > 128) return {1, 1};
-    if (rows <= 32) return {2, 1};
-    return rows <= 64 || d != 128 ? FourbitVariant{2, 2} : FourbitVariant{2, 4};
+    if (rows <= 32 || d != 128) return {2, 1};
+    return rows <= 64 ? FourbitVariant{2, 2} : FourbitVariant{2, 4};
 }
 
 bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan)
@@ -1002,17 +1004,15 @@ int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, co
     if (d.d > 128) {
         go(attn_fourbit_kernel<256, 1, 2>);
     } else if (d.d == 128) {
-        if (v.rg == 4) go(attn_fourbit_shared_kernel<128, 2, 4, 1>);
-        else if (v.rg == 2) go(attn_fourbit_shared_kernel<128, 2, 2, 1>);
+        if (v.rg == 4) go(attn_fourbit_shared_kernel<2, 4>);
+        else if (v.rg == 2) go(attn_fourbit_shared_kernel<2, 2>);
         else if (v.rt == 2) go(attn_fourbit_kernel<128, 2, 1>);
         else go(attn_fourbit_kernel<128, 1, 1>);
     } else if (d.d > 64) {
-        if (v.rg == 2) go(attn_fourbit_shared_kernel<128, 2, 2, 2>);
-        else if (v.rt == 2) go(attn_fourbit_kernel<128, 2, 2>);
+        if (v.rt == 2) go(attn_fourbit_kernel<128, 2, 2>);
         else go(attn_fourbit_kernel<128, 1, 2>);
     } else {
-        if (v.rg == 2) go(attn_fourbit_shared_kernel<64, 2, 2, 2>);
-        else if (v.rt == 2) go(attn_fourbit_kernel<64, 2, 2>);
+        if (v.rt == 2) go(attn_fourbit_kernel<64, 2, 2>);
         else go(attn_fourbit_kernel<64, 1, 2>);
     }
     hipError_t e = hipGetLastError();

@@ -25,10 +25,8 @@ def plan_of(desc):
 
 def form_of(desc, plan):
     """(padded head dimension, 16-row tiles per wavefront, row groups) of the kernel that the launch takes."""
-    if desc.d > 128:
-        assert plan.row_tile == 16
-        return (256, 1, 1)
-    return (64 if desc.d <= 64 else 128,) + {16: (1, 1), 32: (2, 1), 64: (2, 2), 128: (2, 4)}[plan.row_tile]
+    forms = {16: (1, 1), 32: (2, 1), 64: (2, 2), 128: (2, 4)}
+    return (64 if desc.d <= 64 else 128 if desc.d <= 128 else 256,) + forms[plan.row_tile]
 
 
 def segments_of(desc, plan, lens):

@@ -9,7 +9,7 @@ from tests.test_gpu_fourbit import AttnCase, chain, i32, random_tree, star
 
 pytestmark = pytest.mark.gpu
 
-# rows per KV head: nodes, query heads per KV head, (tiles per wavefront, row groups) up to d = 128 (above it is (1, 1))
+# rows per KV head: nodes, query heads per KV head, (tiles per wavefront, row groups) at d = 128 (below at most (2, 1), above (1, 1))
 ROWS = [(1, 4, (1, 1)), (5, 3, (1, 1)), (7, 4, (2, 1)), (20, 3, (2, 2)), (33, 4, (2, 4))]
 
 
@@ -21,7 +21,7 @@ def test_every_form(d, rows, cut):
     lens = [4990, 1301] if cut else [190, 33]
     c = AttnCase(2, 2 * G, 2, d, lens, N, [chain, random_tree, star][d // 32 % 3], 32 if N < 7 else 96, root_row=N == 7, capacity=lens[0] + 90)
     plan = plan_of(c.args.desc)
-    form = (1, 1) if d > 128 else small if d == 128 else min(small, (2, 2))
+    form = (1, 1) if d > 128 else small if d == 128 else min(small, (2, 1))
     assert form_of(c.args.desc, plan) == (64 if d <= 64 else 128 if d <= 128 else 256,) + form
     n = segments_of(c.args.desc, plan, lens)
     assert (min(n) > 1) if cut else (max(n) == 1), n
@@ -37,7 +37,7 @@ def test_every_form(d, rows, cut):
 
 
 def test_several_row_tiles():
-    for d, N, G, groups in ((64, 40, 3, 2), (96, 25, 4, 2), (128, 60, 3, 4), (256, 50, 2, 1)):
+    for d, N, G, groups in ((64, 40, 3, 1), (96, 25, 4, 1), (128, 60, 3, 4), (256, 50, 2, 1)):
         for lens in ([300, 0], [3000, 2000]):
             c = AttnCase(2, 2 * G, 2, d, lens, N, random_tree, 64)
             plan = plan_of(c.args.desc)
