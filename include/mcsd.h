@@ -130,7 +130,7 @@ int32_t mcsd_tree_validate(const int32_t *parent_host, int32_t n_nodes);
  * Inputs are expected to be position-encoded already (each candidate keeps the
  * position it has in its own sequence, i.e. prefix_len + depth - 1).
  * fp32 accumulation on the matrix cores.  The softmax weights enter PV as bf16 for bf16 storage
- * with d == 128, as two bf16 terms (relative error at most 2^-17) for bf16 storage with other d,
+ * with d == 128, as two bf16 terms (relative error at most 2^-16) for bf16 storage with other d,
  * and as fp32 for fp32 storage.
  */
 typedef struct {

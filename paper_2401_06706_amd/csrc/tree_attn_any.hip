@@ -8,7 +8,7 @@
 // In both, a lane of S^T = K Q^T holds scores of one query row, which is the B operand layout of
 // O^T += V^T P^T: the weights never leave their lane.  The fp32 kernel multiplies in fp32
 // (v_mfma_f32_16x16x4_f32); the bf16 kernel feeds PV with two bf16 terms per weight where d != 128, which hold
-// it to 2^-17 (see weight_hi_bits), and with one at d = 128, as the other kernels for it.
+// it to 2^-16 (see weight_hi_bits), and with one at d = 128, as the other kernels for it.
 #include <type_traits>
 
 #include "attn_common.h"
@@ -69,7 +69,7 @@ __host__ __device__ __forceinline__ bool one_resource(const AttnParams &p, uint3
 
 // ------------------------------------------------------------------------------ bf16
 // A weight p >= 0 as hi + lo, both bf16: hi is p cut to bf16, taken one step lower where that cut
-// would be exact, lo the rest rounded to bf16.  |hi + lo - p| <= 2^-17 p (hi alone: 2^-8), so
+// would be exact, lo the rest rounded to bf16.  |hi + lo - p| <= 2^-16 p (hi alone: 2^-8), so
 // that PV rounds far below the bf16 output; and lo > 0 whenever p > 0, so that a weight times an
 // infinite value stays infinite instead of meeting 0 x inf in the second term.
 __device__ __forceinline__ uint32_t weight_hi_bits(float p)
