@@ -431,8 +431,8 @@ typedef struct {
  * calls below; bufs->k_prefix and bufs->v_prefix are ignored.  bf16 only (MCSD_E_UNSUPPORTED otherwise),
  * d a multiple of 32.  A lone token per sequence is a tree of one node.  Prefix keys and values enter the
  * products exactly as what they stand for, accumulation is fp32, and the softmax weights enter PV as in mcsd_tree_attn (bf16 for
- * d == 128, two bf16 terms, at most 2^-17 off, for other d).  Only the pages that hold rows below prefix_len[b] are read, and rows at or past it do not count, whatever
- * they hold.  A table entry outside [0, n_pages) is a data error: its rows read as zeros.  What a node may not see
+ * d == 128, two bf16 terms, at most 2^-17 off, for other d).  Only the pages that hold rows below prefix_len[b] are read, and rows
+ * at or past it do not count, whatever they hold.  A table entry outside [0, n_pages) is a data error: its rows read as zeros.  What a node may not see
  * does not reach it, whatever it holds.  How a sequence's keys are split, and with it the last bits of its rows, follows the lengths of
  * the whole batch. */
 size_t mcsd_attn_fourbit_workspace_bytes(const mcsd_attn_desc *desc);

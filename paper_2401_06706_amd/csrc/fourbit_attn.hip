@@ -13,9 +13,9 @@
 // matrix cores through the converters alone, without LDS.  V has to be transposed: converted, stored to
 // LDS as rows and read back with the transposing load.
 //
-// Measured (inputs that take turns, d = 128): single tokens, 32 sequences of 100 to 8000 keys, 32 heads over 8: 39.4 us for 146 MB, 3.7 TB/s (32 us and
-// 4.5 TB/s where part of it is still in a cache; 6.2 per further byte), bound by memory and the launch's ends.  16 sequences of 256
-// to 4096 keys, 32 heads, 60 nodes: 72.5 us for 197 MB, 2.7 TB/s and 0.52 PFLOP/s.  4 sequences of 16384, 64 heads over 8, 84 nodes: 229 us, 0.79 PFLOP/s.  These
+// Measured (inputs that take turns, d = 128, by the tracer): single tokens, 32 sequences of 100 to 8000 keys, 32 heads over 8: 39.4 us for 146 MB, 3.7 TB/s (32 us and
+// 4.5 TB/s where part of it is still in a cache; 6.2 per further byte), bound by memory and the launch's ends: segments of 10 to 90 tiles, by sequence.  16 sequences of 256
+// to 4096 keys, 32 heads, 60 nodes: 74 us for 197 MB, 2.7 TB/s and 0.51 PFLOP/s.  4 sequences of 16384, 64 heads over 8, 84 nodes: 226 us, 0.80 PFLOP/s.  These
 // two are bound by the instructions between the products: matrix instructions 29 and 37 % of the cycles, vector ones 49 and 48 %, and a wavefront's are not
 // free of each other (products of a step without softmax, conversions or V's reads: 47 to 50 of 53 us for 4096 keys more).
 #include <algorithm>
@@ -38,9 +38,9 @@ struct FourbitParams : AttnParams {
 };
 
 // How the tiles of all sequences are cut: a sequence of T tiles into max(1, T / chunk + bias) segments, with chunk so that there are
-// as many workgroups as aimed at, by the real lengths (a cache's capacity says little about them).  Where they are more than one per
-// CU they are numbered longest first, and if all of them fit the chip at once (two per CU) the second 256 shortest first: the
-// hardware deals them out one per CU in order, so that a long one shares its CU with a short one.
+// as many workgroups as aimed at, by the real lengths (a cache's capacity says little about them).  Where the sequences are enough by themselves
+// (bias 0), at most 64, and their segments more than one per CU, these are numbered longest first, and if all of them fit the chip at once (two per CU) the second 256
+// shortest first: the hardware deals them out one per CU in order, so that a long one shares its CU with a short one.  Otherwise they go by sequence.
 // A wavefront works this out for itself, its lanes take a sequence each.
 struct Segment { int b, L, n, first, i; };       // sequence, its length, its segments, the number of its first one, which of them
 
@@ -361,7 +361,7 @@ void attn_fourbit_kernel(FourbitParams p)
     const int b = my.b, L = my.L;
     if (b < 0) return;
     const int tiles_prefix = (L + KT - 1) / KT, T = tiles_prefix + p.tiles_tree;
-    // whole steps where that leaves no segment empty
+    // (whole steps, so that the last segments may have no tile: their partials are without weight)
     const int seg = (int)(((uint32_t)(T + my.n - 1) / (uint32_t)my.n + STEP - 1) / STEP * STEP);
     const int t_begin = min(T, my.i * seg), t_end = min(T, t_begin + seg);
 
@@ -602,7 +602,7 @@ void attn_fourbit_shared_kernel(FourbitParams p)
     const int b = my.b, L = my.L;
     if (b < 0) return;
     const int tiles_prefix = (L + KT - 1) / KT, T = tiles_prefix + p.tiles_tree;
-    // whole steps where that leaves no segment empty
+    // (whole steps, so that the last segments may have no tile: their partials are without weight)
     const int seg = (int)(((uint32_t)(T + my.n - 1) / (uint32_t)my.n + STEP - 1) / STEP * STEP);
     const int t_begin = min(T, my.i * seg), t_end = min(T, t_begin + seg), t_prefix = min(t_end, tiles_prefix);
     const int my_parent = parent_of_thread(p, b);

@@ -8,8 +8,10 @@ namespace {
 
 constexpr int RULE_THREADS = 256, RULE_SLICE = 4 * RULE_THREADS;       // tokens per workgroup
 constexpr uint32_t IN_PROMPT = 0x80000000u;
-// Workgroups aimed at by dealing the rows out: all that the chip holds at once (eight per CU).  More of them count the history more often and leave a
-// second round half empty, fewer wait for memory: 976 rows of 32000, 512, 1024, 1536, 2048, 2560, 4096 workgroups 117, 80, 64, 56, 68, 60 us.
+// Workgroups aimed at by dealing the rows out: all that the chip holds at once (eight per CU).  More of them count the history more often, fewer wait for memory:
+// 512, 1024, 2048, 4096 workgroups, 976 rows of 32000 in fp32 124, 84, 61, 64 us; 232 of 65536 in bf16 47, 32, 25, 27; 129 of 32000 18, 14.2, 12.5, 14.3; 32 sequences of
+// 7 rows and 4096 tokens of history 20.7, 20.8, 19.0, 22.5; one of 29 rows of 50001 7.0, 6.5, 7.2, 7.1.  Not so with two rows and 16384 tokens of history, which every
+// workgroup reads for 1024 tokens of the vocabulary (32 sequences, 50001): 17.4, 17.5, 24.2, 24.3.
 constexpr long RULE_GROUPS = 2048;
 
 struct RuleParams {
