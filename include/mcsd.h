@@ -27,6 +27,15 @@
  *   mcsd_kv_load_fourbit
  *                       The same attention and commit over a paged prefix cache
  *                       held in 4 bits, and rows into such a cache and back.
+ *   mcsd_kv_store_paged, mcsd_chunk_attn_paged
+ *                       The prompt: rows of new tokens into a paged cache, and
+ *                       attention of a chunk of new tokens over all of it.
+ *   mcsd_attn_weight_sums, mcsd_kv_evict_paged
+ *                       Attention weights added up for every cached position, and
+ *                       a cache cut to a budget by them.
+ *   mcsd_token_logprobs
+ *                       Log probability, rank and entropy for given tokens, with
+ *                       the most probable alternatives.
  *   mcsd_page_assign    Block tables, slot map and free list of a paged cache,
  *                       from the lengths the requests are to have.
  *   mcsd_logits_rules   Penalties, biases and grammar masks on the logits of the
@@ -112,7 +121,8 @@ enum {
     MCSD_FLAG_NEAR_TIE_DRAW = 128,    /* mcsd_draft_sample: u_draw within near_tie_eps of an edge of the chosen CDF interval */
     MCSD_FLAG_CACHE_FULL = 256,       /* mcsd_kv_commit: prefix_len + n_accepted > L_stride, nothing committed for this sequence;
                                          mcsd_page_assign: no pages for it, nothing assigned to this sequence */
-    MCSD_FLAG_BAD_PAGES = 512,        /* mcsd_page_assign: a negative length, or counts that do not fit the table or the pool */
+    MCSD_FLAG_BAD_PAGES = 512,        /* mcsd_page_assign: a negative length, or counts that do not fit the table or the pool;
+                                         mcsd_kv_evict_paged: a table entry outside the pool, rows that it names were not moved */
     MCSD_FLAG_SLOTS_FULL = 1024       /* mcsd_page_assign: the slot map ends before this sequence's last slot */
 };
 
@@ -466,6 +476,159 @@ typedef struct {
 
 int32_t mcsd_kv_store_fourbit(const mcsd_rows_desc *desc, const mcsd_rows_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream);
 int32_t mcsd_kv_load_fourbit(const mcsd_rows_desc *desc, const mcsd_rows_bufs *bufs, const mcsd_fourbit_kv *kv, void *stream);
+
+/* ------------------------------------- prompts in chunks over a paged cache
+ * A prompt (or a piece of it, or one decoded token; each sequence of a batch brings as many new tokens as it likes) joins a paged
+ * cache of full precision (the layout of mcsd_tree_attn_paged) and attends to all that its sequence then holds:
+ * mcsd_page_assign gives the pages and lists the new tokens' slots, mcsd_kv_store_paged writes their rows, mcsd_chunk_attn_paged
+ * attends, and afterwards prefix_len is want_len.
+ *
+ * mcsd_kv_store_paged: row t of the packed arrays goes to slot slot_map[t] = page * page_size + row in the page, all KV heads
+ * and layers, unchanged.  A slot outside [0, n_pages * page_size) is passed over.  The slots of one store have to
+ * differ from each other.  Pools [n_layers][n_pages][H_kv][page_size][d]; d * element size a multiple of 16 bytes, d <= MCSD_MAX_HEAD_DIM;
+ * paged->block_table and max_pages_per_seq are not read (may be NULL, 0); n_pages * page_size < 2^31.  Otherwise mcsd_rows_desc is as
+ * for mcsd_kv_store_fourbit.
+ */
+typedef struct {
+    uint32_t struct_size;
+    const void *k, *v;              /* [n_layers][T][H_kv][d] with the strides of mcsd_rows_desc, 16-byte aligned */
+    const int32_t *slot_map;        /* [T] */
+    void *k_pool, *v_pool;          /* 16-byte aligned, not overlapping k and v */
+} mcsd_store_bufs;
+
+int32_t mcsd_kv_store_paged(const mcsd_rows_desc *desc, const mcsd_store_bufs *bufs, const mcsd_paged_kv *paged, void *stream);
+
+/* mcsd_chunk_attn_paged.  The new tokens of all sequences are packed: those of b are rows chunk_start[b] .. chunk_start[b+1]-1
+ * (slot_start of mcsd_page_assign; ascending, a sequence may bring none).  Row chunk_start[b] + i stands at position prefix_len[b] + i,
+ * and its keys are positions 0 .. prefix_len[b] + i of sequence b, those of the new tokens among them, all read from the pages:
+ *   out[t][h][:] = softmax_over_keys(scale * <q[t][h], K>) . V,   lse[t][h] = ln sum_over_keys exp(scale * <q[t][h], K>)
+ * What a row may not see does not reach it, whatever it holds; rows of out and lse at and past chunk_start[B] are left as they were.  Positions end at
+ * L_stride (a sequence that is longer is a data error: its last rows see the positions below L_stride).  A table entry outside [0, n_pages)
+ * is a data error: its keys and values read as zeros.  fp32 accumulation; the softmax weights enter PV as in mcsd_tree_attn.  How a
+ * sequence's keys are split, and with it the last bits of its rows, follows the lengths of the whole batch.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t B;              /* sequences, <= 65535 */
+    int32_t T;              /* rows of q, out and lse, >= 0; T H_q < 2^30 */
+    int32_t H_q, H_kv;      /* query / KV heads, H_q % H_kv == 0, H_kv <= 65535 */
+    int32_t d;              /* head dim <= MCSD_MAX_HEAD_DIM; d * element size a multiple of 16 bytes */
+    int32_t dtype;          /* MCSD_DTYPE_* of q, the pools and out */
+    int32_t L_stride;       /* logical capacity of a sequence, 1 .. min(2^22, max_pages_per_seq * page_size) */
+    float scale;            /* softmax scale, finite and >= 0 */
+    int64_t q_stride;       /* elements from a row [H_q][d] of q to the next one's, >= H_q d; a multiple of 16 bytes */
+} mcsd_chunk_desc;
+
+typedef struct {
+    uint32_t struct_size;
+    const void *q;                  /* [T][H_q][d], rows q_stride apart, 16-byte aligned */
+    const void *k_pool, *v_pool;    /* [n_pages][H_kv][page_size][d], 16-byte aligned */
+    const int32_t *chunk_start;     /* [B+1], taken within [0, T] */
+    const int32_t *prefix_len;      /* [B], taken within [0, L_stride] */
+    void *out;                      /* [T][H_q][d], 16-byte aligned */
+    float *lse;                     /* [T][H_q], nullable */
+    void *workspace;                /* >= mcsd_chunk_workspace_bytes(desc), 256-byte aligned */
+    size_t workspace_bytes;
+} mcsd_chunk_bufs;
+
+size_t mcsd_chunk_workspace_bytes(const mcsd_chunk_desc *desc);     /* 0 on a bad descriptor */
+int32_t mcsd_chunk_attn_paged(const mcsd_chunk_desc *desc, const mcsd_chunk_bufs *bufs, const mcsd_paged_kv *paged, void *stream);
+
+/* ------------------------------------------- eviction by attention weight
+ * mcsd_attn_weight_sums adds up what every cached position of a sequence was given by the softmax of the new rows:
+ *   sums[b][g][j] = (j < prefix_len[b] ? sums[b][g][j] : 0) + sum exp(scale * <q[t][h], K_j> - lse[t][h])
+ * over the rows t of sequence b that see j, of the last last_rows of its new tokens (0: all of them), and the query heads h of
+ * KV head g; j = 0 .. prefix_len[b] + new tokens - 1 (below L_stride), other entries are left as they were.  Positions of new tokens start from 0, so that
+ * sums needs no clearing; a sequence without new tokens is left alone.  desc, q, chunk_start, prefix_len and the pages are those of the mcsd_chunk_attn_paged that
+ * wrote lse, called before prefix_len is raised.  Sums are fp32 and always added in the same order.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t last_rows;              /* >= 0 */
+    const void *q;
+    const void *k_pool;
+    const int32_t *chunk_start, *prefix_len;
+    const float *lse;               /* [T][H_q] */
+    float *sums;                    /* [B][H_kv][L_stride] in/out */
+} mcsd_sums_bufs;
+
+int32_t mcsd_attn_weight_sums(const mcsd_chunk_desc *desc, const mcsd_sums_bufs *bufs, const mcsd_paged_kv *paged, void *stream);
+
+/* mcsd_kv_evict_paged cuts every sequence to m = min(prefix_len[b], keep_len[b]) tokens.  With n = prefix_len[b], f = min(n_first, m)
+ * and r = min(n_recent, m - f), every layer and KV head keeps by itself its first f tokens, its last r, and of those between
+ * the m - f - r with the largest sums (lowest position on ties; a sum that is no number counts as the smallest).  What is
+ * kept moves to positions 0 .. m-1 in ascending order, keys, values and sums alike (keys are position-encoded, so that attention does
+ * not mind); kept tells where it stood, prefix_len[b] becomes m.  Entries of sums and kept at and past m and rows
+ * at and past m are left as they were, sequences with n <= keep_len[b] keep everything (kept = 0 .. n-1).
+ * In place (out_table NULL) rows move within the pages of block_table, which no other sequence may share; mcsd_page_assign with want_len =
+ * prefix_len takes the surplus back afterwards.  With out_table they are written to its pages instead, all m of them, which
+ * nothing else may share; the pages of block_table are then left as they were (a shared prefix, say).
+ * A table entry outside [0, n_pages) is a data error (MCSD_FLAG_BAD_PAGES): rows that lie there, or were to go there, are not moved.
+ * prefix_len counts what the cache holds: position ids of later tokens come from the caller's own count.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t B;              /* sequences, <= 65535 */
+    int32_t H_kv;           /* n_layers B H_kv < 2^24 */
+    int32_t d;              /* d * element size a multiple of 16 bytes, d <= MCSD_MAX_HEAD_DIM */
+    int32_t dtype;          /* MCSD_DTYPE_* of the pools */
+    int32_t L_stride;       /* row length of sums and kept, logical capacity, 1 .. min(2^22, max_pages_per_seq * page_size) */
+    int32_t n_layers;       /* >= 1 */
+    int32_t n_first, n_recent;      /* >= 0 */
+} mcsd_evict_desc;
+
+typedef struct {
+    uint32_t struct_size;
+    void *k_pool, *v_pool;          /* [n_layers][n_pages][H_kv][page_size][d] in/out, 16-byte aligned */
+    float *sums;                    /* [n_layers][B][H_kv][L_stride] in/out */
+    int32_t *prefix_len;            /* [B] in/out, taken within [0, L_stride] */
+    const int32_t *keep_len;        /* [B] (negative: 0) */
+    const int32_t *out_table;       /* [B][max_pages_per_seq], nullable */
+    int32_t *kept;                  /* [n_layers][B][H_kv][L_stride] out */
+    uint32_t *flags;                /* [B] out */
+} mcsd_evict_bufs;
+
+int32_t mcsd_kv_evict_paged(const mcsd_evict_desc *desc, const mcsd_evict_bufs *bufs, const mcsd_paged_kv *paged, void *stream);
+
+/* --------------------------------------------- log probabilities of tokens
+ * For row i, x = tokens[i], and z = logits[row_map[i]] / T with T = temperature[i] (0, argmax sampling, reads as 1):
+ *   logprob[i] = z(x) - lse,  lse = ln sum_y exp z(y)        entropy[i] = -sum_y p(y) ln p(y),  p = exp(z - lse)
+ *   rank[i] = tokens y that come before x: z(y) > z(x), or z(y) = z(x) and y < x  (0: x is the most probable)
+ *   top_tok[i][0 .. n_top-1], top_logprob: the first n_top tokens of that order and their log probabilities
+ * Tokens at -infinity (masked) have probability 0, log probability -infinity and come last, by id.  The order is that of the logits as they are, before the division.
+ * x outside [0, V): logprob NaN, rank -1, MCSD_FLAG_BAD_TOKEN, the rest as usual.  A row_map entry outside [0, R): NaN, -1, MCSD_FLAG_BAD_TREE.  A
+ * row that holds NaN or +infinity, or nothing but -infinity: NaN, -1, MCSD_FLAG_NONFINITE.  Sums are taken in fp32 per lane and in fp64 across.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t rows;           /* rows asked for, >= 0 */
+    int32_t R;              /* rows of logits, >= 1 */
+    int32_t V;              /* vocabulary, 1 .. 2^30 */
+    int32_t dtype;          /* MCSD_DTYPE_* of logits */
+    int32_t n_top;          /* 0 .. min(V, MCSD_MAX_TOP) */
+    int64_t row_stride;     /* elements from a row of logits to the next one, >= V */
+} mcsd_logprob_desc;
+
+#define MCSD_MAX_TOP 64
+
+typedef struct {
+    uint32_t struct_size;
+    const void *logits;             /* [R][V], rows row_stride apart */
+    const int32_t *row_map;         /* [rows], NULL: row i is row i, rows <= R */
+    const int32_t *tokens;          /* [rows] */
+    const float *temperature;       /* [rows], >= 0, nullable (1) */
+    float *logprob;                 /* [rows] out */
+    float *entropy;                 /* [rows] out, nullable */
+    int32_t *rank;                  /* [rows] out, nullable */
+    int32_t *top_tok;               /* [rows][n_top] out, NULL with n_top = 0 */
+    float *top_logprob;             /* [rows][n_top] out, NULL with n_top = 0 */
+    uint32_t *flags;                /* [rows] out */
+    void *workspace;                /* >= mcsd_logprob_workspace_bytes(desc), 256-byte aligned */
+    size_t workspace_bytes;
+} mcsd_logprob_bufs;
+
+size_t mcsd_logprob_workspace_bytes(const mcsd_logprob_desc *desc);     /* 0 on a bad descriptor */
+int32_t mcsd_token_logprobs(const mcsd_logprob_desc *desc, const mcsd_logprob_bufs *bufs, void *stream);
 
 /* ------------------------------------------------------- pages from lengths
  * mcsd_page_assign brings the block table of every sequence to the pages that want_len[b] tokens

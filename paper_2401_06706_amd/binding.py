@@ -30,6 +30,8 @@ EXPORTS = ["mcsd_last_error", "mcsd_version", "mcsd_tree_validate", "mcsd_attn_w
            "mcsd_draft_sample", "mcsd_tree_size", "mcsd_tree_build", "mcsd_kv_commit", "mcsd_kv_commit_paged",
            "mcsd_tree_attn_fourbit", "mcsd_attn_fourbit_workspace_bytes", "mcsd_kv_commit_fourbit",
            "mcsd_kv_store_fourbit", "mcsd_kv_load_fourbit", "mcsd_page_assign", "mcsd_logits_rules",
+           "mcsd_kv_store_paged", "mcsd_chunk_workspace_bytes", "mcsd_chunk_attn_paged", "mcsd_attn_weight_sums", "mcsd_kv_evict_paged",
+           "mcsd_logprob_workspace_bytes", "mcsd_token_logprobs",
            "mcsd_kernel_timing", "mcsd_kernel_count", "mcsd_kernel_name", "mcsd_kernel_timing_read"]
 
 
@@ -130,6 +132,45 @@ class LogitsBufs(C.Structure):
         "presence", "frequency", "bias_tok", "bias_val", "mask")]
 
 
+class StoreBufs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_void_p) for n in ("k", "v", "slot_map", "k_pool", "v_pool")]
+
+
+class ChunkDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in ("B", "T", "H_q", "H_kv", "d", "dtype", "L_stride")] + [
+        ("scale", C.c_float), ("q_stride", C.c_int64)]
+
+
+class ChunkBufs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_void_p) for n in (
+        "q", "k_pool", "v_pool", "chunk_start", "prefix_len", "out", "lse", "workspace")] + [("workspace_bytes", C.c_size_t)]
+
+
+class SumsBufs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("last_rows", C.c_int32)] + [(n, C.c_void_p) for n in (
+        "q", "k_pool", "chunk_start", "prefix_len", "lse", "sums")]
+
+
+class EvictDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "B", "H_kv", "d", "dtype", "L_stride", "n_layers", "n_first", "n_recent")]
+
+
+class EvictBufs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_void_p) for n in (
+        "k_pool", "v_pool", "sums", "prefix_len", "keep_len", "out_table", "kept", "flags")]
+
+
+class LogprobDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in ("rows", "R", "V", "dtype", "n_top")] + [("row_stride", C.c_int64)]
+
+
+class LogprobBufs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_void_p) for n in (
+        "logits", "row_map", "tokens", "temperature", "logprob", "entropy", "rank", "top_tok", "top_logprob", "flags", "workspace")] + [
+        ("workspace_bytes", C.c_size_t)]
+
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -179,11 +220,20 @@ def lib() -> C.CDLL:
                                      ("mcsd_kv_commit_fourbit", CommitDesc, CommitBufs, FourbitKV),
                                      ("mcsd_kv_store_fourbit", RowsDesc, RowsBufs, FourbitKV),
                                      ("mcsd_kv_load_fourbit", RowsDesc, RowsBufs, FourbitKV),
+                                     ("mcsd_kv_store_paged", RowsDesc, StoreBufs, PagedKV),
+                                     ("mcsd_chunk_attn_paged", ChunkDesc, ChunkBufs, PagedKV),
+                                     ("mcsd_attn_weight_sums", ChunkDesc, SumsBufs, PagedKV),
+                                     ("mcsd_kv_evict_paged", EvictDesc, EvictBufs, PagedKV),
+                                     ("mcsd_token_logprobs", LogprobDesc, LogprobBufs, None),
                                      ("mcsd_page_assign", PageDesc, PageBufs, None),
                                      ("mcsd_logits_rules", LogitsDesc, LogitsBufs, None)):
             f = getattr(L, name)
             f.argtypes = [C.POINTER(t) for t in (desc, bufs, kv) if t is not None] + [C.c_void_p]
             f.restype = C.c_int32
+        for name, desc in (("mcsd_chunk_workspace_bytes", ChunkDesc), ("mcsd_logprob_workspace_bytes", LogprobDesc)):
+            f = getattr(L, name)
+            f.argtypes = [C.POINTER(desc)]
+            f.restype = C.c_size_t
         L.mcsd_kernel_timing.argtypes = [C.c_int32]
         L.mcsd_kernel_timing.restype = C.c_int32
         L.mcsd_kernel_count.restype = C.c_int32
@@ -733,6 +783,197 @@ def mcsd_kv_store_fourbit(args: RowsArgs, stream=None) -> None:
 
 def mcsd_kv_load_fourbit(args: RowsArgs, stream=None) -> None:
     _launch(lib().mcsd_kv_load_fourbit, args.device, stream, args.desc, args.bufs, args.kv)
+
+
+# ------------------------------------------------- prompts in chunks over a paged cache
+def _pools(k_pool, v_pool=None):
+    """(n_layers, n_pages, H_kv, page_size, d) of pools [n_pages][H_kv][page_size][d], with or without layers in front."""
+    if k_pool.dim() not in (4, 5) or (v_pool is not None and (tuple(v_pool.shape) != tuple(k_pool.shape) or v_pool.dtype != k_pool.dtype)):
+        raise ValueError("pools must be [n_pages][H_kv][page_size][d], with or without layers in front, keys and values alike")
+    return (1,) * (5 - k_pool.dim()) + tuple(k_pool.shape)
+
+
+def _paged(k_pool, block_table=None) -> PagedKV:
+    if block_table is not None and block_table.dim() != 2:
+        raise ValueError("block_table must be [B][max_pages_per_seq]")
+    return PagedKV(C.sizeof(PagedKV), k_pool.shape[-2], k_pool.shape[-4], 0 if block_table is None else block_table.shape[1],
+                   _ptr(block_table, torch.int32, "block_table"))
+
+
+def _bytes_of(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+@dataclass
+class StoreArgs:
+    desc: RowsDesc
+    bufs: StoreBufs
+    paged: PagedKV
+    device: int
+    keep: tuple
+
+
+def store_args(k, v, slot_map, k_pool, v_pool) -> StoreArgs:
+    """Rows of tokens for a store into pools [n_pages][H_kv][page_size][d]: k, v [T][H_kv][d] (layers in front of both where the
+    pools have them), a token's row contiguous, any stride from row to row; slot_map int32 [T]."""
+    n_layers, _, H_kv, _, d = _pools(k_pool, v_pool)
+    T = slot_map.shape[0]
+    shape = tuple(k_pool.shape[:-4]) + (T, H_kv, d)
+    if slot_map.dim() != 1 or tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != k_pool.dtype or v.dtype != k_pool.dtype:
+        raise ValueError(f"k and v must be {shape} of the pools' dtype, slot_map [T]")
+    stride = lambda t: t.stride(-3) if T > 1 else H_kv * d
+    layer = lambda t: t.stride(0) if n_layers > 1 else 0
+    desc = RowsDesc(C.sizeof(RowsDesc), T, H_kv, d, _dtype_of(k), n_layers, stride(k), stride(v), layer(k), layer(v))
+    bufs = StoreBufs(C.sizeof(StoreBufs), _rows_ptr(k, "k"), _rows_ptr(v, "v"), _ptr(slot_map, torch.int32, "slot_map"),
+                     _ptr(k_pool, k.dtype, "k_pool"), _ptr(v_pool, k.dtype, "v_pool"))
+    return StoreArgs(desc, bufs, _paged(k_pool), _one_device(k, v, slot_map, k_pool, v_pool), (k, v, slot_map, k_pool, v_pool))
+
+
+def mcsd_kv_store_paged(args: StoreArgs, stream=None) -> None:
+    _launch(lib().mcsd_kv_store_paged, args.device, stream, args.desc, args.bufs, args.paged)
+
+
+def chunk_desc(q, k_pool, block_table, scale: float, L_stride: int) -> ChunkDesc:
+    """q [T][H_q][d] (a row contiguous, any stride from row to row) over pools [n_pages][H_kv][page_size][d] (one layer)."""
+    n_layers, _, H_kv, _, d = _pools(k_pool)
+    if n_layers != 1 or k_pool.dim() != 4 or q.dim() != 3 or q.shape[2] != d or q.dtype != k_pool.dtype or block_table.dim() != 2:
+        raise ValueError("q must be [T][H_q][d] of the pools' dtype and head dimension, the pools of one layer, block_table [B][max_pages_per_seq]")
+    T, H_q, _ = q.shape
+    return ChunkDesc(C.sizeof(ChunkDesc), block_table.shape[0], T, H_q, H_kv, d, _dtype_of(q), int(L_stride), float(scale),
+                     q.stride(0) if T > 1 else H_q * d)
+
+
+def mcsd_chunk_workspace_bytes(desc: ChunkDesc) -> int:
+    return int(lib().mcsd_chunk_workspace_bytes(C.byref(desc)))
+
+
+@dataclass
+class ChunkArgs:
+    desc: ChunkDesc
+    bufs: C.Structure
+    paged: PagedKV
+    device: int
+    keep: tuple
+
+
+def _chunk_shapes(desc, *pairs) -> None:
+    for t, shp in pairs:
+        if t is not None and tuple(t.shape) != shp:
+            raise ValueError(f"shape mismatch: got {tuple(t.shape)}, expected {shp}")
+
+
+def chunk_attn_args(q, k_pool, v_pool, block_table, chunk_start, prefix_len, out, scale, L_stride: int, lse=None,
+                    workspace: Optional[torch.Tensor] = None) -> ChunkArgs:
+    """q as for chunk_desc, out [T][H_q][d], lse fp32 [T][H_q] or None; block_table int32 [B][max_pages_per_seq], chunk_start int32
+    [B+1], prefix_len int32 [B]."""
+    desc = chunk_desc(q, k_pool, block_table, scale, L_stride)
+    _pools(k_pool, v_pool)
+    _chunk_shapes(desc, (out, tuple(q.shape)), (lse, tuple(q.shape[:2])), (chunk_start, (desc.B + 1,)), (prefix_len, (desc.B,)))
+    bufs = ChunkBufs(C.sizeof(ChunkBufs), _rows_ptr(q, "q"), _ptr(k_pool, q.dtype, "k_pool"), _ptr(v_pool, q.dtype, "v_pool"),
+                     _ptr(chunk_start, torch.int32, "chunk_start"), _ptr(prefix_len, torch.int32, "prefix_len"), _ptr(out, q.dtype, "out"),
+                     _ptr(lse, torch.float32, "lse"), _ptr(workspace, None, "workspace"), _bytes_of(workspace))
+    keep = (q, k_pool, v_pool, block_table, chunk_start, prefix_len, out, lse, workspace)
+    return ChunkArgs(desc, bufs, _paged(k_pool, block_table), _one_device(*keep), keep)
+
+
+def mcsd_chunk_attn_paged(args: ChunkArgs, stream=None) -> None:
+    _launch(lib().mcsd_chunk_attn_paged, args.device, stream, args.desc, args.bufs, args.paged)
+
+
+# ------------------------------------------------------ eviction by attention weight
+def weight_sums_args(q, k_pool, block_table, chunk_start, prefix_len, lse, sums, scale, last_rows: int = 0) -> ChunkArgs:
+    """As chunk_attn_args; lse fp32 [T][H_q] as written there, sums fp32 [B][H_kv][L_stride] (in/out)."""
+    if sums.dim() != 3:
+        raise ValueError("sums must be [B][H_kv][L_stride]")
+    desc = chunk_desc(q, k_pool, block_table, scale, sums.shape[2])
+    _chunk_shapes(desc, (sums, (desc.B, desc.H_kv, desc.L_stride)), (lse, tuple(q.shape[:2])), (chunk_start, (desc.B + 1,)), (prefix_len, (desc.B,)))
+    bufs = SumsBufs(C.sizeof(SumsBufs), int(last_rows), _rows_ptr(q, "q"), _ptr(k_pool, q.dtype, "k_pool"), _ptr(chunk_start, torch.int32, "chunk_start"),
+                    _ptr(prefix_len, torch.int32, "prefix_len"), _ptr(lse, torch.float32, "lse"), _ptr(sums, torch.float32, "sums"))
+    keep = (q, k_pool, block_table, chunk_start, prefix_len, lse, sums)
+    return ChunkArgs(desc, bufs, _paged(k_pool, block_table), _one_device(*keep), keep)
+
+
+def mcsd_attn_weight_sums(args: ChunkArgs, stream=None) -> None:
+    _launch(lib().mcsd_attn_weight_sums, args.device, stream, args.desc, args.bufs, args.paged)
+
+
+@dataclass
+class EvictArgs:
+    desc: EvictDesc
+    bufs: EvictBufs
+    paged: PagedKV
+    device: int
+    keep: tuple
+
+
+def evict_args(k_pool, v_pool, block_table, sums, prefix_len, keep_len, kept, flags, n_first: int, n_recent: int, out_table=None) -> EvictArgs:
+    """Pools [n_layers][n_pages][H_kv][page_size][d] with sums fp32 and kept int32 [n_layers][B][H_kv][L_stride] (or all without
+    layers); block_table and out_table int32 [B][max_pages_per_seq]; prefix_len, keep_len, flags int32 [B]."""
+    n_layers, _, H_kv, _, d = _pools(k_pool, v_pool)
+    if block_table.dim() != 2 or sums.dim() != k_pool.dim() - 1:
+        raise ValueError("block_table must be [B][max_pages_per_seq], sums [B][H_kv][L_stride] with layers in front where the pools have them")
+    B, L_stride = block_table.shape[0], sums.shape[-1]
+    _chunk_shapes(None, (sums, tuple(k_pool.shape[:-4]) + (B, H_kv, L_stride)), (kept, tuple(sums.shape)), (out_table, tuple(block_table.shape)),
+                  (prefix_len, (B,)), (keep_len, (B,)), (flags, (B,)))
+    i32 = torch.int32
+    desc = EvictDesc(C.sizeof(EvictDesc), B, H_kv, d, _dtype_of(k_pool), L_stride, n_layers, int(n_first), int(n_recent))
+    bufs = EvictBufs(C.sizeof(EvictBufs), _ptr(k_pool, k_pool.dtype, "k_pool"), _ptr(v_pool, k_pool.dtype, "v_pool"), _ptr(sums, torch.float32, "sums"),
+                     _ptr(prefix_len, i32, "prefix_len"), _ptr(keep_len, i32, "keep_len"), _ptr(out_table, i32, "out_table"),
+                     _ptr(kept, i32, "kept"), _ptr(flags, i32, "flags"))
+    keep = (k_pool, v_pool, block_table, sums, prefix_len, keep_len, kept, flags, out_table)
+    return EvictArgs(desc, bufs, _paged(k_pool, block_table), _one_device(*keep), keep)
+
+
+def mcsd_kv_evict_paged(args: EvictArgs, stream=None) -> None:
+    _launch(lib().mcsd_kv_evict_paged, args.device, stream, args.desc, args.bufs, args.paged)
+
+
+# --------------------------------------------------------- log probabilities of tokens
+@dataclass
+class LogprobArgs:
+    desc: LogprobDesc
+    bufs: LogprobBufs
+    device: int
+    keep: tuple
+
+
+def logprob_desc(logits, tokens, n_top: int = 0) -> LogprobDesc:
+    """logits [R][V] (a row contiguous, any stride from row to row), tokens [rows]."""
+    R, V = logits.shape
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("a row of logits must be contiguous")
+    return LogprobDesc(C.sizeof(LogprobDesc), tokens.shape[0], R, V, _dtype_of(logits), int(n_top), logits.stride(0) if R > 1 else V)
+
+
+def mcsd_logprob_workspace_bytes(desc: LogprobDesc) -> int:
+    return int(lib().mcsd_logprob_workspace_bytes(C.byref(desc)))
+
+
+def logprob_args(logits, tokens, logprob, entropy, rank, top_tok, top_logprob, flags, temperature=None, row_map=None,
+                 workspace: Optional[torch.Tensor] = None) -> LogprobArgs:
+    """logits fp32 or bf16 [R][V]; int32 tokens, flags, rank (or None), row_map (or None: row i) [rows]; fp32 logprob, entropy
+    (or None), temperature (or None: 1) [rows]; top_tok int32 and top_logprob fp32 [rows][n_top] (or both None)."""
+    if not logits.is_cuda:
+        raise ValueError("logits must be a device tensor")
+    if (top_tok is None) != (top_logprob is None):
+        raise ValueError("top_tok and top_logprob come together")
+    rows, n_top = tokens.shape[0], 0 if top_tok is None else top_tok.shape[1]
+    _chunk_shapes(None, *[(t, (rows,)) for t in (tokens, logprob, entropy, rank, flags, temperature, row_map)], (top_tok, (rows, n_top)),
+                  (top_logprob, (rows, n_top)))
+    f32, i32 = torch.float32, torch.int32
+    desc = logprob_desc(logits, tokens, n_top)
+    keep = (row_map, tokens, temperature, logprob, entropy, rank, top_tok, top_logprob, flags)
+    types = (i32, i32, f32, f32, f32, i32, i32, f32, i32)
+    names = [n for n, _ in LogprobBufs._fields_[2:11]]
+    bufs = LogprobBufs(C.sizeof(LogprobBufs), logits.data_ptr(), *[_ptr(t, ty, n) for t, ty, n in zip(keep, types, names)],
+                       _ptr(workspace, None, "workspace"), _bytes_of(workspace))
+    if n_top == 0:
+        bufs.top_tok = bufs.top_logprob = None
+    return LogprobArgs(desc, bufs, _one_device(logits, *keep, workspace), (logits, workspace) + keep)
+
+
+def mcsd_token_logprobs(args: LogprobArgs, stream=None) -> None:
+    _launch(lib().mcsd_token_logprobs, args.device, stream, args.desc, args.bufs)
 
 
 # ------------------------------------------------------------------ pages from lengths

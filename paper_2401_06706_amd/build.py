@@ -10,7 +10,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmcsd.so")
 SOURCES = ["api.hip", "tree_attn.hip", "tree_attn_shared.hip", "tree_attn_any.hip", "verify_sample.hip", "draft_sample.hip", "tree_commit.hip",
-           "fourbit_rows.hip", "fourbit_attn.hip", "pages.hip", "logits_rules.hip"]
+           "fourbit_rows.hip", "fourbit_attn.hip", "pages.hip", "logits_rules.hip",
+           "chunk_attn.hip", "weight_sums.hip", "kv_evict.hip", "token_logprobs.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

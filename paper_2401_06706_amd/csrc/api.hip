@@ -34,7 +34,8 @@ long long g_count[K_COUNT];
 const char *const g_names[K_COUNT] = {"tree_attn_mfma", "tree_attn_generic", "tree_attn_combine",
                                       "verify_rows", "walk", "draft_rows", "tree_build", "kv_copy", "kv_finish",
                                       "kv_store_fourbit", "kv_load_fourbit", "attn_fourbit", "attn_fourbit_combine",
-                                      "page_assign", "page_slots", "logits_rules"};
+                                      "page_assign", "page_slots", "logits_rules",
+                                      "kv_store_paged", "chunk_attn", "chunk_merge", "weight_sums", "evict_select", "evict_move", "token_logprobs", "logprob_merge"};
 }  // namespace
 
 bool timing_new_events(hipEvent_t *start, hipEvent_t *stop)
@@ -467,6 +468,163 @@ int32_t mcsd_kv_load_fourbit(const mcsd_rows_desc *d, const mcsd_rows_bufs *b, c
 {
     const int32_t rc = check_rows(d, b, kv);
     return rc != MCSD_OK ? rc : launch_fourbit_rows(*d, *b, *kv, false, (hipStream_t)stream);
+}
+
+// ------------------------------------------------- prompts in chunks over a paged cache, eviction
+// L_stride > 0: the logical capacity that the block table has to hold (a store by slot has none: 0)
+static int32_t check_pages(const char *what, const mcsd_paged_kv *kv, long L_stride)
+{
+    if (!kv) { set_error("%s: paged descriptor is NULL", what); return MCSD_E_NULL; }
+    if (kv->struct_size != sizeof(mcsd_paged_kv)) { set_error("%s: paged struct_size %u != %zu", what, kv->struct_size, sizeof(mcsd_paged_kv)); return MCSD_E_SHAPE; }
+    if (kv->page_size < 32 || kv->page_size % 32 != 0) { set_error("%s: page_size %d is not a positive multiple of 32", what, kv->page_size); return MCSD_E_SHAPE; }
+    if (kv->n_pages < 1 || (L_stride > 0 && kv->max_pages_per_seq < 1)) { set_error("%s: non-positive size", what); return MCSD_E_SHAPE; }
+    if ((long)kv->n_pages * kv->page_size > 0x7fffffffL) { set_error("%s: n_pages * page_size does not fit a slot", what); return MCSD_E_UNSUPPORTED; }
+    if (L_stride > 0 && !kv->block_table) { set_error("%s: block_table is NULL", what); return MCSD_E_NULL; }
+    if (L_stride > 0 && (long)kv->max_pages_per_seq * kv->page_size < L_stride) { set_error("%s: L_stride %ld exceeds max_pages_per_seq * page_size", what, L_stride); return MCSD_E_SHAPE; }
+    return MCSD_OK;
+}
+
+static int32_t check_head_dim(const char *what, int d, int dtype)
+{
+    if (dtype != MCSD_DTYPE_FP32 && dtype != MCSD_DTYPE_BF16) { set_error("%s: unknown dtype %d", what, dtype); return MCSD_E_UNSUPPORTED; }
+    if (d < 1 || d > MCSD_MAX_HEAD_DIM || d % (dtype == MCSD_DTYPE_BF16 ? 8 : 4) != 0) { set_error("%s: head dim %d unsupported", what, d); return MCSD_E_UNSUPPORTED; }
+    return MCSD_OK;
+}
+
+int32_t mcsd_kv_store_paged(const mcsd_rows_desc *d, const mcsd_store_bufs *b, const mcsd_paged_kv *kv, void *stream)
+{
+    if (!d) { set_error("rows desc is NULL"); return MCSD_E_NULL; }
+    if (d->struct_size != sizeof(mcsd_rows_desc)) { set_error("rows desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_rows_desc)); return MCSD_E_SHAPE; }
+    if (d->T < 0 || d->H_kv < 1 || d->n_layers < 1) { set_error("rows: non-positive size"); return MCSD_E_SHAPE; }
+    int32_t rc = check_head_dim("rows", d->d, d->dtype);
+    if (rc != MCSD_OK) return rc;
+    rc = check_pages("rows", kv, 0);
+    if (rc != MCSD_OK) return rc;
+    const int64_t row = (int64_t)d->H_kv * d->d, per16 = d->dtype == MCSD_DTYPE_FP32 ? 4 : 8;
+    // (a launch has fewer than 2^32 threads)
+    if (d->n_layers > 65535 || d->T > (1 << 30) || d->H_kv > 65535 || d->T * (row / per16) >= 1L << 31) { set_error("rows: grid too large"); return MCSD_E_UNSUPPORTED; }
+    if (d->k_stride < row || d->v_stride < row) { set_error("rows: a stride is less than a row"); return MCSD_E_SHAPE; }
+    if (d->k_stride % per16 != 0 || d->v_stride % per16 != 0) { set_error("rows: strides must be multiples of 16 bytes"); return MCSD_E_SHAPE; }
+    if (d->n_layers > 1 && (d->k_layer_stride % per16 != 0 || d->v_layer_stride % per16 != 0 || d->k_layer_stride < 0 || d->v_layer_stride < 0)) {
+        set_error("rows: layer strides must be multiples of 16 bytes");
+        return MCSD_E_SHAPE;
+    }
+    if (!b) { set_error("rows bufs is NULL"); return MCSD_E_NULL; }
+    if (b->struct_size != sizeof(mcsd_store_bufs)) { set_error("rows bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_store_bufs)); return MCSD_E_SHAPE; }
+    if (d->T == 0) return MCSD_OK;
+    if (!b->k || !b->v || !b->slot_map || !b->k_pool || !b->v_pool) { set_error("rows: NULL buffer"); return MCSD_E_NULL; }
+    if (((uintptr_t)b->k | (uintptr_t)b->v | (uintptr_t)b->k_pool | (uintptr_t)b->v_pool) & 15u) { set_error("rows: k, v and the pools must be 16-byte aligned"); return MCSD_E_SHAPE; }
+    return launch_kv_store_paged(*d, *b, *kv, (hipStream_t)stream);
+}
+
+static int32_t check_chunk(const mcsd_chunk_desc *d)
+{
+    if (!d) { set_error("chunk desc is NULL"); return MCSD_E_NULL; }
+    if (d->struct_size != sizeof(mcsd_chunk_desc)) { set_error("chunk desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_chunk_desc)); return MCSD_E_SHAPE; }
+    if (d->B < 1 || d->T < 0 || d->H_q < 1 || d->H_kv < 1 || d->L_stride < 1) { set_error("chunk: non-positive size"); return MCSD_E_SHAPE; }
+    if (d->H_q % d->H_kv != 0) { set_error("chunk: H_q %d not a multiple of H_kv %d", d->H_q, d->H_kv); return MCSD_E_SHAPE; }
+    const int32_t rc = check_head_dim("chunk", d->d, d->dtype);
+    if (rc != MCSD_OK) return rc;
+    if (d->B > 65535 || d->H_kv > 65535) { set_error("chunk: B %d or H_kv %d > 65535", d->B, d->H_kv); return MCSD_E_UNSUPPORTED; }
+    if (d->L_stride > (1 << 22)) { set_error("chunk: L_stride %d > %d", d->L_stride, 1 << 22); return MCSD_E_UNSUPPORTED; }
+    if ((long)d->T * d->H_q >= 1L << 30) { set_error("chunk: T * H_q %ld >= 2^30", (long)d->T * d->H_q); return MCSD_E_UNSUPPORTED; }
+    if (!(d->scale >= 0.f) || !(d->scale < 1e30f)) { set_error("chunk: scale must be finite and >= 0"); return MCSD_E_SHAPE; }
+    if (d->q_stride < (int64_t)d->H_q * d->d || d->q_stride % (d->dtype == MCSD_DTYPE_FP32 ? 4 : 8) != 0) { set_error("chunk: q_stride is less than a row or no multiple of 16 bytes"); return MCSD_E_SHAPE; }
+    return MCSD_OK;
+}
+
+size_t mcsd_chunk_workspace_bytes(const mcsd_chunk_desc *d)
+{
+    ChunkPlan plan;
+    return check_chunk(d) == MCSD_OK && make_chunk_plan(*d, &plan) ? plan.ws_bytes : 0;
+}
+
+int32_t mcsd_chunk_attn_paged(const mcsd_chunk_desc *d, const mcsd_chunk_bufs *b, const mcsd_paged_kv *kv, void *stream)
+{
+    int32_t rc = check_chunk(d);
+    if (rc != MCSD_OK) return rc;
+    ChunkPlan plan;
+    if (!make_chunk_plan(*d, &plan)) { set_error("chunk: no kernel for this shape"); return MCSD_E_UNSUPPORTED; }
+    rc = check_pages("chunk", kv, d->L_stride);
+    if (rc != MCSD_OK) return rc;
+    if (!b) { set_error("chunk bufs is NULL"); return MCSD_E_NULL; }
+    if (b->struct_size != sizeof(mcsd_chunk_bufs)) { set_error("chunk bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_chunk_bufs)); return MCSD_E_SHAPE; }
+    if (d->T == 0) return MCSD_OK;
+    if (!b->q || !b->k_pool || !b->v_pool || !b->chunk_start || !b->prefix_len || !b->out) { set_error("chunk: NULL buffer"); return MCSD_E_NULL; }
+    if (((uintptr_t)b->q | (uintptr_t)b->k_pool | (uintptr_t)b->v_pool | (uintptr_t)b->out) & 15u) { set_error("chunk: tensors must be 16-byte aligned"); return MCSD_E_SHAPE; }
+    if (plan.ws_bytes > 0) {
+        if (!b->workspace) { set_error("chunk: workspace is NULL, %zu bytes needed", plan.ws_bytes); return MCSD_E_WORKSPACE; }
+        if (b->workspace_bytes < plan.ws_bytes) { set_error("chunk: workspace %zu < %zu bytes", b->workspace_bytes, plan.ws_bytes); return MCSD_E_WORKSPACE; }
+        if (((uintptr_t)b->workspace & 255u) != 0) { set_error("chunk: workspace not 256-byte aligned"); return MCSD_E_WORKSPACE; }
+    }
+    return launch_chunk_attn(*d, *b, *kv, plan, (hipStream_t)stream);
+}
+
+int32_t mcsd_attn_weight_sums(const mcsd_chunk_desc *d, const mcsd_sums_bufs *b, const mcsd_paged_kv *kv, void *stream)
+{
+    int32_t rc = check_chunk(d);
+    if (rc != MCSD_OK) return rc;
+    rc = check_pages("sums", kv, d->L_stride);
+    if (rc != MCSD_OK) return rc;
+    if (!b) { set_error("sums bufs is NULL"); return MCSD_E_NULL; }
+    if (b->struct_size != sizeof(mcsd_sums_bufs)) { set_error("sums bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_sums_bufs)); return MCSD_E_SHAPE; }
+    if (b->last_rows < 0) { set_error("sums: last_rows %d < 0", b->last_rows); return MCSD_E_SHAPE; }
+    if (d->T == 0) return MCSD_OK;
+    if (!b->q || !b->k_pool || !b->chunk_start || !b->prefix_len || !b->lse || !b->sums) { set_error("sums: NULL buffer"); return MCSD_E_NULL; }
+    if (((uintptr_t)b->q | (uintptr_t)b->k_pool) & 15u) { set_error("sums: q and the pool must be 16-byte aligned"); return MCSD_E_SHAPE; }
+    return launch_weight_sums(*d, *b, *kv, (hipStream_t)stream);
+}
+
+int32_t mcsd_kv_evict_paged(const mcsd_evict_desc *d, const mcsd_evict_bufs *b, const mcsd_paged_kv *kv, void *stream)
+{
+    if (!d) { set_error("evict desc is NULL"); return MCSD_E_NULL; }
+    if (d->struct_size != sizeof(mcsd_evict_desc)) { set_error("evict desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_evict_desc)); return MCSD_E_SHAPE; }
+    if (d->B < 1 || d->H_kv < 1 || d->L_stride < 1 || d->n_layers < 1 || d->n_first < 0 || d->n_recent < 0) { set_error("evict: non-positive size"); return MCSD_E_SHAPE; }
+    int32_t rc = check_head_dim("evict", d->d, d->dtype);
+    if (rc != MCSD_OK) return rc;
+    if (d->B > 65535 || d->L_stride > (1 << 22) || (__int128)d->n_layers * d->B * d->H_kv >= 1 << 24) { set_error("evict: B, L_stride or n_layers * B * H_kv too large"); return MCSD_E_UNSUPPORTED; }
+    rc = check_pages("evict", kv, d->L_stride);
+    if (rc != MCSD_OK) return rc;
+    if (!b) { set_error("evict bufs is NULL"); return MCSD_E_NULL; }
+    if (b->struct_size != sizeof(mcsd_evict_bufs)) { set_error("evict bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_evict_bufs)); return MCSD_E_SHAPE; }
+    if (!b->k_pool || !b->v_pool || !b->sums || !b->prefix_len || !b->keep_len || !b->kept || !b->flags) { set_error("evict: NULL buffer"); return MCSD_E_NULL; }
+    if (((uintptr_t)b->k_pool | (uintptr_t)b->v_pool) & 15u) { set_error("evict: pools must be 16-byte aligned"); return MCSD_E_SHAPE; }
+    if (b->out_table == kv->block_table) { set_error("evict: out_table is the block table (NULL moves in place)"); return MCSD_E_SHAPE; }
+    return launch_kv_evict(*d, *b, *kv, (hipStream_t)stream);
+}
+
+// --------------------------------------------------------- log probabilities of tokens
+static int32_t check_logprob(const mcsd_logprob_desc *d)
+{
+    if (!d) { set_error("logprob desc is NULL"); return MCSD_E_NULL; }
+    if (d->struct_size != sizeof(mcsd_logprob_desc)) { set_error("logprob desc struct_size %u != %zu", d->struct_size, sizeof(mcsd_logprob_desc)); return MCSD_E_SHAPE; }
+    if (d->rows < 0 || d->R < 1 || d->V < 1 || d->n_top < 0) { set_error("logprob: non-positive size"); return MCSD_E_SHAPE; }
+    if (d->V > (1 << 30) || d->rows > (1 << 22)) { set_error("logprob: V %d > 2^30 or rows %d > 2^22", d->V, d->rows); return MCSD_E_UNSUPPORTED; }
+    if (d->dtype != MCSD_DTYPE_FP32 && d->dtype != MCSD_DTYPE_BF16) { set_error("logprob: unknown dtype %d", d->dtype); return MCSD_E_UNSUPPORTED; }
+    if (d->n_top > MCSD_MAX_TOP || d->n_top > d->V) { set_error("logprob: n_top %d > %d or V", d->n_top, MCSD_MAX_TOP); return MCSD_E_UNSUPPORTED; }
+    if (d->row_stride < d->V) { set_error("logprob: row_stride is less than V"); return MCSD_E_SHAPE; }
+    return MCSD_OK;
+}
+
+size_t mcsd_logprob_workspace_bytes(const mcsd_logprob_desc *d) { return check_logprob(d) == MCSD_OK ? logprob_workspace(*d) : 0; }
+
+int32_t mcsd_token_logprobs(const mcsd_logprob_desc *d, const mcsd_logprob_bufs *b, void *stream)
+{
+    const int32_t rc = check_logprob(d);
+    if (rc != MCSD_OK) return rc;
+    if (!b) { set_error("logprob bufs is NULL"); return MCSD_E_NULL; }
+    if (b->struct_size != sizeof(mcsd_logprob_bufs)) { set_error("logprob bufs struct_size %u != %zu", b->struct_size, sizeof(mcsd_logprob_bufs)); return MCSD_E_SHAPE; }
+    if (!b->row_map && d->rows > d->R) { set_error("logprob: %d rows of %d without a row_map", d->rows, d->R); return MCSD_E_SHAPE; }
+    if (d->rows == 0) return MCSD_OK;
+    if (!b->logits || !b->tokens || !b->logprob || !b->flags || (d->n_top > 0 && (!b->top_tok || !b->top_logprob))) { set_error("logprob: NULL buffer"); return MCSD_E_NULL; }
+    if ((uintptr_t)b->logits % (d->dtype == MCSD_DTYPE_FP32 ? 4 : 2) != 0) { set_error("logprob: misaligned logits"); return MCSD_E_SHAPE; }
+    const size_t need = logprob_workspace(*d);
+    if (need > 0) {
+        if (!b->workspace) { set_error("logprob: workspace is NULL, %zu bytes needed", need); return MCSD_E_WORKSPACE; }
+        if (b->workspace_bytes < need) { set_error("logprob: workspace %zu < %zu bytes", b->workspace_bytes, need); return MCSD_E_WORKSPACE; }
+        if (((uintptr_t)b->workspace & 255u) != 0) { set_error("logprob: workspace not 256-byte aligned"); return MCSD_E_WORKSPACE; }
+    }
+    return launch_token_logprobs(*d, *b, (hipStream_t)stream);
 }
 
 // ------------------------------------------------------- pages from lengths, rules on logits

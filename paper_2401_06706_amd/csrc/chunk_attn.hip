@@ -1,0 +1,453 @@
+// Attention of a chunk of new tokens over a paged cache (a prompt, a piece of one, a lone token; a batch mixes them), and the
+// store of their keys and values into its pages.
+#include <type_traits>
+
+#include "chunk_common.h"
+
+namespace mcsd {
+namespace {
+
+constexpr int RT = 128;                 // query rows of a workgroup, 32 a wavefront
+constexpr int OFF_NOWHERE = 0x7fff0000; // an offset beyond every buffer's extent: reads as zero
+
+// The work of a launch, the same list in every workgroup and in the merge: rows r = token * G + head in group of a (sequence, KV head) in
+// tiles of RT, a tile's keys in equal segments.  A segment is so long that all of them make about p.target
+// workgroups per KV head, at least p.min_seg tiles; a sequence is cut into kt / segment of them, rounded, one for most.
+struct Item { int b, rt, seg, n_seg, part; ChunkSeq s; };
+
+__device__ __forceinline__ int segment_length(const ChunkParams &p, int lane)
+{
+    float work = 0.f;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        if (b0 + lane >= p.B) break;
+        const ChunkSeq s = chunk_sequence(p, b0 + lane);
+        work += (float)((s.n * p.G + RT - 1) / RT) * (float)((s.keys + KT - 1) / KT);
+    }
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) work += __shfl_xor(work, m);
+    return max(p.min_seg, (int)ceilf(work / p.target));
+}
+
+// item number idx (MERGE: tile of rows number idx of those whose keys are cut); false: there are fewer
+template <bool MERGE>
+__device__ __forceinline__ bool find_item(const ChunkParams &p, int idx, int lane, Item *it)
+{
+    const int len = p.max_parts ? segment_length(p, lane) : 0;
+    int items = 0, parts = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        ChunkSeq s = {0, 0, 0, 0};
+        if (b0 + lane < p.B) s = chunk_sequence(p, b0 + lane);
+        const int rt = (s.n * p.G + RT - 1) / RT, kt = (s.keys + KT - 1) / KT;
+        int n_seg = p.max_parts ? max(1, (kt + len / 2) / len) : 1;
+        const int my_parts = n_seg > 1 ? rt * n_seg : 0;
+        const int parts_to = parts + wave_running_sum(my_parts);
+        if (parts_to > p.max_parts) n_seg = 1;          // (cannot be, but by arrays that contradict themselves)
+        const int my_items = MERGE ? (n_seg > 1 ? rt : 0) : rt * n_seg;
+        const int items_to = items + wave_running_sum(my_items);
+        const unsigned long long found = __ballot(items_to > idx);
+        if (found) {
+            const int o = __ffsll((long long)found) - 1;
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, o); };
+            it->b = b0 + o;
+            it->s = {of(s.s0), of(s.n), of(s.L), of(s.keys)};
+            it->n_seg = of(n_seg);
+            const int local = idx - of(items_to - my_items);
+            it->rt = of(rt) - 1 - (MERGE ? local : local / it->n_seg);      // the last rows, with the most keys, first
+            it->seg = MERGE ? 0 : local % it->n_seg;
+            it->part = of(parts_to - my_parts) + it->rt * it->n_seg + it->seg;
+            return true;
+        }
+        items = __builtin_amdgcn_readlane(items_to, 63);
+        parts = __builtin_amdgcn_readlane(parts_to, 63);
+    }
+    return false;
+}
+
+__device__ __forceinline__ u32x4 finite_or_zero(u32x4 v, bool f32, bool *bad)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t e_lo = f32 ? 0u : 0x00007f80u, e_hi = 0x7f800000u;
+        const bool hi = (v[i] & e_hi) == e_hi, lo = !f32 && (v[i] & e_lo) == e_lo;
+        *bad |= hi | lo;
+        if (f32) v[i] = hi ? 0u : v[i];
+        else v[i] = (hi ? 0u : v[i] & 0xffff0000u) | (lo ? 0u : v[i] & 0xffffu);
+    }
+    return v;
+}
+
+template <int DP, bool F32>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * (F32 ? 4 : 2) <= 256 ? 2 : 1)))
+void chunk_attn_kernel(ChunkParams p)
+{
+    using S = TileShape<DP, F32>;
+    constexpr int NT = DP / 32, BUF_WORDS = KT * (S::PK + S::PV);
+    constexpr bool TWO_TERMS = !F32 && DP != 128;       // of the weights in PV, as in tree attention
+    __shared__ __attribute__((aligned(16))) uint32_t s_tiles[2 * BUF_WORDS];
+    __shared__ int s_bad;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = lane >> 5, l32 = lane & 31, lj = lane >> 4, lc = lane & 15;
+    const int g = blockIdx.x;
+    Item it;
+    if (!find_item<false>(p, blockIdx.y, lane, &it)) return;
+    const int M = it.s.n * p.G, row0 = it.rt * RT + 32 * wave;
+    auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
+    const int kt = position(min(it.rt * RT + RT, M) - 1) / KT + 1;           // key tiles that some row of this tile sees
+    const int seg = (kt + it.n_seg - 1) / it.n_seg, t_begin = it.seg * seg, t_end = min(kt, t_begin + seg);
+    const int diagonal = (position(it.rt * RT) + 1) / KT;                    // from this tile on there are keys that some row does not see
+    const bool active = row0 < M;
+    const int my_row = min(row0 + l32, M - 1), my_pos = position(my_row);
+    // tiles that every row of this wavefront sees whole; tiles that any of them sees
+    const int t_plain = active ? min(t_end, (position(row0) + 1) / KT) : t_begin;
+    const int t_seen = active ? min(t_end, position(min(row0 + 32, M) - 1) / KT + 1) : t_begin;
+    if (tid == 0) s_bad = 0;
+
+    u32x4 q[S::KK];
+    {
+        const int head = g * p.G + my_row % p.G;
+        const char *src = static_cast<const char *>(p.q) + (size_t)(it.s.s0 + my_row / p.G) * p.q_row + (size_t)head * p.d * S::ES;
+#pragma unroll
+        for (int kk = 0; kk < S::KK; ++kk) {
+            const int at = 32 * kk + 16 * h;
+            const u32x4 zero = {0, 0, 0, 0};
+            q[kk] = DP * S::ES == 256 && p.d == DP ? *reinterpret_cast<const u32x4 *>(src + at)
+                                                   : (at < p.d * S::ES ? *reinterpret_cast<const u32x4 *>(src + at) : zero);
+        }
+    }
+    f32x16 o[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[nt][i] = 0.f;
+    float m_used = M_INIT, l_part = 0.f;
+    const float c2 = p.scale_log2;
+
+    // ---- tiles: global -> registers -> LDS
+    const int row_bytes = p.d * S::ES;
+    uint32_t load_at[S::PER_THREAD], k_st[S::PER_THREAD], v_st[S::PER_THREAD];
+#pragma unroll
+    for (int j = 0; j < S::PER_THREAD; ++j) {
+        const int e = tid + 256 * j, row = e / S::GRANULES, c = e % S::GRANULES;
+        load_at[j] = e < KT * S::GRANULES && 16 * c < row_bytes ? row * row_bytes + 16 * c : OFF_NOWHERE;
+        k_st[j] = row * S::PK + 4 * c;
+        v_st[j] = KT * S::PK + row * S::PV + 4 * c;
+    }
+    const const_i32_ptr table = (const_i32_ptr)(uintptr_t)(p.block_table + (size_t)it.b * p.max_pages);
+    u32x4 kr[2][S::PER_THREAD], vr[2][S::PER_THREAD];
+    auto load_kv = [&](int t, int st) __attribute__((always_inline)) {
+        const int page = t < t_end ? (int)table[t * KT / p.page_size] : -1;
+        const bool in = (unsigned)page < (unsigned)p.n_pages;
+        const size_t off = in ? (((size_t)page * p.H_kv + g) * p.page_size + t * KT % p.page_size) * row_bytes : 0;
+        const uint32_t extent = in ? (uint32_t)max(0, min(KT, it.s.keys - t * KT)) * row_bytes : 0u;
+        const __amdgpu_buffer_rsrc_t rk = make_rsrc(static_cast<const char *>(p.k_pool) + off, extent);
+        const __amdgpu_buffer_rsrc_t rv = make_rsrc(static_cast<const char *>(p.v_pool) + off, extent);
+#pragma unroll
+        for (int j = 0; j < S::PER_THREAD; ++j) {
+            kr[st][j] = __builtin_amdgcn_raw_buffer_load_b128(rk, load_at[j], 0, 0);
+            vr[st][j] = __builtin_amdgcn_raw_buffer_load_b128(rv, load_at[j], 0, 0);
+        }
+    };
+    bool bad = false;
+    auto store_kv = [&](int t, uint32_t *buf, int st) __attribute__((always_inline)) {
+        if (t >= diagonal && t < t_end) {
+            // A weight of 0 times a value that is no number is none either: here, where rows do not see all keys, such values
+            // enter the products as zeros and are added in the epilogue to the rows that see them.
+#pragma unroll
+            for (int j = 0; j < S::PER_THREAD; ++j) vr[st][j] = finite_or_zero(vr[st][j], F32, &bad);
+        }
+#pragma unroll
+        for (int j = 0; j < S::PER_THREAD; ++j)
+            if (KT * S::GRANULES % 256 == 0 || tid + 256 * j < KT * S::GRANULES) {
+                *reinterpret_cast<u32x4 *>(buf + k_st[j]) = kr[st][j];
+                *reinterpret_cast<u32x4 *>(buf + v_st[j]) = vr[st][j];
+            }
+    };
+    const uint32_t k_ld = l32 * S::PK + 4 * h;
+    const uint32_t v_ld = F32 ? KT * S::PK + 4 * h * S::PV + l32
+                              : KT * S::PK + (4 * h + (lc >> 2)) * S::PV + 8 * (lj & 1) + 2 * (lc & 3);
+    typedef short v4i16 __attribute__((ext_vector_type(4)));
+    typedef v4i16 __attribute__((address_space(3))) *lds_v4i16_ptr;
+
+    auto compute = [&](int t, const uint32_t *cb, auto masked_tag) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked_tag)::value;
+        f32x16 s = tile_scores<DP, F32>(cb + k_ld, q);
+        const int seen = my_pos - t * KT - 4 * h;       // key_of_score(i) <= seen: row sees it
+        float w[16], sum;
+        auto weights = [&]() __attribute__((always_inline)) {
+            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                w[i] = fast_exp2(fmaf(s[i], c2, -m_used));
+                if (MASKED && key_of_score(i) > seen) w[i] = 0.f;
+                sum += w[i];
+            }
+        };
+        weights();
+        // The maximum is raised only where the weights outgrow it: their sum, which is formed anyway, tells.
+        if (__builtin_expect(__any(!(sum <= 4096.f)), 0)) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!MASKED || key_of_score(i) <= seen) mx = fmaxf(mx, s[i] * c2);
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            // (row by row, so that no row's bits depend on its neighbours')
+            const bool raise = __shfl_xor((int)!(sum <= 4096.f), 32) | (int)!(sum <= 4096.f);
+            const float m_new = raise ? fmaxf(m_used, mx) : m_used, alpha = fast_exp2(m_used - m_new);
+            m_used = m_new;
+            l_part *= alpha;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[nt][i] *= alpha;
+            weights();
+        }
+        l_part += sum;
+        if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+                    o[nt] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(cb[v_ld + key_of_score(i) * S::PV + 32 * nt]), w[i], o[nt], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                u32x4 hi, lo;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w0 = w[8 * m + 2 * i], w1 = w[8 * m + 2 * i + 1];
+                    if constexpr (TWO_TERMS) {
+                        // The first term is cut, so that the second is never negative, nor, by the 2^-23 added, zero for a weight
+                        // that is not: with an infinite value both terms then agree.
+                        hi[i] = __builtin_amdgcn_perm(__float_as_uint(w1), __float_as_uint(w0), 0x07060302);
+                        lo[i] = pack_bf16(fmaf(w0, 1.0f + 0x1p-23f, -__uint_as_float(hi[i] << 16)), fmaf(w1, 1.0f + 0x1p-23f, -__uint_as_float(hi[i] & 0xffff0000u)));
+                    } else {
+                        hi[i] = pack_bf16(w0, w1);
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(cb + v_ld + 16 * m * S::PV + 16 * nt));
+                    const v4i16 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(cb + v_ld + (16 * m + 8) * S::PV + 16 * nt));
+                    const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, hi), o[nt], 0, 0, 0);
+                    if constexpr (TWO_TERMS) o[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, lo), o[nt], 0, 0, 0);
+                }
+            }
+        }
+    };
+
+    // Tile t is in buffer t % 2 of LDS behind the barrier of its step; t + 1 is stored and t + 3 asked for during it.
+    auto step = [&](int t, auto stage) __attribute__((always_inline)) {
+        constexpr int ST = decltype(stage)::value;
+        __syncthreads();
+        store_kv(t + 1, s_tiles + (ST ^ 1) * BUF_WORDS, ST ^ 1);
+        load_kv(t + 3, ST ^ 1);
+        if (t < t_plain) compute(t, s_tiles + ST * BUF_WORDS, std::false_type());
+        else if (t < t_seen) compute(t, s_tiles + ST * BUF_WORDS, std::true_type());
+    };
+    int t = t_begin;
+    load_kv(t, 0);
+    load_kv(t + 1, 1);
+    store_kv(t, s_tiles, 0);
+    load_kv(t + 2, 0);
+    for (; t + 1 < t_end; t += 2) {
+        step(t, std::integral_constant<int, 0>());
+        step(t + 1, std::integral_constant<int, 1>());
+    }
+    if (t < t_end) step(t, std::integral_constant<int, 0>());
+    if (__any(bad) && lane == 0) s_bad = 1;
+    __syncthreads();
+    if (!active) return;
+
+    // ---- epilogue: a lane holds columns 32 nt + 8 a + 4 h .. + 3 of its row
+    if (__builtin_expect(s_bad, 0)) {
+        for (int key = max(diagonal, t_begin) * KT; key <= min(my_pos, t_end * KT - 1); ++key) {
+            const int page = p.block_table[(size_t)it.b * p.max_pages + key / p.page_size];
+            if ((unsigned)page >= (unsigned)p.n_pages) continue;
+            const char *v = static_cast<const char *>(p.v_pool) + (((size_t)page * p.H_kv + g) * p.page_size + key % p.page_size) * row_bytes;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int c = 32 * nt + 8 * (i >> 2) + 4 * h + (i & 3);
+                    if (c >= p.d) continue;
+                    const float x = F32 ? reinterpret_cast<const float *>(v)[c] : bf16_bits_to_float(reinterpret_cast<const uint16_t *>(v)[c]);
+                    if (!(fabsf(x) < INFINITY)) o[nt][i] += x;
+                }
+        }
+    }
+    const float l_row = l_part + __shfl_xor(l_part, 32);
+    if (row0 + l32 >= M) return;
+    const int token = it.s.s0 + my_row / p.G, head = g * p.G + my_row % p.G;
+    if (it.n_seg == 1) {
+        const float f = 1.0f / l_row;
+        char *dst = static_cast<char *>(p.out) + ((size_t)token * p.H_q + head) * row_bytes;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const int c = 32 * nt + 8 * a + 4 * h;
+                if (c >= p.d) continue;
+                const float x0 = o[nt][4 * a] * f, x1 = o[nt][4 * a + 1] * f, x2 = o[nt][4 * a + 2] * f, x3 = o[nt][4 * a + 3] * f;
+                if (F32) *reinterpret_cast<float4 *>(dst + 4 * c) = make_float4(x0, x1, x2, x3);
+                else *reinterpret_cast<uint2 *>(dst + 2 * c) = make_uint2(pack_bf16(x0, x1), pack_bf16(x2, x3));
+            }
+        if (p.lse && h == 0) p.lse[(size_t)token * p.H_q + head] = (m_used + __builtin_amdgcn_logf(l_row)) * LN2_F;
+        return;
+    }
+    const size_t prow = ((size_t)it.part * p.H_kv + g) * RT + 32 * wave + l32;
+    if (h == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * prow) = make_float2(m_used, l_row);
+    float *dst = p.part_o + prow * DP;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+            *reinterpret_cast<float4 *>(dst + 32 * nt + 8 * a + 4 * h) = make_float4(o[nt][4 * a], o[nt][4 * a + 1], o[nt][4 * a + 2], o[nt][4 * a + 3]);
+}
+
+// The segments of the rows whose keys are cut.  Eight lanes a row, four columns each; grid (KV heads, tiles of rows, quarters of a tile).
+template <int DP, bool F32>
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p)
+{
+    const int tid = threadIdx.x, lane = tid & 63, g = blockIdx.x;
+    Item it;
+    if (!find_item<true>(p, blockIdx.y, lane, &it)) return;
+    const int M = it.s.n * p.G, in_tile = 32 * blockIdx.z + tid / 8, row = it.rt * RT + in_tile;
+    if (row >= M) return;
+    const size_t step = (size_t)p.H_kv * RT, first = ((size_t)it.part * p.H_kv + g) * RT + in_tile;
+    float m = M_INIT;
+    for (int s = 0; s < it.n_seg; ++s) m = fmaxf(m, p.part_ml[2 * (first + s * step)]);
+    float4 acc[DP / 32];
+#pragma unroll
+    for (int k = 0; k < DP / 32; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+    for (int s = 0; s < it.n_seg; ++s) {
+        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * (first + s * step));
+        if (ml.y == 0.f) continue;              // a segment that the row sees nothing of
+        const float f = fast_exp2(ml.x - m);
+        l += f * ml.y;
+#pragma unroll
+        for (int k = 0; k < DP / 32; ++k) {
+            const float4 x = *reinterpret_cast<const float4 *>(p.part_o + (first + s * step) * DP + 32 * k + 4 * (tid & 7));
+            acc[k].x += f * x.x; acc[k].y += f * x.y; acc[k].z += f * x.z; acc[k].w += f * x.w;
+        }
+    }
+    const float f = 1.0f / l;
+    const int token = it.s.s0 + row / p.G, head = g * p.G + row % p.G;
+    const size_t at = (size_t)token * p.H_q + head;
+#pragma unroll
+    for (int k = 0; k < DP / 32; ++k) {
+        const int c = 32 * k + 4 * (tid & 7);
+        if (c >= p.d) continue;
+        if (F32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at * p.d + c) = make_float4(acc[k].x * f, acc[k].y * f, acc[k].z * f, acc[k].w * f);
+        else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at * p.d + c) = make_uint2(pack_bf16(acc[k].x * f, acc[k].y * f), pack_bf16(acc[k].z * f, acc[k].w * f));
+    }
+    if (p.lse && (tid & 7) == 0) p.lse[at] = (m + __builtin_amdgcn_logf(l)) * LN2_F;
+}
+
+// ---- rows of new tokens into their pages: 16 bytes of K and of V a thread
+struct StoreParams {
+    size_t pieces;                      // T * pieces of a row
+    int row_pieces, head_pieces, page_size, n_slots, H_kv;
+    const char *k, *v;
+    char *k_pool, *v_pool;
+    size_t k_stride, v_stride, k_layer, v_layer, pool_layer;        // bytes
+    const int32_t *slot_map;
+};
+
+__global__ __launch_bounds__(256) void kv_store_paged_kernel(StoreParams p)
+{
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= p.pieces) return;
+    const int t = (int)(i / p.row_pieces), c = (int)(i % p.row_pieces), head = c / p.head_pieces, in_head = c % p.head_pieces;
+    const u32x4 k = *reinterpret_cast<const u32x4 *>(p.k + blockIdx.y * p.k_layer + t * p.k_stride + 16 * (size_t)c);
+    const u32x4 v = *reinterpret_cast<const u32x4 *>(p.v + blockIdx.y * p.v_layer + t * p.v_stride + 16 * (size_t)c);
+    const int slot = p.slot_map[t];
+    if ((unsigned)slot >= (unsigned)p.n_slots) return;
+    const size_t at = blockIdx.y * p.pool_layer +
+                      ((((size_t)(slot / p.page_size) * p.H_kv + head) * p.page_size + slot % p.page_size) * p.head_pieces + in_head) * 16;
+    *reinterpret_cast<u32x4 *>(p.k_pool + at) = k;
+    *reinterpret_cast<u32x4 *>(p.v_pool + at) = v;
+}
+
+int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
+
+template <int DP, bool F32>
+void launch_shape(const ChunkParams &p, const ChunkPlan &plan, hipStream_t stream)
+{
+    launch_kernel(K_CHUNK_ATTN, chunk_attn_kernel<DP, F32>, dim3(p.H_kv, plan.max_items), dim3(256), stream, p);
+    if (plan.max_parts) launch_kernel(K_CHUNK_MERGE, chunk_merge_kernel<DP, F32>, dim3(p.H_kv, plan.max_parts / 2, RT / 32), dim3(256), stream, p);
+}
+
+template <bool F32>
+void launch_type(const ChunkParams &p, const ChunkPlan &plan, hipStream_t stream)
+{
+    switch (padded_dim(p.d)) {
+    case 32: return launch_shape<32, F32>(p, plan, stream);
+    case 64: return launch_shape<64, F32>(p, plan, stream);
+    case 96: return launch_shape<96, F32>(p, plan, stream);
+    case 128: return launch_shape<128, F32>(p, plan, stream);
+    default: return launch_shape<256, F32>(p, plan, stream);
+    }
+}
+
+}  // namespace
+
+bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
+{
+    const long G = d.H_q / d.H_kv, T = d.T;
+    const long tiles = (T * G) / RT + (T < d.B ? T : d.B), by_token = T * ((G + RT - 1) / RT);
+    plan->row_tile = RT;
+    plan->max_row_tiles = (int)(tiles < by_token ? tiles : by_token);
+    plan->target = 512;
+    plan->min_seg = 8;
+    const long kt = (d.L_stride + KT - 1) / KT, n_seg = (kt + plan->min_seg / 2) / plan->min_seg;
+    const long target = plan->target / d.H_kv > 1 ? plan->target / d.H_kv : 1;
+    // a sequence that is cut has kt / len segments, rounded, two at least: 4/3 of kt / len at most
+    long parts = n_seg < 2 ? 0 : (4 * target + 2) / 3 + 2;
+    if (parts > plan->max_row_tiles * n_seg) parts = plan->max_row_tiles * n_seg;
+    plan->max_parts = (int)parts;
+    long items = plan->max_row_tiles + parts;
+    if (n_seg > 0 && items > plan->max_row_tiles * n_seg) items = plan->max_row_tiles * n_seg;
+    plan->max_items = (int)items;
+    const size_t rows = (size_t)parts * d.H_kv * RT;
+    plan->ws_bytes = (rows * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256;
+    return items <= 65535L * 16;
+}
+
+int32_t launch_chunk_attn(const mcsd_chunk_desc &d, const mcsd_chunk_bufs &b, const mcsd_paged_kv &kv, const ChunkPlan &plan, hipStream_t stream)
+{
+    ChunkParams p = chunk_params(d, kv);
+    p.q = b.q; p.k_pool = b.k_pool; p.v_pool = b.v_pool; p.chunk_start = b.chunk_start; p.prefix_len = b.prefix_len; p.out = b.out; p.lse = b.lse;
+    p.min_seg = plan.min_seg; p.max_parts = plan.max_parts;
+    p.target = (float)(plan.target / d.H_kv > 1 ? plan.target / d.H_kv : 1);
+    p.part_o = static_cast<float *>(b.workspace);
+    if (plan.max_parts) p.part_ml = p.part_o + (size_t)plan.max_parts * d.H_kv * RT * padded_dim(d.d);
+    if (d.dtype == MCSD_DTYPE_FP32) launch_type<true>(p, plan, stream);
+    else launch_type<false>(p, plan, stream);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_error("chunk attention launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
+    return MCSD_OK;
+}
+
+int32_t launch_kv_store_paged(const mcsd_rows_desc &d, const mcsd_store_bufs &b, const mcsd_paged_kv &kv, hipStream_t stream)
+{
+    if (d.T == 0) return MCSD_OK;
+    const size_t esize = d.dtype == MCSD_DTYPE_FP32 ? 4 : 2;
+    StoreParams p;
+    p.head_pieces = (int)(d.d * esize / 16); p.row_pieces = p.head_pieces * d.H_kv; p.pieces = (size_t)d.T * p.row_pieces;
+    p.page_size = kv.page_size; p.n_slots = kv.n_pages * kv.page_size; p.H_kv = d.H_kv;
+    p.k = static_cast<const char *>(b.k); p.v = static_cast<const char *>(b.v);
+    p.k_pool = static_cast<char *>(b.k_pool); p.v_pool = static_cast<char *>(b.v_pool);
+    p.k_stride = d.k_stride * esize; p.v_stride = d.v_stride * esize;
+    p.k_layer = d.n_layers > 1 ? d.k_layer_stride * esize : 0; p.v_layer = d.n_layers > 1 ? d.v_layer_stride * esize : 0;
+    p.pool_layer = (size_t)p.n_slots * p.row_pieces * 16;
+    p.slot_map = b.slot_map;
+    launch_kernel(K_KV_STORE_PAGED, kv_store_paged_kernel, dim3((unsigned)((p.pieces + 255) / 256), d.n_layers), dim3(256), stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_error("kv store (pages) launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
+    return MCSD_OK;
+}
+
+}  // namespace mcsd

@@ -1,0 +1,100 @@
+// Shared by the kernels of chunks of new tokens over a paged cache: the sequences of a packed batch, tiles of 32 rows
+// in LDS, and small wavefront helpers.
+#pragma once
+
+#include "attn_common.h"
+
+namespace mcsd {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef const int32_t __attribute__((address_space(4))) *const_i32_ptr;      // wave-uniform reads through it are scalar loads
+
+constexpr float LN2_F = 0.69314718055994530942f;
+
+struct ChunkParams {
+    const void *q, *k_pool, *v_pool;
+    const int32_t *chunk_start, *prefix_len, *block_table;
+    void *out;
+    float *lse, *part_o, *part_ml;
+    int B, T, H_q, H_kv, G, d, L_stride, page_size, n_pages, max_pages;
+    int min_seg, max_parts;
+    float target;         // workgroups per KV head aimed at where keys are split
+    size_t q_row;         // bytes from a row of q to the next one's
+    float scale_log2;     // scale * log2(e)
+};
+
+inline ChunkParams chunk_params(const mcsd_chunk_desc &d, const mcsd_paged_kv &kv)
+{
+    ChunkParams p = {};
+    p.B = d.B; p.T = d.T; p.H_q = d.H_q; p.H_kv = d.H_kv; p.G = d.H_q / d.H_kv; p.d = d.d; p.L_stride = d.L_stride;
+    p.page_size = kv.page_size; p.n_pages = kv.n_pages; p.max_pages = kv.max_pages_per_seq; p.block_table = kv.block_table;
+    p.q_row = (size_t)d.q_stride * (d.dtype == MCSD_DTYPE_FP32 ? 4 : 2);
+    p.scale_log2 = d.scale * LOG2E_F;
+    return p;
+}
+
+// New tokens s0 .. s0 + n - 1 of a sequence stand at positions L .. L + n - 1; `keys` positions are there (below the capacity).
+// Whatever the caller's arrays hold, s0 + n <= T and keys <= L_stride.
+struct ChunkSeq { int s0, n, L, keys; };
+
+__device__ __forceinline__ ChunkSeq chunk_sequence(const ChunkParams &p, int b)
+{
+    ChunkSeq s;
+    s.s0 = max(0, min(p.chunk_start[b], p.T));
+    s.n = max(s.s0, min(p.chunk_start[b + 1], p.T)) - s.s0;
+    s.L = max(0, min(p.prefix_len[b], p.L_stride));
+    s.keys = min(s.L + s.n, p.L_stride);
+    return s;
+}
+
+// running sum over the lanes of a wavefront
+__device__ __forceinline__ int wave_running_sum(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // inside the rows of 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // rows 0, 2 into 1, 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // and into 2, 3
+    return v;
+}
+
+// A tile of 32 rows of DP (padded head dimension) values in LDS, pitches in words.
+//   K  read 16 bytes a lane, lanes 0..31 in 32 rows: a pitch of 4 x an odd number spreads 16 lanes over the 64 banks.
+//   V  bf16, transposing reads of 4 rows x 16 words: a pitch of 16 or 48 modulo 64 keeps the rows apart.
+//      fp32, rows 4 apart read 32 words each: a pitch of 8 modulo 16 puts them 32 banks apart.
+template <int DP, bool F32>
+struct TileShape {
+    static constexpr int ES = F32 ? 4 : 2, ROW_WORDS = DP * ES / 4, GRANULES = ROW_WORDS / 4;
+    static constexpr int PK = ROW_WORDS + 4;
+    static constexpr int PV = F32 ? ROW_WORDS + 8 : ROW_WORDS + (ROW_WORDS % 64 == 16 || ROW_WORDS % 64 == 48 ? 0 : 16);
+    static constexpr int PER_THREAD = (KT * GRANULES + 255) / 256;       // 16-byte pieces of a tile per thread of 256
+    static constexpr int KK = DP / (F32 ? 8 : 16);                       // 16-byte operand pieces a lane holds of a row
+};
+
+// scores of 32 keys x 32 rows: s = K Q^T, K from LDS rows at `k` (this lane's row and half), q this lane's row in registers.
+// Score i of a lane is key 8 (i / 4) + 4 h + i % 4 of row lane % 32, h = lane / 32.  (bf16: the pieces of a lane are the operands of
+// v_mfma_f32_32x32x16_bf16; fp32: v_mfma_f32_32x32x2_f32 takes the contraction four values of a piece after the other)
+template <int DP, bool F32>
+__device__ __forceinline__ f32x16 tile_scores(const uint32_t *k, const u32x4 *q)
+{
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < TileShape<DP, F32>::KK; ++kk) {
+        const u32x4 a = *reinterpret_cast<const u32x4 *>(k + 8 * kk);
+        if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(q[kk][j]), s, 0, 0, 0);
+        } else {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, q[kk]), s, 0, 0, 0);
+        }
+    }
+    return s;
+}
+
+// key of score i inside a tile, without the lane's 4 h
+__device__ __forceinline__ constexpr int key_of_score(int i) { return 8 * (i >> 2) + (i & 3); }
+
+}  // namespace mcsd

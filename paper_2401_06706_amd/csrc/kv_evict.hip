@@ -1,0 +1,229 @@
+// A paged cache cut to a budget: what every (layer, sequence, KV head) keeps, by the sums of its attention weights, and
+// the move of what is kept.
+#include "chunk_common.h"
+
+namespace mcsd {
+namespace {
+
+struct EvictParams {
+    int B, H_kv, L_stride, n_layers, n_first, n_recent, page_size, n_pages, max_pages, row_bytes, in_place;
+    size_t pool_layer;              // bytes of one layer's pool
+    char *k_pool, *v_pool;
+    float *sums;
+    int32_t *prefix_len, *kept;
+    const int32_t *keep_len, *block_table, *out_table;
+    uint32_t *flags;
+};
+
+constexpr int SEL_NT = 1024, SEL_PER = 16, SEL_CHUNK = SEL_NT * SEL_PER, SEL_WAVES = SEL_NT / 64;
+
+// order of sums as whole numbers: no number first, then -infinity .. infinity, both zeros alike
+__device__ __forceinline__ uint32_t order_key(float x)
+{
+    if (x != x) return 0u;
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+// A workgroup per (layer, sequence, KV head).  The sum that decides is found digit by digit (four of 8 bits, counts of all digits
+// in LDS), then what is kept is written down in ascending order: positions are dealt out in rows of 1024, so that the counts per row and
+// wavefront, summed up, give every position its place.  Up to 16384 positions stay in registers; longer ones are
+// read again by every pass.
+__global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
+{
+    __shared__ uint32_t s_count[256], s_scan[SEL_PER * SEL_WAVES], s_wave[4], s_pick[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int head = blockIdx.x, b = head / p.H_kv % p.B;
+    const int n = max(0, min(p.prefix_len[b], p.L_stride)), m = min(n, max(0, p.keep_len[b]));
+    const int f = min(p.n_first, m), r = min(p.n_recent, m - f);
+    float *sums = p.sums + (size_t)head * p.L_stride;
+    int32_t *kept = p.kept + (size_t)head * p.L_stride;
+    if (head < p.B * p.H_kv && head % p.H_kv == 0 && tid == 0) p.flags[b] = 0;      // (the move's workgroups add to it)
+    if (m == n) {
+        for (int j = tid; j < n; j += SEL_NT) kept[j] = j;
+        return;
+    }
+    const int chunks = (n + SEL_CHUNK - 1) / SEL_CHUNK, to = n - r;                 // between f and `to` the sums decide
+    float val[SEL_PER];
+    auto load = [&](int chunk) {
+#pragma unroll
+        for (int i = 0; i < SEL_PER; ++i) {
+            const int at = chunk * SEL_CHUNK + i * SEL_NT + tid;
+            val[i] = at < n ? sums[at] : 0.f;
+        }
+    };
+    load(0);
+    uint32_t prefix = 0, left = m - f - r;      // digits so far; how many of those that begin with them are kept
+    if (left > 0) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            if (tid < 256) s_count[tid] = 0;
+            __syncthreads();
+            for (int c = 0; c < chunks; ++c) {
+                if (chunks > 1) load(c);
+#pragma unroll
+                for (int i = 0; i < SEL_PER; ++i) {
+                    const int at = c * SEL_CHUNK + i * SEL_NT + tid;
+                    const uint32_t key = order_key(val[i]);
+                    const bool on = at >= f && at < to && (shift == 24 || (key >> (shift + 8)) == prefix);
+                    const uint32_t digit = (key >> shift) & 255u;
+                    const unsigned long long all = __ballot(on);
+                    if (!all) continue;
+                    // one addition for the lanes that agree with the first of them (sums of 0 are many)
+                    const uint32_t d0 = __builtin_amdgcn_readlane(digit, __ffsll((long long)all) - 1);
+                    const unsigned long long same = __ballot(on && digit == d0);
+                    if (lane == 0) atomicAdd(&s_count[d0], (uint32_t)__popcll(same));
+                    if (on && digit != d0) atomicAdd(&s_count[digit], 1u);
+                }
+            }
+            __syncthreads();
+            // the digit at which the counts from the top reach `left`
+            uint32_t mine = 0, upto = 0;
+            if (tid < 256) {
+                mine = s_count[255 - tid];
+                upto = wave_running_sum(mine);
+                if (lane == 63) s_wave[wave] = upto;
+            }
+            __syncthreads();
+            if (tid < 256) {
+                for (int w = 0; w < wave; ++w) upto += s_wave[w];
+                if (upto >= left && upto - mine < left) { s_pick[0] = 255 - tid; s_pick[1] = left - (upto - mine); }
+            }
+            __syncthreads();
+            prefix = (prefix << 8) | s_pick[0];
+            left = s_pick[1];
+            __syncthreads();
+        }
+    }
+    const bool some = m - f - r > 0;            // keys above `prefix` are kept, and the first `left` of those that are equal
+    int equal_before = 0, kept_before = 0;
+    // running sum of the 256 counts of (row, wavefront), in place; returns their total
+    auto scan_counts = [&]() -> int {
+        uint32_t mine = 0, upto = 0;
+        __syncthreads();
+        if (tid < SEL_PER * SEL_WAVES) {
+            mine = s_scan[tid];
+            upto = wave_running_sum(mine);
+            if (lane == 63) s_wave[wave] = upto;
+        }
+        __syncthreads();
+        if (tid < SEL_PER * SEL_WAVES) {
+            for (int w = 0; w < wave; ++w) upto += s_wave[w];
+            s_scan[tid] = upto - mine;
+        }
+        const int total = s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
+        __syncthreads();
+        return total;
+    };
+    static_assert(SEL_PER * SEL_WAVES == 256, "four wavefronts sum the counts up");
+    const unsigned long long below = (1ull << lane) - 1;
+    for (int c = 0; c < chunks; ++c) {
+        if (chunks > 1) load(c);
+        uint32_t take = 0, equal = 0;
+#pragma unroll
+        for (int i = 0; i < SEL_PER; ++i) {
+            const int at = c * SEL_CHUNK + i * SEL_NT + tid;
+            const uint32_t key = order_key(val[i]);
+            const bool between = at >= f && at < to;
+            if (at < n && (!between || (some && key > prefix))) take |= 1u << i;
+            const bool eq = between && some && key == prefix;
+            if (eq) equal |= 1u << i;
+            const int cnt = __popcll(__ballot(eq));
+            if (lane == 0) s_scan[i * SEL_WAVES + wave] = cnt;
+        }
+        const int equals = scan_counts();
+#pragma unroll
+        for (int i = 0; i < SEL_PER; ++i) {
+            const unsigned long long eq = __ballot((equal >> i) & 1u);
+            const uint32_t rank = equal_before + s_scan[i * SEL_WAVES + wave] + __popcll(eq & below);
+            if (((equal >> i) & 1u) && rank < left) take |= 1u << i;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < SEL_PER; ++i) {
+            const int cnt = __popcll(__ballot((take >> i) & 1u));
+            if (lane == 0) s_scan[i * SEL_WAVES + wave] = cnt;
+        }
+        const int takes = scan_counts();
+        // (all sums of this chunk have been read; those kept go no farther back than they stood)
+#pragma unroll
+        for (int i = 0; i < SEL_PER; ++i) {
+            const unsigned long long on = __ballot((take >> i) & 1u);
+            if ((take >> i) & 1u) {
+                const int place = kept_before + s_scan[i * SEL_WAVES + wave] + __popcll(on & below);
+                kept[place] = c * SEL_CHUNK + i * SEL_NT + tid;
+                sums[place] = val[i];
+            }
+        }
+        equal_before += equals;
+        kept_before += takes;
+        __syncthreads();
+    }
+}
+
+// Rows of K or V to their new places: a workgroup takes 128 bytes of the rows of a (layer, sequence, KV head), 256 rows at a time.
+// In place it takes all of them in ascending order, everything of a step read before any of it is written: a row moves to a lower
+// position or stays, so that a step writes only what itself and the steps before it have read.  grid (heads, 2 x slices of 128 bytes, steps or 1)
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p)
+{
+    constexpr int U = 8, ROWS = 32 * U;
+    const int tid = threadIdx.x, head = blockIdx.x, g = head % p.H_kv, b = head / p.H_kv % p.B, layer = head / p.H_kv / p.B;
+    const int m = min(max(0, min(p.prefix_len[b], p.L_stride)), max(0, p.keep_len[b]));
+    const bool value = blockIdx.y & 1;
+    const int col = (blockIdx.y >> 1) * 128 + 16 * (tid & 7);
+    char *pool = (value ? p.v_pool : p.k_pool) + (size_t)layer * p.pool_layer;
+    const int32_t *kept = p.kept + (size_t)head * p.L_stride;
+    const int32_t *from = p.block_table + (size_t)b * p.max_pages;
+    const int32_t *to = p.in_place ? from : p.out_table + (size_t)b * p.max_pages;
+    bool bad = false;
+    for (int base = blockIdx.z * ROWS; base < m; base += gridDim.z * ROWS) {
+        u32x4 x[U];
+        size_t dst[U];
+        uint32_t on = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = base + 32 * u + (tid >> 3);
+            if (j >= m || col >= p.row_bytes) continue;
+            const int i = kept[j];
+            if (p.in_place && i == j) continue;
+            const int src_page = from[i / p.page_size], dst_page = to[j / p.page_size];
+            if ((unsigned)src_page >= (unsigned)p.n_pages || (unsigned)dst_page >= (unsigned)p.n_pages) { bad = true; continue; }
+            x[u] = *reinterpret_cast<const u32x4 *>(pool + (((size_t)src_page * p.H_kv + g) * p.page_size + i % p.page_size) * p.row_bytes + col);
+            dst[u] = (((size_t)dst_page * p.H_kv + g) * p.page_size + j % p.page_size) * p.row_bytes + col;
+            on |= 1u << u;
+        }
+        if (p.in_place) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (the rows have arrived before others write)
+            __syncthreads();
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if ((on >> u) & 1u) *reinterpret_cast<u32x4 *>(pool + dst[u]) = x[u];
+    }
+    if (bad) atomicOr(&p.flags[b], (uint32_t)MCSD_FLAG_BAD_PAGES);
+    // (every workgroup reads the smaller of this and keep_len, which is m before and after)
+    if (head < p.B * p.H_kv && g == 0 && blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) p.prefix_len[b] = m;
+}
+
+}  // namespace
+
+int32_t launch_kv_evict(const mcsd_evict_desc &d, const mcsd_evict_bufs &b, const mcsd_paged_kv &kv, hipStream_t stream)
+{
+    EvictParams p;
+    p.B = d.B; p.H_kv = d.H_kv; p.L_stride = d.L_stride; p.n_layers = d.n_layers; p.n_first = d.n_first; p.n_recent = d.n_recent;
+    p.page_size = kv.page_size; p.n_pages = kv.n_pages; p.max_pages = kv.max_pages_per_seq;
+    p.row_bytes = d.d * (d.dtype == MCSD_DTYPE_FP32 ? 4 : 2);
+    p.in_place = b.out_table == nullptr;
+    p.pool_layer = (size_t)kv.n_pages * kv.page_size * d.H_kv * p.row_bytes;
+    p.k_pool = static_cast<char *>(b.k_pool); p.v_pool = static_cast<char *>(b.v_pool);
+    p.sums = b.sums; p.prefix_len = b.prefix_len; p.kept = b.kept; p.keep_len = b.keep_len;
+    p.block_table = kv.block_table; p.out_table = b.out_table; p.flags = b.flags;
+    const unsigned heads = (unsigned)(d.n_layers * d.B * d.H_kv);
+    const unsigned steps = p.in_place ? 1u : (unsigned)((d.L_stride + 255) / 256);
+    launch_kernel(K_EVICT_SELECT, evict_select_kernel, dim3(heads), dim3(SEL_NT), stream, p);
+    launch_kernel(K_EVICT_MOVE, evict_move_kernel, dim3(heads, 2 * ((p.row_bytes + 127) / 128), steps), dim3(256), stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_error("evict launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
+    return MCSD_OK;
+}
+
+}  // namespace mcsd

@@ -11,7 +11,8 @@ namespace mcsd {
 
 // Kernel ids for the optional per-kernel event timing.
 enum KernelId { K_ATTN_MFMA = 0, K_ATTN_GENERIC = 1, K_ATTN_COMBINE = 2, K_VERIFY_ROWS = 3, K_WALK = 4, K_DRAFT_ROWS = 5, K_TREE_BUILD = 6, K_KV_COPY = 7, K_KV_FINISH = 8, K_KV_STORE = 9, K_KV_LOAD = 10,
-                K_ATTN_FOURBIT = 11, K_ATTN_FOURBIT_COMBINE = 12, K_PAGE_ASSIGN = 13, K_PAGE_SLOTS = 14, K_LOGITS_RULES = 15, K_COUNT = 16 };
+                K_ATTN_FOURBIT = 11, K_ATTN_FOURBIT_COMBINE = 12, K_PAGE_ASSIGN = 13, K_PAGE_SLOTS = 14, K_LOGITS_RULES = 15,
+                K_KV_STORE_PAGED = 16, K_CHUNK_ATTN = 17, K_CHUNK_MERGE = 18, K_WEIGHT_SUMS = 19, K_EVICT_SELECT = 20, K_EVICT_MOVE = 21, K_TOKEN_LOGPROBS = 22, K_LOGPROB_MERGE = 23, K_COUNT = 24 };
 
 void set_error(const char *fmt, ...);
 
@@ -140,6 +141,26 @@ struct FourbitPlan {
 bool make_fourbit_plan(const mcsd_attn_desc &d, FourbitPlan *plan);
 int32_t launch_attn_fourbit(const mcsd_attn_desc &d, const mcsd_attn_bufs &b, const mcsd_fourbit_kv &kv, const FourbitPlan &plan, hipStream_t stream);
 int32_t launch_fourbit_rows(const mcsd_rows_desc &d, const mcsd_rows_bufs &b, const mcsd_fourbit_kv &kv, bool store, hipStream_t stream);
+
+// ---- prompts in chunks over a paged cache -----------------------------------
+struct ChunkPlan {
+    int row_tile;         // query rows per workgroup
+    int max_row_tiles;    // row tiles of one KV head at most
+    int target;           // workgroups aimed at where keys are split
+    int min_seg;          // key tiles of a segment at least
+    int max_items;        // workgroups per KV head at most
+    int max_parts;        // of them, those that write a partial (0: nothing is split)
+    size_t ws_bytes;
+};
+bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan);
+int32_t launch_chunk_attn(const mcsd_chunk_desc &d, const mcsd_chunk_bufs &b, const mcsd_paged_kv &kv, const ChunkPlan &plan, hipStream_t stream);
+int32_t launch_weight_sums(const mcsd_chunk_desc &d, const mcsd_sums_bufs &b, const mcsd_paged_kv &kv, hipStream_t stream);
+int32_t launch_kv_store_paged(const mcsd_rows_desc &d, const mcsd_store_bufs &b, const mcsd_paged_kv &kv, hipStream_t stream);
+int32_t launch_kv_evict(const mcsd_evict_desc &d, const mcsd_evict_bufs &b, const mcsd_paged_kv &kv, hipStream_t stream);
+
+// ---- log probabilities of tokens ---------------------------------------------
+size_t logprob_workspace(const mcsd_logprob_desc &d);
+int32_t launch_token_logprobs(const mcsd_logprob_desc &d, const mcsd_logprob_bufs &b, hipStream_t stream);
 
 // ---- pages from lengths, rules on logits ------------------------------------
 int32_t launch_page_assign(const mcsd_page_desc &d, const mcsd_page_bufs &b, hipStream_t stream);

@@ -1,0 +1,278 @@
+// Log probability, rank and entropy for given tokens, with the most probable alternatives.
+#include <float.h>
+
+#include "attn_common.h"
+
+namespace mcsd {
+namespace {
+
+struct LogprobParams {
+    int rows, R, V, n_top;
+    size_t row_stride;              // elements
+    const void *logits;
+    const int32_t *row_map, *tokens;
+    const float *temperature;
+    float *logprob, *entropy, *top_logprob;
+    int32_t *rank, *top_tok;
+    uint32_t *flags;
+};
+
+constexpr int NT = 512, CAP = 1024;         // candidates for the top that fit; those equal to the smallest of them
+constexpr float LOWEST = -200.0f;           // 2^-200 is 0: a bound that keeps 0 * infinity out of the entropy
+
+template <bool BF16>
+__device__ __forceinline__ float logit_at(const void *row, int i)
+{
+    return BF16 ? bf16_bits_to_float(static_cast<const uint16_t *>(row)[i]) : static_cast<const float *>(row)[i];
+}
+
+// Where 16-byte pieces begin and end in a row that starts anywhere: elements [0, head), pieces, elements [tail, V).
+template <bool BF16>
+struct Pieces {
+    static constexpr int W = BF16 ? 8 : 4;
+    int head, n, tail;
+    __device__ __forceinline__ Pieces(const void *row, int V)
+    {
+        const int es = BF16 ? 2 : 4, off = (int)((16 - ((uintptr_t)row & 15u)) & 15u) / es;
+        head = min(off, V);
+        n = (V - head) / W;
+        tail = head + n * W;
+    }
+    __device__ __forceinline__ void load(const void *row, int piece, float *z) const
+    {
+        const char *at = static_cast<const char *>(row) + (size_t)(head + piece * W) * (BF16 ? 2 : 4);
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(at);
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            z[i] = BF16 ? ((i & 1) ? __uint_as_float(x[i >> 1] & 0xffff0000u) : __uint_as_float(x[i >> 1] << 16)) : __uint_as_float(x[i & 3]);
+    }
+};
+
+// Sums of a row relative to the largest logit seen: s = sum 2^t, u = sum t 2^t with t = (z - m) c, c = log2(e) / T.
+struct Sums {
+    float m = -FLT_MAX, s = 0.f, u = 0.f;
+    __device__ __forceinline__ void raise(float to, float c)
+    {
+        const float t = fmaxf((m - to) * c, LOWEST), f = fast_exp2(t);
+        u = f * (u + t * s);
+        s *= f;
+        m = to;
+    }
+    __device__ __forceinline__ void add(float z, float c)
+    {
+        const float t = (z - m) * c, e = fast_exp2(t);
+        s += e;
+        u = fmaf(e, fmaxf(t, LOWEST), u);
+    }
+};
+
+// A workgroup per row, which is read once: every thread keeps running sums, its largest logit and how many tokens come before the given
+// one.  For the top, the n-th largest of 64 maxima (of every eighth thread) bounds it from below: only the few threads whose
+// largest logit reaches that bound have their pieces read again, by all threads together.
+template <bool BF16>
+__global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
+{
+    constexpr int W = Pieces<BF16>::W, WAVES = NT / 64;
+    __shared__ float s_max[NT];
+    __shared__ double s_sum[2][WAVES];
+    __shared__ int s_rank[WAVES], s_hot[NT], s_n_hot, s_n_above, s_n_equal;
+    __shared__ float s_val[CAP];
+    __shared__ int s_id[CAP], s_eq[CAP];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i_row = blockIdx.x;
+    const int map = p.row_map ? p.row_map[i_row] : i_row;
+    auto refuse = [&](uint32_t flag) {
+        if (tid == 0) {
+            p.logprob[i_row] = NAN;
+            if (p.entropy) p.entropy[i_row] = NAN;
+            if (p.rank) p.rank[i_row] = -1;
+            p.flags[i_row] = flag;
+        }
+        if (tid < p.n_top) {
+            p.top_tok[(size_t)i_row * p.n_top + tid] = -1;
+            p.top_logprob[(size_t)i_row * p.n_top + tid] = NAN;
+        }
+    };
+    if ((unsigned)map >= (unsigned)p.R) return refuse(MCSD_FLAG_BAD_TREE);
+    const void *row = static_cast<const char *>(p.logits) + (size_t)map * p.row_stride * (BF16 ? 2 : 4);
+    const Pieces<BF16> pc(row, p.V);
+    const int x = p.tokens[i_row];
+    const bool known = (unsigned)x < (unsigned)p.V;
+    const float zx = known ? logit_at<BF16>(row, x) : INFINITY;
+    const float T = p.temperature ? p.temperature[i_row] : 1.f, c = LOG2E_F / (T > 0.f ? T : 1.f);
+    if (tid == 0) s_n_hot = s_n_above = s_n_equal = 0;
+
+    Sums sums;
+    float top = -INFINITY;
+    int before = 0;
+    auto take = [&](float z, int id) {
+        if (z > sums.m) sums.raise(z, c);
+        top = fmaxf(top, z);
+        sums.add(z, c);
+        before += (z > zx || (z == zx && id < x)) ? 1 : 0;
+    };
+    for (int piece = tid; piece < pc.n; piece += NT) {
+        float z[W];
+        pc.load(row, piece, z);
+        float most = z[0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) most = fmaxf(most, z[i]);
+        if (most > sums.m) sums.raise(most, c);
+        top = fmaxf(top, most);
+        const int d = x - (pc.head + piece * W);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            sums.add(z[i], c);
+            before += (z[i] > zx || (z[i] == zx && i < d)) ? 1 : 0;
+        }
+    }
+    // (elements outside the pieces: fewer than 16)
+    if (tid < pc.head) take(logit_at<BF16>(row, tid), tid);
+    if (pc.tail + tid < p.V) take(logit_at<BF16>(row, pc.tail + tid), pc.tail + tid);
+
+    // ---- the row's sums
+    s_max[tid] = top;
+    __syncthreads();
+    float group = s_max[lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) group = fmaxf(group, s_max[64 * w + lane]);
+    float m = group;
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    sums.raise(fmaxf(m, -FLT_MAX), c);
+    double s = sums.s, u = sums.u;
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) {
+        s += __shfl_xor(s, k);
+        u += __shfl_xor(u, k);
+        before += __shfl_xor(before, k);
+    }
+    if (lane == 0) { s_sum[0][wave] = s; s_sum[1][wave] = u; s_rank[wave] = before; }
+    // ---- the bound of the top: n_top-th largest of the 64 maxima
+    float bound = INFINITY;
+    if (p.n_top) {
+        int ahead = 0;
+        for (int k = 0; k < 64; ++k) {
+            const float other = __shfl(group, k);
+            ahead += (other > group || (other == group && k < lane)) ? 1 : 0;
+        }
+        const unsigned long long at = __ballot(ahead == p.n_top - 1);
+        bound = __shfl(group, at ? __ffsll((long long)at) - 1 : 0);
+        if (top >= bound) s_hot[atomicAdd(&s_n_hot, 1)] = tid;
+    }
+    __syncthreads();
+    s = u = 0.0;
+    before = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) { s += s_sum[0][w]; u += s_sum[1][w]; before += s_rank[w]; }
+    // a NaN anywhere is in s; an infinity is the maximum
+    if (!(s > 0.0 && s < (double)INFINITY) || !(m < INFINITY) || !(m > -INFINITY)) return refuse(MCSD_FLAG_NONFINITE);
+    const double lse = log(s), to_ln = 1.0 / 1.44269504088896340736;
+    const double inv_T = (double)c * to_ln;
+    auto logprob_of = [&](float z) { return z == -INFINITY ? -INFINITY : (float)(((double)z - (double)m) * inv_T - lse); };
+    if (tid == 0) {
+        p.logprob[i_row] = known ? logprob_of(zx) : NAN;
+        if (p.entropy) p.entropy[i_row] = (float)fmax(lse - u / s * to_ln, 0.0);
+        if (p.rank) p.rank[i_row] = known ? before : -1;
+        p.flags[i_row] = known ? 0u : (uint32_t)MCSD_FLAG_BAD_TOKEN;
+    }
+    if (!p.n_top) return;
+
+    // ---- candidates: all that reach the bound
+    auto candidate = [&](float z, int id) {
+        if (z > bound) {
+            const int at = atomicAdd(&s_n_above, 1);
+            if (at < CAP) { s_val[at] = z; s_id[at] = id; }
+        } else if (z == bound) {
+            const int at = atomicAdd(&s_n_equal, 1);
+            if (at < CAP) s_eq[at] = id;
+        }
+    };
+    const int per = (pc.n + NT - 1) / NT, n_hot = s_n_hot;
+    for (int k = tid; k < n_hot * per; k += NT) {
+        const int piece = s_hot[k / per] + k % per * NT;
+        if (piece >= pc.n) continue;
+        float z[W];
+        pc.load(row, piece, z);
+#pragma unroll
+        for (int i = 0; i < W; ++i) candidate(z[i], pc.head + piece * W + i);
+    }
+    if (tid < pc.head) candidate(logit_at<BF16>(row, tid), tid);
+    if (pc.tail + tid < p.V) candidate(logit_at<BF16>(row, pc.tail + tid), pc.tail + tid);
+    __syncthreads();
+    int32_t *tok = p.top_tok + (size_t)i_row * p.n_top;
+    float *lp = p.top_logprob + (size_t)i_row * p.n_top;
+    const int above = s_n_above, equal = s_n_equal;
+    if (above <= CAP) {
+        for (int k = tid; k < above; k += NT) {
+            const float z = s_val[k];
+            const int id = s_id[k];
+            int place = 0;
+            for (int j = 0; j < above; ++j) place += (s_val[j] > z || (s_val[j] == z && s_id[j] < id)) ? 1 : 0;
+            if (place < p.n_top) { tok[place] = id; lp[place] = logprob_of(z); }
+        }
+        const int missing = p.n_top - above;            // of those equal to the bound, the lowest ids
+        if (missing > 0 && equal <= CAP) {
+            for (int k = tid; k < equal; k += NT) {
+                const int id = s_eq[k];
+                int place = 0;
+                for (int j = 0; j < equal; ++j) place += s_eq[j] < id ? 1 : 0;
+                if (place < missing) { tok[above + place] = id; lp[above + place] = logprob_of(bound); }
+            }
+        } else if (missing > 0 && wave == 0) {          // very many: looked for in the row, in order
+            int found = 0;
+            for (int base = 0; base < p.V && found < missing; base += 64) {
+                const bool is = base + lane < p.V && logit_at<BF16>(row, base + lane) == bound;
+                const unsigned long long who = __ballot(is);
+                const int place = found + __popcll(who & ((1ull << lane) - 1));
+                if (is && place < missing) { tok[above + place] = base + lane; lp[above + place] = logprob_of(bound); }
+                found += __popcll(who);
+            }
+        }
+        return;
+    }
+    // More than CAP above the bound (one thread's pieces hold them all): the top one by one, each the first behind the one before it.
+    float last = INFINITY;
+    int last_id = -1;
+    for (int k = 0; k < p.n_top; ++k) {
+        float best = -INFINITY;
+        int best_id = 0x7fffffff;
+        for (int i = tid; i < p.V; i += NT) {
+            const float z = logit_at<BF16>(row, i);
+            const bool behind = z < last || (z == last && i > last_id);
+            if (behind && (z > best || (z == best && i < best_id))) { best = z; best_id = i; }
+        }
+#pragma unroll
+        for (int q = 32; q > 0; q >>= 1) {
+            const float z = __shfl_xor(best, q);
+            const int id = __shfl_xor(best_id, q);
+            if (z > best || (z == best && id < best_id)) { best = z; best_id = id; }
+        }
+        __syncthreads();
+        if (lane == 0) { s_val[wave] = best; s_id[wave] = best_id; }
+        __syncthreads();
+        for (int w = 0; w < WAVES; ++w)
+            if (s_val[w] > best || (s_val[w] == best && s_id[w] < best_id)) { best = s_val[w]; best_id = s_id[w]; }
+        last = best;
+        last_id = best_id;
+        if (tid == 0) { tok[k] = best_id; lp[k] = logprob_of(best); }
+    }
+}
+
+}  // namespace
+
+size_t logprob_workspace(const mcsd_logprob_desc &) { return 0; }
+
+int32_t launch_token_logprobs(const mcsd_logprob_desc &d, const mcsd_logprob_bufs &b, hipStream_t stream)
+{
+    LogprobParams p;
+    p.rows = d.rows; p.R = d.R; p.V = d.V; p.n_top = d.n_top; p.row_stride = (size_t)d.row_stride;
+    p.logits = b.logits; p.row_map = b.row_map; p.tokens = b.tokens; p.temperature = b.temperature;
+    p.logprob = b.logprob; p.entropy = b.entropy; p.rank = b.rank; p.top_tok = b.top_tok; p.top_logprob = b.top_logprob; p.flags = b.flags;
+    if (d.dtype == MCSD_DTYPE_BF16) launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<true>, dim3(d.rows), dim3(NT), stream, p);
+    else launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<false>, dim3(d.rows), dim3(NT), stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_error("token log probabilities launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
+    return MCSD_OK;
+}
+
+}  // namespace mcsd

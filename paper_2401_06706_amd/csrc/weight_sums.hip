@@ -1,0 +1,160 @@
+// What every cached position was given by the softmax of new rows, added up (the measure by which a cache is cut).
+#include "chunk_common.h"
+
+namespace mcsd {
+namespace {
+
+struct SumsParams { ChunkParams c; const float *lse; float *sums; int last_rows; };
+
+// A workgroup owns 128 positions of a (sequence, KV head), 32 a wavefront with their keys in registers, and goes through the rows
+// that see them in tiles of 32 (through LDS): S = K Q^T as in attention, weights 2^(s c2 - lse), added up in the
+// lane that holds them.  No other workgroup adds to these positions, so the order of the sum is fixed.  A partial sum of 64 tiles is
+// added to the whole at a time: over n rows of a lane the error stays below (64 + n / 64) 2^-24 of the sum.
+template <int DP, bool F32>
+__global__ __launch_bounds__(256) void weight_sums_kernel(SumsParams sp)
+{
+    using S = TileShape<DP, F32>;
+    const ChunkParams &p = sp.c;
+    __shared__ __attribute__((aligned(16))) uint32_t s_q[2][KT * S::PK];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
+    const int g = blockIdx.x, b = blockIdx.z, key0 = blockIdx.y * 128;
+    const ChunkSeq sq = chunk_sequence(p, b);
+    if (sq.n == 0 || key0 >= sq.keys) return;
+    const int M = sq.n * p.G, wkey = key0 + 32 * wave, row_bytes = p.d * S::ES;
+    const int first_token = max(sp.last_rows ? sq.n - min(sp.last_rows, sq.n) : 0, key0 - sq.L);
+    const int tiles = (M - first_token * p.G + KT - 1) / KT, row_first = first_token * p.G;
+
+    // ---- this wavefront's keys
+    u32x4 k[S::KK];
+    {
+        const int page = wkey < sq.keys ? p.block_table[(size_t)b * p.max_pages + wkey / p.page_size] : -1;
+        const bool in = (unsigned)page < (unsigned)p.n_pages;
+        const size_t off = in ? (((size_t)page * p.H_kv + g) * p.page_size + wkey % p.page_size) * row_bytes : 0;
+        const __amdgpu_buffer_rsrc_t rk = make_rsrc(static_cast<const char *>(p.k_pool) + off, in ? (uint32_t)min(KT, sq.keys - wkey) * row_bytes : 0u);
+#pragma unroll
+        for (int kk = 0; kk < S::KK; ++kk) {
+            const int at = 32 * kk + 16 * h;
+            k[kk] = __builtin_amdgcn_raw_buffer_load_b128(rk, at < row_bytes ? l32 * row_bytes + at : 0x7fff0000, 0, 0);
+        }
+    }
+    // ---- tiles of rows: global -> registers -> LDS, one tile ahead
+    u32x4 qr[S::PER_THREAD];
+    float lse_next;
+    auto load_q = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < S::PER_THREAD; ++j) {
+            const int e = tid + 256 * j, r = row_first + tile * KT + e / S::GRANULES, c = e % S::GRANULES;
+            const u32x4 zero = {0, 0, 0, 0};
+            qr[j] = zero;
+            if (e < KT * S::GRANULES && r < M && 16 * c < row_bytes)
+                qr[j] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(p.q) + (size_t)(sq.s0 + r / p.G) * p.q_row +
+                                                         (size_t)(g * p.G + r % p.G) * row_bytes + 16 * c);
+        }
+        const int r = row_first + tile * KT + l32;
+        // (a row past the last one gives nothing)
+        lse_next = r < M ? sp.lse[(size_t)(sq.s0 + r / p.G) * p.H_q + g * p.G + r % p.G] * LOG2E_F : INFINITY;
+    };
+    auto store_q = [&](uint32_t *buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < S::PER_THREAD; ++j) {
+            const int e = tid + 256 * j;
+            if (KT * S::GRANULES % 256 == 0 || e < KT * S::GRANULES)
+                *reinterpret_cast<u32x4 *>(buf + e / S::GRANULES * S::PK + 4 * (e % S::GRANULES)) = qr[j];
+        }
+    };
+    float part[16], total[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) part[i] = total[i] = 0.f;
+    load_q(0);
+    store_q(s_q[0]);
+    float lse = lse_next;
+    __syncthreads();
+    for (int tile = 0; tile < tiles; ++tile) {
+        if (tile + 1 < tiles) load_q(tile + 1);
+        if (wkey < sq.keys) {
+            const uint32_t *qb = s_q[tile & 1] + l32 * S::PK + 4 * h;
+            f32x16 s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < S::KK; ++kk) {
+                const u32x4 a = *reinterpret_cast<const u32x4 *>(qb + 8 * kk);
+                if constexpr (F32) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[kk][j]), __uint_as_float(a[j]), s, 0, 0, 0);
+                } else {
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[kk]), __builtin_bit_cast(bf16x8, a), s, 0, 0, 0);
+                }
+            }
+            const int token0 = (row_first + tile * KT) / p.G;
+            if (min(sq.L + token0, sq.keys - 1) < wkey + KT - 1) {      // some row does not see some of these keys
+                const int r = row_first + tile * KT + l32, seen = min(sq.L + min(r, M - 1) / p.G, sq.keys - 1) - wkey - 4 * h;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key_of_score(i) <= seen) part[i] += fast_exp2(fmaf(s[i], p.scale_log2, -lse));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[i] += fast_exp2(fmaf(s[i], p.scale_log2, -lse));
+            }
+            if ((tile & 63) == 63) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) { total[i] += part[i]; part[i] = 0.f; }
+            }
+        }
+        if (tile + 1 < tiles) store_q(s_q[(tile + 1) & 1]);
+        lse = lse_next;
+        __syncthreads();
+    }
+    if (wkey >= sq.keys) return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) total[i] += part[i];
+    // sum over the 32 rows of a tile: every exchange halves what a lane holds, so that lane l32 ends up with score
+    // 8 (l32 & 1) + 4 (l32 >> 1 & 1) + 2 (l32 >> 2 & 1) + (l32 >> 3 & 1) of its half
+#pragma unroll
+    for (int bit = 0; bit < 4; ++bit) {
+        const int n = 8 >> bit;
+        const bool up = (lane >> bit) & 1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) {
+                const float keep = up ? total[j + n] : total[j], give = up ? total[j] : total[j + n];
+                total[j] = keep + __shfl_xor(give, 1 << bit);
+            }
+    }
+    total[0] += __shfl_xor(total[0], 16);
+    const int i = 8 * (l32 & 1) + 4 * ((l32 >> 1) & 1) + 2 * ((l32 >> 2) & 1) + ((l32 >> 3) & 1);
+    const int key = wkey + key_of_score(i) + 4 * h;
+    if (l32 < 16 && key < sq.keys) {
+        float *at = sp.sums + ((size_t)b * p.H_kv + g) * p.L_stride + key;
+        *at = (key < sq.L ? *at : 0.f) + total[0];
+    }
+}
+
+template <bool F32>
+void launch_type(const SumsParams &sp, hipStream_t stream)
+{
+    const dim3 grid(sp.c.H_kv, (sp.c.L_stride + 127) / 128, sp.c.B), block(256);
+    const int d = sp.c.d;
+    if (d <= 32) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<32, F32>, grid, block, stream, sp);
+    else if (d <= 64) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<64, F32>, grid, block, stream, sp);
+    else if (d <= 96) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<96, F32>, grid, block, stream, sp);
+    else if (d <= 128) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<128, F32>, grid, block, stream, sp);
+    else launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<256, F32>, grid, block, stream, sp);
+}
+
+}  // namespace
+
+int32_t launch_weight_sums(const mcsd_chunk_desc &d, const mcsd_sums_bufs &b, const mcsd_paged_kv &kv, hipStream_t stream)
+{
+    SumsParams sp;
+    sp.c = chunk_params(d, kv);
+    sp.c.q = b.q; sp.c.k_pool = b.k_pool; sp.c.chunk_start = b.chunk_start; sp.c.prefix_len = b.prefix_len;
+    sp.lse = b.lse; sp.sums = b.sums; sp.last_rows = b.last_rows;
+    if (d.dtype == MCSD_DTYPE_FP32) launch_type<true>(sp, stream);
+    else launch_type<false>(sp, stream);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_error("weight sums launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
+    return MCSD_OK;
+}
+
+}  // namespace mcsd

@@ -1,0 +1,157 @@
+"""Chunk attention over a paged cache and the store of its rows, on the GPU against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from paper_2401_06706_amd import binding as M
+from tests import chunk_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def run(batch, scale, want_lse=True, stream=None):
+    q = batch["q"]
+    T, H_q, d = q.shape
+    out = torch.full((T + 3, H_q, d), 7.0, dtype=q.dtype, device=DEV)        # rows behind the last one stay as they were
+    lse = torch.full((T, H_q), 7.0, device=DEV)
+    need = M.mcsd_chunk_workspace_bytes(M.chunk_desc(q, batch["k_pool"], batch["table"], scale, batch["capacity"]))
+    ws = torch.full((max(need, 1),), 0xff, dtype=torch.uint8, device=DEV)
+    args = M.chunk_attn_args(q, batch["k_pool"], batch["v_pool"], batch["table"], batch["chunk_start"], batch["prefix_len"], out[:T], scale,
+                             batch["capacity"], lse if want_lse else None, ws if need else None)
+    M.mcsd_chunk_attn_paged(args, stream)
+    torch.cuda.synchronize()
+    assert (out[T:] == 7.0).all()
+    return out[:T], lse
+
+
+def check(batch, scale, dtype):
+    out, lse = run(batch, scale)
+    want, bound, want_lse, lse_bound = R.attention(batch, scale, dtype)
+    err = (out.double() - want).abs()
+    assert (err <= bound).all(), f"{float((err - bound).max())} over at {torch.nonzero(~(err <= bound))[:4].tolist()}, largest error {float(err.max())}"
+    err = (lse.double() - want_lse).abs()
+    assert (err <= lse_bound).all(), f"lse: {float(err.max())}"
+
+
+SHAPES = [  # lens, news, H_q, H_kv, d, page
+    ([0], [1], 1, 1, 128, 32),
+    ([0], [33], 4, 2, 128, 32),
+    ([517], [1], 12, 12, 64, 64),
+    ([31, 0, 64, 200], [1, 1, 1, 1], 8, 1, 128, 64),
+    ([0, 5, 0], [129, 0, 64], 4, 4, 128, 64),
+    ([100, 2000, 1], [1, 40, 300], 8, 2, 128, 96),
+    ([4000, 300], [1, 7], 16, 2, 128, 128),
+    ([1000], [260], 6, 2, 96, 32),
+    ([70, 1], [50, 31], 3, 3, 32, 32),
+    ([900, 63], [1, 65], 10, 5, 80, 64),
+    ([333], [70], 4, 2, 256, 64),
+    ([20, 0, 17], [9, 200, 1], 14, 2, 128, 32),
+    ([8], [100], 2, 1, 8, 32),
+    ([40], [40], 300, 1, 64, 32),
+    ([8000], [1], 8, 8, 128, 64),
+]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attention(shape, dtype):
+    lens, news, H_q, H_kv, d, page = shape
+    check(R.make_batch(gen(1), DEV, dtype, lens, news, H_q, H_kv, d, page), 1 / math.sqrt(d), dtype)
+
+
+@pytest.mark.parametrize("scale", [0.0, 0.02, 1.0])
+def test_scale(scale):
+    check(R.make_batch(gen(2), DEV, torch.bfloat16, [100, 0], [40, 70], 4, 2, 128, 64), scale, torch.bfloat16)
+
+
+@pytest.mark.parametrize("B", [65, 130, 300])
+def test_many_sequences(B):
+    lens = [(37 * b) % 300 for b in range(B)]
+    news = [0 if b % 5 == 3 else 1 + (b % 7 == 0) * 40 for b in range(B)]
+    check(R.make_batch(gen(3), DEV, torch.bfloat16, lens, news, 4, 2, 128, 32), 0.1, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_no_number_stays_with_those_who_see_it(d, dtype):
+    """NaN and infinities in later keys and values do not reach earlier rows; those who see them get them."""
+    batch = R.make_batch(gen(4), DEV, dtype, [40, 500], [100, 3], 4, 2, d, 32)
+    clean, clean_lse = run(batch, 0.1)
+    clean, clean_lse = clean.clone(), clean_lse.clone()
+    at = 40 + 50                                        # a position in the middle of the first chunk
+    page, row = int(batch["table"][0, at // 32]), at % 32
+    batch["v_pool"][page, 0, row, 3] = float("nan")
+    batch["v_pool"][page, 1, row, 5] = float("inf")
+    out, lse = run(batch, 0.1)
+    assert torch.equal(out[:50], clean[:50]) and torch.equal(lse, clean_lse) and torch.equal(out[100:], clean[100:])
+    assert torch.isnan(out[50:100, :2, 3]).all() and (out[50:100, 2:, 5] == float("inf")).all()
+    rest = torch.ones_like(out, dtype=torch.bool)
+    rest[50:100, :2, 3] = rest[50:100, 2:, 5] = False
+    assert torch.equal(out[rest], clean[rest])
+    batch["k_pool"][page, :, row] = float("nan")
+    out, lse = run(batch, 0.1)
+    assert torch.equal(out[:50], clean[:50]) and torch.equal(lse[:50], clean_lse[:50]) and torch.isnan(lse[50:100]).all()
+
+
+def test_bad_pages_read_as_zeros():
+    batch = R.make_batch(gen(5), DEV, torch.bfloat16, [100, 64], [30, 1], 4, 2, 128, 32)
+    batch["table"][0, 1] = -1
+    batch["table"][1, 0] = batch["k_pool"].shape[0]
+    batch["table"][1, 1] = 2 ** 31 - 1
+    check(batch, 0.1, torch.bfloat16)
+
+
+def test_lengths_beyond_the_capacity():
+    """Rows past the capacity see what lies below it; arrays out of range are taken within theirs."""
+    batch = R.make_batch(gen(6), DEV, torch.bfloat16, [60], [36], 2, 1, 128, 32)
+    full, _ = run(batch, 0.1)
+    batch["capacity"] = 64
+    out, _ = run(batch, 0.1)
+    batch["capacity"] = 96
+    assert torch.equal(out[:4], full[:4])
+    batch["prefix_len"][0] = 2 ** 30
+    batch["chunk_start"][1] = 2 ** 30
+    out, _ = run(batch, 0.1)
+    k, v = (R.rows_of(batch[x], batch["table"][0], 32, 96)[0] for x in ("k_pool", "v_pool"))
+    want = torch.softmax(batch["q"].double() @ k.t() * 0.1, -1) @ v
+    assert (out.double() - want).abs().max() < 2.0 ** -7 * 4
+    batch["chunk_start"][0], batch["chunk_start"][1] = 5, -3
+    before = out.clone()
+    run(batch, 0.1)
+    assert torch.equal(out, before)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("layers", [None, 3])
+def test_store(layers, dtype):
+    T, H_kv, d, page, n_pages = 45, 3, 40, 32, 4
+    lead = () if layers is None else (layers,)
+    pool = lambda: torch.full(lead + (n_pages, H_kv, page, d), 5.0, dtype=dtype, device=DEV)
+    k_pool, v_pool = pool(), pool()
+    wide = torch.randn(*lead, T, 2, H_kv, d, device=DEV).to(dtype)
+    k, v = wide[..., 0, :, :], wide[..., 1, :, :]
+    slots = torch.randperm(n_pages * page, generator=gen(1))[:T].int()
+    slots[3], slots[9], slots[11] = -1, n_pages * page, 2 ** 31 - 1
+    want_k, want_v = k_pool.clone(), v_pool.clone()
+    for t, s in enumerate(slots.tolist()):
+        if 0 <= s < n_pages * page:
+            want_k[..., s // page, :, s % page, :] = k[..., t, :, :]
+            want_v[..., s // page, :, s % page, :] = v[..., t, :, :]
+    M.mcsd_kv_store_paged(M.store_args(k, v, slots.to(DEV), k_pool, v_pool))
+    torch.cuda.synchronize()
+    assert torch.equal(k_pool, want_k) and torch.equal(v_pool, want_v)
+
+
+def test_no_tokens():
+    batch = R.make_batch(gen(7), DEV, torch.bfloat16, [10, 20], [0, 0], 4, 2, 128, 32)
+    run(batch, 0.1)
+    e = torch.empty(0, 2, 128, dtype=torch.bfloat16, device=DEV)
+    M.mcsd_kv_store_paged(M.store_args(e, e, torch.empty(0, dtype=torch.int32, device=DEV), batch["k_pool"], batch["v_pool"]))
