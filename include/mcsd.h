@@ -569,7 +569,7 @@ int32_t mcsd_attn_weight_sums(const mcsd_chunk_desc *desc, const mcsd_sums_bufs 
 typedef struct {
     uint32_t struct_size;
     int32_t B;              /* sequences, <= 65535 */
-    int32_t H_kv;           /* n_layers B H_kv < 2^24 */
+    int32_t H_kv;           /* n_layers B H_kv < 2^22 */
     int32_t d;              /* d * element size a multiple of 16 bytes, d <= MCSD_MAX_HEAD_DIM */
     int32_t dtype;          /* MCSD_DTYPE_* of the pools */
     int32_t L_stride;       /* row length of sums and kept, logical capacity, 1 .. min(2^22, max_pages_per_seq * page_size) */

@@ -35,7 +35,7 @@ const char *const g_names[K_COUNT] = {"tree_attn_mfma", "tree_attn_generic", "tr
                                       "verify_rows", "walk", "draft_rows", "tree_build", "kv_copy", "kv_finish",
                                       "kv_store_fourbit", "kv_load_fourbit", "attn_fourbit", "attn_fourbit_combine",
                                       "page_assign", "page_slots", "logits_rules",
-                                      "kv_store_paged", "chunk_attn", "chunk_merge", "weight_sums", "evict_select", "evict_move", "token_logprobs", "logprob_merge"};
+                                      "kv_store_paged", "chunk_attn", "chunk_merge", "weight_sums", "evict_select", "evict_move", "token_logprobs", "logprob_merge", "chunk_wide"};
 }  // namespace
 
 bool timing_new_events(hipEvent_t *start, hipEvent_t *stop)
@@ -582,7 +582,7 @@ int32_t mcsd_kv_evict_paged(const mcsd_evict_desc *d, const mcsd_evict_bufs *b, 
     if (d->B < 1 || d->H_kv < 1 || d->L_stride < 1 || d->n_layers < 1 || d->n_first < 0 || d->n_recent < 0) { set_error("evict: non-positive size"); return MCSD_E_SHAPE; }
     int32_t rc = check_head_dim("evict", d->d, d->dtype);
     if (rc != MCSD_OK) return rc;
-    if (d->B > 65535 || d->L_stride > (1 << 22) || (__int128)d->n_layers * d->B * d->H_kv >= 1 << 24) { set_error("evict: B, L_stride or n_layers * B * H_kv too large"); return MCSD_E_UNSUPPORTED; }
+    if (d->B > 65535 || d->L_stride > (1 << 22) || (__int128)d->n_layers * d->B * d->H_kv >= 1 << 22) { set_error("evict: B, L_stride or n_layers * B * H_kv too large"); return MCSD_E_UNSUPPORTED; }
     rc = check_pages("evict", kv, d->L_stride);
     if (rc != MCSD_OK) return rc;
     if (!b) { set_error("evict bufs is NULL"); return MCSD_E_NULL; }

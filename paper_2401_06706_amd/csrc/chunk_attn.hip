@@ -7,74 +7,7 @@
 namespace mcsd {
 namespace {
 
-constexpr int RT = 128;                 // query rows of a workgroup, 32 a wavefront
 constexpr int OFF_NOWHERE = 0x7fff0000; // an offset beyond every buffer's extent: reads as zero
-
-// The work of a launch, the same list in every workgroup and in the merge: rows r = token * G + head in group of a (sequence, KV head) in
-// tiles of RT, a tile's keys in equal segments.  A segment is so long that all of them make about p.target
-// workgroups per KV head, at least p.min_seg tiles; a sequence is cut into kt / segment of them, rounded, one for most.
-struct Item { int b, rt, seg, n_seg, part; ChunkSeq s; };
-
-__device__ __forceinline__ int segment_length(const ChunkParams &p, int lane)
-{
-    float work = 0.f;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        if (b0 + lane >= p.B) break;
-        const ChunkSeq s = chunk_sequence(p, b0 + lane);
-        work += (float)((s.n * p.G + RT - 1) / RT) * (float)((s.keys + KT - 1) / KT);
-    }
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) work += __shfl_xor(work, m);
-    return max(p.min_seg, (int)ceilf(work / p.target));
-}
-
-// item number idx (MERGE: tile of rows number idx of those whose keys are cut); false: there are fewer
-template <bool MERGE>
-__device__ __forceinline__ bool find_item(const ChunkParams &p, int idx, int lane, Item *it)
-{
-    const int len = p.max_parts ? segment_length(p, lane) : 0;
-    int items = 0, parts = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        ChunkSeq s = {0, 0, 0, 0};
-        if (b0 + lane < p.B) s = chunk_sequence(p, b0 + lane);
-        const int rt = (s.n * p.G + RT - 1) / RT, kt = (s.keys + KT - 1) / KT;
-        int n_seg = p.max_parts ? max(1, (kt + len / 2) / len) : 1;
-        const int my_parts = n_seg > 1 ? rt * n_seg : 0;
-        const int parts_to = parts + wave_running_sum(my_parts);
-        if (parts_to > p.max_parts) n_seg = 1;          // (cannot be, but by arrays that contradict themselves)
-        const int my_items = MERGE ? (n_seg > 1 ? rt : 0) : rt * n_seg;
-        const int items_to = items + wave_running_sum(my_items);
-        const unsigned long long found = __ballot(items_to > idx);
-        if (found) {
-            const int o = __ffsll((long long)found) - 1;
-            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, o); };
-            it->b = b0 + o;
-            it->s = {of(s.s0), of(s.n), of(s.L), of(s.keys)};
-            it->n_seg = of(n_seg);
-            const int local = idx - of(items_to - my_items);
-            it->rt = of(rt) - 1 - (MERGE ? local : local / it->n_seg);      // the last rows, with the most keys, first
-            it->seg = MERGE ? 0 : local % it->n_seg;
-            it->part = of(parts_to - my_parts) + it->rt * it->n_seg + it->seg;
-            return true;
-        }
-        items = __builtin_amdgcn_readlane(items_to, 63);
-        parts = __builtin_amdgcn_readlane(parts_to, 63);
-    }
-    return false;
-}
-
-__device__ __forceinline__ u32x4 finite_or_zero(u32x4 v, bool f32, bool *bad)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t e_lo = f32 ? 0u : 0x00007f80u, e_hi = 0x7f800000u;
-        const bool hi = (v[i] & e_hi) == e_hi, lo = !f32 && (v[i] & e_lo) == e_lo;
-        *bad |= hi | lo;
-        if (f32) v[i] = hi ? 0u : v[i];
-        else v[i] = (hi ? 0u : v[i] & 0xffff0000u) | (lo ? 0u : v[i] & 0xffffu);
-    }
-    return v;
-}
 
 template <int DP, bool F32>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * (F32 ? 4 : 2) <= 256 ? 2 : 1)))
@@ -88,14 +21,14 @@ void chunk_attn_kernel(ChunkParams p)
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, l32 = lane & 31, lj = lane >> 4, lc = lane & 15;
-    const int g = blockIdx.x;
+    const int g = blockIdx.x % p.H_kv;          // (KV head fastest: the row tiles of one meet in one XCD's L2 where their number is a multiple of 8)
     Item it;
-    if (!find_item<false>(p, blockIdx.y, lane, &it)) return;
-    const int M = it.s.n * p.G, row0 = it.rt * RT + 32 * wave;
+    if (!find_item<FEW_ROWS>(p, blockIdx.x / p.H_kv, lane, &it)) return;
+    const int M = it.s.n * p.G, row0 = it.rt * ROWS_FEW + 32 * wave;
     auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
-    const int kt = position(min(it.rt * RT + RT, M) - 1) / KT + 1;           // key tiles that some row of this tile sees
+    const int kt = position(min(it.rt * ROWS_FEW + ROWS_FEW, M) - 1) / KT + 1;           // key tiles that some row of this tile sees
     const int seg = (kt + it.n_seg - 1) / it.n_seg, t_begin = it.seg * seg, t_end = min(kt, t_begin + seg);
-    const int diagonal = (position(it.rt * RT) + 1) / KT;                    // from this tile on there are keys that some row does not see
+    const int diagonal = (position(it.rt * ROWS_FEW) + 1) / KT;                    // from this tile on there are keys that some row does not see
     const bool active = row0 < M;
     const int my_row = min(row0 + l32, M - 1), my_pos = position(my_row);
     // tiles that every row of this wavefront sees whole; tiles that any of them sees
@@ -296,7 +229,7 @@ void chunk_attn_kernel(ChunkParams p)
         if (p.lse && h == 0) p.lse[(size_t)token * p.H_q + head] = (m_used + __builtin_amdgcn_logf(l_row)) * LN2_F;
         return;
     }
-    const size_t prow = ((size_t)it.part * p.H_kv + g) * RT + 32 * wave + l32;
+    const size_t prow = ((size_t)it.part * p.H_kv + g) * 32 + (size_t)wave * 32 * p.H_kv + l32;
     if (h == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * prow) = make_float2(m_used, l_row);
     float *dst = p.part_o + prow * DP;
 #pragma unroll
@@ -306,16 +239,16 @@ void chunk_attn_kernel(ChunkParams p)
             *reinterpret_cast<float4 *>(dst + 32 * nt + 8 * a + 4 * h) = make_float4(o[nt][4 * a], o[nt][4 * a + 1], o[nt][4 * a + 2], o[nt][4 * a + 3]);
 }
 
-// The segments of the rows whose keys are cut.  Eight lanes a row, four columns each; grid (KV heads, tiles of rows, quarters of a tile).
+// The segments of the rows whose keys are cut.  Eight lanes a row, four columns each; grid (KV heads x tiles of rows, blocks of 32 of their rows).
 template <int DP, bool F32>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p)
 {
-    const int tid = threadIdx.x, lane = tid & 63, g = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, g = blockIdx.x % p.H_kv;
     Item it;
-    if (!find_item<true>(p, blockIdx.y, lane, &it)) return;
-    const int M = it.s.n * p.G, in_tile = 32 * blockIdx.z + tid / 8, row = it.rt * RT + in_tile;
-    if (row >= M) return;
-    const size_t step = (size_t)p.H_kv * RT, first = ((size_t)it.part * p.H_kv + g) * RT + in_tile;
+    if (!find_item<MERGE>(p, blockIdx.x / p.H_kv, lane, &it)) return;
+    const int M = it.s.n * p.G, row = it.rt * it.rows + 32 * blockIdx.y + tid / 8;
+    if (32 * (int)blockIdx.y >= it.rows || row >= M) return;
+    const size_t step = (size_t)(it.rows / 32) * p.H_kv * 32, first = ((size_t)(it.part + blockIdx.y) * p.H_kv + g) * 32 + tid / 8;
     float m = M_INIT;
     for (int s = 0; s < it.n_seg; ++s) m = fmaxf(m, p.part_ml[2 * (first + s * step)]);
     float4 acc[DP / 32];
@@ -376,8 +309,10 @@ int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <=
 template <int DP, bool F32>
 void launch_shape(const ChunkParams &p, const ChunkPlan &plan, hipStream_t stream)
 {
-    launch_kernel(K_CHUNK_ATTN, chunk_attn_kernel<DP, F32>, dim3(p.H_kv, plan.max_items), dim3(256), stream, p);
-    if (plan.max_parts) launch_kernel(K_CHUNK_MERGE, chunk_merge_kernel<DP, F32>, dim3(p.H_kv, plan.max_parts / 2, RT / 32), dim3(256), stream, p);
+    if (plan.max_items_many) launch_chunk_wide(p, plan.max_items_many, stream);
+    if (plan.max_items) launch_kernel(K_CHUNK_ATTN, chunk_attn_kernel<DP, F32>, dim3(p.H_kv * plan.max_items), dim3(256), stream, p);
+    if (plan.max_parts)
+        launch_kernel(K_CHUNK_MERGE, chunk_merge_kernel<DP, F32>, dim3(p.H_kv * plan.max_cut, plan.max_items_many ? ROWS_MANY / 32 : ROWS_FEW / 32), dim3(256), stream, p);
 }
 
 template <bool F32>
@@ -394,36 +329,49 @@ void launch_type(const ChunkParams &p, const ChunkPlan &plan, hipStream_t stream
 
 }  // namespace
 
+// Row tiles of `rows` of one KV head at most, where T tokens make sequences of any length.
+static long most_tiles(long T, long B, long G, long rows)
+{
+    const long by_rows = T * G / rows + (T < B ? T : B), by_token = T * ((G + rows - 1) / rows);
+    return by_rows < by_token ? by_rows : by_token;
+}
+
 bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
 {
-    const long G = d.H_q / d.H_kv, T = d.T;
-    const long tiles = (T * G) / RT + (T < d.B ? T : d.B), by_token = T * ((G + RT - 1) / RT);
-    plan->row_tile = RT;
-    plan->max_row_tiles = (int)(tiles < by_token ? tiles : by_token);
-    plan->target = 512;
+    const long G = d.H_q / d.H_kv, T = d.T, kt = (d.L_stride + KT - 1) / KT;
+    // bf16, d = 128: sequences of more than MANY rows have a kernel of their own where a launch has so many on average
+    // (it would find nothing to do in a batch that decodes, for 4 us)
+    const bool many = d.dtype == MCSD_DTYPE_BF16 && d.d == 128 && T * G > (long)MANY * d.B;
+    plan->many = many ? MANY : 0x7fffffff;
+    // Segments of about as many workgroups as the chip takes at once (two a compute unit, one of the wide kernel), of 8 tiles at least.  A sequence that is cut
+    // has kt / len of them, rounded, two at least: 4/3 of kt / len at most.
     plan->min_seg = 8;
-    const long kt = (d.L_stride + KT - 1) / KT, n_seg = (kt + plan->min_seg / 2) / plan->min_seg;
-    const long target = plan->target / d.H_kv > 1 ? plan->target / d.H_kv : 1;
-    // a sequence that is cut has kt / len segments, rounded, two at least: 4/3 of kt / len at most
-    long parts = n_seg < 2 ? 0 : (4 * target + 2) / 3 + 2;
-    if (parts > plan->max_row_tiles * n_seg) parts = plan->max_row_tiles * n_seg;
-    plan->max_parts = (int)parts;
-    long items = plan->max_row_tiles + parts;
-    if (n_seg > 0 && items > plan->max_row_tiles * n_seg) items = plan->max_row_tiles * n_seg;
+    plan->target = d.H_kv < 512 ? 512 / d.H_kv : 1;
+    plan->target_many = d.H_kv < 256 ? 256 / d.H_kv : 1;
+    const long n_seg = (kt + plan->min_seg / 2) / plan->min_seg, tiles = most_tiles(T, d.B, G, ROWS_FEW), tiles_many = many ? most_tiles(T, d.B, G, ROWS_MANY) : 0;
+    auto parts_of = [&](long target, long row_tiles) {
+        const long parts = n_seg < 2 ? 0 : (4 * target + 2) / 3 + 2;
+        return parts < row_tiles * n_seg ? parts : row_tiles * n_seg;
+    };
+    const long parts = parts_of(plan->target, tiles), parts_many = parts_of(plan->target_many, tiles_many);
+    auto items_of = [&](long row_tiles, long cut) { return row_tiles + cut < row_tiles * n_seg || n_seg < 1 ? row_tiles + cut : row_tiles * n_seg; };
+    const long items = items_of(tiles, parts), items_many = items_of(tiles_many, parts_many);
     plan->max_items = (int)items;
-    const size_t rows = (size_t)parts * d.H_kv * RT;
-    plan->ws_bytes = (rows * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256;
-    return items <= 65535L * 16;
+    plan->max_items_many = (int)items_many;
+    plan->max_cut = (int)((parts + parts_many) / 2);
+    plan->max_parts = (int)(parts * (ROWS_FEW / 32) + parts_many * (ROWS_MANY / 32));
+    plan->ws_bytes = ((size_t)plan->max_parts * d.H_kv * 32 * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256;
+    return items * d.H_kv < 1L << 24 && items_many * d.H_kv < 1L << 24;     // (a launch has fewer than 2^32 threads)
 }
 
 int32_t launch_chunk_attn(const mcsd_chunk_desc &d, const mcsd_chunk_bufs &b, const mcsd_paged_kv &kv, const ChunkPlan &plan, hipStream_t stream)
 {
     ChunkParams p = chunk_params(d, kv);
     p.q = b.q; p.k_pool = b.k_pool; p.v_pool = b.v_pool; p.chunk_start = b.chunk_start; p.prefix_len = b.prefix_len; p.out = b.out; p.lse = b.lse;
-    p.min_seg = plan.min_seg; p.max_parts = plan.max_parts;
-    p.target = (float)(plan.target / d.H_kv > 1 ? plan.target / d.H_kv : 1);
+    p.min_seg = plan.min_seg; p.max_parts = plan.max_parts; p.many = plan.many;
+    p.target = (float)plan.target; p.target_many = (float)plan.target_many;
     p.part_o = static_cast<float *>(b.workspace);
-    if (plan.max_parts) p.part_ml = p.part_o + (size_t)plan.max_parts * d.H_kv * RT * padded_dim(d.d);
+    if (plan.max_parts) p.part_ml = p.part_o + (size_t)plan.max_parts * d.H_kv * 32 * padded_dim(d.d);
     if (d.dtype == MCSD_DTYPE_FP32) launch_type<true>(p, plan, stream);
     else launch_type<false>(p, plan, stream);
     const hipError_t e = hipGetLastError();

@@ -17,8 +17,9 @@ struct ChunkParams {
     void *out;
     float *lse, *part_o, *part_ml;
     int B, T, H_q, H_kv, G, d, L_stride, page_size, n_pages, max_pages;
+    int many;             // rows beyond which a sequence belongs to the wide kernel
     int min_seg, max_parts;
-    float target;         // workgroups per KV head aimed at where keys are split
+    float target, target_many;      // workgroups per KV head aimed at where keys are cut, of either kernel
     size_t q_row;         // bytes from a row of q to the next one's
     float scale_log2;     // scale * log2(e)
 };
@@ -58,6 +59,90 @@ __device__ __forceinline__ int wave_running_sum(int v)
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // and into 2, 3
     return v;
 }
+
+// ---- the work of a launch
+// Rows r = token * G + head in group of a (sequence, KV head) go in tiles, of ROWS_MANY for sequences of more than p.many rows and
+// of ROWS_FEW for others (one kernel each), the keys of a tile in equal segments.  A segment is so long that all of a kernel's
+// make about `target` workgroups per KV head, at least min_seg key tiles; a sequence is cut into kt / segment of them, rounded, one for most.
+// Every workgroup of both kernels and of the merge works out the same list, a sequence a lane.  Partial results are numbered in
+// blocks of 32 rows, row tile by row tile, segment by segment.
+constexpr int ROWS_FEW = 128, ROWS_MANY = 256, MANY = 64;
+enum ItemKind { FEW_ROWS, MANY_ROWS, MERGE };
+struct Item { int b, rt, rows, seg, n_seg, part; ChunkSeq s; };
+
+__device__ __forceinline__ bool has_many(const ChunkParams &p, const ChunkSeq &s) { return s.n * p.G > p.many; }
+__device__ __forceinline__ int row_tiles(const ChunkParams &p, const ChunkSeq &s)
+{
+    return has_many(p, s) ? (s.n * p.G + ROWS_MANY - 1) / ROWS_MANY : (s.n * p.G + ROWS_FEW - 1) / ROWS_FEW;
+}
+
+// item number idx (MERGE: row tile number idx of those whose keys are cut); false: there are fewer
+template <ItemKind KIND>
+__device__ __forceinline__ bool find_item(const ChunkParams &p, int idx, int lane, Item *it)
+{
+    int len = 0, len_many = 0;
+    if (p.max_parts) {
+        float work = 0.f, work_many = 0.f;
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            if (b0 + lane >= p.B) break;
+            const ChunkSeq s = chunk_sequence(p, b0 + lane);
+            const float w = (float)row_tiles(p, s) * (float)((s.keys + KT - 1) / KT);
+            if (has_many(p, s)) work_many += w;
+            else work += w;
+        }
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) { work += __shfl_xor(work, m); work_many += __shfl_xor(work_many, m); }
+        len = max(p.min_seg, (int)ceilf(work / p.target));
+        len_many = max(p.min_seg, (int)ceilf(work_many / p.target_many));
+    }
+    int items = 0, parts = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        ChunkSeq s = {0, 0, 0, 0};
+        if (b0 + lane < p.B) s = chunk_sequence(p, b0 + lane);
+        const bool many = has_many(p, s);
+        const int rt = row_tiles(p, s), kt = (s.keys + KT - 1) / KT, blocks = (many ? ROWS_MANY : ROWS_FEW) / 32, my_len = many ? len_many : len;
+        int n_seg = p.max_parts ? max(1, (kt + my_len / 2) / my_len) : 1;
+        const int my_parts = n_seg > 1 ? rt * n_seg * blocks : 0;
+        const int parts_to = parts + wave_running_sum(my_parts);
+        if (parts_to > p.max_parts) n_seg = 1;          // (cannot be, but by arrays that contradict themselves)
+        const bool mine = KIND == MERGE ? n_seg > 1 : many == (KIND == MANY_ROWS);
+        const int my_items = mine ? (KIND == MERGE ? rt : rt * n_seg) : 0;
+        const int items_to = items + wave_running_sum(my_items);
+        const unsigned long long found = __ballot(items_to > idx);
+        if (found) {
+            const int o = __ffsll((long long)found) - 1;
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, o); };
+            it->b = b0 + o;
+            it->s = {of(s.s0), of(s.n), of(s.L), of(s.keys)};
+            it->n_seg = of(n_seg);
+            it->rows = 32 * of(blocks);
+            const int local = idx - of(items_to - my_items);
+            it->rt = of(rt) - 1 - (KIND == MERGE ? local : local / it->n_seg);      // the last rows, with the most keys, first
+            it->seg = KIND == MERGE ? 0 : local % it->n_seg;
+            it->part = of(parts_to - my_parts) + (it->rt * it->n_seg + it->seg) * of(blocks);
+            return true;
+        }
+        items = __builtin_amdgcn_readlane(items_to, 63);
+        parts = __builtin_amdgcn_readlane(parts_to, 63);
+    }
+    return false;
+}
+
+__device__ __forceinline__ u32x4 finite_or_zero(u32x4 v, bool f32, bool *bad)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t e_lo = f32 ? 0u : 0x00007f80u, e_hi = 0x7f800000u;
+        const bool hi = (v[i] & e_hi) == e_hi, lo = !f32 && (v[i] & e_lo) == e_lo;
+        *bad |= hi | lo;
+        if (f32) v[i] = hi ? 0u : v[i];
+        else v[i] = (hi ? 0u : v[i] & 0xffff0000u) | (lo ? 0u : v[i] & 0xffffu);
+    }
+    return v;
+}
+
+// bf16, d = 128, sequences of more than p.many rows (chunk_wide.hip)
+void launch_chunk_wide(const ChunkParams &p, int max_items, hipStream_t stream);
 
 // A tile of 32 rows of DP (padded head dimension) values in LDS, pitches in words.
 //   K  read 16 bytes a lane, lanes 0..31 in 32 rows: a pitch of 4 x an odd number spreads 16 lanes over the 64 banks.

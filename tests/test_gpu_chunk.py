@@ -155,3 +155,47 @@ def test_no_tokens():
     run(batch, 0.1)
     e = torch.empty(0, 2, 128, dtype=torch.bfloat16, device=DEV)
     M.mcsd_kv_store_paged(M.store_args(e, e, torch.empty(0, dtype=torch.int32, device=DEV), batch["k_pool"], batch["v_pool"]))
+
+
+WIDE = [  # sequences with more rows than the kernel for few takes: (lens, news, H_q, H_kv, page)
+    ([0], [65], 1, 1, 32),
+    ([0], [700], 2, 2, 64),
+    ([63], [257], 4, 2, 32),
+    ([31, 500, 0], [300, 1, 513], 2, 1, 96),
+    ([5000], [100], 8, 1, 128),
+    ([5000, 40, 1], [70, 1, 1], 16, 2, 64),
+    ([1, 2, 3], [22, 129, 400], 12, 4, 32),
+    ([2000, 2016, 2017], [96, 96, 96], 7, 1, 32),
+    ([0], [64], 16, 2, 32),
+]
+
+
+@pytest.mark.parametrize("shape", WIDE)
+def test_many_rows(shape):
+    lens, news, H_q, H_kv, page = shape
+    check(R.make_batch(gen(11), DEV, torch.bfloat16, lens, news, H_q, H_kv, 128, page), 1 / math.sqrt(128), torch.bfloat16)
+
+
+def test_many_rows_no_number():
+    """As above where 256 rows share their keys: before, inside and behind the tiles that rows see in part."""
+    batch = R.make_batch(gen(12), DEV, torch.bfloat16, [70], [300], 2, 2, 128, 32)
+    clean, clean_lse = run(batch, 0.1)
+    clean, clean_lse = clean.clone(), clean_lse.clone()
+    for pos in (30, 75, 200, 369):
+        page, row = int(batch["table"][0, pos // 32]), pos % 32
+        old = batch["v_pool"][page, :, row].clone()
+        batch["v_pool"][page, 0, row, 7], batch["v_pool"][page, 1, row, 9] = float("nan"), -float("inf")
+        out, lse = run(batch, 0.1)
+        first = max(0, pos - 70)
+        assert torch.equal(lse, clean_lse) and torch.equal(out[:first], clean[:first])
+        assert torch.isnan(out[first:, 0, 7]).all() and (out[first:, 1, 9] == -float("inf")).all()
+        rest = torch.ones_like(out, dtype=torch.bool)
+        rest[first:, 0, 7] = rest[first:, 1, 9] = False
+        assert torch.equal(out[rest], clean[rest])
+        batch["v_pool"][page, :, row] = old
+
+
+def test_many_rows_bad_pages():
+    batch = R.make_batch(gen(13), DEV, torch.bfloat16, [100, 64], [300, 200], 4, 2, 128, 32)
+    batch["table"][0, 1], batch["table"][0, 5], batch["table"][1, 0], batch["table"][1, 7] = -1, 2 ** 31 - 1, batch["k_pool"].shape[0], -2 ** 31
+    check(batch, 0.1, torch.bfloat16)
