@@ -194,49 +194,50 @@ void chunk_attn_kernel(ChunkParams p)
     if (!active) return;
 
     // ---- epilogue: a lane holds columns 32 nt + 8 a + 4 h .. + 3 of its row
+    const float l_row = l_part + __shfl_xor(l_part, 32);
+    if (row0 + l32 >= M) return;
+    const int token = it.s.s0 + my_row / p.G, head = g * p.G + my_row % p.G;
+    const bool direct = it.n_seg == 1;
+    // row of out and lse, or of the partial results
+    const size_t at = direct ? (size_t)token * p.H_q + head : ((size_t)(it.part + wave) * p.H_kv + g) * 32 + l32;
+    const float f = direct ? 1.0f / l_row : 1.0f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int c = 32 * nt + 8 * a + 4 * h;
+            const float4 x = make_float4(o[nt][4 * a] * f, o[nt][4 * a + 1] * f, o[nt][4 * a + 2] * f, o[nt][4 * a + 3] * f);
+            if (!direct) *reinterpret_cast<float4 *>(p.part_o + at * DP + c) = x;
+            else if (c >= p.d) continue;
+            else if (F32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at * p.d + c) = x;
+            else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at * p.d + c) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+        }
+    if (h == 0) {
+        if (!direct) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(m_used, l_row);
+        else if (p.lse) p.lse[at] = (m_used + __builtin_amdgcn_logf(l_row)) * LN2_F;
+    }
     if (__builtin_expect(s_bad, 0)) {
+        // what is no number joins what was written, by the lane that wrote it
         for (int key = max(diagonal, t_begin) * KT; key <= min(my_pos, t_end * KT - 1); ++key) {
             const int page = p.block_table[(size_t)it.b * p.max_pages + key / p.page_size];
             if ((unsigned)page >= (unsigned)p.n_pages) continue;
             const char *v = static_cast<const char *>(p.v_pool) + (((size_t)page * p.H_kv + g) * p.page_size + key % p.page_size) * row_bytes;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int c = 32 * nt + 8 * (i >> 2) + 4 * h + (i & 3);
-                    if (c >= p.d) continue;
-                    const float x = F32 ? reinterpret_cast<const float *>(v)[c] : bf16_bits_to_float(reinterpret_cast<const uint16_t *>(v)[c]);
-                    if (!(fabsf(x) < INFINITY)) o[nt][i] += x;
+            for (int c = 4 * h; c < p.d; c += (c & 3) == 3 ? 5 : 1) {
+                const float y = F32 ? reinterpret_cast<const float *>(v)[c] : bf16_bits_to_float(reinterpret_cast<const uint16_t *>(v)[c]);
+                if (fabsf(y) < INFINITY) continue;
+                if (!direct) {
+                    volatile float *z = p.part_o + at * DP + c;
+                    *z = *z + y;
+                } else if (F32) {
+                    volatile float *z = static_cast<float *>(p.out) + at * p.d + c;
+                    *z = *z + y;
+                } else {
+                    volatile uint16_t *z = static_cast<uint16_t *>(p.out) + at * p.d + c;
+                    *z = (uint16_t)pack_bf16(bf16_bits_to_float(*z) + y, 0.f);
                 }
+            }
         }
     }
-    const float l_row = l_part + __shfl_xor(l_part, 32);
-    if (row0 + l32 >= M) return;
-    const int token = it.s.s0 + my_row / p.G, head = g * p.G + my_row % p.G;
-    if (it.n_seg == 1) {
-        const float f = 1.0f / l_row;
-        char *dst = static_cast<char *>(p.out) + ((size_t)token * p.H_q + head) * row_bytes;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const int c = 32 * nt + 8 * a + 4 * h;
-                if (c >= p.d) continue;
-                const float x0 = o[nt][4 * a] * f, x1 = o[nt][4 * a + 1] * f, x2 = o[nt][4 * a + 2] * f, x3 = o[nt][4 * a + 3] * f;
-                if (F32) *reinterpret_cast<float4 *>(dst + 4 * c) = make_float4(x0, x1, x2, x3);
-                else *reinterpret_cast<uint2 *>(dst + 2 * c) = make_uint2(pack_bf16(x0, x1), pack_bf16(x2, x3));
-            }
-        if (p.lse && h == 0) p.lse[(size_t)token * p.H_q + head] = (m_used + __builtin_amdgcn_logf(l_row)) * LN2_F;
-        return;
-    }
-    const size_t prow = ((size_t)it.part * p.H_kv + g) * 32 + (size_t)wave * 32 * p.H_kv + l32;
-    if (h == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * prow) = make_float2(m_used, l_row);
-    float *dst = p.part_o + prow * DP;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-            *reinterpret_cast<float4 *>(dst + 32 * nt + 8 * a + 4 * h) = make_float4(o[nt][4 * a], o[nt][4 * a + 1], o[nt][4 * a + 2], o[nt][4 * a + 3]);
 }
 
 // The segments of the rows whose keys are cut.  Eight lanes a row, four columns each; grid (KV heads x tiles of rows, blocks of 32 of their rows).

@@ -48,6 +48,10 @@ __device__ __forceinline__ ChunkSeq chunk_sequence(const ChunkParams &p, int b)
     return s;
 }
 
+// A value that is the same in all lanes, back in a scalar register: divisions are vector arithmetic, and what stands behind one in a loop
+// would follow it.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // running sum over the lanes of a wavefront
 __device__ __forceinline__ int wave_running_sum(int v)
 {
@@ -76,56 +80,86 @@ __device__ __forceinline__ int row_tiles(const ChunkParams &p, const ChunkSeq &s
     return has_many(p, s) ? (s.n * p.G + ROWS_MANY - 1) / ROWS_MANY : (s.n * p.G + ROWS_FEW - 1) / ROWS_FEW;
 }
 
-// item number idx (MERGE: row tile number idx of those whose keys are cut); false: there are fewer
+template <ItemKind KIND>
+struct ItemList {
+    int len = 0, len_many = 0;              // key tiles of a segment of either kernel
+    // of sequence `lane` (further ones are read again by every search)
+    ChunkSeq s = {0, 0, 0, 0};
+    int rt = 0, n_seg = 1, blocks = 1, mine = 0, part = 0, parts = 0;
+
+    __device__ __forceinline__ ItemList(const ChunkParams &p, int lane)
+    {
+        if (lane < p.B) s = chunk_sequence(p, lane);
+        if (p.max_parts) {
+            float work = 0.f, work_many = 0.f;
+            auto add = [&](const ChunkSeq &q) {
+                const float w = (float)row_tiles(p, q) * (float)((q.keys + KT - 1) / KT);
+                work_many += has_many(p, q) ? w : 0.f;
+                work += has_many(p, q) ? 0.f : w;
+            };
+            add(s);
+            for (int b = lane + 64; b < p.B; b += 64) add(chunk_sequence(p, b));
+#pragma unroll
+            for (int m = 32; m > 0; m >>= 1) { work += __shfl_xor(work, m); work_many += __shfl_xor(work_many, m); }
+            len = max(p.min_seg, (int)ceilf(work / p.target));
+            len_many = max(p.min_seg, (int)ceilf(work_many / p.target_many));
+        }
+        parts = count(p, 0);
+    }
+    // items and partial results of the lane's sequence, behind those of `before`; returns the partial results up to lane 63
+    __device__ __forceinline__ int count(const ChunkParams &p, int before)
+    {
+        const bool many = has_many(p, s);
+        const int kt = (s.keys + KT - 1) / KT, my_len = many ? len_many : len;
+        rt = row_tiles(p, s);
+        blocks = (many ? ROWS_MANY : ROWS_FEW) / 32;
+        n_seg = p.max_parts ? max(1, (kt + my_len / 2) / my_len) : 1;
+        const int my_parts = n_seg > 1 ? rt * n_seg * blocks : 0;
+        const int parts_to = before + wave_running_sum(my_parts);
+        if (parts_to > p.max_parts) n_seg = 1;          // (cannot be, but by arrays that contradict themselves)
+        part = parts_to - my_parts;
+        mine = KIND == MERGE ? n_seg > 1 : many == (KIND == MANY_ROWS);
+        return __builtin_amdgcn_readlane(parts_to, 63);
+    }
+    __device__ __forceinline__ void fill(int o, int b, int from_end, int seg, Item *it) const
+    {
+        auto of = [&](int v) { return __builtin_amdgcn_readlane(v, o); };
+        it->b = b;
+        it->s = {of(s.s0), of(s.n), of(s.L), of(s.keys)};
+        it->n_seg = of(n_seg);
+        it->rows = 32 * of(blocks);
+        it->rt = of(rt) - 1 - from_end;
+        it->seg = seg;
+        it->part = of(part) + (it->rt * it->n_seg + seg) * of(blocks);
+    }
+    // Item number idx; false: there are fewer.  Sequence by sequence (their row tiles share keys and values), the last rows, which see the most keys, first.
+    __device__ __forceinline__ bool find(const ChunkParams &p, int idx, int lane, Item *it) const
+    {
+        ItemList l = *this;
+        int items = 0, behind = parts;
+        for (int b0 = 0;;) {
+            const int per = KIND == MERGE ? 1 : l.n_seg, my_items = l.mine ? l.rt * per : 0, items_to = items + wave_running_sum(my_items);
+            const unsigned long long found = __ballot(items_to > idx);
+            if (found) {
+                const int o = __ffsll((long long)found) - 1, local = idx - __builtin_amdgcn_readlane(items_to - my_items, o), n = __builtin_amdgcn_readlane(per, o);
+                const int from_end = uniform(local / n);
+                l.fill(o, b0 + o, from_end, local - from_end * n, it);
+                return true;
+            }
+            items = __builtin_amdgcn_readlane(items_to, 63);
+            b0 += 64;
+            if (b0 >= p.B) return false;
+            l.s = {0, 0, 0, 0};
+            if (b0 + lane < p.B) l.s = chunk_sequence(p, b0 + lane);
+            behind = l.count(p, behind);
+        }
+    }
+};
+
 template <ItemKind KIND>
 __device__ __forceinline__ bool find_item(const ChunkParams &p, int idx, int lane, Item *it)
 {
-    int len = 0, len_many = 0;
-    if (p.max_parts) {
-        float work = 0.f, work_many = 0.f;
-        for (int b0 = 0; b0 < p.B; b0 += 64) {
-            if (b0 + lane >= p.B) break;
-            const ChunkSeq s = chunk_sequence(p, b0 + lane);
-            const float w = (float)row_tiles(p, s) * (float)((s.keys + KT - 1) / KT);
-            if (has_many(p, s)) work_many += w;
-            else work += w;
-        }
-#pragma unroll
-        for (int m = 32; m > 0; m >>= 1) { work += __shfl_xor(work, m); work_many += __shfl_xor(work_many, m); }
-        len = max(p.min_seg, (int)ceilf(work / p.target));
-        len_many = max(p.min_seg, (int)ceilf(work_many / p.target_many));
-    }
-    int items = 0, parts = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        ChunkSeq s = {0, 0, 0, 0};
-        if (b0 + lane < p.B) s = chunk_sequence(p, b0 + lane);
-        const bool many = has_many(p, s);
-        const int rt = row_tiles(p, s), kt = (s.keys + KT - 1) / KT, blocks = (many ? ROWS_MANY : ROWS_FEW) / 32, my_len = many ? len_many : len;
-        int n_seg = p.max_parts ? max(1, (kt + my_len / 2) / my_len) : 1;
-        const int my_parts = n_seg > 1 ? rt * n_seg * blocks : 0;
-        const int parts_to = parts + wave_running_sum(my_parts);
-        if (parts_to > p.max_parts) n_seg = 1;          // (cannot be, but by arrays that contradict themselves)
-        const bool mine = KIND == MERGE ? n_seg > 1 : many == (KIND == MANY_ROWS);
-        const int my_items = mine ? (KIND == MERGE ? rt : rt * n_seg) : 0;
-        const int items_to = items + wave_running_sum(my_items);
-        const unsigned long long found = __ballot(items_to > idx);
-        if (found) {
-            const int o = __ffsll((long long)found) - 1;
-            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, o); };
-            it->b = b0 + o;
-            it->s = {of(s.s0), of(s.n), of(s.L), of(s.keys)};
-            it->n_seg = of(n_seg);
-            it->rows = 32 * of(blocks);
-            const int local = idx - of(items_to - my_items);
-            it->rt = of(rt) - 1 - (KIND == MERGE ? local : local / it->n_seg);      // the last rows, with the most keys, first
-            it->seg = KIND == MERGE ? 0 : local % it->n_seg;
-            it->part = of(parts_to - my_parts) + (it->rt * it->n_seg + it->seg) * of(blocks);
-            return true;
-        }
-        items = __builtin_amdgcn_readlane(items_to, 63);
-        parts = __builtin_amdgcn_readlane(parts_to, 63);
-    }
-    return false;
+    return ItemList<KIND>(p, lane).find(p, idx, lane, it);
 }
 
 __device__ __forceinline__ u32x4 finite_or_zero(u32x4 v, bool f32, bool *bad)

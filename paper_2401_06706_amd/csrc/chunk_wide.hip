@@ -9,13 +9,15 @@ namespace {
 constexpr int ROWS = ROWS_MANY, D = 128, ROW_BYTES = 2 * D, DEPTH = 4;
 constexpr int SIDE_BYTES = KT * ROW_BYTES, TILE_BYTES = 2 * SIDE_BYTES;      // K, then V
 
-// what a page outside the pool reads as: four rows, a load's worth
-__device__ __attribute__((aligned(16))) uint32_t zero_rows[ROW_BYTES] = {0};
+// what a page outside the pool reads as: a wavefront's rows of a tile
+__device__ __attribute__((aligned(16))) uint32_t zero_rows[8 * ROW_BYTES / 4] = {0};
 
-// 64 lanes x 16 bytes from base + offset straight into LDS at `to` (lane after lane); arrived once the wavefront has counted vmcnt down to it
-__device__ __forceinline__ void fetch16(uint32_t to, const void *base, uint32_t offset)
+// 2 x 64 lanes x 16 bytes from base + offset, and from 1 KB behind, straight into LDS at `to` (lane after lane) and 1 KB behind (the
+// instruction's offset counts on both sides); arrived once the wavefront has counted vmcnt down to them
+__device__ __forceinline__ void fetch(uint32_t to, const void *base, uint32_t offset, uint32_t offset_behind)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(offset), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024"
+                 :: "s"(to), "v"(offset), "v"(offset_behind), "s"(base) : "memory", "m0");
 }
 
 // A workgroup of four wavefronts, one per SIMD, owns 256 rows of a (sequence, KV head) and a segment of its key tiles; a wavefront owns
@@ -28,95 +30,130 @@ __device__ __forceinline__ void fetch16(uint32_t to, const void *base, uint32_t 
 //   - K and V go from memory straight into a ring of four tiles in LDS, asked for three tiles ahead.  16-byte pieces lie permuted: K piece c of row r
 //     at c ^ (r % 16), V piece c at c ^ 4 (r % 4), which keeps the 16 rows of an operand read, and the four rows
 //     of a transposing read, in banks of their own.
+//   - A workgroup goes through several row tiles, and asks for the next one's first tiles and Q ahead of the present one's epilogue:
+//     there is no other workgroup on its CU that would run meanwhile.  Row tiles are dealt out
+//     forth and back, the heavy ones of a sequence first, which evens the workgroups out and keeps those of one head on one XCD at a time.
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void chunk_wide_kernel(ChunkParams p)
 {
     __shared__ __attribute__((aligned(1024))) uint32_t s_ring[DEPTH * TILE_BYTES / 4];
-    __shared__ int s_bad;
+    __shared__ int s_bad[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, l32 = lane & 31, lj = lane >> 4, lc = lane & 15;
-    const int g = blockIdx.x % p.H_kv;
-    Item it;
-    if (!find_item<MANY_ROWS>(p, blockIdx.x / p.H_kv, lane, &it)) return;
-    const int M = it.s.n * p.G, tile0 = it.rt * ROWS, row0 = tile0 + 64 * wave;
-    auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
-    const int kt = position(min(tile0 + ROWS, M) - 1) / KT + 1;                  // key tiles that some row of this tile sees
-    const int seg = (kt + it.n_seg - 1) / it.n_seg, t_begin = it.seg * seg, t_end = min(kt, t_begin + seg);
-    const int diagonal = (position(tile0) + 1) / KT;                             // from here on there are keys that some row does not see
-    const bool active = row0 < M;
-    // tiles that every row of this wavefront sees whole; tiles that any of them sees
-    const int t_plain = active ? max(t_begin, min(t_end, (position(row0) + 1) / KT)) : t_begin;
-    const int t_seen = active ? max(t_begin, min(t_end, position(min(row0 + 64, M) - 1) / KT + 1)) : t_begin;
-    if (tid == 0) s_bad = 0;
+    const ItemList<MANY_ROWS> list(p, lane);
+    int round = 0;
+    auto next_item = [&](Item *it, int *g) __attribute__((always_inline)) {
+        // (number `round` of this workgroup's; every other round is dealt out backwards)
+        const int at = round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+        ++round;
+        const int in_head = uniform(at / p.H_kv);
+        *g = at - in_head * p.H_kv;           // (KV head fastest: the row tiles of one meet in one XCD's L2 where their number is a multiple of 8)
+        return list.find(p, in_head, lane, it);
+    };
 
-    // ---- requests: this wavefront's 8 rows of K and of V of a tile.  Past the end the last tile is asked for again, so that what is
-    // waited for can be counted.
+    // ---- an item, worked out ahead of its turn
+    struct Plan {
+        int b, g, n_seg, part, s0;
+        int M, row0, t_begin, t_end;
+        int diagonal;           // from this tile on there are keys that some row does not see
+        int t_plain, t_seen;    // tiles that every row of this wavefront sees whole; tiles that any of them sees
+        int page;               // of the first tile
+        int row[2], pos[2];     // of this lane's row in each block (lanes past the last row repeat it)
+        int entries;            // block table from that page on, a lane each
+    } now, ahead;
+    auto plan_item = [&](Plan *n) __attribute__((always_inline)) {
+        Item it;
+        if (!next_item(&it, &n->g)) return false;
+        n->b = it.b;
+        n->n_seg = it.n_seg;
+        n->part = it.part;
+        n->s0 = it.s.s0;
+        n->M = it.s.n * p.G;
+        const int tile0 = it.rt * ROWS;
+        n->row0 = tile0 + 64 * wave;
+        auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
+        const int kt = uniform(position(min(tile0 + ROWS, n->M) - 1)) / KT + 1;          // key tiles that some row of this tile sees
+        const int seg = uniform((kt + it.n_seg - 1) / it.n_seg);
+        n->t_begin = uniform(min(kt, it.seg * seg));
+        n->t_end = uniform(min(kt, n->t_begin + seg));
+        n->diagonal = (uniform(position(tile0)) + 1) / KT;
+        const bool active = n->row0 < n->M;
+        n->t_plain = active ? max(n->t_begin, min(n->t_end, (uniform(position(n->row0)) + 1) / KT)) : n->t_begin;
+        n->t_seen = active ? max(n->t_begin, min(n->t_end, uniform(position(min(n->row0 + 64, n->M) - 1)) / KT + 1)) : n->t_begin;
+        n->page = uniform(n->t_begin * KT / p.page_size);
+        n->entries = p.block_table[(size_t)it.b * p.max_pages + min(n->page + lane, (p.L_stride - 1) / p.page_size)];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            n->row[x] = max(0, min(n->row0 + 32 * x + l32, n->M - 1));
+            n->pos[x] = position(n->row[x]);
+        }
+        return true;
+    };
+
+    // ---- requests: this wavefront's 8 rows of K and of V of a tile, four loads.  Past the end the last tile is asked for again, so that what
+    // is waited for can be counted.
     const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t *)s_ring;
     const uint32_t row_off = (uint32_t)lj * ROW_BYTES;
     const uint32_t k_off0 = row_off + 16 * (lc ^ ((8 * wave + lj) & 15)), k_off1 = row_off + 16 * (lc ^ ((8 * wave + 4 + lj) & 15));
     const uint32_t v_off = row_off + 16 * (lc ^ (4 * lj));
-    const const_i32_ptr table = (const_i32_ptr)(uintptr_t)(p.block_table + (size_t)it.b * p.max_pages);
-    const int t_last = max(t_begin, t_end - 1);
-    // (advance() works out, among the matrix instructions, where the next tile lies)
-    int ask = t_begin - 1, ask_page = t_begin * KT / p.page_size, ask_row = t_begin * KT % p.page_size - KT;
-    int entry = t_begin < t_end ? (int)table[ask_page] : -1, next;
-    const size_t page_bytes = (size_t)p.H_kv * p.page_size * ROW_BYTES, head_at = ((size_t)g * p.page_size + 8 * wave) * ROW_BYTES;
-    const char *const k_head = static_cast<const char *>(p.k_pool) + head_at, *const v_head = static_cast<const char *>(p.v_pool) + head_at;
+    const size_t page_bytes = (size_t)p.H_kv * p.page_size * ROW_BYTES;
     const char *zeros = reinterpret_cast<const char *>(zero_rows);
     asm volatile("" : "+s"(zeros));
-    const char *k_at, *v_at;
-    uint32_t to;
+    const char *k_head = nullptr, *v_head = nullptr, *k_at = nullptr, *v_at = nullptr;
+    int ask = 0, ask_row = 0, n_entry = 0, entry = -1;
+    // works out, among the matrix instructions, where the next tile lies
     auto advance = [&]() __attribute__((always_inline)) {
         ++ask;
-        to = ring_at + (ask & (DEPTH - 1)) * TILE_BYTES + wave * (8 * ROW_BYTES);
-        if (ask <= t_last) {
+        if (ask < now.t_end) {
             ask_row += KT;
             if (ask_row >= p.page_size) {
                 ask_row = 0;
-                entry = table[++ask_page];
+                if (++n_entry == 64) {
+                    n_entry = 0;
+                    now.page += 64;
+                    now.entries = p.block_table[(size_t)now.b * p.max_pages + min(now.page + lane, (p.L_stride - 1) / p.page_size)];
+                    asm volatile("s_waitcnt vmcnt(0)" : "+v"(now.entries) :: "memory");     // (here, not in the loop)
+                }
+                entry = __builtin_amdgcn_readlane(now.entries, n_entry);
             }
         }
         const bool in = (unsigned)entry < (unsigned)p.n_pages;
         const size_t at = (size_t)(uint32_t)entry * page_bytes + (uint32_t)ask_row * ROW_BYTES;
         k_at = in ? k_head + at : zeros;
         v_at = in ? v_head + at : zeros;
-        next = in ? 4 * ROW_BYTES : 0;
     };
     auto request = [&]() __attribute__((always_inline)) {
-        fetch16(to, k_at, k_off0);
-        fetch16(to + 4 * ROW_BYTES, k_at + next, k_off1);
-        fetch16(to + SIDE_BYTES, v_at, v_off);
-        fetch16(to + SIDE_BYTES + 4 * ROW_BYTES, v_at + next, v_off);
+        const uint32_t to = ring_at + (ask & (DEPTH - 1)) * TILE_BYTES + wave * (8 * ROW_BYTES);
+        fetch(to, k_at, k_off0, k_off1);
+        fetch(to + SIDE_BYTES, v_at, v_off, v_off);
     };
-    advance();
-    if (t_begin < t_end) {
+    bf16x8 q[2][8];             // lane holds Q[row][16 kk + 8 h .. + 7] of a row of each block
+    auto begin_item = [&]() __attribute__((always_inline)) {
+        asm volatile("" : "+v"(now.entries));
+        if (now.t_begin < now.t_end) {
+            const size_t head_at = ((size_t)now.g * p.page_size + 8 * wave) * ROW_BYTES;
+            k_head = static_cast<const char *>(p.k_pool) + head_at;
+            v_head = static_cast<const char *>(p.v_pool) + head_at;
+            ask = uniform(now.t_begin) - 1;
+            ask_row = now.t_begin * KT - now.page * p.page_size - KT;
+            n_entry = 0;
+            entry = __builtin_amdgcn_readlane(now.entries, 0);
+            advance();
 #pragma unroll
-        for (int i = 0; i < DEPTH - 1; ++i) { request(); advance(); }
-    }
+            for (int i = 0; i < DEPTH - 1; ++i) { request(); advance(); }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int token = now.row[x] / p.G;
+            const char *src = static_cast<const char *>(p.q) + (size_t)(now.s0 + token) * p.q_row + (size_t)(now.g * p.G + now.row[x] - token * p.G) * ROW_BYTES + 16 * h;
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) q[x][kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(src + 32 * kk));
+        }
+    };
 
-    // ---- Q: lane holds Q[row][16 kk + 8 h .. + 7] of a row of each block (lanes past the last row repeat it)
-    int my_row[2], my_pos[2];
-    bf16x8 q[2][8];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        my_row[x] = min(row0 + 32 * x + l32, M - 1);
-        my_pos[x] = position(my_row[x]);
-        const char *src = static_cast<const char *>(p.q) + (size_t)(it.s.s0 + my_row[x] / p.G) * p.q_row + (size_t)(g * p.G + my_row[x] % p.G) * ROW_BYTES + 16 * h;
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) q[x][kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(src + 32 * kk));
-    }
     f32x16 o[2][4], s[2];
-    float m_used[2] = {M_INIT, M_INIT}, l_part[2] = {0.f, 0.f};
+    float m_used[2], l_part[2];
     bf16x8 w[2][2];             // packed weights
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[x][nt][i] = 0.f;
-        const u32x4 zero = {0, 0, 0, 0};
-        w[x][0] = w[x][1] = __builtin_bit_cast(bf16x8, zero);
-    }
     const float c2 = p.scale_log2;
 
     // ---- operands out of LDS
@@ -128,25 +165,19 @@ void chunk_wide_kernel(ChunkParams p)
     const char *const ring = reinterpret_cast<const char *>(s_ring);
     typedef short v4i16 __attribute__((ext_vector_type(4)));
     typedef v4i16 __attribute__((address_space(3))) *lds_v4i16_ptr;
-    auto read_k = [&](int t, bf16x8 *k) __attribute__((always_inline)) {
-        const char *at = ring + (t & (DEPTH - 1)) * TILE_BYTES;
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) k[kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(at + (k_ld ^ (32 * kk))));
+    bf16x8 k[8], v[2][4];       // operands of a tile of K, of a tile of V
+    auto read_k = [&](const int kk, int t) __attribute__((always_inline)) {
+        k[kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(ring + (t & (DEPTH - 1)) * TILE_BYTES + (k_ld ^ (32 * kk))));
     };
-    auto read_v = [&](int t, bf16x8 (*v)[4]) __attribute__((always_inline)) {
-        const char *at = ring + (t & (DEPTH - 1)) * TILE_BYTES;
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int nt = 0; nt < 4; ++nt) {
-                const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(at + v_ld[nt] + 16 * m * ROW_BYTES));
-                const v4i16 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(at + v_ld[nt] + (16 * m + 8) * ROW_BYTES));
-                v[m][nt] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
+    auto read_v = [&](const int m, const int nt, int t) __attribute__((always_inline)) {
+        const char *from = ring + (t & (DEPTH - 1)) * TILE_BYTES + v_ld[nt] + 16 * m * ROW_BYTES;
+        const v4i16 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)from);
+        const v4i16 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(from + 8 * ROW_BYTES));
+        v[m][nt] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     // weights of block x from its scores of tile t
     auto weights = [&](const int x, int t, auto masked, u32x4 *pk) __attribute__((always_inline)) {
-        const int seen = my_pos[x] - t * KT - 4 * h;
+        const int seen = now.pos[x] - t * KT - 4 * h;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
@@ -163,7 +194,7 @@ void chunk_wide_kernel(ChunkParams p)
     // The maximum is raised only where the weights outgrow it (their sum, which is formed anyway, tells), row by row.
     auto settle = [&](const int x, int t, auto masked, float sum, u32x4 *pk) __attribute__((always_inline)) {
         if (__builtin_expect(__any(!(sum <= 4096.f)), 0)) {
-            const int seen = my_pos[x] - t * KT - 4 * h;
+            const int seen = now.pos[x] - t * KT - 4 * h;
             float mx = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -183,176 +214,235 @@ void chunk_wide_kernel(ChunkParams p)
         w[x][0] = __builtin_bit_cast(bf16x8, pk[0]);
         w[x][1] = __builtin_bit_cast(bf16x8, pk[1]);
     };
-    auto pv = [&](const int x, const int m, const int nt, const bf16x8 (*v)[4]) __attribute__((always_inline)) {
+    auto pv = [&](const int x, const int m, const int nt) __attribute__((always_inline)) {
         o[x][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[m][nt], w[x][m], o[x][nt], 0, 0, 0);
     };
     auto zero_scores = [&](const int x) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
     };
-    auto qk = [&](const int x, const int kk, const bf16x8 *k) __attribute__((always_inline)) {
+    auto qk = [&](const int x, const int kk) __attribute__((always_inline)) {
         s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk], q[x][kk], s[x], 0, 0, 0);
     };
 
     // ---- steps
     bool bad = false;
     // Where rows do not see all keys, values that are no numbers enter the products as zeros (0 times such a value is none either)
-    // and are added in the epilogue to the rows that see them.  This wavefront's own rows of the tile.
-    auto clean = [&](int t) __attribute__((always_inline)) {
-        char *at = const_cast<char *>(ring) + (t & (DEPTH - 1)) * TILE_BYTES + SIDE_BYTES + wave * (8 * ROW_BYTES) + 16 * lane;
+    // and are added in the epilogue to the rows that see them.  A wavefront looks at its own rows of a tile: `look` reads them, `clean` has an
+    // exponent of all ones carry into the bit above it.
+    auto mine_of = [&](int t) __attribute__((always_inline)) { return const_cast<char *>(ring) + (t & (DEPTH - 1)) * TILE_BYTES + SIDE_BYTES + wave * (8 * ROW_BYTES) + 16 * lane; };
+    auto look = [&](int t, u32x4 *x) __attribute__((always_inline)) {
+        x[0] = *reinterpret_cast<const u32x4 *>(mine_of(t));
+        x[1] = *reinterpret_cast<const u32x4 *>(mine_of(t) + 4 * ROW_BYTES);
+    };
+    auto clean = [&](int t, const u32x4 *x) __attribute__((always_inline)) {
+        uint32_t any = 0;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(at + 4 * j * ROW_BYTES);
-            bool here = false;
-            const u32x4 y = finite_or_zero(x, false, &here);
-            if (here) *reinterpret_cast<u32x4 *>(at + 4 * j * ROW_BYTES) = y;
-            bad |= here;
+        for (int i = 0; i < 8; ++i) any |= (x[i / 4][i % 4] & 0x7f807f80u) + 0x00800080u;
+        if (__builtin_expect((any & 0x80008000u) != 0, 0)) {
+            bad = true;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                u32x4 y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = x[j][i] & ~(((((x[j][i] & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xffffu);
+                *reinterpret_cast<u32x4 *>(mine_of(t) + 4 * j * ROW_BYTES) = y;
+            }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
-    // Tile t + 1 has arrived (4 requests per tile, those of t + 2 may still be on their way) and, behind the barrier, everybody's part of it; what
-    // lay where t + 3 goes, t - 1, was last read ahead of it.
-    auto begin_step = [&](int t) __attribute__((always_inline)) {
+    // Ahead of it: tile t + 1 has arrived (4 loads per tile, those of t + 2 may still be on their way); behind the barrier: everybody's part of
+    // it.  What lay where t + 3 goes, t - 1, was last read ahead of it.
+    auto arrival = [&]() __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-        if (t + 1 >= diagonal && t + 1 < t_end) clean(t + 1);
         __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
         request();
     };
-    // One tile: k, v hold K(t) and V(t - 1), afterwards k_next, v_now hold K(t + 1) and V(t).
-    auto step = [&](int t, auto masked, const bf16x8 (&k)[8], const bf16x8 (&v)[2][4], bf16x8 (&k_next)[8], bf16x8 (&v_now)[2][4]) __attribute__((always_inline)) {
-        begin_step(t);
-        u32x4 pk[2];
-        float sum;
-        read_v(t, v_now);
-        read_k(t + 1, k_next);
-        sum = weights(0, t, masked, pk);
+    // One tile: k, v hold K(t) and V(t - 1), afterwards K(t + 1) and V(t); each operand is replaced as soon as block B has used it.
+    // partial: some row does not see all of its keys, or V(t + 1) is to be cleaned before the next step.
+    auto step = [&](int t, auto partial) __attribute__((always_inline)) {
+        constexpr bool PARTIAL = decltype(partial)::value;
+        constexpr int BESIDE = PARTIAL ? 6 : 4;     // vector instructions per matrix instruction
+        u32x4 raw[2], pk[2];
         zero_scores(1);
+        // (products that need nothing of what the barrier stands for run while it is waited at)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) { pv(1, 0, i); qk(1, i); }
+        __builtin_amdgcn_sched_barrier(0);
+        arrival();
+        __builtin_amdgcn_sched_barrier(0);
+        if (PARTIAL) look(t + 1, raw);
+        float sum = weights(0, t, partial, pk);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            pv(1, i / 4, i % 4, v);
-            qk(1, i, k);
+            if (i >= 2) pv(1, i / 4, i % 4);
+            read_v(i / 4, i % 4, t);
+            if (i >= 2) qk(1, i);
+            read_k(i, t + 1);
         }
-        if (!decltype(masked)::value) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x402, 4, 0);
-            }
+        for (int i = 0; i < 6; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, BESIDE + 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, BESIDE + 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
-        settle(0, t, masked, sum, pk);
+        settle(0, t, partial, sum, pk);
         advance();
-        sum = weights(1, t, masked, pk);
+        sum = weights(1, t, partial, pk);
         zero_scores(0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            pv(0, i / 4, i % 4, v_now);
-            qk(0, i, k_next);
+            pv(0, i / 4, i % 4);
+            qk(0, i);
         }
-        if (!decltype(masked)::value) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x402, 4, 0);
+        for (int i = 0; i < 16; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, BESIDE, 0);
+        }
+        settle(1, t, partial, sum, pk);
+        if (PARTIAL) clean(t + 1, raw);
+    };
+    if (tid < 2) s_bad[tid] = 0;
+    bool more = plan_item(&ahead), done = false, direct = false, poisoned = false, mine[2] = {false, false};    // an item is done, and what its epilogue needs
+    int done_b = 0, done_g = 0, key_from = 0, key_end = 0, done_pos[2] = {0, 0};
+    size_t at[2] = {0, 0};      // row of out and lse, or of the partial results
+    // ---- epilogue: a lane holds columns 32 nt + 8 a + 4 h .. + 3 of its row in each block
+    auto epilogue = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const float l_row = l_part[x] + __shfl_xor(l_part[x], 32);
+            if (direct) {
+                const float f = 1.0f / l_row;
+                char *dst = static_cast<char *>(p.out) + at[x] * ROW_BYTES + 16 * h;
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                    for (int a = 0; a < 4; a += 2) {
+                        // lanes l32 and l32 + 32 exchange so that each holds eight neighbouring columns
+                        u32x4 y;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const uint32_t even = pack_bf16(o[x][nt][4 * a + 2 * k] * f, o[x][nt][4 * a + 2 * k + 1] * f);
+                            const uint32_t odd = pack_bf16(o[x][nt][4 * a + 4 + 2 * k] * f, o[x][nt][4 * a + 5 + 2 * k] * f);
+                            const auto both = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
+                            y[k] = both[0];
+                            y[2 + k] = both[1];
+                        }
+                        if (mine[x]) *reinterpret_cast<u32x4 *>(dst + 2 * (32 * nt + 8 * a)) = y;
+                    }
+                if (p.lse && h == 0 && mine[x]) p.lse[at[x]] = (m_used[x] + __builtin_amdgcn_logf(l_row)) * LN2_F;
+            } else if (mine[x]) {
+                if (h == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at[x]) = make_float2(m_used[x], l_row);
+                float *dst = p.part_o + at[x] * D;
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                    for (int a = 0; a < 4; ++a)
+                        *reinterpret_cast<float4 *>(dst + 32 * nt + 8 * a + 4 * h) = make_float4(o[x][nt][4 * a], o[x][nt][4 * a + 1], o[x][nt][4 * a + 2], o[x][nt][4 * a + 3]);
+            }
+            if (__builtin_expect(poisoned, 0) && mine[x]) {
+                // what is no number joins what was written, lane l32 + 32 h takes columns 64 h .. 64 h + 63
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                for (int key = key_from; key <= min(done_pos[x], key_end); ++key) {
+                    const int page = p.block_table[(size_t)done_b * p.max_pages + key / p.page_size];
+                    if ((unsigned)page >= (unsigned)p.n_pages) continue;
+                    const uint16_t *v = static_cast<const uint16_t *>(p.v_pool) + (((size_t)page * p.H_kv + done_g) * p.page_size + key % p.page_size) * D;
+                    for (int c = 64 * h; c < 64 * h + 64; ++c) {
+                        const float y = bf16_bits_to_float(v[c]);
+                        if (fabsf(y) < INFINITY) continue;
+                        if (direct) {
+                            volatile uint16_t *z = static_cast<uint16_t *>(p.out) + at[x] * D + c;
+                            *z = (uint16_t)pack_bf16(bf16_bits_to_float(*z) + y, 0.f);
+                        } else {
+                            volatile float *z = p.part_o + at[x] * D + c;
+                            *z = *z + y;
+                        }
+                    }
+                }
             }
         }
-        settle(1, t, masked, sum, pk);
     };
-    if (t_begin < t_end) {
-        int t = t_begin;
+    for (int n_item = 0;; ++n_item) {
+        const bool here = more;
+        if (here) {
+            now = ahead;
+            begin_item();
+            more = plan_item(&ahead);           // (while the first tiles are on their way)
+        }
+        if (done) epilogue();
+        if (!here) break;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[x][nt][i] = 0.f;
+            const u32x4 zero = {0, 0, 0, 0};
+            w[x][0] = w[x][1] = __builtin_bit_cast(bf16x8, zero);
+            m_used[x] = M_INIT;
+            l_part[x] = 0.f;
+        }
+        bad = false;
         // the first tiles and Q (the compiler waits for what it knows of, Q, ahead of this: not in the loop, where it would wait for all requests)
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+a"(q[x][kk]));
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (t >= diagonal) clean(t);
+        int t = now.t_begin;
+        if (t >= now.diagonal && t < now.t_end) {
+            u32x4 raw[2];
+            look(t, raw);
+            clean(t, raw);
+        }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (t < t_seen) {
+        if (tid == 0) s_bad[(n_item + 1) & 1] = 0;              // (the epilogue that read it lies behind everybody)
+        if (t < now.t_seen) {
             const u32x4 zero = {0, 0, 0, 0};
-            bf16x8 k0[8], v0[2][4], k1[8], v1[2][4];        // (two sets that take turns)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v0[i / 4][i % 4] = __builtin_bit_cast(bf16x8, zero);
-            read_k(t, k0);
+            for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = __builtin_bit_cast(bf16x8, zero);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) read_k(i, t);
             zero_scores(0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) qk(0, i, k0);
-            for (; t + 1 < t_plain; t += 2) {
-                step(t, std::false_type(), k0, v0, k1, v1);
-                step(t + 1, std::false_type(), k1, v1, k0, v0);
-            }
-            for (; t + 1 < t_seen; t += 2) {
-                step(t, std::true_type(), k0, v0, k1, v1);
-                step(t + 1, std::true_type(), k1, v1, k0, v0);
-            }
-            if (t < t_seen) {
-                step(t, std::true_type(), k0, v0, k1, v1);
-                ++t;
+            for (int i = 0; i < 8; ++i) qk(0, i);
+            for (const int whole = min(now.t_plain, now.diagonal - 1); t < whole; ++t) step(t, std::false_type());
+            for (; t < now.t_seen; ++t) step(t, std::true_type());
 #pragma unroll
-                for (int i = 0; i < 8; ++i) pv(1, i / 4, i % 4, v1);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) pv(1, i / 4, i % 4, v0);
-            }
+            for (int i = 0; i < 8; ++i) pv(1, i / 4, i % 4);
         }
-        for (; t < t_end; ++t) { begin_step(t); advance(); }                   // (this wavefront only helps to load)
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // nothing may be on its way into LDS when the workgroup ends
-    if (__any(bad) && lane == 0) s_bad = 1;
-    __syncthreads();
-    if (!active) return;
+        for (; t < now.t_end; ++t) {                            // (this wavefront only helps to load)
+            u32x4 raw[2];
+            arrival();
+            if (t + 1 >= now.diagonal) look(t + 1, raw);
+            advance();
+            if (t + 1 >= now.diagonal) clean(t + 1, raw);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (nothing is on its way into LDS any more)
+        if (__any(bad) && lane == 0) s_bad[n_item & 1] = 1;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
 
-    // ---- epilogue: a lane holds columns 32 nt + 8 a + 4 h .. + 3 of its row in each block
+        done = true;
+        direct = now.n_seg == 1;
+        poisoned = s_bad[n_item & 1] != 0;
+        done_b = now.b;
+        done_g = now.g;
+        key_from = max(now.diagonal, now.t_begin) * KT;
+        key_end = now.t_end * KT - 1;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        if (__builtin_expect(s_bad, 0)) {
-            for (int key = max(diagonal, t_begin) * KT; key <= min(my_pos[x], t_end * KT - 1); ++key) {
-                const int page = p.block_table[(size_t)it.b * p.max_pages + key / p.page_size];
-                if ((unsigned)page >= (unsigned)p.n_pages) continue;
-                const uint16_t *v = static_cast<const uint16_t *>(p.v_pool) + (((size_t)page * p.H_kv + g) * p.page_size + key % p.page_size) * D;
-#pragma unroll
-                for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float y = bf16_bits_to_float(v[32 * nt + 8 * (i >> 2) + 4 * h + (i & 3)]);
-                        if (!(fabsf(y) < INFINITY)) o[x][nt][i] += y;
-                    }
-            }
-        }
-        const float l_row = l_part[x] + __shfl_xor(l_part[x], 32);
-        const bool mine = row0 + 32 * x + l32 < M;
-        const int token = it.s.s0 + my_row[x] / p.G, head = g * p.G + my_row[x] % p.G;
-        if (it.n_seg == 1) {
-            const float f = 1.0f / l_row;
-            char *dst = static_cast<char *>(p.out) + ((size_t)token * p.H_q + head) * ROW_BYTES + 16 * h;
-#pragma unroll
-            for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-                for (int a = 0; a < 4; a += 2) {
-                    // lanes l32 and l32 + 32 exchange so that each holds eight neighbouring columns
-                    u32x4 y;
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const uint32_t even = pack_bf16(o[x][nt][4 * a + 2 * k] * f, o[x][nt][4 * a + 2 * k + 1] * f);
-                        const uint32_t odd = pack_bf16(o[x][nt][4 * a + 4 + 2 * k] * f, o[x][nt][4 * a + 5 + 2 * k] * f);
-                        const auto both = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
-                        y[k] = both[0];
-                        y[2 + k] = both[1];
-                    }
-                    if (mine) *reinterpret_cast<u32x4 *>(dst + 2 * (32 * nt + 8 * a)) = y;
-                }
-            if (p.lse && h == 0 && mine) p.lse[(size_t)token * p.H_q + head] = (m_used[x] + __builtin_amdgcn_logf(l_row)) * LN2_F;
-        } else if (mine) {
-            const size_t prow = ((size_t)(it.part + 2 * wave + x) * p.H_kv + g) * 32 + l32;
-            if (h == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * prow) = make_float2(m_used[x], l_row);
-            float *dst = p.part_o + prow * D;
-#pragma unroll
-            for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-                for (int a = 0; a < 4; ++a)
-                    *reinterpret_cast<float4 *>(dst + 32 * nt + 8 * a + 4 * h) = make_float4(o[x][nt][4 * a], o[x][nt][4 * a + 1], o[x][nt][4 * a + 2], o[x][nt][4 * a + 3]);
+        for (int x = 0; x < 2; ++x) {
+            mine[x] = now.row0 + 32 * x + l32 < now.M;
+            done_pos[x] = now.pos[x];
+            const int token = now.row[x] / p.G;
+            at[x] = direct ? (size_t)(now.s0 + token) * p.H_q + (now.g * p.G + now.row[x] - token * p.G)
+                           : ((size_t)(now.part + 2 * wave + x) * p.H_kv + now.g) * 32 + l32;
         }
     }
 }
@@ -361,7 +451,7 @@ void chunk_wide_kernel(ChunkParams p)
 
 void launch_chunk_wide(const ChunkParams &p, int max_items, hipStream_t stream)
 {
-    launch_kernel(K_CHUNK_WIDE, chunk_wide_kernel, dim3(p.H_kv * max_items), dim3(256), stream, p);
+    launch_kernel(K_CHUNK_WIDE, chunk_wide_kernel, dim3(min(p.H_kv * max_items, 256)), dim3(256), stream, p);
 }
 
 }  // namespace mcsd
