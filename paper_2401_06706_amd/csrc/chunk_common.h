@@ -17,6 +17,8 @@ struct ChunkParams {
     void *out;
     float *lse, *part_o, *part_ml;
     int B, T, H_q, H_kv, G, d, L_stride, page_size, n_pages, max_pages;
+    uint32_t group_magic; // ceil-like reciprocal of G, see by_group
+    int group_shift;
     int many;             // rows beyond which a sequence belongs to the wide kernel
     int min_seg, max_parts;
     float target, target_many;      // workgroups per KV head aimed at where keys are cut, of either kernel
@@ -31,7 +33,18 @@ inline ChunkParams chunk_params(const mcsd_chunk_desc &d, const mcsd_paged_kv &k
     p.page_size = kv.page_size; p.n_pages = kv.n_pages; p.max_pages = kv.max_pages_per_seq; p.block_table = kv.block_table;
     p.q_row = (size_t)d.q_stride * (d.dtype == MCSD_DTYPE_FP32 ? 4 : 2);
     p.scale_log2 = d.scale * LOG2E_F;
+    int bits = 0;
+    while ((1LL << bits) < p.G) ++bits;
+    p.group_shift = bits - 1;
+    p.group_magic = p.G > 1 ? (uint32_t)((1ULL << (31 + bits)) / (unsigned)p.G + 1) : 0;
     return p;
+}
+
+// row / G for 0 <= row < 2^31: with 2^(b-1) < G <= 2^b, m = floor(2^(31+b) / G) + 1 exceeds the quotient by less than one part in 2^(31+b) / G, so that
+// row m / 2^(31+b) is too large by less than 1 / G.
+__device__ __forceinline__ int by_group(const ChunkParams &p, int row)
+{
+    return p.G == 1 ? row : (int)(__umulhi((uint32_t)row, p.group_magic) >> p.group_shift);
 }
 
 // New tokens s0 .. s0 + n - 1 of a sequence stand at positions L .. L + n - 1; `keys` positions are there (below the capacity).

@@ -20,6 +20,12 @@ __device__ __forceinline__ void fetch(uint32_t to, const void *base, uint32_t of
                  :: "s"(to), "v"(offset), "v"(offset_behind), "s"(base) : "memory", "m0");
 }
 
+// the same from an address of each lane's own
+__device__ __forceinline__ void fetch_from(uint32_t to, const void *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(uniform((int)to)), "v"(from) : "memory", "m0");
+}
+
 // A workgroup of four wavefronts, one per SIMD, owns 256 rows of a (sequence, KV head) and a segment of its key tiles; a wavefront owns
 // 64 rows in two blocks of 32, A and B, and shares every K and V operand between them.  S^T = K Q^T and O^T += V^T P^T
 // with v_mfma_f32_32x32x16_bf16 as in tree attention (a weight never leaves its lane).
@@ -37,7 +43,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void chunk_wide_kernel(ChunkParams p)
 {
     __shared__ __attribute__((aligned(1024))) uint32_t s_ring[DEPTH * TILE_BYTES / 4];
-    __shared__ int s_bad[2];
+    __shared__ __attribute__((aligned(1024))) uint32_t s_rows[4][64 * ROW_BYTES / 4];       // Q of the next item, a wavefront's rows; results on their way out
+    __shared__ int s_odd[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, l32 = lane & 31, lj = lane >> 4, lc = lane & 15;
     const ItemList<MANY_ROWS> list(p, lane);
@@ -71,7 +78,7 @@ void chunk_wide_kernel(ChunkParams p)
         n->M = it.s.n * p.G;
         const int tile0 = it.rt * ROWS;
         n->row0 = tile0 + 64 * wave;
-        auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
+        auto position = [&](int row) { return min(it.s.L + by_group(p, row), it.s.keys - 1); };
         const int kt = uniform(position(min(tile0 + ROWS, n->M) - 1)) / KT + 1;          // key tiles that some row of this tile sees
         const int seg = uniform((kt + it.n_seg - 1) / it.n_seg);
         n->t_begin = uniform(min(kt, it.seg * seg));
@@ -100,7 +107,7 @@ void chunk_wide_kernel(ChunkParams p)
     const char *zeros = reinterpret_cast<const char *>(zero_rows);
     asm volatile("" : "+s"(zeros));
     const char *k_head = nullptr, *v_head = nullptr, *k_at = nullptr, *v_at = nullptr;
-    int ask = 0, ask_row = 0, n_entry = 0, entry = -1;
+    int ask = 0, ask_page = 0, ask_row = 0, entries = -1, n_entry = 0, entry = -1;
     // works out, among the matrix instructions, where the next tile lies
     auto advance = [&]() __attribute__((always_inline)) {
         ++ask;
@@ -110,11 +117,11 @@ void chunk_wide_kernel(ChunkParams p)
                 ask_row = 0;
                 if (++n_entry == 64) {
                     n_entry = 0;
-                    now.page += 64;
-                    now.entries = p.block_table[(size_t)now.b * p.max_pages + min(now.page + lane, (p.L_stride - 1) / p.page_size)];
-                    asm volatile("s_waitcnt vmcnt(0)" : "+v"(now.entries) :: "memory");     // (here, not in the loop)
+                    ask_page += 64;
+                    entries = p.block_table[(size_t)now.b * p.max_pages + min(ask_page + lane, (p.L_stride - 1) / p.page_size)];
+                    asm volatile("s_waitcnt vmcnt(0)" : "+v"(entries) :: "memory");     // (here, not in the loop)
                 }
-                entry = __builtin_amdgcn_readlane(now.entries, n_entry);
+                entry = __builtin_amdgcn_readlane(entries, n_entry);
             }
         }
         const bool in = (unsigned)entry < (unsigned)p.n_pages;
@@ -127,28 +134,46 @@ void chunk_wide_kernel(ChunkParams p)
         fetch(to, k_at, k_off0, k_off1);
         fetch(to + SIDE_BYTES, v_at, v_off, v_off);
     };
-    bf16x8 q[2][8];             // lane holds Q[row][16 kk + 8 h .. + 7] of a row of each block
     auto begin_item = [&]() __attribute__((always_inline)) {
-        asm volatile("" : "+v"(now.entries));
+        entries = now.entries;
+        asm volatile("" : "+v"(entries));
         if (now.t_begin < now.t_end) {
             const size_t head_at = ((size_t)now.g * p.page_size + 8 * wave) * ROW_BYTES;
             k_head = static_cast<const char *>(p.k_pool) + head_at;
             v_head = static_cast<const char *>(p.v_pool) + head_at;
             ask = uniform(now.t_begin) - 1;
             ask_row = now.t_begin * KT - now.page * p.page_size - KT;
+            ask_page = now.page;
             n_entry = 0;
-            entry = __builtin_amdgcn_readlane(now.entries, 0);
+            entry = __builtin_amdgcn_readlane(entries, 0);
             advance();
 #pragma unroll
             for (int i = 0; i < DEPTH - 1; ++i) { request(); advance(); }
         }
+    };
+    // ---- Q of an item: into this wavefront's part of LDS (16 loads of four rows each, permuted as K is), then as operands: lane holds
+    // Q[row][16 kk + 8 h .. + 7] of a row of each block.  (Loaded as operands, 32 bytes of each of 32 rows at a time, the 64 KB of a
+    // workgroup took 2.4 us.)  Rows past the last one repeat it.
+    constexpr int Q_LOADS = 16;
+    char *const my_rows = reinterpret_cast<char *>(s_rows[wave]);
+    const uint32_t rows_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t *)s_rows[wave];
+    bf16x8 q[2][8];
+    auto fetch_q = [&](const Plan &n) __attribute__((always_inline)) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int token = now.row[x] / p.G;
-            const char *src = static_cast<const char *>(p.q) + (size_t)(now.s0 + token) * p.q_row + (size_t)(now.g * p.G + now.row[x] - token * p.G) * ROW_BYTES + 16 * h;
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk) q[x][kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(src + 32 * kk));
+        for (int i = 0; i < Q_LOADS; ++i) {
+            const int r = max(0, min(n.row0 + 4 * i + lj, n.M - 1)), token = by_group(p, r);
+            const char *src = static_cast<const char *>(p.q) + (size_t)(n.s0 + token) * p.q_row + (size_t)(n.g * p.G + r - token * p.G) * ROW_BYTES + 16 * (lc ^ ((4 * i + lj) & 15));
+            fetch_from(rows_at + 4 * i * ROW_BYTES, src);
         }
+    };
+    auto read_q = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) {
+                q[x][kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(my_rows + (32 * x + l32) * ROW_BYTES + ((16 * (h ^ (l32 & 15))) ^ (32 * kk))));
+                asm volatile("" : "+a"(q[x][kk]));
+            }
     };
 
     f32x16 o[2][4], s[2];
@@ -226,21 +251,17 @@ void chunk_wide_kernel(ChunkParams p)
     };
 
     // ---- steps
-    bool bad = false;
-    // Where rows do not see all keys, values that are no numbers enter the products as zeros (0 times such a value is none either)
-    // and are added in the epilogue to the rows that see them.  A wavefront looks at its own rows of a tile: `look` reads them, `clean` has an
-    // exponent of all ones carry into the bit above it.
+    // Where rows do not see all keys, a value that is no number would reach them: 0 times it is none either.  An item whose results hold
+    // such a value is done again, with such values of these tiles as zeros, and the epilogue adds them to the rows that see
+    // them.  A wavefront looks at its own rows of a tile; an exponent of all ones carries into the bit above it.
     auto mine_of = [&](int t) __attribute__((always_inline)) { return const_cast<char *>(ring) + (t & (DEPTH - 1)) * TILE_BYTES + SIDE_BYTES + wave * (8 * ROW_BYTES) + 16 * lane; };
-    auto look = [&](int t, u32x4 *x) __attribute__((always_inline)) {
-        x[0] = *reinterpret_cast<const u32x4 *>(mine_of(t));
-        x[1] = *reinterpret_cast<const u32x4 *>(mine_of(t) + 4 * ROW_BYTES);
-    };
-    auto clean = [&](int t, const u32x4 *x) __attribute__((always_inline)) {
+    auto clean = [&](int t) __attribute__((always_inline)) {
+        if (t < now.diagonal || t >= now.t_end) return;
+        const u32x4 x[2] = {*reinterpret_cast<const u32x4 *>(mine_of(t)), *reinterpret_cast<const u32x4 *>(mine_of(t) + 4 * ROW_BYTES)};
         uint32_t any = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) any |= (x[i / 4][i % 4] & 0x7f807f80u) + 0x00800080u;
         if (__builtin_expect((any & 0x80008000u) != 0, 0)) {
-            bad = true;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 u32x4 y;
@@ -253,17 +274,23 @@ void chunk_wide_kernel(ChunkParams p)
     };
     // Ahead of it: tile t + 1 has arrived (4 loads per tile, those of t + 2 may still be on their way); behind the barrier: everybody's part of
     // it.  What lay where t + 3 goes, t - 1, was last read ahead of it.
+    int behind_q = 0;
     auto arrival = [&]() __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+        if (behind_q > 0) {         // (the next item's Q was asked for behind t + 2)
+            --behind_q;
+            asm volatile("s_waitcnt vmcnt(%0)" :: "n"(4 + Q_LOADS) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+        }
         __builtin_amdgcn_s_barrier();
         request();
     };
     // One tile: k, v hold K(t) and V(t - 1), afterwards K(t + 1) and V(t); each operand is replaced as soon as block B has used it.
-    // partial: some row does not see all of its keys, or V(t + 1) is to be cleaned before the next step.
-    auto step = [&](int t, auto partial) __attribute__((always_inline)) {
-        constexpr bool PARTIAL = decltype(partial)::value;
-        constexpr int BESIDE = PARTIAL ? 6 : 4;     // vector instructions per matrix instruction
-        u32x4 raw[2], pk[2];
+    // partial: some row does not see all of its keys; cleaned: V(t + 1) is cleaned before the next step.
+    auto step = [&](int t, auto partial, auto cleaned) __attribute__((always_inline)) {
+        constexpr bool CLEAN = decltype(cleaned)::value;
+        constexpr int BESIDE = decltype(partial)::value ? 6 : 4;     // vector instructions per matrix instruction
+        u32x4 pk[2];
         zero_scores(1);
         // (products that need nothing of what the barrier stands for run while it is waited at)
 #pragma unroll
@@ -271,7 +298,6 @@ void chunk_wide_kernel(ChunkParams p)
         __builtin_amdgcn_sched_barrier(0);
         arrival();
         __builtin_amdgcn_sched_barrier(0);
-        if (PARTIAL) look(t + 1, raw);
         float sum = weights(0, t, partial, pk);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -304,9 +330,9 @@ void chunk_wide_kernel(ChunkParams p)
             __builtin_amdgcn_sched_group_barrier(0x402, BESIDE, 0);
         }
         settle(1, t, partial, sum, pk);
-        if (PARTIAL) clean(t + 1, raw);
+        if (CLEAN) clean(t + 1);
     };
-    if (tid < 2) s_bad[tid] = 0;
+    if (tid < 2) s_odd[tid] = 0;
     bool more = plan_item(&ahead), done = false, direct = false, poisoned = false, mine[2] = {false, false};    // an item is done, and what its epilogue needs
     int done_b = 0, done_g = 0, key_from = 0, key_end = 0, done_pos[2] = {0, 0};
     size_t at[2] = {0, 0};      // row of out and lse, or of the partial results
@@ -316,8 +342,8 @@ void chunk_wide_kernel(ChunkParams p)
         for (int x = 0; x < 2; ++x) {
             const float l_row = l_part[x] + __shfl_xor(l_part[x], 32);
             if (direct) {
+                // through LDS, so that whole rows go out (16-byte pieces permuted as K's are)
                 const float f = 1.0f / l_row;
-                char *dst = static_cast<char *>(p.out) + at[x] * ROW_BYTES + 16 * h;
 #pragma unroll
                 for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
@@ -332,8 +358,15 @@ void chunk_wide_kernel(ChunkParams p)
                             y[k] = both[0];
                             y[2 + k] = both[1];
                         }
-                        if (mine[x]) *reinterpret_cast<u32x4 *>(dst + 2 * (32 * nt + 8 * a)) = y;
+                        *reinterpret_cast<u32x4 *>(my_rows + (32 * x + l32) * ROW_BYTES + 16 * ((4 * nt + a + h) ^ (l32 & 15))) = y;
                     }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int r = 4 * i + lj;
+                    const size_t row = __shfl(at[x], r);
+                    const u32x4 y = *reinterpret_cast<const u32x4 *>(my_rows + (32 * x + r) * ROW_BYTES + 16 * (lc ^ (r & 15)));
+                    if (__shfl((int)mine[x], r)) *reinterpret_cast<u32x4 *>(static_cast<char *>(p.out) + row * ROW_BYTES + 16 * lc) = y;
+                }
                 if (p.lse && h == 0 && mine[x]) p.lse[at[x]] = (m_used[x] + __builtin_amdgcn_logf(l_row)) * LN2_F;
             } else if (mine[x]) {
                 if (h == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at[x]) = make_float2(m_used[x], l_row);
@@ -366,15 +399,21 @@ void chunk_wide_kernel(ChunkParams p)
             }
         }
     };
-    for (int n_item = 0;; ++n_item) {
+    if (more) {
+        now = ahead;
+        fetch_q(now);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    bool careful = false, again = false;        // this item is done again; there is one behind it
+    for (int pass = 0;; ++pass) {
         const bool here = more;
         if (here) {
-            now = ahead;
             begin_item();
-            more = plan_item(&ahead);           // (while the first tiles are on their way)
+            read_q();           // (arrived during the item before)
         }
         if (done) epilogue();
         if (!here) break;
+        if (!careful) more = plan_item(&ahead);         // (while the first tiles are on their way)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
 #pragma unroll
@@ -386,22 +425,16 @@ void chunk_wide_kernel(ChunkParams p)
             m_used[x] = M_INIT;
             l_part[x] = 0.f;
         }
-        bad = false;
-        // the first tiles and Q (the compiler waits for what it knows of, Q, ahead of this: not in the loop, where it would wait for all requests)
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+a"(q[x][kk]));
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         int t = now.t_begin;
-        if (t >= now.diagonal && t < now.t_end) {
-            u32x4 raw[2];
-            look(t, raw);
-            clean(t, raw);
-        }
+        if (careful) clean(t);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (tid == 0) s_bad[(n_item + 1) & 1] = 0;              // (the epilogue that read it lies behind everybody)
+        if (tid == 0) s_odd[(pass + 1) & 1] = 0;                // (whoever read it is past this barrier)
+        // Q of the next item (of this one, should it be done again: it is in LDS once more then)
+        const bool prefetch = more && !careful;
+        if (prefetch) fetch_q(ahead);
+        behind_q = prefetch ? 2 : 0;
         if (t < now.t_seen) {
             const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
@@ -411,27 +444,55 @@ void chunk_wide_kernel(ChunkParams p)
             zero_scores(0);
 #pragma unroll
             for (int i = 0; i < 8; ++i) qk(0, i);
-            for (const int whole = min(now.t_plain, now.diagonal - 1); t < whole; ++t) step(t, std::false_type());
-            for (; t < now.t_seen; ++t) step(t, std::true_type());
+            if (!careful) {
+                for (; t < now.t_plain; ++t) step(t, std::false_type(), std::false_type());
+                for (; t < now.t_seen; ++t) step(t, std::true_type(), std::false_type());
+            } else {
+                for (; t < now.t_seen; ++t) step(t, std::true_type(), std::true_type());
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) pv(1, i / 4, i % 4);
         }
         for (; t < now.t_end; ++t) {                            // (this wavefront only helps to load)
-            u32x4 raw[2];
             arrival();
-            if (t + 1 >= now.diagonal) look(t + 1, raw);
             advance();
-            if (t + 1 >= now.diagonal) clean(t + 1, raw);
+            if (careful) clean(t + 1);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (nothing is on its way into LDS any more)
-        if (__any(bad) && lane == 0) s_bad[n_item & 1] = 1;
+        if (!careful) {
+            float sum = 0.f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum = fmaf(o[x][nt][i], 0.f, sum);         // (0 times it is 0, or no number)
+            if (__any(sum != 0.f) && lane == 0) s_odd[pass & 1] = 1;
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        const bool odd = s_odd[pass & 1] != 0;
+        if (!careful && uniform(odd) && now.t_begin < now.t_end) {
+            // once more; the next item's Q, which has taken this one's place in LDS, is loaded again too, then
+            careful = true;
+            done = false;
+            again = more;
+            more = true;
+            fetch_q(now);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            continue;
+        }
+        if (careful) {
+            more = again;
+            if (more) fetch_q(ahead);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
 
         done = true;
         direct = now.n_seg == 1;
-        poisoned = s_bad[n_item & 1] != 0;
+        poisoned = careful;
+        careful = false;
         done_b = now.b;
         done_g = now.g;
         key_from = max(now.diagonal, now.t_begin) * KT;
@@ -440,10 +501,11 @@ void chunk_wide_kernel(ChunkParams p)
         for (int x = 0; x < 2; ++x) {
             mine[x] = now.row0 + 32 * x + l32 < now.M;
             done_pos[x] = now.pos[x];
-            const int token = now.row[x] / p.G;
+            const int token = by_group(p, now.row[x]);
             at[x] = direct ? (size_t)(now.s0 + token) * p.H_q + (now.g * p.G + now.row[x] - token * p.G)
                            : ((size_t)(now.part + 2 * wave + x) * p.H_kv + now.g) * 32 + l32;
         }
+        if (more) now = ahead;
     }
 }
 
