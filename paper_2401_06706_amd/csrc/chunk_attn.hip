@@ -23,6 +23,7 @@ void chunk_attn_kernel(ChunkParams p)
     const int h = lane >> 5, l32 = lane & 31, lj = lane >> 4, lc = lane & 15;
     const int g = blockIdx.x % p.H_kv;          // (KV head fastest: the row tiles of one meet in one XCD's L2 where their number is a multiple of 8)
     Item it;
+    if (p.counter && blockIdx.x == 0 && tid == 0) *p.counter = 0;
     if (!find_item<FEW_ROWS>(p, blockIdx.x / p.H_kv, lane, &it)) return;
     const int M = it.s.n * p.G, row0 = it.rt * ROWS_FEW + 32 * wave;
     auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
@@ -310,8 +311,8 @@ int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <=
 template <int DP, bool F32>
 void launch_shape(const ChunkParams &p, const ChunkPlan &plan, hipStream_t stream)
 {
+    launch_kernel(K_CHUNK_ATTN, chunk_attn_kernel<DP, F32>, dim3(p.H_kv * plan.max_items), dim3(256), stream, p);
     if (plan.max_items_many) launch_chunk_wide(p, plan.max_items_many, stream);
-    if (plan.max_items) launch_kernel(K_CHUNK_ATTN, chunk_attn_kernel<DP, F32>, dim3(p.H_kv * plan.max_items), dim3(256), stream, p);
     if (plan.max_parts)
         launch_kernel(K_CHUNK_MERGE, chunk_merge_kernel<DP, F32>, dim3(p.H_kv * plan.max_cut, plan.max_items_many ? ROWS_MANY / 32 : ROWS_FEW / 32), dim3(256), stream, p);
 }
@@ -361,7 +362,7 @@ bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
     plan->max_items_many = (int)items_many;
     plan->max_cut = (int)((parts + parts_many) / 2);
     plan->max_parts = (int)(parts * (ROWS_FEW / 32) + parts_many * (ROWS_MANY / 32));
-    plan->ws_bytes = ((size_t)plan->max_parts * d.H_kv * 32 * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256;
+    plan->ws_bytes = ((size_t)plan->max_parts * d.H_kv * 32 * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256 + (many ? 256 : 0);
     return items * d.H_kv < 1L << 24 && items_many * d.H_kv < 1L << 24;     // (a launch has fewer than 2^32 threads)
 }
 
@@ -372,6 +373,7 @@ int32_t launch_chunk_attn(const mcsd_chunk_desc &d, const mcsd_chunk_bufs &b, co
     p.min_seg = plan.min_seg; p.max_parts = plan.max_parts; p.many = plan.many;
     p.target = (float)plan.target; p.target_many = (float)plan.target_many;
     p.part_o = static_cast<float *>(b.workspace);
+    p.counter = plan.max_items_many ? reinterpret_cast<int *>(static_cast<char *>(b.workspace) + plan.ws_bytes - 256) : nullptr;
     if (plan.max_parts) p.part_ml = p.part_o + (size_t)plan.max_parts * d.H_kv * 32 * padded_dim(d.d);
     if (d.dtype == MCSD_DTYPE_FP32) launch_type<true>(p, plan, stream);
     else launch_type<false>(p, plan, stream);

@@ -16,6 +16,7 @@ struct ChunkParams {
     const int32_t *chunk_start, *prefix_len, *block_table;
     void *out;
     float *lse, *part_o, *part_ml;
+    int *counter;         // of the wide kernel's items
     int B, T, H_q, H_kv, G, d, L_stride, page_size, n_pages, max_pages;
     uint32_t group_magic; // ceil-like reciprocal of G, see by_group
     int group_shift;
@@ -63,7 +64,13 @@ __device__ __forceinline__ ChunkSeq chunk_sequence(const ChunkParams &p, int b)
 
 // A value that is the same in all lanes, back in a scalar register: divisions are vector arithmetic, and what stands behind one in a loop
 // would follow it.
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// (the statement keeps the compiler from following the value back)
+__device__ __forceinline__ int uniform(int x)
+{
+    int r = __builtin_amdgcn_readfirstlane(x);
+    asm("" : "+s"(r));
+    return r;
+}
 
 // running sum over the lanes of a wavefront
 __device__ __forceinline__ int wave_running_sum(int v)

@@ -37,24 +37,25 @@ __device__ __forceinline__ void fetch_from(uint32_t to, const void *from)
 //     at c ^ (r % 16), V piece c at c ^ 4 (r % 4), which keeps the 16 rows of an operand read, and the four rows
 //     of a transposing read, in banks of their own.
 //   - A workgroup goes through several row tiles, and asks for the next one's first tiles and Q ahead of the present one's epilogue:
-//     there is no other workgroup on its CU that would run meanwhile.  Row tiles are dealt out
-//     forth and back, the heavy ones of a sequence first, which evens the workgroups out and keeps those of one head on one XCD at a time.
+//     there is no other workgroup on its CU that would run meanwhile.  Items are taken
+//     as workgroups come to them, the heavy row tiles of a sequence first: dealt out beforehand, forth and back, eight prompts
+//     of 1000 to 2048 tokens, 32 heads, gave the busiest workgroup 18 % more than the mean.
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void chunk_wide_kernel(ChunkParams p)
 {
     __shared__ __attribute__((aligned(1024))) uint32_t s_ring[DEPTH * TILE_BYTES / 4];
     __shared__ __attribute__((aligned(1024))) uint32_t s_rows[4][64 * ROW_BYTES / 4];       // Q of the next item, a wavefront's rows; results on their way out
-    __shared__ int s_odd[2];
+    __shared__ int s_odd[2], s_next;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, l32 = lane & 31, lj = lane >> 4, lc = lane & 15;
+    const int page_size = uniform(p.page_size), H_kv = uniform(p.H_kv);         // (scalars beside the vector copies that divisions make of them)
     const ItemList<MANY_ROWS> list(p, lane);
-    int round = 0;
+    // The first item of a workgroup is its own, each further one the next that nobody has (the counter starts from 0: the kernel for few rows clears
+    // it).  Which workgroup takes an item changes nothing in its results.
+    int next = blockIdx.x;
     auto next_item = [&](Item *it, int *g) __attribute__((always_inline)) {
-        // (number `round` of this workgroup's; every other round is dealt out backwards)
-        const int at = round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
-        ++round;
-        const int in_head = uniform(at / p.H_kv);
-        *g = at - in_head * p.H_kv;           // (KV head fastest: the row tiles of one meet in one XCD's L2 where their number is a multiple of 8)
+        const int in_head = uniform(next / H_kv);
+        *g = next - in_head * H_kv;           // (KV head fastest: the row tiles of one meet in one XCD's L2 where their number is a multiple of 8)
         return list.find(p, in_head, lane, it);
     };
 
@@ -87,8 +88,8 @@ void chunk_wide_kernel(ChunkParams p)
         const bool active = n->row0 < n->M;
         n->t_plain = active ? max(n->t_begin, min(n->t_end, (uniform(position(n->row0)) + 1) / KT)) : n->t_begin;
         n->t_seen = active ? max(n->t_begin, min(n->t_end, uniform(position(min(n->row0 + 64, n->M) - 1)) / KT + 1)) : n->t_begin;
-        n->page = uniform(n->t_begin * KT / p.page_size);
-        n->entries = p.block_table[(size_t)it.b * p.max_pages + min(n->page + lane, (p.L_stride - 1) / p.page_size)];
+        n->page = uniform(n->t_begin * KT / page_size);
+        n->entries = p.block_table[(size_t)it.b * p.max_pages + min(n->page + lane, (p.L_stride - 1) / page_size)];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             n->row[x] = max(0, min(n->row0 + 32 * x + l32, n->M - 1));
@@ -103,7 +104,7 @@ void chunk_wide_kernel(ChunkParams p)
     const uint32_t row_off = (uint32_t)lj * ROW_BYTES;
     const uint32_t k_off0 = row_off + 16 * (lc ^ ((8 * wave + lj) & 15)), k_off1 = row_off + 16 * (lc ^ ((8 * wave + 4 + lj) & 15));
     const uint32_t v_off = row_off + 16 * (lc ^ (4 * lj));
-    const size_t page_bytes = (size_t)p.H_kv * p.page_size * ROW_BYTES;
+    const size_t page_bytes = (size_t)H_kv * page_size * ROW_BYTES;
     const char *zeros = reinterpret_cast<const char *>(zero_rows);
     asm volatile("" : "+s"(zeros));
     const char *k_head = nullptr, *v_head = nullptr, *k_at = nullptr, *v_at = nullptr;
@@ -113,15 +114,15 @@ void chunk_wide_kernel(ChunkParams p)
         ++ask;
         if (ask < now.t_end) {
             ask_row += KT;
-            if (ask_row >= p.page_size) {
+            if (ask_row >= page_size) {
                 ask_row = 0;
                 if (++n_entry == 64) {
                     n_entry = 0;
                     ask_page += 64;
-                    entries = p.block_table[(size_t)now.b * p.max_pages + min(ask_page + lane, (p.L_stride - 1) / p.page_size)];
+                    entries = p.block_table[(size_t)now.b * p.max_pages + min(ask_page + lane, (p.L_stride - 1) / page_size)];
                     asm volatile("s_waitcnt vmcnt(0)" : "+v"(entries) :: "memory");     // (here, not in the loop)
                 }
-                entry = __builtin_amdgcn_readlane(entries, n_entry);
+                entry = uniform(__builtin_amdgcn_readlane(entries, n_entry));
             }
         }
         const bool in = (unsigned)entry < (unsigned)p.n_pages;
@@ -135,17 +136,26 @@ void chunk_wide_kernel(ChunkParams p)
         fetch(to + SIDE_BYTES, v_at, v_off, v_off);
     };
     auto begin_item = [&]() __attribute__((always_inline)) {
+        // (scalars again: what the compiler keeps between items in vector registers would bring vector arithmetic into the loops)
+        now.b = uniform(now.b);
+        now.g = uniform(now.g);
+        now.t_begin = uniform(now.t_begin);
+        now.t_end = uniform(now.t_end);
+        now.t_plain = uniform(now.t_plain);
+        now.t_seen = uniform(now.t_seen);
+        now.diagonal = uniform(now.diagonal);
+        now.page = uniform(now.page);
         entries = now.entries;
         asm volatile("" : "+v"(entries));
         if (now.t_begin < now.t_end) {
-            const size_t head_at = ((size_t)now.g * p.page_size + 8 * wave) * ROW_BYTES;
+            const size_t head_at = ((size_t)now.g * page_size + 8 * wave) * ROW_BYTES;
             k_head = static_cast<const char *>(p.k_pool) + head_at;
             v_head = static_cast<const char *>(p.v_pool) + head_at;
             ask = uniform(now.t_begin) - 1;
-            ask_row = now.t_begin * KT - now.page * p.page_size - KT;
+            ask_row = now.t_begin * KT - now.page * page_size - KT;
             ask_page = now.page;
             n_entry = 0;
-            entry = __builtin_amdgcn_readlane(entries, 0);
+            entry = uniform(__builtin_amdgcn_readlane(entries, 0));
             advance();
 #pragma unroll
             for (int i = 0; i < DEPTH - 1; ++i) { request(); advance(); }
@@ -164,6 +174,7 @@ void chunk_wide_kernel(ChunkParams p)
             const int r = max(0, min(n.row0 + 4 * i + lj, n.M - 1)), token = by_group(p, r);
             const char *src = static_cast<const char *>(p.q) + (size_t)(n.s0 + token) * p.q_row + (size_t)(n.g * p.G + r - token * p.G) * ROW_BYTES + 16 * (lc ^ ((4 * i + lj) & 15));
             fetch_from(rows_at + 4 * i * ROW_BYTES, src);
+            __builtin_amdgcn_sched_barrier(0);      // (or all addresses are held at once)
         }
     };
     auto read_q = [&]() __attribute__((always_inline)) {
@@ -172,8 +183,11 @@ void chunk_wide_kernel(ChunkParams p)
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) {
                 q[x][kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(my_rows + (32 * x + l32) * ROW_BYTES + ((16 * (h ^ (l32 & 15))) ^ (32 * kk))));
-                asm volatile("" : "+a"(q[x][kk]));
             }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+a"(q[x][kk]));
     };
 
     f32x16 o[2][4], s[2];
@@ -200,20 +214,24 @@ void chunk_wide_kernel(ChunkParams p)
         const v4i16 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(from + 8 * ROW_BYTES));
         v[m][nt] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    // weights of block x from its scores of tile t
+    // Weights of block x from its scores of tile t: two at a time (pair), which join the sum and are packed a step later (fold), so that nothing
+    // waits for an exponential.
+    float we[16];
+    auto pair = [&](const int x, const int j, int t, auto masked) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 2 * j; i < 2 * j + 2; ++i) {
+            we[i] = fast_exp2(fmaf(s[x][i], c2, -m_used[x]));
+            if (decltype(masked)::value && key_of_score(i) > now.pos[x] - t * KT - 4 * h) we[i] = 0.f;
+        }
+    };
+    auto fold = [&](const int j, float &sum, u32x4 *pk) __attribute__((always_inline)) {
+        sum += we[2 * j] + we[2 * j + 1];
+        pk[j / 4][j % 4] = pack_bf16(we[2 * j], we[2 * j + 1]);
+    };
     auto weights = [&](const int x, int t, auto masked, u32x4 *pk) __attribute__((always_inline)) {
-        const int seen = now.pos[x] - t * KT - 4 * h;
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            float w0 = fast_exp2(fmaf(s[x][i], c2, -m_used[x])), w1 = fast_exp2(fmaf(s[x][i + 1], c2, -m_used[x]));
-            if constexpr (decltype(masked)::value) {
-                if (key_of_score(i) > seen) w0 = 0.f;
-                if (key_of_score(i + 1) > seen) w1 = 0.f;
-            }
-            sum += w0 + w1;
-            pk[i / 8][i / 2 % 4] = pack_bf16(w0, w1);
-        }
+        for (int j = 0; j < 8; ++j) { pair(x, j, t, masked); fold(j, sum, pk); }
         return sum;
     };
     // The maximum is raised only where the weights outgrow it (their sum, which is formed anyway, tells), row by row.
@@ -286,11 +304,10 @@ void chunk_wide_kernel(ChunkParams p)
         request();
     };
     // One tile: k, v hold K(t) and V(t - 1), afterwards K(t + 1) and V(t); each operand is replaced as soon as block B has used it.
-    // partial: some row does not see all of its keys; cleaned: V(t + 1) is cleaned before the next step.
-    auto step = [&](int t, auto partial, auto cleaned) __attribute__((always_inline)) {
-        constexpr bool CLEAN = decltype(cleaned)::value;
-        constexpr int BESIDE = decltype(partial)::value ? 6 : 4;     // vector instructions per matrix instruction
+    // partial: some row may not see all of its keys.
+    auto step = [&](int t, auto partial) __attribute__((always_inline)) {
         u32x4 pk[2];
+        float sum = 0.f;
         zero_scores(1);
         // (products that need nothing of what the barrier stands for run while it is waited at)
 #pragma unroll
@@ -298,43 +315,45 @@ void chunk_wide_kernel(ChunkParams p)
         __builtin_amdgcn_sched_barrier(0);
         arrival();
         __builtin_amdgcn_sched_barrier(0);
-        float sum = weights(0, t, partial, pk);
+        // A matrix instruction, the operands that take the place of an earlier one's, two weights: in this order, which the compiler would not find
+        // by itself.
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (i >= 2) pv(1, i / 4, i % 4);
-            read_v(i / 4, i % 4, t);
-            if (i >= 2) qk(1, i);
-            read_k(i, t + 1);
-        }
-#pragma unroll
-        for (int i = 0; i < 6; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x402, BESIDE + 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x402, BESIDE + 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        for (int n = 4; n < 16; ++n) {
+            const int i = n / 2;
+            if (n % 2 == 0) pv(1, i / 4, i % 4);
+            else qk(1, i);
+            if (n < 12) {
+                const int r = (n - 4) / 2;          // 0 .. 3
+                if (n % 2 == 0) read_v(r / 4, r % 4, t);
+                else read_k(r, t + 1);
+            } else {
+                const int r = n - 8;                // 4 .. 7
+                read_v(r / 4, r % 4, t);
+                if (n > 12) read_k(r - 1, t + 1);
+                if (n == 15) read_k(7, t + 1);
+            }
+            if (n < 12) pair(0, n - 4, t, partial);
+            if (n > 4 && n < 13) fold(n - 5, sum, pk);
+            __builtin_amdgcn_sched_barrier(0);
         }
         settle(0, t, partial, sum, pk);
         advance();
-        sum = weights(1, t, partial, pk);
+        sum = 0.f;
         zero_scores(0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            pv(0, i / 4, i % 4);
-            qk(0, i);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x402, BESIDE, 0);
+        for (int n = 0; n < 16; ++n) {
+            const int i = n / 2;
+            if (n % 2 == 0) pv(0, i / 4, i % 4);
+            else qk(0, i);
+            if (n > 1 && n < 10) pair(1, n - 2, t, partial);
+            if (n > 2 && n < 11) fold(n - 3, sum, pk);
+            __builtin_amdgcn_sched_barrier(0);
         }
         settle(1, t, partial, sum, pk);
-        if (CLEAN) clean(t + 1);
     };
     if (tid < 2) s_odd[tid] = 0;
     bool more = plan_item(&ahead), done = false, direct = false, poisoned = false, mine[2] = {false, false};    // an item is done, and what its epilogue needs
-    int done_b = 0, done_g = 0, key_from = 0, key_end = 0, done_pos[2] = {0, 0};
+    int done_b = 0, done_g = 0, done_s0 = 0, done_row0 = 0, done_M = 0, key_from = 0, key_end = 0, done_pos[2] = {0, 0};
     size_t at[2] = {0, 0};      // row of out and lse, or of the partial results
     // ---- epilogue: a lane holds columns 32 nt + 8 a + 4 h .. + 3 of its row in each block
     auto epilogue = [&]() __attribute__((always_inline)) {
@@ -363,9 +382,10 @@ void chunk_wide_kernel(ChunkParams p)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int r = 4 * i + lj;
-                    const size_t row = __shfl(at[x], r);
+                    const int row = done_row0 + 32 * x + r, token = by_group(p, row);
                     const u32x4 y = *reinterpret_cast<const u32x4 *>(my_rows + (32 * x + r) * ROW_BYTES + 16 * (lc ^ (r & 15)));
-                    if (__shfl((int)mine[x], r)) *reinterpret_cast<u32x4 *>(static_cast<char *>(p.out) + row * ROW_BYTES + 16 * lc) = y;
+                    if (row < done_M)
+                        *reinterpret_cast<u32x4 *>(static_cast<char *>(p.out) + ((size_t)(done_s0 + token) * p.H_q + (done_g * p.G + row - token * p.G)) * ROW_BYTES + 16 * lc) = y;
                 }
                 if (p.lse && h == 0 && mine[x]) p.lse[at[x]] = (m_used[x] + __builtin_amdgcn_logf(l_row)) * LN2_F;
             } else if (mine[x]) {
@@ -381,9 +401,9 @@ void chunk_wide_kernel(ChunkParams p)
                 // what is no number joins what was written, lane l32 + 32 h takes columns 64 h .. 64 h + 63
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 for (int key = key_from; key <= min(done_pos[x], key_end); ++key) {
-                    const int page = p.block_table[(size_t)done_b * p.max_pages + key / p.page_size];
+                    const int page = p.block_table[(size_t)done_b * p.max_pages + key / page_size];
                     if ((unsigned)page >= (unsigned)p.n_pages) continue;
-                    const uint16_t *v = static_cast<const uint16_t *>(p.v_pool) + (((size_t)page * p.H_kv + done_g) * p.page_size + key % p.page_size) * D;
+                    const uint16_t *v = static_cast<const uint16_t *>(p.v_pool) + (((size_t)page * H_kv + done_g) * page_size + key % page_size) * D;
                     for (int c = 64 * h; c < 64 * h + 64; ++c) {
                         const float y = bf16_bits_to_float(v[c]);
                         if (fabsf(y) < INFINITY) continue;
@@ -402,99 +422,100 @@ void chunk_wide_kernel(ChunkParams p)
     if (more) {
         now = ahead;
         fetch_q(now);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (tid == 0) s_next = (int)gridDim.x + atomicAdd(p.counter, 1);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     }
-    bool careful = false, again = false;        // this item is done again; there is one behind it
     for (int pass = 0;; ++pass) {
-        const bool here = more;
+        const bool here = uniform(more) != 0;
         if (here) {
             begin_item();
             read_q();           // (arrived during the item before)
         }
         if (done) epilogue();
         if (!here) break;
-        if (!careful) more = plan_item(&ahead);         // (while the first tiles are on their way)
+        // the next item and its Q, while the first tiles are on their way
+        next = uniform(s_next);
+        more = plan_item(&ahead);
+        if (more) fetch_q(ahead);
+        behind_q = uniform(more ? 2 : 0);
+        int careful = 0;            // (the item is done a second time)
+        for (;; ++pass) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-#pragma unroll
-            for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[x][nt][i] = 0.f;
-            const u32x4 zero = {0, 0, 0, 0};
-            w[x][0] = w[x][1] = __builtin_bit_cast(bf16x8, zero);
-            m_used[x] = M_INIT;
-            l_part[x] = 0.f;
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        int t = now.t_begin;
-        if (careful) clean(t);
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (tid == 0) s_odd[(pass + 1) & 1] = 0;                // (whoever read it is past this barrier)
-        // Q of the next item (of this one, should it be done again: it is in LDS once more then)
-        const bool prefetch = more && !careful;
-        if (prefetch) fetch_q(ahead);
-        behind_q = prefetch ? 2 : 0;
-        if (t < now.t_seen) {
-            const u32x4 zero = {0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = __builtin_bit_cast(bf16x8, zero);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) read_k(i, t);
-            zero_scores(0);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) qk(0, i);
-            if (!careful) {
-                for (; t < now.t_plain; ++t) step(t, std::false_type(), std::false_type());
-                for (; t < now.t_seen; ++t) step(t, std::true_type(), std::false_type());
-            } else {
-                for (; t < now.t_seen; ++t) step(t, std::true_type(), std::true_type());
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pv(1, i / 4, i % 4);
-        }
-        for (; t < now.t_end; ++t) {                            // (this wavefront only helps to load)
-            arrival();
-            advance();
-            if (careful) clean(t + 1);
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (nothing is on its way into LDS any more)
-        if (!careful) {
-            float sum = 0.f;
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < 2; ++x) {
 #pragma unroll
                 for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sum = fmaf(o[x][nt][i], 0.f, sum);         // (0 times it is 0, or no number)
-            if (__any(sum != 0.f) && lane == 0) s_odd[pass & 1] = 1;
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        const bool odd = s_odd[pass & 1] != 0;
-        if (!careful && uniform(odd) && now.t_begin < now.t_end) {
-            // once more; the next item's Q, which has taken this one's place in LDS, is loaded again too, then
-            careful = true;
-            done = false;
-            again = more;
-            more = true;
-            fetch_q(now);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            continue;
-        }
-        if (careful) {
-            more = again;
-            if (more) fetch_q(ahead);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    for (int i = 0; i < 16; ++i) o[x][nt][i] = 0.f;
+                const u32x4 zero = {0, 0, 0, 0};
+                w[x][0] = w[x][1] = __builtin_bit_cast(bf16x8, zero);
+                m_used[x] = M_INIT;
+                l_part[x] = 0.f;
+            }
+            if (behind_q) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(Q_LOADS) : "memory");       // (the first tiles)
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            int t = now.t_begin;
+            if (careful) clean(t);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (tid == 0) s_odd[(pass + 1) & 1] = 0;            // (whoever read it is past this barrier)
+            if (t < now.t_seen) {
+                const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = __builtin_bit_cast(bf16x8, zero);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) read_k(i, t);
+                zero_scores(0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) qk(0, i);
+                asm volatile(".p2align 6");             // (the loop starts on an instruction-cache line)
+                if (!careful)
+                    for (; t < now.t_plain; ++t) step(t, std::false_type());
+                for (; t < now.t_seen; ++t) {
+                    step(t, std::true_type());
+                    if (careful) clean(t + 1);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) pv(1, i / 4, i % 4);
+            }
+            int taken = 0;
+            if (!careful)
+                if (tid == 0) taken = atomicAdd(p.counter, 1);
+            for (; t < now.t_end; ++t) {                        // (this wavefront only helps to load)
+                arrival();
+                advance();
+                if (careful) clean(t + 1);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // (nothing is on its way into LDS any more)
+            if (!careful) {
+                if (tid == 0) s_next = (int)gridDim.x + taken;
+                float sum = 0.f;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum = fmaf(o[x][nt][i], 0.f, sum);         // (0 times it is 0, or no number)
+                if (__any(sum != 0.f) && lane == 0) s_odd[pass & 1] = 1;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (careful || !uniform(s_odd[pass & 1])) break;
+            careful = 1;
+            behind_q = 0;
+            begin_item();
         }
 
         done = true;
         direct = now.n_seg == 1;
-        poisoned = careful;
-        careful = false;
+        poisoned = careful != 0;
         done_b = now.b;
         done_g = now.g;
+        done_s0 = now.s0;
+        done_row0 = now.row0;
+        done_M = now.M;
         key_from = max(now.diagonal, now.t_begin) * KT;
         key_end = now.t_end * KT - 1;
 #pragma unroll
@@ -503,7 +524,7 @@ void chunk_wide_kernel(ChunkParams p)
             done_pos[x] = now.pos[x];
             const int token = by_group(p, now.row[x]);
             at[x] = direct ? (size_t)(now.s0 + token) * p.H_q + (now.g * p.G + now.row[x] - token * p.G)
-                           : ((size_t)(now.part + 2 * wave + x) * p.H_kv + now.g) * 32 + l32;
+                           : ((size_t)(now.part + 2 * wave + x) * H_kv + now.g) * 32 + l32;
         }
         if (more) now = ahead;
     }
