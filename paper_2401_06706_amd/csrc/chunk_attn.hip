@@ -241,44 +241,107 @@ void chunk_attn_kernel(ChunkParams p)
     }
 }
 
-// The segments of the rows whose keys are cut.  Eight lanes a row, four columns each; grid (KV heads x tiles of rows, blocks of 32 of their rows).
+// A row's segments, one partial result after the other with a running maximum: columns c, c + 32 .. of a row.
+template <int DP, int COLS>
+struct Merged {
+    float m = M_INIT, l = 0.f;
+    float4 acc[COLS];
+    __device__ __forceinline__ void add(float m2, float l2, const float4 *x)
+    {
+        const float m_new = fmaxf(m, m2), old = fast_exp2(m - m_new), f = l2 == 0.f ? 0.f : fast_exp2(m2 - m_new);     // (no weight: a segment that the row sees nothing of)
+        m = m_new;
+        l = l * old + f * l2;
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) {
+            acc[k].x = acc[k].x * old + f * x[k].x; acc[k].y = acc[k].y * old + f * x[k].y;
+            acc[k].z = acc[k].z * old + f * x[k].z; acc[k].w = acc[k].w * old + f * x[k].w;
+        }
+    }
+};
+
+// The segments of the rows whose keys are cut.  grid (KV heads x tiles of rows, 4 or 8).  Few segments: eight lanes a row, four columns of every
+// 32 each.  Many, as a lone long sequence has: eight groups of 32 lanes take every eighth segment of a row, and meet in LDS
+// (one sequence of 16000 keys, 128 segments of 4 rows: 15.3 us in the first way).
 template <int DP, bool F32>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p)
 {
+    constexpr int GROUPS = 8, WIDE = (DP + 127) / 128;
+    __shared__ float s_ml[GROUPS][2], s_acc[GROUPS][WIDE * 128];
     const int tid = threadIdx.x, lane = tid & 63, g = blockIdx.x % p.H_kv;
     Item it;
     if (!find_item<MERGE>(p, blockIdx.x / p.H_kv, lane, &it)) return;
-    const int M = it.s.n * p.G, row = it.rt * it.rows + 32 * blockIdx.y + tid / 8;
-    if (32 * (int)blockIdx.y >= it.rows || row >= M) return;
-    const size_t step = (size_t)(it.rows / 32) * p.H_kv * 32, first = ((size_t)(it.part + blockIdx.y) * p.H_kv + g) * 32 + tid / 8;
-    float m = M_INIT;
-    for (int s = 0; s < it.n_seg; ++s) m = fmaxf(m, p.part_ml[2 * (first + s * step)]);
-    float4 acc[DP / 32];
+    const int M = it.s.n * p.G;
+    const size_t step = (size_t)(it.rows / 32) * p.H_kv * 32;
+    auto write = [&](size_t at, int c, const float4 &x, float f) {
+        if (F32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at * p.d + c) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+        else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at * p.d + c) = make_uint2(pack_bf16(x.x * f, x.y * f), pack_bf16(x.z * f, x.w * f));
+    };
+    auto row_of_out = [&](int row) {
+        const int token = by_group(p, row);
+        return (size_t)(it.s.s0 + token) * p.H_q + (g * p.G + row - token * p.G);
+    };
+    const bool by_segments = it.n_seg >= 2 * GROUPS;        // then the grid's y are rows of a block, otherwise blocks
+    for (int block = by_segments ? 0 : blockIdx.y; block < it.rows / 32; block += by_segments ? 1 : gridDim.y) {
+        const int row0 = it.rt * it.rows + 32 * block;
+        const size_t first = ((size_t)(it.part + block) * p.H_kv + g) * 32;
+        if (!by_segments) {
+            constexpr int COLS = DP / 32;
+            const int row = row0 + tid / 8;
+            if (row >= M) return;
+            Merged<DP, COLS> a;
 #pragma unroll
-    for (int k = 0; k < DP / 32; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-    for (int s = 0; s < it.n_seg; ++s) {
-        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * (first + s * step));
-        if (ml.y == 0.f) continue;              // a segment that the row sees nothing of
-        const float f = fast_exp2(ml.x - m);
-        l += f * ml.y;
+            for (int k = 0; k < COLS; ++k) a.acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+            for (int s = 0; s < it.n_seg; ++s) {
+                const size_t at = first + tid / 8 + s * step;
+                const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+                float4 x[COLS];
 #pragma unroll
-        for (int k = 0; k < DP / 32; ++k) {
-            const float4 x = *reinterpret_cast<const float4 *>(p.part_o + (first + s * step) * DP + 32 * k + 4 * (tid & 7));
-            acc[k].x += f * x.x; acc[k].y += f * x.y; acc[k].z += f * x.z; acc[k].w += f * x.w;
+                for (int k = 0; k < COLS; ++k) x[k] = *reinterpret_cast<const float4 *>(p.part_o + at * DP + 32 * k + 4 * (tid & 7));
+                a.add(ml.x, ml.y, x);
+            }
+            const size_t at = row_of_out(row);
+#pragma unroll
+            for (int k = 0; k < COLS; ++k)
+                if (32 * k + 4 * (tid & 7) < p.d) write(at, 32 * k + 4 * (tid & 7), a.acc[k], 1.0f / a.l);
+            if (p.lse && (tid & 7) == 0) p.lse[at] = (a.m + __builtin_amdgcn_logf(a.l)) * LN2_F;
+            continue;
+        }
+        const int group = tid >> 5, l32 = tid & 31;
+        for (int r = blockIdx.y; r < 32 && row0 + r < M; r += gridDim.y) {
+            Merged<DP, WIDE> a;
+#pragma unroll
+            for (int k = 0; k < WIDE; ++k) a.acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int s = group; s < it.n_seg; s += GROUPS) {
+                const size_t at = first + r + s * step;
+                const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+                float4 x[WIDE];
+#pragma unroll
+                for (int k = 0; k < WIDE; ++k) x[k] = 128 * k + 4 * l32 < DP ? *reinterpret_cast<const float4 *>(p.part_o + at * DP + 128 * k + 4 * l32) : make_float4(0.f, 0.f, 0.f, 0.f);
+                a.add(ml.x, ml.y, x);
+            }
+            __syncthreads();                // (the row before has been read)
+            if (l32 == 0) { s_ml[group][0] = a.m; s_ml[group][1] = a.l; }
+#pragma unroll
+            for (int k = 0; k < WIDE; ++k) *reinterpret_cast<float4 *>(&s_acc[group][128 * k + 4 * l32]) = a.acc[k];
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int j = 1; j < GROUPS; ++j) {
+                    float4 x[WIDE];
+#pragma unroll
+                    for (int k = 0; k < WIDE; ++k) x[k] = *reinterpret_cast<const float4 *>(&s_acc[j][128 * k + 4 * l32]);
+                    a.add(s_ml[j][0], s_ml[j][1], x);
+                }
+                const size_t at = row_of_out(row0 + r);
+#pragma unroll
+                for (int k = 0; k < WIDE; ++k)
+                    if (128 * k + 4 * l32 < p.d) write(at, 128 * k + 4 * l32, a.acc[k], 1.0f / a.l);
+                if (p.lse && l32 == 0) p.lse[at] = (a.m + __builtin_amdgcn_logf(a.l)) * LN2_F;
+            }
         }
     }
-    const float f = 1.0f / l;
-    const int token = it.s.s0 + row / p.G, head = g * p.G + row % p.G;
-    const size_t at = (size_t)token * p.H_q + head;
-#pragma unroll
-    for (int k = 0; k < DP / 32; ++k) {
-        const int c = 32 * k + 4 * (tid & 7);
-        if (c >= p.d) continue;
-        if (F32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at * p.d + c) = make_float4(acc[k].x * f, acc[k].y * f, acc[k].z * f, acc[k].w * f);
-        else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at * p.d + c) = make_uint2(pack_bf16(acc[k].x * f, acc[k].y * f), pack_bf16(acc[k].z * f, acc[k].w * f));
-    }
-    if (p.lse && (tid & 7) == 0) p.lse[at] = (m + __builtin_amdgcn_logf(l)) * LN2_F;
 }
 
 // ---- rows of new tokens into their pages: 16 bytes of K and of V a thread
@@ -306,6 +369,9 @@ __global__ __launch_bounds__(256) void kv_store_paged_kernel(StoreParams p)
     *reinterpret_cast<u32x4 *>(p.v_pool + at) = v;
 }
 
+#ifndef TARGET_FEW
+#define TARGET_FEW 1024
+#endif
 int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
 
 template <int DP, bool F32>
@@ -345,22 +411,26 @@ bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
     // (it would find nothing to do in a batch that decodes, for 4 us)
     const bool many = d.dtype == MCSD_DTYPE_BF16 && d.d == 128 && T * G > (long)MANY * d.B;
     plan->many = many ? MANY : 0x7fffffff;
-    // Segments of about as many workgroups as the chip takes at once (two a compute unit, one of the wide kernel), of 8 tiles at least.  A sequence that is cut
-    // has kt / len of them, rounded, two at least: 4/3 of kt / len at most.
+    // Segments of 8 tiles at least; of few rows twice as many as the chip takes at once (two workgroups a compute unit), which evens the lengths out, of
+    // many as many (one).  A sequence that is cut has kt / len of them, rounded up, 2 kt / len at most, or to nearest, 4/3 kt / len at most.
     plan->min_seg = 8;
-    plan->target = d.H_kv < 512 ? 512 / d.H_kv : 1;
+    plan->target = d.H_kv < TARGET_FEW ? TARGET_FEW / d.H_kv : 1;
     plan->target_many = d.H_kv < 256 ? 256 / d.H_kv : 1;
-    const long n_seg = (kt + plan->min_seg / 2) / plan->min_seg, tiles = most_tiles(T, d.B, G, ROWS_FEW), tiles_many = many ? most_tiles(T, d.B, G, ROWS_MANY) : 0;
-    auto parts_of = [&](long target, long row_tiles) {
-        const long parts = n_seg < 2 ? 0 : (4 * target + 2) / 3 + 2;
+    const long n_seg = (kt + plan->min_seg - 1) / plan->min_seg;
+    // (a sequence of few rows is one row tile where those of many are not here)
+    const long tiles = many ? (T < d.B ? T : d.B) : most_tiles(T, d.B, G, ROWS_FEW), tiles_many = many ? most_tiles(T, d.B, G, ROWS_MANY) : 0;
+    auto parts_of = [&](long most, long row_tiles) {
+        const long parts = n_seg < 2 ? 0 : most + 2;
         return parts < row_tiles * n_seg ? parts : row_tiles * n_seg;
     };
-    const long parts = parts_of(plan->target, tiles), parts_many = parts_of(plan->target_many, tiles_many);
-    auto items_of = [&](long row_tiles, long cut) { return row_tiles + cut < row_tiles * n_seg || n_seg < 1 ? row_tiles + cut : row_tiles * n_seg; };
-    const long items = items_of(tiles, parts), items_many = items_of(tiles_many, parts_many);
+    const long parts = parts_of(2L * plan->target, tiles), parts_many = parts_of((4L * plan->target_many + 2) / 3, tiles_many);
+    // kt / len and one more of every row tile
+    auto items_of = [&](long target, long row_tiles) { return n_seg < 2 ? row_tiles : target + row_tiles < row_tiles * n_seg ? target + row_tiles : row_tiles * n_seg; };
+    const long items = items_of(plan->target, tiles), items_many = tiles_many ? items_of(plan->target_many, tiles_many) : 0;
+    const long cut = parts / 2 < tiles ? parts / 2 : tiles, cut_many = parts_many / 2 < tiles_many ? parts_many / 2 : tiles_many;
     plan->max_items = (int)items;
     plan->max_items_many = (int)items_many;
-    plan->max_cut = (int)((parts + parts_many) / 2);
+    plan->max_cut = (int)(cut + cut_many);
     plan->max_parts = (int)(parts * (ROWS_FEW / 32) + parts_many * (ROWS_MANY / 32));
     plan->ws_bytes = ((size_t)plan->max_parts * d.H_kv * 32 * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256 + (many ? 256 : 0);
     return items * d.H_kv < 1L << 24 && items_many * d.H_kv < 1L << 24;     // (a launch has fewer than 2^32 threads)

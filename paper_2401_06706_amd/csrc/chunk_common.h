@@ -11,6 +11,22 @@ typedef const int32_t __attribute__((address_space(4))) *const_i32_ptr;      // 
 
 constexpr float LN2_F = 0.69314718055994530942f;
 
+// x / d for 0 <= x < 2^31: with 2^(b-1) < d <= 2^b, m = floor(2^(31+b) / d) + 1 exceeds 2^(31+b) / d by at most 1, so that
+// x m / 2^(31+b) is too large by less than 1 / d and its whole part right.
+struct FastDiv {
+    uint32_t magic;
+    int shift;            // -1: d = 1
+    FastDiv() = default;
+    explicit FastDiv(int d)
+    {
+        int bits = 0;
+        while ((1LL << bits) < d) ++bits;
+        shift = bits - 1;
+        magic = d > 1 ? (uint32_t)((1ULL << (31 + bits)) / (unsigned)d + 1) : 0;
+    }
+    __device__ __forceinline__ int of(int x) const { return shift < 0 ? x : (int)(__umulhi((uint32_t)x, magic) >> shift); }
+};
+
 struct ChunkParams {
     const void *q, *k_pool, *v_pool;
     const int32_t *chunk_start, *prefix_len, *block_table;
@@ -18,8 +34,7 @@ struct ChunkParams {
     float *lse, *part_o, *part_ml;
     int *counter;         // of the wide kernel's items
     int B, T, H_q, H_kv, G, d, L_stride, page_size, n_pages, max_pages;
-    uint32_t group_magic; // ceil-like reciprocal of G, see by_group
-    int group_shift;
+    FastDiv group;        // by G
     int many;             // rows beyond which a sequence belongs to the wide kernel
     int min_seg, max_parts;
     float target, target_many;      // workgroups per KV head aimed at where keys are cut, of either kernel
@@ -34,19 +49,11 @@ inline ChunkParams chunk_params(const mcsd_chunk_desc &d, const mcsd_paged_kv &k
     p.page_size = kv.page_size; p.n_pages = kv.n_pages; p.max_pages = kv.max_pages_per_seq; p.block_table = kv.block_table;
     p.q_row = (size_t)d.q_stride * (d.dtype == MCSD_DTYPE_FP32 ? 4 : 2);
     p.scale_log2 = d.scale * LOG2E_F;
-    int bits = 0;
-    while ((1LL << bits) < p.G) ++bits;
-    p.group_shift = bits - 1;
-    p.group_magic = p.G > 1 ? (uint32_t)((1ULL << (31 + bits)) / (unsigned)p.G + 1) : 0;
+    p.group = FastDiv(p.G);
     return p;
 }
 
-// row / G for 0 <= row < 2^31: with 2^(b-1) < G <= 2^b, m = floor(2^(31+b) / G) + 1 exceeds the quotient by less than one part in 2^(31+b) / G, so that
-// row m / 2^(31+b) is too large by less than 1 / G.
-__device__ __forceinline__ int by_group(const ChunkParams &p, int row)
-{
-    return p.G == 1 ? row : (int)(__umulhi((uint32_t)row, p.group_magic) >> p.group_shift);
-}
+__device__ __forceinline__ int by_group(const ChunkParams &p, int row) { return p.group.of(row); }
 
 // New tokens s0 .. s0 + n - 1 of a sequence stand at positions L .. L + n - 1; `keys` positions are there (below the capacity).
 // Whatever the caller's arrays hold, s0 + n <= T and keys <= L_stride.
@@ -87,7 +94,8 @@ __device__ __forceinline__ int wave_running_sum(int v)
 // ---- the work of a launch
 // Rows r = token * G + head in group of a (sequence, KV head) go in tiles, of ROWS_MANY for sequences of more than p.many rows and
 // of ROWS_FEW for others (one kernel each), the keys of a tile in equal segments.  A segment is so long that all of a kernel's
-// make about `target` workgroups per KV head, at least min_seg key tiles; a sequence is cut into kt / segment of them, rounded, one for most.
+// make about `target` workgroups per KV head, at least min_seg key tiles; a sequence is cut into kt / segment of them, rounded up (few rows: a
+// partial result is small) or to nearest.
 // Every workgroup of both kernels and of the merge works out the same list, a sequence a lane.  Partial results are numbered in
 // blocks of 32 rows, row tile by row tile, segment by segment.
 constexpr int ROWS_FEW = 128, ROWS_MANY = 256, MANY = 64;
@@ -133,7 +141,7 @@ struct ItemList {
         const int kt = (s.keys + KT - 1) / KT, my_len = many ? len_many : len;
         rt = row_tiles(p, s);
         blocks = (many ? ROWS_MANY : ROWS_FEW) / 32;
-        n_seg = p.max_parts ? max(1, (kt + my_len / 2) / my_len) : 1;
+        n_seg = p.max_parts ? max(1, (kt + (many ? my_len / 2 : my_len - 1)) / my_len) : 1;
         const int my_parts = n_seg > 1 ? rt * n_seg * blocks : 0;
         const int parts_to = before + wave_running_sum(my_parts);
         if (parts_to > p.max_parts) n_seg = 1;          // (cannot be, but by arrays that contradict themselves)

@@ -6,7 +6,8 @@ namespace mcsd {
 namespace {
 
 struct EvictParams {
-    int B, H_kv, L_stride, n_layers, n_first, n_recent, page_size, n_pages, max_pages, row_bytes, in_place;
+    int B, H_kv, L_stride, n_layers, n_first, n_recent, page_size, n_pages, max_pages, row_bytes, row_lanes;
+    FastDiv page;                   // by the page size
     size_t pool_layer;              // bytes of one layer's pool
     char *k_pool, *v_pool;
     float *sums;
@@ -62,6 +63,7 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
                 if (chunks > 1) load(c);
 #pragma unroll
                 for (int i = 0; i < SEL_PER; ++i) {
+                    if (c * SEL_CHUNK + i * SEL_NT >= n) break;
                     const int at = c * SEL_CHUNK + i * SEL_NT + tid;
                     const uint32_t key = order_key(val[i]);
                     const bool on = at >= f && at < to && (shift == 24 || (key >> (shift + 8)) == prefix);
@@ -160,44 +162,62 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
     }
 }
 
-// Rows of K or V to their new places: a workgroup takes 128 bytes of the rows of a (layer, sequence, KV head), 256 rows at a time.
-// In place it takes all of them in ascending order, everything of a step read before any of it is written: a row moves to a lower
-// position or stays, so that a step writes only what itself and the steps before it have read.  grid (heads, 2 x slices of 128 bytes, steps or 1)
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p)
+// Rows of K or V to their new places, 8 pieces of 16 bytes a thread: kept position, page entries, row, three trips to memory behind each
+// other, so that many rows are under way at a time.
+// In place a workgroup of 1024 takes 128 bytes of all rows of a (layer, sequence, KV head), 1024 rows a step in ascending order, everything of a step read
+// before any of it is written: a row moves to a lower position or stays, so that a step writes only what itself and the
+// steps before it have read.  To pages of their own, a workgroup of 256 takes a step of whole rows.  grid (heads, 2 x slices, steps or 1)
+template <bool IN_PLACE>
+__global__ __launch_bounds__(IN_PLACE ? 1024 : 256) void evict_move_kernel(EvictParams p)
 {
-    constexpr int U = 8, ROWS = 32 * U;
+    constexpr int U = 8;
     const int tid = threadIdx.x, head = blockIdx.x, g = head % p.H_kv, b = head / p.H_kv % p.B, layer = head / p.H_kv / p.B;
     const int m = min(max(0, min(p.prefix_len[b], p.L_stride)), max(0, p.keep_len[b]));
     const bool value = blockIdx.y & 1;
-    const int col = (blockIdx.y >> 1) * 128 + 16 * (tid & 7);
+    // (to other pages: as many lanes a row as it has pieces, rounded up to a power of two)
+    const int lanes = IN_PLACE ? 8 : p.row_lanes, rows = IN_PLACE ? 128 : 256 / lanes;
+    const int col = IN_PLACE ? (blockIdx.y >> 1) * 128 + 16 * (tid & 7) : 16 * (tid & (lanes - 1)), my_row = IN_PLACE ? tid >> 3 : tid / lanes;
     char *pool = (value ? p.v_pool : p.k_pool) + (size_t)layer * p.pool_layer;
     const int32_t *kept = p.kept + (size_t)head * p.L_stride;
     const int32_t *from = p.block_table + (size_t)b * p.max_pages;
-    const int32_t *to = p.in_place ? from : p.out_table + (size_t)b * p.max_pages;
+    const int32_t *to = IN_PLACE ? from : p.out_table + (size_t)b * p.max_pages;
     bool bad = false;
-    for (int base = blockIdx.z * ROWS; base < m; base += gridDim.z * ROWS) {
+    for (int base = blockIdx.z * rows * U; base < m; base += gridDim.z * rows * U) {
         u32x4 x[U];
-        size_t dst[U];
+        int i[U], src[U], dst[U];
         uint32_t on = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = base + 32 * u + (tid >> 3);
-            if (j >= m || col >= p.row_bytes) continue;
-            const int i = kept[j];
-            if (p.in_place && i == j) continue;
-            const int src_page = from[i / p.page_size], dst_page = to[j / p.page_size];
-            if ((unsigned)src_page >= (unsigned)p.n_pages || (unsigned)dst_page >= (unsigned)p.n_pages) { bad = true; continue; }
-            x[u] = *reinterpret_cast<const u32x4 *>(pool + (((size_t)src_page * p.H_kv + g) * p.page_size + i % p.page_size) * p.row_bytes + col);
-            dst[u] = (((size_t)dst_page * p.H_kv + g) * p.page_size + j % p.page_size) * p.row_bytes + col;
+            const int j = base + rows * u + my_row;
+            i[u] = j < m && col < p.row_bytes ? kept[j] : -1;
+            if (IN_PLACE && i[u] == j) i[u] = -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = base + rows * u + my_row;
+            src[u] = dst[u] = 0;
+            if (i[u] >= 0) {
+                src[u] = from[p.page.of(i[u])];
+                dst[u] = to[p.page.of(j)];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i[u] < 0) continue;
+            if ((unsigned)src[u] >= (unsigned)p.n_pages || (unsigned)dst[u] >= (unsigned)p.n_pages) { bad = true; continue; }
+            x[u] = *reinterpret_cast<const u32x4 *>(pool + (((size_t)src[u] * p.H_kv + g) * p.page_size + (i[u] - p.page.of(i[u]) * p.page_size)) * p.row_bytes + col);
             on |= 1u << u;
         }
-        if (p.in_place) {
+        if (IN_PLACE) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (the rows have arrived before others write)
             __syncthreads();
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if ((on >> u) & 1u) *reinterpret_cast<u32x4 *>(pool + dst[u]) = x[u];
+        for (int u = 0; u < U; ++u) {
+            const int j = base + rows * u + my_row;
+            if ((on >> u) & 1u)
+                *reinterpret_cast<u32x4 *>(pool + (((size_t)dst[u] * p.H_kv + g) * p.page_size + (j - p.page.of(j) * p.page_size)) * p.row_bytes + col) = x[u];
+        }
     }
     if (bad) atomicOr(&p.flags[b], (uint32_t)MCSD_FLAG_BAD_PAGES);
     // (every workgroup reads the smaller of this and keep_len, which is m before and after)
@@ -211,16 +231,22 @@ int32_t launch_kv_evict(const mcsd_evict_desc &d, const mcsd_evict_bufs &b, cons
     EvictParams p;
     p.B = d.B; p.H_kv = d.H_kv; p.L_stride = d.L_stride; p.n_layers = d.n_layers; p.n_first = d.n_first; p.n_recent = d.n_recent;
     p.page_size = kv.page_size; p.n_pages = kv.n_pages; p.max_pages = kv.max_pages_per_seq;
+    p.page = FastDiv(kv.page_size);
     p.row_bytes = d.d * (d.dtype == MCSD_DTYPE_FP32 ? 4 : 2);
-    p.in_place = b.out_table == nullptr;
+    p.row_lanes = 1;
+    while (p.row_lanes * 16 < p.row_bytes) p.row_lanes *= 2;
     p.pool_layer = (size_t)kv.n_pages * kv.page_size * d.H_kv * p.row_bytes;
     p.k_pool = static_cast<char *>(b.k_pool); p.v_pool = static_cast<char *>(b.v_pool);
     p.sums = b.sums; p.prefix_len = b.prefix_len; p.kept = b.kept; p.keep_len = b.keep_len;
     p.block_table = kv.block_table; p.out_table = b.out_table; p.flags = b.flags;
     const unsigned heads = (unsigned)(d.n_layers * d.B * d.H_kv);
-    const unsigned steps = p.in_place ? 1u : (unsigned)((d.L_stride + 255) / 256);
     launch_kernel(K_EVICT_SELECT, evict_select_kernel, dim3(heads), dim3(SEL_NT), stream, p);
-    launch_kernel(K_EVICT_MOVE, evict_move_kernel, dim3(heads, 2 * ((p.row_bytes + 127) / 128), steps), dim3(256), stream, p);
+    if (!b.out_table) {
+        launch_kernel(K_EVICT_MOVE, evict_move_kernel<true>, dim3(heads, 2 * ((p.row_bytes + 127) / 128)), dim3(1024), stream, p);
+    } else {
+        const int step = 8 * 256 / p.row_lanes;
+        launch_kernel(K_EVICT_MOVE, evict_move_kernel<false>, dim3(heads, 2, (d.L_stride + step - 1) / step), dim3(256), stream, p);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("evict launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     return MCSD_OK;

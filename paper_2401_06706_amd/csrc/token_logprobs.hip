@@ -38,14 +38,17 @@ struct Pieces {
         n = (V - head) / W;
         tail = head + n * W;
     }
-    __device__ __forceinline__ void load(const void *row, int piece, float *z) const
+    __device__ __forceinline__ u32x4 raw(const void *row, int piece) const
     {
-        const char *at = static_cast<const char *>(row) + (size_t)(head + piece * W) * (BF16 ? 2 : 4);
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(at);
+        return *reinterpret_cast<const u32x4 *>(static_cast<const char *>(row) + (size_t)(head + piece * W) * (BF16 ? 2 : 4));
+    }
+    __device__ __forceinline__ void values(const u32x4 &x, float *z) const
+    {
 #pragma unroll
         for (int i = 0; i < W; ++i)
             z[i] = BF16 ? ((i & 1) ? __uint_as_float(x[i >> 1] & 0xffff0000u) : __uint_as_float(x[i >> 1] << 16)) : __uint_as_float(x[i & 3]);
     }
+    __device__ __forceinline__ void load(const void *row, int piece, float *z) const { values(raw(row, piece), z); }
 };
 
 // Sums of a row relative to the largest logit seen: s = sum 2^t, u = sum t 2^t with t = (z - m) c, c = log2(e) / T.
@@ -110,9 +113,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
         sums.add(z, c);
         before += (z > zx || (z == zx && id < x)) ? 1 : 0;
     };
-    for (int piece = tid; piece < pc.n; piece += NT) {
-        float z[W];
-        pc.load(row, piece, z);
+    auto take_piece = [&](const float *z, int piece) {
         float most = z[0];
 #pragma unroll
         for (int i = 1; i < W; ++i) most = fmaxf(most, z[i]);
@@ -124,6 +125,25 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
             sums.add(z[i], c);
             before += (z[i] > zx || (z[i] == zx && i < d)) ? 1 : 0;
         }
+    };
+    // AHEAD pieces are asked for at a time
+    constexpr int AHEAD = 4;
+    int piece = tid;
+    for (; piece + (AHEAD - 1) * NT < pc.n; piece += AHEAD * NT) {
+        u32x4 raw[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) raw[k] = pc.raw(row, piece + k * NT);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            float z[W];
+            pc.values(raw[k], z);
+            take_piece(z, piece + k * NT);
+        }
+    }
+    for (; piece < pc.n; piece += NT) {
+        float z[W];
+        pc.load(row, piece, z);
+        take_piece(z, piece);
     }
     // (elements outside the pieces: fewer than 16)
     if (tid < pc.head) take(logit_at<BF16>(row, tid), tid);

@@ -4,12 +4,14 @@
 namespace mcsd {
 namespace {
 
-struct SumsParams { ChunkParams c; const float *lse; float *sums; int last_rows; };
+struct SumsParams { ChunkParams c; const float *lse; float *sums; int last_rows, blocks; };
 
-// A workgroup owns 128 positions of a (sequence, KV head), 32 a wavefront with their keys in registers, and goes through the rows
+// A workgroup owns 128 positions of a (sequence, KV head) at a time, 32 a wavefront with their keys in registers, and goes through the rows
 // that see them in tiles of 32 (through LDS): S = K Q^T as in attention, weights 2^(s c2 - lse), added up in the
 // lane that holds them.  No other workgroup adds to these positions, so the order of the sum is fixed.  A partial sum of 64 tiles is
-// added to the whole at a time: over n rows of a lane the error stays below (64 + n / 64) 2^-24 of the sum.
+// added to the whole at a time: over n tiles the error stays below (64 + n / 64) 2^-24 of the sum.
+// Few rows: a workgroup goes through `blocks` of 128 positions, the next one's keys asked for ahead, so that lengths, table and rows are
+// waited for once.
 template <int DP, bool F32>
 __global__ __launch_bounds__(256) void weight_sums_kernel(SumsParams sp)
 {
@@ -17,16 +19,15 @@ __global__ __launch_bounds__(256) void weight_sums_kernel(SumsParams sp)
     const ChunkParams &p = sp.c;
     __shared__ __attribute__((aligned(16))) uint32_t s_q[2][KT * S::PK];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
-    const int g = blockIdx.x, b = blockIdx.z, key0 = blockIdx.y * 128;
+    const int g = blockIdx.x, b = blockIdx.z, key0 = blockIdx.y * 128 * sp.blocks;
     const ChunkSeq sq = chunk_sequence(p, b);
     if (sq.n == 0 || key0 >= sq.keys) return;
-    const int M = sq.n * p.G, wkey = key0 + 32 * wave, row_bytes = p.d * S::ES;
+    const int M = sq.n * p.G, row_bytes = p.d * S::ES;
     const int first_token = max(sp.last_rows ? sq.n - min(sp.last_rows, sq.n) : 0, key0 - sq.L);
-    const int tiles = (M - first_token * p.G + KT - 1) / KT, row_first = first_token * p.G;
+    const int row_first = first_token * p.G, tiles = (M - row_first + KT - 1) / KT;
 
-    // ---- this wavefront's keys
-    u32x4 k[S::KK];
-    {
+    // ---- keys of a block
+    auto load_keys = [&](int wkey, u32x4 *k) __attribute__((always_inline)) {
         const int page = wkey < sq.keys ? p.block_table[(size_t)b * p.max_pages + wkey / p.page_size] : -1;
         const bool in = (unsigned)page < (unsigned)p.n_pages;
         const size_t off = in ? (((size_t)page * p.H_kv + g) * p.page_size + wkey % p.page_size) * row_bytes : 0;
@@ -36,104 +37,135 @@ __global__ __launch_bounds__(256) void weight_sums_kernel(SumsParams sp)
             const int at = 32 * kk + 16 * h;
             k[kk] = __builtin_amdgcn_raw_buffer_load_b128(rk, at < row_bytes ? l32 * row_bytes + at : 0x7fff0000, 0, 0);
         }
-    }
-    // ---- tiles of rows: global -> registers -> LDS, one tile ahead
-    u32x4 qr[S::PER_THREAD];
-    float lse_next;
-    auto load_q = [&](int tile) __attribute__((always_inline)) {
+    };
+    // ---- tiles of rows: global -> registers -> LDS, two tiles ahead
+    u32x4 qr[2][S::PER_THREAD];
+    float lse_of[2];
+    auto load_q = [&](int tile, int st) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < S::PER_THREAD; ++j) {
             const int e = tid + 256 * j, r = row_first + tile * KT + e / S::GRANULES, c = e % S::GRANULES;
             const u32x4 zero = {0, 0, 0, 0};
-            qr[j] = zero;
-            if (e < KT * S::GRANULES && r < M && 16 * c < row_bytes)
-                qr[j] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(p.q) + (size_t)(sq.s0 + r / p.G) * p.q_row +
-                                                         (size_t)(g * p.G + r % p.G) * row_bytes + 16 * c);
+            qr[st][j] = zero;
+            if (e < KT * S::GRANULES && r < M && 16 * c < row_bytes) {
+                const int token = by_group(p, r);
+                qr[st][j] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(p.q) + (size_t)(sq.s0 + token) * p.q_row +
+                                                             (size_t)(g * p.G + r - token * p.G) * row_bytes + 16 * c);
+            }
         }
         const int r = row_first + tile * KT + l32;
         // (a row past the last one gives nothing)
-        lse_next = r < M ? sp.lse[(size_t)(sq.s0 + r / p.G) * p.H_q + g * p.G + r % p.G] * LOG2E_F : INFINITY;
+        lse_of[st] = INFINITY;
+        if (r < M) {
+            const int token = by_group(p, r);
+            lse_of[st] = sp.lse[(size_t)(sq.s0 + token) * p.H_q + g * p.G + r - token * p.G] * LOG2E_F;
+        }
     };
-    auto store_q = [&](uint32_t *buf) __attribute__((always_inline)) {
+    auto store_q = [&](int st) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < S::PER_THREAD; ++j) {
             const int e = tid + 256 * j;
             if (KT * S::GRANULES % 256 == 0 || e < KT * S::GRANULES)
-                *reinterpret_cast<u32x4 *>(buf + e / S::GRANULES * S::PK + 4 * (e % S::GRANULES)) = qr[j];
+                *reinterpret_cast<u32x4 *>(s_q[st] + e / S::GRANULES * S::PK + 4 * (e % S::GRANULES)) = qr[st][j];
         }
     };
-    float part[16], total[16];
+    u32x4 k[S::KK], k_next[S::KK];
+    load_keys(key0 + 32 * wave, k);
+    load_q(0, 0);
+    float first_lse = lse_of[0];
+    store_q(0);
+    for (int block = 0; block < sp.blocks && key0 + 128 * block < sq.keys; ++block) {
+        const int wkey = key0 + 128 * block + 32 * wave;
+        if (block + 1 < sp.blocks) load_keys(wkey + 128, k_next);
+        float part[16], total[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) part[i] = total[i] = 0.f;
-    load_q(0);
-    store_q(s_q[0]);
-    float lse = lse_next;
-    __syncthreads();
-    for (int tile = 0; tile < tiles; ++tile) {
-        if (tile + 1 < tiles) load_q(tile + 1);
-        if (wkey < sq.keys) {
-            const uint32_t *qb = s_q[tile & 1] + l32 * S::PK + 4 * h;
-            f32x16 s;
+        for (int i = 0; i < 16; ++i) part[i] = total[i] = 0.f;
+        auto step = [&](int tile, const int st, float lse) __attribute__((always_inline)) {
+            if (wkey < sq.keys) {
+                const uint32_t *qb = s_q[st] + l32 * S::PK + 4 * h;
+                f32x16 s;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+                for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-            for (int kk = 0; kk < S::KK; ++kk) {
-                const u32x4 a = *reinterpret_cast<const u32x4 *>(qb + 8 * kk);
-                if constexpr (F32) {
+                for (int kk = 0; kk < S::KK; ++kk) {
+                    const u32x4 a = *reinterpret_cast<const u32x4 *>(qb + 8 * kk);
+                    if constexpr (F32) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[kk][j]), __uint_as_float(a[j]), s, 0, 0, 0);
+                        for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[kk][j]), __uint_as_float(a[j]), s, 0, 0, 0);
+                    } else {
+                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[kk]), __builtin_bit_cast(bf16x8, a), s, 0, 0, 0);
+                    }
+                }
+                const int row0 = row_first + tile * KT;
+                if (min(sq.L + by_group(p, row0), sq.keys - 1) < wkey + KT - 1) {       // some row does not see some of these keys
+                    const int seen = min(sq.L + by_group(p, min(row0 + l32, M - 1)), sq.keys - 1) - wkey - 4 * h;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (key_of_score(i) <= seen) part[i] += fast_exp2(fmaf(s[i], p.scale_log2, -lse));
                 } else {
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[kk]), __builtin_bit_cast(bf16x8, a), s, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) part[i] += fast_exp2(fmaf(s[i], p.scale_log2, -lse));
+                }
+                if ((tile & 63) == 63) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) { total[i] += part[i]; part[i] = 0.f; }
                 }
             }
-            const int token0 = (row_first + tile * KT) / p.G;
-            if (min(sq.L + token0, sq.keys - 1) < wkey + KT - 1) {      // some row does not see some of these keys
-                const int r = row_first + tile * KT + l32, seen = min(sq.L + min(r, M - 1) / p.G, sq.keys - 1) - wkey - 4 * h;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key_of_score(i) <= seen) part[i] += fast_exp2(fmaf(s[i], p.scale_log2, -lse));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) part[i] += fast_exp2(fmaf(s[i], p.scale_log2, -lse));
-            }
-            if ((tile & 63) == 63) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) { total[i] += part[i]; part[i] = 0.f; }
+        };
+        if (tiles == 1) {
+            if (block == 0) __syncthreads();
+            step(0, 0, first_lse);
+        } else {
+            if (block > 0) { load_q(0, 0); store_q(0); }        // (every wavefront is past the barrier behind the last tile)
+            load_q(1, 1);
+            float lse = lse_of[0];
+            __syncthreads();
+            // tile t in buffer t % 2; t + 1 is stored, and t + 2 asked for, while it is worked on
+            for (int tile = 0; tile < tiles; tile += 2) {
+                float lse1 = lse_of[1];
+                store_q(1);
+                if (tile + 2 < tiles) load_q(tile + 2, 0);
+                step(tile, 0, lse);
+                __syncthreads();
+                if (tile + 1 >= tiles) break;
+                lse = lse_of[0];
+                if (tile + 2 < tiles) store_q(0);
+                if (tile + 3 < tiles) load_q(tile + 3, 1);
+                step(tile + 1, 1, lse1);
+                __syncthreads();
             }
         }
-        if (tile + 1 < tiles) store_q(s_q[(tile + 1) & 1]);
-        lse = lse_next;
-        __syncthreads();
-    }
-    if (wkey >= sq.keys) return;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) total[i] += part[i];
-    // sum over the 32 rows of a tile: every exchange halves what a lane holds, so that lane l32 ends up with score
-    // 8 (l32 & 1) + 4 (l32 >> 1 & 1) + 2 (l32 >> 2 & 1) + (l32 >> 3 & 1) of its half
+        for (int i = 0; i < 16; ++i) total[i] += part[i];
+        // sum over the 32 rows of a tile: every exchange halves what a lane holds, so that lane l32 ends up with score
+        // 8 (l32 & 1) + 4 (l32 >> 1 & 1) + 2 (l32 >> 2 & 1) + (l32 >> 3 & 1) of its half
 #pragma unroll
-    for (int bit = 0; bit < 4; ++bit) {
-        const int n = 8 >> bit;
-        const bool up = (lane >> bit) & 1;
+        for (int bit = 0; bit < 4; ++bit) {
+            const int n = 8 >> bit;
+            const bool up = (lane >> bit) & 1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) {
-                const float keep = up ? total[j + n] : total[j], give = up ? total[j] : total[j + n];
-                total[j] = keep + __shfl_xor(give, 1 << bit);
-            }
-    }
-    total[0] += __shfl_xor(total[0], 16);
-    const int i = 8 * (l32 & 1) + 4 * ((l32 >> 1) & 1) + 2 * ((l32 >> 2) & 1) + ((l32 >> 3) & 1);
-    const int key = wkey + key_of_score(i) + 4 * h;
-    if (l32 < 16 && key < sq.keys) {
-        float *at = sp.sums + ((size_t)b * p.H_kv + g) * p.L_stride + key;
-        *at = (key < sq.L ? *at : 0.f) + total[0];
+            for (int j = 0; j < 8; ++j)
+                if (j < n) {
+                    const float keep = up ? total[j + n] : total[j], give = up ? total[j] : total[j + n];
+                    total[j] = keep + __shfl_xor(give, 1 << bit);
+                }
+        }
+        total[0] += __shfl_xor(total[0], 16);
+        const int i = 8 * (l32 & 1) + 4 * ((l32 >> 1) & 1) + 2 * ((l32 >> 2) & 1) + ((l32 >> 3) & 1);
+        const int key = wkey + key_of_score(i) + 4 * h;
+        if (l32 < 16 && key < sq.keys) {
+            float *at = sp.sums + ((size_t)b * p.H_kv + g) * p.L_stride + key;
+            *at = (key < sq.L ? *at : 0.f) + total[0];
+        }
+#pragma unroll
+        for (int kk = 0; kk < S::KK; ++kk) k[kk] = k_next[kk];
     }
 }
 
 template <bool F32>
 void launch_type(const SumsParams &sp, hipStream_t stream)
 {
-    const dim3 grid(sp.c.H_kv, (sp.c.L_stride + 127) / 128, sp.c.B), block(256);
+    const dim3 grid(sp.c.H_kv, (sp.c.L_stride + 128 * sp.blocks - 1) / (128 * sp.blocks), sp.c.B), block(256);
     const int d = sp.c.d;
     if (d <= 32) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<32, F32>, grid, block, stream, sp);
     else if (d <= 64) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<64, F32>, grid, block, stream, sp);
@@ -150,6 +182,9 @@ int32_t launch_weight_sums(const mcsd_chunk_desc &d, const mcsd_sums_bufs &b, co
     sp.c = chunk_params(d, kv);
     sp.c.q = b.q; sp.c.k_pool = b.k_pool; sp.c.chunk_start = b.chunk_start; sp.c.prefix_len = b.prefix_len;
     sp.lse = b.lse; sp.sums = b.sums; sp.last_rows = b.last_rows;
+    // several blocks a workgroup where sequences bring up to two tiles of rows on average and workgroups are plenty
+    const long rows = (long)d.T * (d.H_q / d.H_kv), groups = (long)d.H_kv * d.B * ((d.L_stride + 127) / 128);
+    sp.blocks = rows <= 64L * d.B ? (groups >= 8192 ? 4 : groups >= 4096 ? 2 : 1) : 1;
     if (d.dtype == MCSD_DTYPE_FP32) launch_type<true>(sp, stream);
     else launch_type<false>(sp, stream);
     const hipError_t e = hipGetLastError();
