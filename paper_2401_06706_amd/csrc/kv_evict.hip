@@ -26,13 +26,13 @@ __device__ __forceinline__ uint32_t order_key(float x)
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// A workgroup per (layer, sequence, KV head).  The sum that decides is found digit by digit (four of 8 bits, counts of all digits
+// A workgroup per (layer, sequence, KV head).  The sum that decides is found digit by digit (of 11, 11 and 10 bits, counts of all digits
 // in LDS), then what is kept is written down in ascending order: positions are dealt out in rows of 1024, so that the counts per row and
 // wavefront, summed up, give every position its place.  Up to 16384 positions stay in registers; longer ones are
 // read again by every pass.
 __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
 {
-    __shared__ uint32_t s_count[256], s_scan[SEL_PER * SEL_WAVES], s_wave[4], s_pick[2];
+    __shared__ uint32_t s_count[2048], s_scan[SEL_PER * SEL_WAVES], s_wave[SEL_WAVES], s_pick[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int head = blockIdx.x, b = head / p.H_kv % p.B;
     const int n = max(0, min(p.prefix_len[b], p.L_stride)), m = min(n, max(0, p.keep_len[b]));
@@ -56,8 +56,10 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
     load(0);
     uint32_t prefix = 0, left = m - f - r;      // digits so far; how many of those that begin with them are kept
     if (left > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) s_count[tid] = 0;
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10;
+            const uint32_t digits = pass == 2 ? 1023u : 2047u;
+            s_count[tid] = s_count[SEL_NT + tid] = 0;
             __syncthreads();
             for (int c = 0; c < chunks; ++c) {
                 if (chunks > 1) load(c);
@@ -66,8 +68,8 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
                     if (c * SEL_CHUNK + i * SEL_NT >= n) break;
                     const int at = c * SEL_CHUNK + i * SEL_NT + tid;
                     const uint32_t key = order_key(val[i]);
-                    const bool on = at >= f && at < to && (shift == 24 || (key >> (shift + 8)) == prefix);
-                    const uint32_t digit = (key >> shift) & 255u;
+                    const bool on = at >= f && at < to && (pass == 0 || (key >> above) == prefix);
+                    const uint32_t digit = (key >> shift) & digits;
                     const unsigned long long all = __ballot(on);
                     if (!all) continue;
                     // one addition for the lanes that agree with the first of them (sums of 0 are many)
@@ -78,22 +80,21 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
                 }
             }
             __syncthreads();
-            // the digit at which the counts from the top reach `left`
-            uint32_t mine = 0, upto = 0;
-            if (tid < 256) {
-                mine = s_count[255 - tid];
-                upto = wave_running_sum(mine);
-                if (lane == 63) s_wave[wave] = upto;
+            // the digit at which the counts from the top reach `left`: two digits a thread
+            const uint32_t hi = s_count[2047 - 2 * tid], lo = s_count[2046 - 2 * tid];
+            uint32_t upto = wave_running_sum(hi + lo);
+            if (lane == 63) s_wave[wave] = upto;
+            __syncthreads();
+            for (int w = 0; w < wave; ++w) upto += s_wave[w];
+            const uint32_t before = upto - hi - lo;
+            if (upto >= left && before < left) {
+                const bool first = before + hi >= left;
+                s_pick[0] = first ? 2047 - 2 * tid : 2046 - 2 * tid;
+                s_pick[1] = left - before - (first ? 0 : hi);
             }
             __syncthreads();
-            if (tid < 256) {
-                for (int w = 0; w < wave; ++w) upto += s_wave[w];
-                if (upto >= left && upto - mine < left) { s_pick[0] = 255 - tid; s_pick[1] = left - (upto - mine); }
-            }
-            __syncthreads();
-            prefix = (prefix << 8) | s_pick[0];
+            prefix = (prefix << (pass == 2 ? 10 : 11)) | s_pick[0];
             left = s_pick[1];
-            __syncthreads();
         }
     }
     const bool some = m - f - r > 0;            // keys above `prefix` are kept, and the first `left` of those that are equal
@@ -124,6 +125,10 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
 #pragma unroll
         for (int i = 0; i < SEL_PER; ++i) {
             const int at = c * SEL_CHUNK + i * SEL_NT + tid;
+            if (c * SEL_CHUNK + i * SEL_NT >= n) {
+                if (lane == 0) s_scan[i * SEL_WAVES + wave] = 0;
+                continue;
+            }
             const uint32_t key = order_key(val[i]);
             const bool between = at >= f && at < to;
             if (at < n && (!between || (some && key > prefix))) take |= 1u << i;
@@ -135,6 +140,7 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
         const int equals = scan_counts();
 #pragma unroll
         for (int i = 0; i < SEL_PER; ++i) {
+            if (c * SEL_CHUNK + i * SEL_NT >= n) break;
             const unsigned long long eq = __ballot((equal >> i) & 1u);
             const uint32_t rank = equal_before + s_scan[i * SEL_WAVES + wave] + __popcll(eq & below);
             if (((equal >> i) & 1u) && rank < left) take |= 1u << i;
@@ -149,6 +155,7 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
         // (all sums of this chunk have been read; those kept go no farther back than they stood)
 #pragma unroll
         for (int i = 0; i < SEL_PER; ++i) {
+            if (c * SEL_CHUNK + i * SEL_NT >= n) break;
             const unsigned long long on = __ballot((take >> i) & 1u);
             if ((take >> i) & 1u) {
                 const int place = kept_before + s_scan[i * SEL_WAVES + wave] + __popcll(on & below);
@@ -244,8 +251,9 @@ int32_t launch_kv_evict(const mcsd_evict_desc &d, const mcsd_evict_bufs &b, cons
     if (!b.out_table) {
         launch_kernel(K_EVICT_MOVE, evict_move_kernel<true>, dim3(heads, 2 * ((p.row_bytes + 127) / 128)), dim3(1024), stream, p);
     } else {
-        const int step = 8 * 256 / p.row_lanes;
-        launch_kernel(K_EVICT_MOVE, evict_move_kernel<false>, dim3(heads, 2, (d.L_stride + step - 1) / step), dim3(256), stream, p);
+        // (workgroups that find nothing to move are many where the caches are longer than what is kept: a few per CU go through all steps)
+        const unsigned step = 8 * 256 / p.row_lanes, steps = (d.L_stride + step - 1) / step, wanted = (8192 + 2 * heads - 1) / (2 * heads);
+        launch_kernel(K_EVICT_MOVE, evict_move_kernel<false>, dim3(heads, 2, steps < wanted ? steps : wanted), dim3(256), stream, p);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("evict launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }

@@ -98,21 +98,26 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     if ((unsigned)map >= (unsigned)p.R) return refuse(MCSD_FLAG_BAD_TREE);
     const void *row = static_cast<const char *>(p.logits) + (size_t)map * p.row_stride * (BF16 ? 2 : 4);
     const Pieces<BF16> pc(row, p.V);
-    const int x = p.tokens[i_row];
-    const bool known = (unsigned)x < (unsigned)p.V;
-    const float zx = known ? logit_at<BF16>(row, x) : INFINITY;
-    const float T = p.temperature ? p.temperature[i_row] : 1.f, c = LOG2E_F / (T > 0.f ? T : 1.f);
     if (tid == 0) s_n_hot = s_n_above = s_n_equal = 0;
 
     Sums sums;
     float top = -INFINITY;
     int before = 0;
-    auto take = [&](float z, int id) {
-        if (z > sums.m) sums.raise(z, c);
-        top = fmaxf(top, z);
-        sums.add(z, c);
-        before += (z > zx || (z == zx && id < x)) ? 1 : 0;
+    // AHEAD pieces are asked for at a time
+    constexpr int AHEAD = 8;
+    int piece = tid;
+    u32x4 raw[AHEAD];
+    auto ask = [&]() {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) raw[k] = pc.raw(row, piece + k * NT);
     };
+    auto whole = [&]() { return piece + (AHEAD - 1) * NT < pc.n; };
+    bool asked = whole();
+    if (asked) ask();           // (ahead of the token's logit)
+    const int x = p.tokens[i_row];
+    const bool known = (unsigned)x < (unsigned)p.V;
+    const float zx = known ? logit_at<BF16>(row, x) : INFINITY;
+    const float T = p.temperature ? p.temperature[i_row] : 1.f, c = LOG2E_F / (T > 0.f ? T : 1.f);
     auto take_piece = [&](const float *z, int piece) {
         float most = z[0];
 #pragma unroll
@@ -126,25 +131,29 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
             before += (z[i] > zx || (z[i] == zx && i < d)) ? 1 : 0;
         }
     };
-    // AHEAD pieces are asked for at a time
-    constexpr int AHEAD = 4;
-    int piece = tid;
-    for (; piece + (AHEAD - 1) * NT < pc.n; piece += AHEAD * NT) {
-        u32x4 raw[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) raw[k] = pc.raw(row, piece + k * NT);
+    while (asked) {
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             float z[W];
             pc.values(raw[k], z);
+            // (the place of a piece that is taken is free for one of the next)
+            raw[k] = piece + (AHEAD + k) * NT < pc.n ? pc.raw(row, piece + (AHEAD + k) * NT) : raw[k];
             take_piece(z, piece + k * NT);
         }
+        piece += AHEAD * NT;
+        asked = whole();
     }
     for (; piece < pc.n; piece += NT) {
         float z[W];
         pc.load(row, piece, z);
         take_piece(z, piece);
     }
+    auto take = [&](float z, int id) {
+        if (z > sums.m) sums.raise(z, c);
+        top = fmaxf(top, z);
+        sums.add(z, c);
+        before += (z > zx || (z == zx && id < x)) ? 1 : 0;
+    };
     // (elements outside the pieces: fewer than 16)
     if (tid < pc.head) take(logit_at<BF16>(row, tid), tid);
     if (pc.tail + tid < p.V) take(logit_at<BF16>(row, pc.tail + tid), pc.tail + tid);
@@ -171,8 +180,9 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     float bound = INFINITY;
     if (p.n_top) {
         int ahead = 0;
+#pragma unroll
         for (int k = 0; k < 64; ++k) {
-            const float other = __shfl(group, k);
+            const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(group), k));
             ahead += (other > group || (other == group && k < lane)) ? 1 : 0;
         }
         const unsigned long long at = __ballot(ahead == p.n_top - 1);

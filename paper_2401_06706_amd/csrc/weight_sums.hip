@@ -12,14 +12,14 @@ struct SumsParams { ChunkParams c; const float *lse; float *sums; int last_rows,
 // added to the whole at a time: over n tiles the error stays below (64 + n / 64) 2^-24 of the sum.
 // Few rows: a workgroup goes through `blocks` of 128 positions, the next one's keys asked for ahead, so that lengths, table and rows are
 // waited for once.
-template <int DP, bool F32>
-__global__ __launch_bounds__(256) void weight_sums_kernel(SumsParams sp)
+template <int DP, bool F32, bool MULTI>
+__global__ __launch_bounds__(256, DP * (F32 ? 4 : 2) <= 256 ? 3 : 1) void weight_sums_kernel(SumsParams sp)
 {
     using S = TileShape<DP, F32>;
     const ChunkParams &p = sp.c;
     __shared__ __attribute__((aligned(16))) uint32_t s_q[2][KT * S::PK];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
-    const int g = blockIdx.x, b = blockIdx.z, key0 = blockIdx.y * 128 * sp.blocks;
+    const int g = blockIdx.x, b = blockIdx.z, blocks = MULTI ? sp.blocks : 1, key0 = blockIdx.y * 128 * blocks;
     const ChunkSeq sq = chunk_sequence(p, b);
     if (sq.n == 0 || key0 >= sq.keys) return;
     const int M = sq.n * p.G, row_bytes = p.d * S::ES;
@@ -74,9 +74,15 @@ __global__ __launch_bounds__(256) void weight_sums_kernel(SumsParams sp)
     load_q(0, 0);
     float first_lse = lse_of[0];
     store_q(0);
-    for (int block = 0; block < sp.blocks && key0 + 128 * block < sq.keys; ++block) {
+    for (int block = 0; block < blocks && key0 + 128 * block < sq.keys; ++block) {
         const int wkey = key0 + 128 * block + 32 * wave;
-        if (block + 1 < sp.blocks) load_keys(wkey + 128, k_next);
+        if (MULTI && block + 1 < blocks) load_keys(wkey + 128, k_next);
+        // (lane l32 < 16 ends up with this position, see below; what it held is asked for now)
+        const int mine = 8 * (l32 & 1) + 4 * ((l32 >> 1) & 1) + 2 * ((l32 >> 2) & 1) + ((l32 >> 3) & 1);
+        const int key = wkey + key_of_score(mine) + 4 * h;
+        float *const at = sp.sums + ((size_t)b * p.H_kv + g) * p.L_stride + key;
+        const bool writes = l32 < 16 && key < sq.keys;
+        const float old = writes && key < sq.L ? *at : 0.f;
         float part[16], total[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) part[i] = total[i] = 0.f;
@@ -115,8 +121,16 @@ __global__ __launch_bounds__(256) void weight_sums_kernel(SumsParams sp)
         if (tiles == 1) {
             if (block == 0) __syncthreads();
             step(0, 0, first_lse);
+        } else if (MULTI) {
+            // (a sequence with more rows than most: without look-ahead)
+            for (int tile = 0; tile < tiles; ++tile) {
+                if (block + tile > 0) { load_q(tile, 0); store_q(0); }
+                const float lse = lse_of[0];
+                __syncthreads();
+                step(tile, 0, lse);
+                __syncthreads();
+            }
         } else {
-            if (block > 0) { load_q(0, 0); store_q(0); }        // (every wavefront is past the barrier behind the last tile)
             load_q(1, 1);
             float lse = lse_of[0];
             __syncthreads();
@@ -151,27 +165,23 @@ __global__ __launch_bounds__(256) void weight_sums_kernel(SumsParams sp)
                 }
         }
         total[0] += __shfl_xor(total[0], 16);
-        const int i = 8 * (l32 & 1) + 4 * ((l32 >> 1) & 1) + 2 * ((l32 >> 2) & 1) + ((l32 >> 3) & 1);
-        const int key = wkey + key_of_score(i) + 4 * h;
-        if (l32 < 16 && key < sq.keys) {
-            float *at = sp.sums + ((size_t)b * p.H_kv + g) * p.L_stride + key;
-            *at = (key < sq.L ? *at : 0.f) + total[0];
-        }
+        if (writes) *at = old + total[0];
+        if (MULTI)
 #pragma unroll
-        for (int kk = 0; kk < S::KK; ++kk) k[kk] = k_next[kk];
+            for (int kk = 0; kk < S::KK; ++kk) k[kk] = k_next[kk];
     }
 }
 
-template <bool F32>
+template <bool F32, bool MULTI>
 void launch_type(const SumsParams &sp, hipStream_t stream)
 {
     const dim3 grid(sp.c.H_kv, (sp.c.L_stride + 128 * sp.blocks - 1) / (128 * sp.blocks), sp.c.B), block(256);
     const int d = sp.c.d;
-    if (d <= 32) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<32, F32>, grid, block, stream, sp);
-    else if (d <= 64) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<64, F32>, grid, block, stream, sp);
-    else if (d <= 96) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<96, F32>, grid, block, stream, sp);
-    else if (d <= 128) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<128, F32>, grid, block, stream, sp);
-    else launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<256, F32>, grid, block, stream, sp);
+    if (d <= 32) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<32, F32, MULTI>, grid, block, stream, sp);
+    else if (d <= 64) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<64, F32, MULTI>, grid, block, stream, sp);
+    else if (d <= 96) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<96, F32, MULTI>, grid, block, stream, sp);
+    else if (d <= 128) launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<128, F32, MULTI>, grid, block, stream, sp);
+    else launch_kernel(K_WEIGHT_SUMS, weight_sums_kernel<256, F32, MULTI>, grid, block, stream, sp);
 }
 
 }  // namespace
@@ -185,8 +195,8 @@ int32_t launch_weight_sums(const mcsd_chunk_desc &d, const mcsd_sums_bufs &b, co
     // several blocks a workgroup where sequences bring up to two tiles of rows on average and workgroups are plenty
     const long rows = (long)d.T * (d.H_q / d.H_kv), groups = (long)d.H_kv * d.B * ((d.L_stride + 127) / 128);
     sp.blocks = rows <= 64L * d.B ? (groups >= 8192 ? 4 : groups >= 4096 ? 2 : 1) : 1;
-    if (d.dtype == MCSD_DTYPE_FP32) launch_type<true>(sp, stream);
-    else launch_type<false>(sp, stream);
+    if (d.dtype == MCSD_DTYPE_FP32) sp.blocks > 1 ? launch_type<true, true>(sp, stream) : launch_type<true, false>(sp, stream);
+    else sp.blocks > 1 ? launch_type<false, true>(sp, stream) : launch_type<false, false>(sp, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("weight sums launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     return MCSD_OK;
