@@ -16,7 +16,7 @@ struct EvictParams {
     uint32_t *flags;
 };
 
-constexpr int SEL_NT = 1024, SEL_PER = 16, SEL_CHUNK = SEL_NT * SEL_PER, SEL_WAVES = SEL_NT / 64;
+constexpr int SEL_PER = 16;
 
 // order of sums as whole numbers: no number first, then -infinity .. infinity, both zeros alike
 __device__ __forceinline__ uint32_t order_key(float x)
@@ -27,11 +27,13 @@ __device__ __forceinline__ uint32_t order_key(float x)
 }
 
 // A workgroup per (layer, sequence, KV head).  The sum that decides is found digit by digit (of 11, 11 and 10 bits, counts of all digits
-// in LDS), then what is kept is written down in ascending order: positions are dealt out in rows of 1024, so that the counts per row and
-// wavefront, summed up, give every position its place.  Up to 16384 positions stay in registers; longer ones are
-// read again by every pass.
+// in LDS), then what is kept is written down in ascending order: positions are dealt out in rows of NT, so that the counts per row and
+// wavefront, summed up, give every position its place.  Up to 16 NT positions stay in registers (NT by the caches' capacity: barriers of few wavefronts are
+// cheap, and more workgroups share a CU); longer ones are read again by every pass.
+template <int SEL_NT>
 __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
 {
+    constexpr int SEL_CHUNK = SEL_NT * SEL_PER, SEL_WAVES = SEL_NT / 64, BINS = 2048 / SEL_NT;
     __shared__ uint32_t s_count[2048], s_scan[SEL_PER * SEL_WAVES], s_wave[SEL_WAVES], s_pick[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int head = blockIdx.x, b = head / p.H_kv % p.B;
@@ -59,7 +61,8 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10;
             const uint32_t digits = pass == 2 ? 1023u : 2047u;
-            s_count[tid] = s_count[SEL_NT + tid] = 0;
+#pragma unroll
+            for (int k = 0; k < BINS; ++k) s_count[k * SEL_NT + tid] = 0;
             __syncthreads();
             for (int c = 0; c < chunks; ++c) {
                 if (chunks > 1) load(c);
@@ -80,17 +83,21 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
                 }
             }
             __syncthreads();
-            // the digit at which the counts from the top reach `left`: two digits a thread
-            const uint32_t hi = s_count[2047 - 2 * tid], lo = s_count[2046 - 2 * tid];
-            uint32_t upto = wave_running_sum(hi + lo);
+            // the digit at which the counts from the top reach `left`: BINS digits a thread
+            uint32_t bins[BINS], mine = 0;
+#pragma unroll
+            for (int k = 0; k < BINS; ++k) { bins[k] = s_count[2047 - BINS * tid - k]; mine += bins[k]; }
+            uint32_t upto = wave_running_sum(mine);
             if (lane == 63) s_wave[wave] = upto;
             __syncthreads();
             for (int w = 0; w < wave; ++w) upto += s_wave[w];
-            const uint32_t before = upto - hi - lo;
+            uint32_t before = upto - mine;
             if (upto >= left && before < left) {
-                const bool first = before + hi >= left;
-                s_pick[0] = first ? 2047 - 2 * tid : 2046 - 2 * tid;
-                s_pick[1] = left - before - (first ? 0 : hi);
+#pragma unroll
+                for (int k = 0; k < BINS; ++k) {
+                    if (before < left && before + bins[k] >= left) { s_pick[0] = 2047 - BINS * tid - k; s_pick[1] = left - before; }
+                    before += bins[k];
+                }
             }
             __syncthreads();
             prefix = (prefix << (pass == 2 ? 10 : 11)) | s_pick[0];
@@ -99,25 +106,28 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
     }
     const bool some = m - f - r > 0;            // keys above `prefix` are kept, and the first `left` of those that are equal
     int equal_before = 0, kept_before = 0;
-    // running sum of the 256 counts of (row, wavefront), in place; returns their total
+    // running sum of the counts of (row, wavefront), in place; returns their total
+    constexpr int COUNTS = SEL_PER * SEL_WAVES, COUNT_WAVES = COUNTS / 64;
+    static_assert(COUNT_WAVES <= SEL_WAVES && COUNTS % 64 == 0, "a count a thread");
     auto scan_counts = [&]() -> int {
         uint32_t mine = 0, upto = 0;
         __syncthreads();
-        if (tid < SEL_PER * SEL_WAVES) {
+        if (tid < COUNTS) {
             mine = s_scan[tid];
             upto = wave_running_sum(mine);
             if (lane == 63) s_wave[wave] = upto;
         }
         __syncthreads();
-        if (tid < SEL_PER * SEL_WAVES) {
+        if (tid < COUNTS) {
             for (int w = 0; w < wave; ++w) upto += s_wave[w];
             s_scan[tid] = upto - mine;
         }
-        const int total = s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
+        int total = 0;
+#pragma unroll
+        for (int w = 0; w < COUNT_WAVES; ++w) total += s_wave[w];
         __syncthreads();
         return total;
     };
-    static_assert(SEL_PER * SEL_WAVES == 256, "four wavefronts sum the counts up");
     const unsigned long long below = (1ull << lane) - 1;
     for (int c = 0; c < chunks; ++c) {
         if (chunks > 1) load(c);
@@ -247,7 +257,9 @@ int32_t launch_kv_evict(const mcsd_evict_desc &d, const mcsd_evict_bufs &b, cons
     p.sums = b.sums; p.prefix_len = b.prefix_len; p.kept = b.kept; p.keep_len = b.keep_len;
     p.block_table = kv.block_table; p.out_table = b.out_table; p.flags = b.flags;
     const unsigned heads = (unsigned)(d.n_layers * d.B * d.H_kv);
-    launch_kernel(K_EVICT_SELECT, evict_select_kernel, dim3(heads), dim3(SEL_NT), stream, p);
+    if (d.L_stride <= 256 * SEL_PER) launch_kernel(K_EVICT_SELECT, evict_select_kernel<256>, dim3(heads), dim3(256), stream, p);
+    else if (d.L_stride <= 512 * SEL_PER) launch_kernel(K_EVICT_SELECT, evict_select_kernel<512>, dim3(heads), dim3(512), stream, p);
+    else launch_kernel(K_EVICT_SELECT, evict_select_kernel<1024>, dim3(heads), dim3(1024), stream, p);
     if (!b.out_table) {
         launch_kernel(K_EVICT_MOVE, evict_move_kernel<true>, dim3(heads, 2 * ((p.row_bytes + 127) / 128)), dim3(1024), stream, p);
     } else {

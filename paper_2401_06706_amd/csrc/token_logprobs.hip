@@ -17,7 +17,7 @@ struct LogprobParams {
     uint32_t *flags;
 };
 
-constexpr int NT = 512, CAP = 1024;         // candidates for the top that fit; those equal to the smallest of them
+constexpr int CAP = 1024;         // candidates for the top that fit; those equal to the smallest of them
 constexpr float LOWEST = -200.0f;           // 2^-200 is 0: a bound that keeps 0 * infinity out of the entropy
 
 template <bool BF16>
@@ -72,7 +72,7 @@ struct Sums {
 // A workgroup per row, which is read once: every thread keeps running sums, its largest logit and how many tokens come before the given
 // one.  For the top, the n-th largest of 64 maxima (of every eighth thread) bounds it from below: only the few threads whose
 // largest logit reaches that bound have their pieces read again, by all threads together.
-template <bool BF16>
+template <bool BF16, int NT, int AHEAD>
 __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
 {
     constexpr int W = Pieces<BF16>::W, WAVES = NT / 64;
@@ -81,6 +81,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     __shared__ int s_rank[WAVES], s_hot[NT], s_n_hot, s_n_above, s_n_equal;
     __shared__ float s_val[CAP];
     __shared__ int s_id[CAP], s_eq[CAP];
+    static_assert(WAVES <= CAP, "");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i_row = blockIdx.x;
     const int map = p.row_map ? p.row_map[i_row] : i_row;
     auto refuse = [&](uint32_t flag) {
@@ -103,8 +104,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     Sums sums;
     float top = -INFINITY;
     int before = 0;
-    // AHEAD pieces are asked for at a time
-    constexpr int AHEAD = 8;
+    // AHEAD pieces are under way at a time
     int piece = tid;
     u32x4 raw[AHEAD];
     auto ask = [&]() {
@@ -298,8 +298,15 @@ int32_t launch_token_logprobs(const mcsd_logprob_desc &d, const mcsd_logprob_buf
     p.rows = d.rows; p.R = d.R; p.V = d.V; p.n_top = d.n_top; p.row_stride = (size_t)d.row_stride;
     p.logits = b.logits; p.row_map = b.row_map; p.tokens = b.tokens; p.temperature = b.temperature;
     p.logprob = b.logprob; p.entropy = b.entropy; p.rank = b.rank; p.top_tok = b.top_tok; p.top_logprob = b.top_logprob; p.flags = b.flags;
-    if (d.dtype == MCSD_DTYPE_BF16) launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<true>, dim3(d.rows), dim3(NT), stream, p);
-    else launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<false>, dim3(d.rows), dim3(NT), stream, p);
+    // Few rows, a CU each at most: 1024 threads a row.  More: 512, four rows a CU, with fewer registers for pieces under way.
+    const bool few = d.rows <= 256;
+    if (d.dtype == MCSD_DTYPE_BF16) {
+        if (few) launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<true, 1024, 4>, dim3(d.rows), dim3(1024), stream, p);
+        else launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<true, 512, 4>, dim3(d.rows), dim3(512), stream, p);
+    } else {
+        if (few) launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<false, 1024, 8>, dim3(d.rows), dim3(1024), stream, p);
+        else launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<false, 512, 4>, dim3(d.rows), dim3(512), stream, p);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("token log probabilities launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     return MCSD_OK;
