@@ -2,6 +2,7 @@
 #include <float.h>
 
 #include "attn_common.h"
+#include "vocab_row.h"
 
 namespace mcsd {
 namespace {
@@ -164,18 +165,16 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     float group = s_max[lane];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) group = fmaxf(group, s_max[64 * w + lane]);
-    float m = group;
-#pragma unroll
-    for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    const float m = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vocab::wave_max(group)), 63));
     sums.raise(fmaxf(m, -FLT_MAX), c);
-    double s = sums.s, u = sums.u;
-#pragma unroll
-    for (int k = 32; k > 0; k >>= 1) {
-        s += __shfl_xor(s, k);
-        u += __shfl_xor(u, k);
-        before += __shfl_xor(before, k);
-    }
-    if (lane == 0) { s_sum[0][wave] = s; s_sum[1][wave] = u; s_rank[wave] = before; }
+    double s = vocab::wave_sum(sums.s), u = vocab::wave_sum(sums.u);        // (in lane 63, as the count)
+    before += __builtin_amdgcn_update_dpp(0, before, 0xB1, 0xf, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x4E, 0xf, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x141, 0xf, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x140, 0xf, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x142, 0xa, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x143, 0xc, 0xf, false);
+    if (lane == 63) { s_sum[0][wave] = s; s_sum[1][wave] = u; s_rank[wave] = before; }
     // ---- the bound of the top: n_top-th largest of the 64 maxima
     float bound = INFINITY;
     if (p.n_top) {
@@ -233,12 +232,27 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     float *lp = p.top_logprob + (size_t)i_row * p.n_top;
     const int above = s_n_above, equal = s_n_equal;
     if (above <= CAP) {
-        for (int k = tid; k < above; k += NT) {
-            const float z = s_val[k];
-            const int id = s_id[k];
-            int place = 0;
-            for (int j = 0; j < above; ++j) place += (s_val[j] > z || (s_val[j] == z && s_id[j] < id)) ? 1 : 0;
-            if (place < p.n_top) { tok[place] = id; lp[place] = logprob_of(z); }
+        // the place of each among them; up to 64 by one wavefront, from registers
+        if (above <= 64) {
+            if (wave == 0) {
+                const float z = lane < above ? s_val[lane] : 0.f;
+                const int id = lane < above ? s_id[lane] : 0;
+                int place = 0;
+                for (int j = 0; j < above; ++j) {
+                    const float zj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(z), j));
+                    const int idj = __builtin_amdgcn_readlane(id, j);
+                    place += (zj > z || (zj == z && idj < id)) ? 1 : 0;
+                }
+                if (lane < above && place < p.n_top) { tok[place] = id; lp[place] = logprob_of(z); }
+            }
+        } else {
+            for (int k = tid; k < above; k += NT) {
+                const float z = s_val[k];
+                const int id = s_id[k];
+                int place = 0;
+                for (int j = 0; j < above; ++j) place += (s_val[j] > z || (s_val[j] == z && s_id[j] < id)) ? 1 : 0;
+                if (place < p.n_top) { tok[place] = id; lp[place] = logprob_of(z); }
+            }
         }
         const int missing = p.n_top - above;            // of those equal to the bound, the lowest ids
         if (missing > 0 && equal <= CAP) {
