@@ -23,8 +23,12 @@ void chunk_attn_kernel(ChunkParams p)
     const int h = lane >> 5, l32 = lane & 31, lj = lane >> 4, lc = lane & 15;
     const int g = blockIdx.x % p.H_kv;          // (KV head fastest: the row tiles of one meet in one XCD's L2 where their number is a multiple of 8)
     Item it;
-    if (p.counter && blockIdx.x == 0 && tid == 0) *p.counter = 0;
-    if (!find_item<FEW_ROWS>(p, blockIdx.x / p.H_kv, lane, &it)) return;
+    const ItemList<FEW_ROWS> list(p, lane);
+    if (p.notes && blockIdx.x == gridDim.x - 1) {           // (as a rule it has no item)
+        const int len_many = p.max_parts_many ? list.many_segment(p, lane) : 0;
+        if (tid == 0) *p.notes = {0, list.many, list.len, len_many};
+    }
+    if (!list.find(p, blockIdx.x / p.H_kv, lane, &it)) return;
     const int M = it.s.n * p.G, row0 = it.rt * ROWS_FEW + 32 * wave;
     auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
     const int kt = position(min(it.rt * ROWS_FEW + ROWS_FEW, M) - 1) / KT + 1;           // key tiles that some row of this tile sees
@@ -280,14 +284,14 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p)
         const int token = by_group(p, row);
         return (size_t)(it.s.s0 + token) * p.H_q + (g * p.G + row - token * p.G);
     };
-    const bool by_segments = it.n_seg >= 2 * GROUPS;        // then the grid's y are rows of a block, otherwise blocks
-    for (int block = by_segments ? 0 : blockIdx.y; block < it.rows / 32; block += by_segments ? 1 : gridDim.y) {
-        const int row0 = it.rt * it.rows + 32 * block;
-        const size_t first = ((size_t)(it.part + block) * p.H_kv + g) * 32;
-        if (!by_segments) {
+    const bool by_segments = it.n_seg >= 2 * GROUPS;        // then the grid's y are rows, otherwise blocks of 32
+    if (!by_segments) {
+        for (int block = blockIdx.y; block < it.rows / 32; block += gridDim.y) {
+            const int row0 = it.rt * it.rows + 32 * block;
+            const size_t first = ((size_t)(it.part + block) * p.H_kv + g) * 32;
             constexpr int COLS = DP / 32;
             const int row = row0 + tid / 8;
-            if (row >= M) return;
+            if (row >= M) break;
             Merged<DP, COLS> a;
 #pragma unroll
             for (int k = 0; k < COLS; ++k) a.acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -305,41 +309,42 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p)
             for (int k = 0; k < COLS; ++k)
                 if (32 * k + 4 * (tid & 7) < p.d) write(at, 32 * k + 4 * (tid & 7), a.acc[k], 1.0f / a.l);
             if (p.lse && (tid & 7) == 0) p.lse[at] = (a.m + __builtin_amdgcn_logf(a.l)) * LN2_F;
-            continue;
         }
-        const int group = tid >> 5, l32 = tid & 31;
-        for (int r = blockIdx.y; r < 32 && row0 + r < M; r += gridDim.y) {
-            Merged<DP, WIDE> a;
+        return;
+    }
+    const int group = tid >> 5, l32 = tid & 31;
+    for (int r = blockIdx.y; r < it.rows && it.rt * it.rows + r < M; r += gridDim.y) {
+        const size_t first = ((size_t)(it.part + r / 32) * p.H_kv + g) * 32 + r % 32;
+        Merged<DP, WIDE> a;
 #pragma unroll
-            for (int k = 0; k < WIDE; ++k) a.acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < WIDE; ++k) a.acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-            for (int s = group; s < it.n_seg; s += GROUPS) {
-                const size_t at = first + r + s * step;
-                const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+        for (int s = group; s < it.n_seg; s += GROUPS) {
+            const size_t at = first + s * step;
+            const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+            float4 x[WIDE];
+#pragma unroll
+            for (int k = 0; k < WIDE; ++k) x[k] = 128 * k + 4 * l32 < DP ? *reinterpret_cast<const float4 *>(p.part_o + at * DP + 128 * k + 4 * l32) : make_float4(0.f, 0.f, 0.f, 0.f);
+            a.add(ml.x, ml.y, x);
+        }
+        __syncthreads();                // (the row before has been read)
+        if (l32 == 0) { s_ml[group][0] = a.m; s_ml[group][1] = a.l; }
+#pragma unroll
+        for (int k = 0; k < WIDE; ++k) *reinterpret_cast<float4 *>(&s_acc[group][128 * k + 4 * l32]) = a.acc[k];
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int j = 1; j < GROUPS; ++j) {
                 float4 x[WIDE];
 #pragma unroll
-                for (int k = 0; k < WIDE; ++k) x[k] = 128 * k + 4 * l32 < DP ? *reinterpret_cast<const float4 *>(p.part_o + at * DP + 128 * k + 4 * l32) : make_float4(0.f, 0.f, 0.f, 0.f);
-                a.add(ml.x, ml.y, x);
+                for (int k = 0; k < WIDE; ++k) x[k] = *reinterpret_cast<const float4 *>(&s_acc[j][128 * k + 4 * l32]);
+                a.add(s_ml[j][0], s_ml[j][1], x);
             }
-            __syncthreads();                // (the row before has been read)
-            if (l32 == 0) { s_ml[group][0] = a.m; s_ml[group][1] = a.l; }
+            const size_t at = row_of_out(it.rt * it.rows + r);
 #pragma unroll
-            for (int k = 0; k < WIDE; ++k) *reinterpret_cast<float4 *>(&s_acc[group][128 * k + 4 * l32]) = a.acc[k];
-            __syncthreads();
-            if (group == 0) {
-#pragma unroll
-                for (int j = 1; j < GROUPS; ++j) {
-                    float4 x[WIDE];
-#pragma unroll
-                    for (int k = 0; k < WIDE; ++k) x[k] = *reinterpret_cast<const float4 *>(&s_acc[j][128 * k + 4 * l32]);
-                    a.add(s_ml[j][0], s_ml[j][1], x);
-                }
-                const size_t at = row_of_out(row0 + r);
-#pragma unroll
-                for (int k = 0; k < WIDE; ++k)
-                    if (128 * k + 4 * l32 < p.d) write(at, 128 * k + 4 * l32, a.acc[k], 1.0f / a.l);
-                if (p.lse && l32 == 0) p.lse[at] = (a.m + __builtin_amdgcn_logf(a.l)) * LN2_F;
-            }
+            for (int k = 0; k < WIDE; ++k)
+                if (128 * k + 4 * l32 < p.d) write(at, 128 * k + 4 * l32, a.acc[k], 1.0f / a.l);
+            if (p.lse && l32 == 0) p.lse[at] = (a.m + __builtin_amdgcn_logf(a.l)) * LN2_F;
         }
     }
 }
@@ -369,9 +374,6 @@ __global__ __launch_bounds__(256) void kv_store_paged_kernel(StoreParams p)
     *reinterpret_cast<u32x4 *>(p.v_pool + at) = v;
 }
 
-#ifndef TARGET_FEW
-#define TARGET_FEW 1024
-#endif
 int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
 
 template <int DP, bool F32>
@@ -379,8 +381,8 @@ void launch_shape(const ChunkParams &p, const ChunkPlan &plan, hipStream_t strea
 {
     launch_kernel(K_CHUNK_ATTN, chunk_attn_kernel<DP, F32>, dim3(p.H_kv * plan.max_items), dim3(256), stream, p);
     if (plan.max_items_many) launch_chunk_wide(p, plan.max_items_many, stream);
-    if (plan.max_parts)
-        launch_kernel(K_CHUNK_MERGE, chunk_merge_kernel<DP, F32>, dim3(p.H_kv * plan.max_cut, plan.max_items_many ? ROWS_MANY / 32 : ROWS_FEW / 32), dim3(256), stream, p);
+    if (plan.max_parts + plan.max_parts_many)
+        launch_kernel(K_CHUNK_MERGE, chunk_merge_kernel<DP, F32>, dim3(p.H_kv * plan.max_cut, plan.merge_y), dim3(256), stream, p);
 }
 
 template <bool F32>
@@ -407,32 +409,41 @@ static long most_tiles(long T, long B, long G, long rows)
 bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
 {
     const long G = d.H_q / d.H_kv, T = d.T, kt = (d.L_stride + KT - 1) / KT;
-    // bf16, d = 128: sequences of more than MANY rows have a kernel of their own where a launch has so many on average
-    // (it would find nothing to do in a batch that decodes, for 4 us)
+    // bf16, d = 128: sequences of more than MANY rows have a kernel of their own where a launch has so many on average (it would find
+    // nothing to do in a batch that decodes, for 4 us).  Up to one of its row tiles on average the arrays decide, on the device: sequences of few
+    // rows that have most of the work are bound by memory, and those of many run beside them (32 sequences, four with 200 to 512 tokens, 32/8 heads:
+    // 137 us, 159 in two kernels one after the other); otherwise the kernel for many is faster (8 sequences of 128 to 256 tokens on 2000 to 4000,
+    // 32/32 heads: 158 us, 204 in one kernel).
     const bool many = d.dtype == MCSD_DTYPE_BF16 && d.d == 128 && T * G > (long)MANY * d.B;
-    plan->many = many ? MANY : 0x7fffffff;
-    // Segments of 8 tiles at least; of few rows twice as many as the chip takes at once (two workgroups a compute unit), which evens the lengths out, of
-    // many as many (one).  A sequence that is cut has kt / len of them, rounded up, 2 kt / len at most, or to nearest, 4/3 kt / len at most.
+    plan->many = many ? MANY : NEVER_MANY;
+    plan->by_work = many && T * G <= (long)ROWS_MANY * d.B;
+    // Segments of 8 tiles at least.  A sequence that is cut has kt / len of them, of few rows rounded up, 2 kt / len at most, of many to nearest,
+    // 4/3 kt / len at most.  Two workgroups of few rows run on a compute unit, one of many.
     plan->min_seg = 8;
-    plan->target = d.H_kv < TARGET_FEW ? TARGET_FEW / d.H_kv : 1;
-    plan->target_many = d.H_kv < 256 ? 256 / d.H_kv : 1;
+    plan->at_once = d.H_kv < 512 ? 512 / d.H_kv : 1;
+    plan->at_once_many = d.H_kv < 256 ? 256 / d.H_kv : 1;
+    const long target = 2L * plan->at_once, target_many = (long)(cut_at(CUTS - 1) * plan->at_once_many);
     const long n_seg = (kt + plan->min_seg - 1) / plan->min_seg;
     // (a sequence of few rows is one row tile where those of many are not here)
-    const long tiles = many ? (T < d.B ? T : d.B) : most_tiles(T, d.B, G, ROWS_FEW), tiles_many = many ? most_tiles(T, d.B, G, ROWS_MANY) : 0;
-    auto parts_of = [&](long most, long row_tiles) {
-        const long parts = n_seg < 2 ? 0 : most + 2;
-        return parts < row_tiles * n_seg ? parts : row_tiles * n_seg;
-    };
-    const long parts = parts_of(2L * plan->target, tiles), parts_many = parts_of((4L * plan->target_many + 2) / 3, tiles_many);
+    const long tiles = many && !plan->by_work ? (T < d.B ? T : d.B) : most_tiles(T, d.B, G, ROWS_FEW), tiles_many = many ? most_tiles(T, d.B, G, ROWS_MANY) : 0;
+    // a sequence of n segments has its keys cut where n >= 2
+    auto parts_of = [&](long most, long row_tiles) { return n_seg < 2 ? 0 : most < row_tiles * n_seg ? most : row_tiles * n_seg; };
+    auto less = [](long x, long y) { return x < y ? x : y; };
+    const long parts = parts_of(less(2 * target, target + tiles) + 2, tiles);
+    const long parts_many = parts_of(less((4 * target_many + 2) / 3, target_many + tiles_many / 2) + 2, tiles_many);
     // kt / len and one more of every row tile
     auto items_of = [&](long target, long row_tiles) { return n_seg < 2 ? row_tiles : target + row_tiles < row_tiles * n_seg ? target + row_tiles : row_tiles * n_seg; };
-    const long items = items_of(plan->target, tiles), items_many = tiles_many ? items_of(plan->target_many, tiles_many) : 0;
+    const long items = items_of(target, tiles), items_many = tiles_many ? items_of(target_many, tiles_many) : 0;
     const long cut = parts / 2 < tiles ? parts / 2 : tiles, cut_many = parts_many / 2 < tiles_many ? parts_many / 2 : tiles_many;
+    const long rows = many ? ROWS_MANY : ROWS_FEW, cells = 2048 / (d.H_kv * (cut + cut_many) + 1);
+    plan->merge_y = (int)(cells < rows / 32 ? rows / 32 : cells < rows ? cells : rows);
     plan->max_items = (int)items;
     plan->max_items_many = (int)items_many;
     plan->max_cut = (int)(cut + cut_many);
-    plan->max_parts = (int)(parts * (ROWS_FEW / 32) + parts_many * (ROWS_MANY / 32));
-    plan->ws_bytes = ((size_t)plan->max_parts * d.H_kv * 32 * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256 + (many ? 256 : 0);
+    plan->max_parts = (int)(parts * (ROWS_FEW / 32));
+    plan->max_parts_many = (int)(parts_many * (ROWS_MANY / 32));
+    const size_t rows_cut = (size_t)(plan->max_parts + plan->max_parts_many) * d.H_kv * 32;
+    plan->ws_bytes = rows_cut || many ? (rows_cut * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256 + 256 : 0;
     return items * d.H_kv < 1L << 24 && items_many * d.H_kv < 1L << 24;     // (a launch has fewer than 2^32 threads)
 }
 
@@ -440,11 +451,12 @@ int32_t launch_chunk_attn(const mcsd_chunk_desc &d, const mcsd_chunk_bufs &b, co
 {
     ChunkParams p = chunk_params(d, kv);
     p.q = b.q; p.k_pool = b.k_pool; p.v_pool = b.v_pool; p.chunk_start = b.chunk_start; p.prefix_len = b.prefix_len; p.out = b.out; p.lse = b.lse;
-    p.min_seg = plan.min_seg; p.max_parts = plan.max_parts; p.many = plan.many;
-    p.target = (float)plan.target; p.target_many = (float)plan.target_many;
+    p.min_seg = plan.min_seg; p.max_parts = plan.max_parts; p.max_parts_many = plan.max_parts_many; p.many = plan.many; p.by_work = plan.by_work;
+    p.at_once = (float)plan.at_once; p.at_once_many = (float)plan.at_once_many;
     p.part_o = static_cast<float *>(b.workspace);
-    p.counter = plan.max_items_many ? reinterpret_cast<int *>(static_cast<char *>(b.workspace) + plan.ws_bytes - 256) : nullptr;
-    if (plan.max_parts) p.part_ml = p.part_o + (size_t)plan.max_parts * d.H_kv * 32 * padded_dim(d.d);
+    const size_t parts = (size_t)(plan.max_parts + plan.max_parts_many) * d.H_kv * 32;
+    p.part_ml = p.part_o + parts * padded_dim(d.d);
+    p.notes = plan.ws_bytes ? reinterpret_cast<ChunkNotes *>(static_cast<char *>(b.workspace) + plan.ws_bytes - 256) : nullptr;
     if (d.dtype == MCSD_DTYPE_FP32) launch_type<true>(p, plan, stream);
     else launch_type<false>(p, plan, stream);
     const hipError_t e = hipGetLastError();

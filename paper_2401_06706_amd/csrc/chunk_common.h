@@ -32,12 +32,12 @@ struct ChunkParams {
     const int32_t *chunk_start, *prefix_len, *block_table;
     void *out;
     float *lse, *part_o, *part_ml;
-    int *counter;         // of the wide kernel's items
+    struct ChunkNotes *notes;
     int B, T, H_q, H_kv, G, d, L_stride, page_size, n_pages, max_pages;
     FastDiv group;        // by G
-    int many;             // rows beyond which a sequence belongs to the wide kernel
-    int min_seg, max_parts;
-    float target, target_many;      // workgroups per KV head aimed at where keys are cut, of either kernel
+    int many, by_work;    // rows beyond which a sequence belongs to the wide kernel; 1: where those have most of the work
+    int min_seg, max_parts, max_parts_many;
+    float at_once, at_once_many;    // workgroups per KV head that the chip takes at once, of either kernel
     size_t q_row;         // bytes from a row of q to the next one's
     float scale_log2;     // scale * log2(e)
 };
@@ -91,6 +91,22 @@ __device__ __forceinline__ int wave_running_sum(int v)
     return v;
 }
 
+// sum and maximum (of values >= 0) over the lanes of a wavefront, in all of them
+template <bool MAX>
+__device__ __forceinline__ float wave_reduce(float v)
+{
+    auto join = [&](int x) { const float y = __int_as_float(x); v = MAX ? fmaxf(v, y) : v + y; };
+    join(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
+    join(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
+    join(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
+    join(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
+    join(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+    join(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ float wave_sum(float v) { return wave_reduce<false>(v); }
+__device__ __forceinline__ float wave_max(float v) { return wave_reduce<true>(v); }
+
 // ---- the work of a launch
 // Rows r = token * G + head in group of a (sequence, KV head) go in tiles, of ROWS_MANY for sequences of more than p.many rows and
 // of ROWS_FEW for others (one kernel each), the keys of a tile in equal segments.  A segment is so long that all of a kernel's
@@ -98,56 +114,121 @@ __device__ __forceinline__ int wave_running_sum(int v)
 // partial result is small) or to nearest.
 // Every workgroup of both kernels and of the merge works out the same list, a sequence a lane.  Partial results are numbered in
 // blocks of 32 rows, row tile by row tile, segment by segment.
-constexpr int ROWS_FEW = 128, ROWS_MANY = 256, MANY = 64;
+constexpr int ROWS_FEW = 128, ROWS_MANY = 256, MANY = 64, NEVER_MANY = 0x7fffffff;
+// segments aimed at, times the workgroups at once
+constexpr int CUTS = 4;
+__host__ __device__ constexpr float cut_at(int j) { return j == 0 ? 1.f : j == 1 ? 1.5f : j == 2 ? 2.f : 3.f; }
 enum ItemKind { FEW_ROWS, MANY_ROWS, MERGE };
 struct Item { int b, rt, rows, seg, n_seg, part; ChunkSeq s; };
 
-__device__ __forceinline__ bool has_many(const ChunkParams &p, const ChunkSeq &s) { return s.n * p.G > p.many; }
-__device__ __forceinline__ int row_tiles(const ChunkParams &p, const ChunkSeq &s)
-{
-    return has_many(p, s) ? (s.n * p.G + ROWS_MANY - 1) / ROWS_MANY : (s.n * p.G + ROWS_FEW - 1) / ROWS_FEW;
-}
+// what the kernel for few rows, which comes first, leaves to those behind it: items of the wide kernel that were taken; rows beyond which a
+// sequence belongs to that; key tiles of a segment of either kernel
+struct ChunkNotes { int taken, many, len, len_many; };
+
+template <bool MANY_ROW_TILES> __device__ __forceinline__ int segments(int kt, int len) { return max(1, (kt + (MANY_ROW_TILES ? len / 2 : len - 1)) / len); }
+
+// The sequences' row tiles and key tiles, one of the first 64 a lane, further ones read again by every search.
+struct ChunkWork {
+    ChunkSeq s = {0, 0, 0, 0};
+    int many;           // rows beyond which a sequence belongs to the wide kernel
+
+    __device__ __forceinline__ bool has_many(const ChunkParams &p, const ChunkSeq &q) const { return q.n * p.G > many; }
+    __device__ __forceinline__ int row_tiles(const ChunkParams &p, const ChunkSeq &q) const
+    {
+        return has_many(p, q) ? (q.n * p.G + ROWS_MANY - 1) / ROWS_MANY : (q.n * p.G + ROWS_FEW - 1) / ROWS_FEW;
+    }
+    // f(many rows?, row tiles, key tiles) of every sequence
+    template <class F>
+    __device__ __forceinline__ void each(const ChunkParams &p, int lane, F &&f) const
+    {
+        f(has_many(p, s), row_tiles(p, s), (s.keys + KT - 1) / KT);
+        for (int b = lane + 64; b < p.B; b += 64) {
+            const ChunkSeq q = chunk_sequence(p, b);
+            f(has_many(p, q), row_tiles(p, q), (q.keys + KT - 1) / KT);
+        }
+    }
+    // Key tiles of a segment.  Few rows: so that there are about twice as many segments as the chip takes at once.
+    __device__ __forceinline__ int few_segment(const ChunkParams &p, int lane)
+    {
+        float work, work_many;
+        auto sum = [&]() {
+            work = work_many = 0.f;
+            each(p, lane, [&](bool m, int rt, int kt) {
+                work += m ? 0.f : (float)rt * (float)kt;
+                work_many += m ? (float)rt * (float)kt : 0.f;
+            });
+            work = wave_sum(work);
+        };
+        sum();
+        if (p.by_work && many != NEVER_MANY && wave_sum(work_many) < work) {
+            many = NEVER_MANY;
+            sum();
+        }
+        return uniform(max(p.min_seg, (int)ceilf(work / (2.f * p.at_once))));
+    }
+    // Many rows: of CUTS lengths the one with which the kernel should end first.  An item costs 8 tiles' time beside its own, one that leaves
+    // partial results 16.  Items are taken in rounds, or all work goes over the workgroups and half the longest item is left over.
+    __device__ __forceinline__ int many_segment(const ChunkParams &p, int lane) const
+    {
+        float work = 0.f, least = INFINITY;
+        each(p, lane, [&](bool m, int rt, int kt) { work += m ? (float)rt * (float)kt : 0.f; });
+        work = wave_sum(work);
+        int best = p.min_seg;
+        for (int j = 0; j < CUTS; ++j) {
+            const int len = max(p.min_seg, (int)ceilf(work / (p.at_once_many * cut_at(j))));
+            float items = 0.f, total = 0.f, longest = 0.f;
+            each(p, lane, [&](bool m, int rt, int kt) {
+                const int n = segments<true>(kt, len);
+                const float own = (float)((kt + n - 1) / n) + (n > 1 ? 16.f : 8.f);
+                items += m ? (float)(rt * n) : 0.f;
+                total += m ? (float)(rt * n) * own : 0.f;
+                longest = fmaxf(longest, m ? own : 0.f);
+            });
+            items = wave_sum(items), total = wave_sum(total), longest = wave_max(longest);
+            const float end = fminf(ceilf(items / p.at_once_many) * longest, fmaxf(longest, total / p.at_once_many + 0.5f * longest));
+            if (end < least) { least = end; best = len; }
+        }
+        return uniform(best);
+    }
+};
 
 template <ItemKind KIND>
-struct ItemList {
+struct ItemList : ChunkWork {
     int len = 0, len_many = 0;              // key tiles of a segment of either kernel
-    // of sequence `lane` (further ones are read again by every search)
-    ChunkSeq s = {0, 0, 0, 0};
-    int rt = 0, n_seg = 1, blocks = 1, mine = 0, part = 0, parts = 0;
+    int rt = 0, n_seg = 1, blocks = 1, mine = 0, part = 0;      // of sequence `lane`
+    struct Parts { int few, many; } parts;
 
     __device__ __forceinline__ ItemList(const ChunkParams &p, int lane)
     {
         if (lane < p.B) s = chunk_sequence(p, lane);
-        if (p.max_parts) {
-            float work = 0.f, work_many = 0.f;
-            auto add = [&](const ChunkSeq &q) {
-                const float w = (float)row_tiles(p, q) * (float)((q.keys + KT - 1) / KT);
-                work_many += has_many(p, q) ? w : 0.f;
-                work += has_many(p, q) ? 0.f : w;
-            };
-            add(s);
-            for (int b = lane + 64; b < p.B; b += 64) add(chunk_sequence(p, b));
-#pragma unroll
-            for (int m = 32; m > 0; m >>= 1) { work += __shfl_xor(work, m); work_many += __shfl_xor(work_many, m); }
-            len = max(p.min_seg, (int)ceilf(work / p.target));
-            len_many = max(p.min_seg, (int)ceilf(work_many / p.target_many));
+        many = p.many;
+        if (KIND == FEW_ROWS) {
+            if (p.notes) len = few_segment(p, lane);
+        } else {
+            many = uniform(p.notes->many);
+            len = uniform(p.notes->len);
+            len_many = uniform(p.notes->len_many);
         }
-        parts = count(p, 0);
+        parts = count(p, {0, p.max_parts});
     }
     // items and partial results of the lane's sequence, behind those of `before`; returns the partial results up to lane 63
-    __device__ __forceinline__ int count(const ChunkParams &p, int before)
+    __device__ __forceinline__ Parts count(const ChunkParams &p, Parts before)
     {
         const bool many = has_many(p, s);
-        const int kt = (s.keys + KT - 1) / KT, my_len = many ? len_many : len;
+        const int kt = (s.keys + KT - 1) / KT;
         rt = row_tiles(p, s);
         blocks = (many ? ROWS_MANY : ROWS_FEW) / 32;
-        n_seg = p.max_parts ? max(1, (kt + (many ? my_len / 2 : my_len - 1)) / my_len) : 1;
+        n_seg = 1;
+        if (many && p.max_parts_many && KIND != FEW_ROWS) n_seg = segments<true>(kt, len_many);
+        if (!many && p.max_parts && KIND != MANY_ROWS) n_seg = segments<false>(kt, len);
         const int my_parts = n_seg > 1 ? rt * n_seg * blocks : 0;
-        const int parts_to = before + wave_running_sum(my_parts);
-        if (parts_to > p.max_parts) n_seg = 1;          // (cannot be, but by arrays that contradict themselves)
-        part = parts_to - my_parts;
+        Parts to = before;
+        if (KIND != MANY_ROWS) to.few += wave_running_sum(many ? 0 : my_parts);
+        if (KIND != FEW_ROWS) to.many += wave_running_sum(many ? my_parts : 0);
+        if (many ? to.many > p.max_parts + p.max_parts_many : to.few > p.max_parts) n_seg = 1;      // (cannot be, but by arrays that contradict themselves)
+        part = (many ? to.many : to.few) - my_parts;
         mine = KIND == MERGE ? n_seg > 1 : many == (KIND == MANY_ROWS);
-        return __builtin_amdgcn_readlane(parts_to, 63);
+        return {__builtin_amdgcn_readlane(to.few, 63), __builtin_amdgcn_readlane(to.many, 63)};
     }
     __device__ __forceinline__ void fill(int o, int b, int from_end, int seg, Item *it) const
     {
@@ -164,7 +245,8 @@ struct ItemList {
     __device__ __forceinline__ bool find(const ChunkParams &p, int idx, int lane, Item *it) const
     {
         ItemList l = *this;
-        int items = 0, behind = parts;
+        int items = 0;
+        Parts behind = parts;
         for (int b0 = 0;;) {
             const int per = KIND == MERGE ? 1 : l.n_seg, my_items = l.mine ? l.rt * per : 0, items_to = items + wave_running_sum(my_items);
             const unsigned long long found = __ballot(items_to > idx);

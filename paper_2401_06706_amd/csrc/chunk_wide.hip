@@ -422,7 +422,7 @@ void chunk_wide_kernel(ChunkParams p)
     if (more) {
         now = ahead;
         fetch_q(now);
-        if (tid == 0) s_next = (int)gridDim.x + atomicAdd(p.counter, 1);
+        if (tid == 0) s_next = (int)gridDim.x + atomicAdd(&p.notes->taken, 1);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -481,7 +481,7 @@ void chunk_wide_kernel(ChunkParams p)
             }
             int taken = 0;
             if (!careful)
-                if (tid == 0) taken = atomicAdd(p.counter, 1);
+                if (tid == 0) taken = atomicAdd(&p.notes->taken, 1);
             for (; t < now.t_end; ++t) {                        // (this wavefront only helps to load)
                 arrival();
                 advance();

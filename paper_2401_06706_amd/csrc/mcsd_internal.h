@@ -12,7 +12,7 @@ namespace mcsd {
 // Kernel ids for the optional per-kernel event timing.
 enum KernelId { K_ATTN_MFMA = 0, K_ATTN_GENERIC = 1, K_ATTN_COMBINE = 2, K_VERIFY_ROWS = 3, K_WALK = 4, K_DRAFT_ROWS = 5, K_TREE_BUILD = 6, K_KV_COPY = 7, K_KV_FINISH = 8, K_KV_STORE = 9, K_KV_LOAD = 10,
                 K_ATTN_FOURBIT = 11, K_ATTN_FOURBIT_COMBINE = 12, K_PAGE_ASSIGN = 13, K_PAGE_SLOTS = 14, K_LOGITS_RULES = 15,
-                K_KV_STORE_PAGED = 16, K_CHUNK_ATTN = 17, K_CHUNK_MERGE = 18, K_WEIGHT_SUMS = 19, K_EVICT_SELECT = 20, K_EVICT_MOVE = 21, K_TOKEN_LOGPROBS = 22, K_LOGPROB_MERGE = 23, K_CHUNK_WIDE = 24, K_COUNT = 25 };
+                K_KV_STORE_PAGED = 16, K_CHUNK_ATTN = 17, K_CHUNK_MERGE = 18, K_WEIGHT_SUMS = 19, K_EVICT_SELECT = 20, K_EVICT_MOVE = 21, K_TOKEN_LOGPROBS = 22, K_CHUNK_WIDE = 23, K_COUNT = 24 };
 
 void set_error(const char *fmt, ...);
 
@@ -145,11 +145,13 @@ int32_t launch_fourbit_rows(const mcsd_rows_desc &d, const mcsd_rows_bufs &b, co
 // ---- prompts in chunks over a paged cache -----------------------------------
 struct ChunkPlan {
     int many;                   // rows beyond which a sequence belongs to the wide kernel
-    int target, target_many;    // workgroups per KV head aimed at where keys are cut, of either kernel
+    int by_work;                // 1: where those have most of the work
+    int at_once, at_once_many;  // workgroups per KV head that the chip takes at once, of either kernel
     int min_seg;                // key tiles of a segment at least
     int max_items, max_items_many;      // workgroups per KV head at most
     int max_cut;                // row tiles whose keys are cut at most
-    int max_parts;              // partial results per KV head at most, in blocks of 32 rows (0: nothing is cut)
+    int merge_y;                // workgroups of the merge for each
+    int max_parts, max_parts_many;      // partial results of either kernel per KV head at most, in blocks of 32 rows (0: nothing is cut)
     size_t ws_bytes;
 };
 bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan);
