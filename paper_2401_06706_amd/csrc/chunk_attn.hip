@@ -9,14 +9,25 @@ namespace {
 
 constexpr int OFF_NOWHERE = 0x7fff0000; // an offset beyond every buffer's extent: reads as zero
 
-template <int DP, bool F32>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * (F32 ? 4 : 2) <= 256 ? 2 : 1)))
+// softmax(scale Q K^T) V of a tile of rows over a segment of its keys, one pass: with a running maximum m, weights 2^(s c - m) and their
+// sum l, o = sum w V; out = o / l, lse = (m + log2 l) ln 2, or (o, m, l) as a partial result.
+// 32 keys at a time stand in LDS, two tiles more are on their way in registers.  Four wavefronts take 32 rows each; or (SPLIT) all take the same
+// 32, form the scores together (fp32: a quarter of the contraction each, summed in a fixed order through LDS; bf16: all of them, which is
+// cheaper) and the output a quarter of the columns each: a lone token's few rows then keep four matrix units busy, and its tiles leave
+// registers for three workgroups a compute unit.
+// A decoding batch is bound by the reading of its keys and values: 32 sequences of 100 to 8000 tokens, 32/8 heads, d = 128: 116 us, 4.7 TB/s.
+template <int DP, bool F32, bool SPLIT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(F32 && DP == 256 ? 1 : 2)))
 void chunk_attn_kernel(ChunkParams p)
 {
     using S = TileShape<DP, F32>;
-    constexpr int NT = DP / 32, BUF_WORDS = KT * (S::PK + S::PV);
+    constexpr int ROWS = SPLIT ? ROWS_SPLIT : ROWS_FEW, BUF_WORDS = KT * (S::PK + S::PV);
+    constexpr int NT = SPLIT ? (DP / 32 + 3) / 4 : DP / 32;             // column tiles of a wavefront
+    constexpr bool SHARE = SPLIT && F32;                                // the products of the scores are shared out too
+    constexpr int KK = SHARE ? S::KK / 4 : S::KK;
     constexpr bool TWO_TERMS = !F32 && DP != 128;       // of the weights in PV, as in tree attention
-    __shared__ __attribute__((aligned(16))) uint32_t s_tiles[2 * BUF_WORDS];
+    __shared__ __attribute__((aligned(16))) uint32_t s_tiles[(SHARE ? 1 : 2) * BUF_WORDS];
+    __shared__ __attribute__((aligned(16))) float s_share[SHARE ? 4 : 1][4][64][4];
     __shared__ int s_bad;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -29,11 +40,13 @@ void chunk_attn_kernel(ChunkParams p)
         if (tid == 0) *p.notes = {0, list.many, list.len, len_many};
     }
     if (!list.find(p, blockIdx.x / p.H_kv, lane, &it)) return;
-    const int M = it.s.n * p.G, row0 = it.rt * ROWS_FEW + 32 * wave;
+    const int M = it.s.n * p.G, row0 = it.rt * ROWS + (SPLIT ? 0 : 32 * wave);
+    const int nt0 = SPLIT && NT * wave < DP / 32 ? NT * wave : 0, kk0 = SHARE ? KK * wave : 0;
+    const bool writes = !SPLIT || NT * wave < DP / 32;          // (96 columns are three tiles)
     auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
-    const int kt = position(min(it.rt * ROWS_FEW + ROWS_FEW, M) - 1) / KT + 1;           // key tiles that some row of this tile sees
+    const int kt = position(min(it.rt * ROWS + ROWS, M) - 1) / KT + 1;           // key tiles that some row of this tile sees
     const int seg = (kt + it.n_seg - 1) / it.n_seg, t_begin = it.seg * seg, t_end = min(kt, t_begin + seg);
-    const int diagonal = (position(it.rt * ROWS_FEW) + 1) / KT;                    // from this tile on there are keys that some row does not see
+    const int diagonal = (position(it.rt * ROWS) + 1) / KT;                    // from this tile on there are keys that some row does not see
     const bool active = row0 < M;
     const int my_row = min(row0 + l32, M - 1), my_pos = position(my_row);
     // tiles that every row of this wavefront sees whole; tiles that any of them sees
@@ -41,13 +54,13 @@ void chunk_attn_kernel(ChunkParams p)
     const int t_seen = active ? min(t_end, position(min(row0 + 32, M) - 1) / KT + 1) : t_begin;
     if (tid == 0) s_bad = 0;
 
-    u32x4 q[S::KK];
+    u32x4 q[KK];
     {
         const int head = g * p.G + my_row % p.G;
         const char *src = static_cast<const char *>(p.q) + (size_t)(it.s.s0 + my_row / p.G) * p.q_row + (size_t)head * p.d * S::ES;
 #pragma unroll
-        for (int kk = 0; kk < S::KK; ++kk) {
-            const int at = 32 * kk + 16 * h;
+        for (int kk = 0; kk < KK; ++kk) {
+            const int at = 32 * (kk0 + kk) + 16 * h;
             const u32x4 zero = {0, 0, 0, 0};
             q[kk] = DP * S::ES == 256 && p.d == DP ? *reinterpret_cast<const u32x4 *>(src + at)
                                                    : (at < p.d * S::ES ? *reinterpret_cast<const u32x4 *>(src + at) : zero);
@@ -101,15 +114,30 @@ void chunk_attn_kernel(ChunkParams p)
                 *reinterpret_cast<u32x4 *>(buf + v_st[j]) = vr[st][j];
             }
     };
-    const uint32_t k_ld = l32 * S::PK + 4 * h;
-    const uint32_t v_ld = F32 ? KT * S::PK + 4 * h * S::PV + l32
-                              : KT * S::PK + (4 * h + (lc >> 2)) * S::PV + 8 * (lj & 1) + 2 * (lc & 3);
+    const uint32_t k_ld = l32 * S::PK + 4 * h + 8 * kk0;
+    const uint32_t v_ld = F32 ? KT * S::PK + 4 * h * S::PV + l32 + 32 * nt0
+                              : KT * S::PK + (4 * h + (lc >> 2)) * S::PV + 8 * (lj & 1) + 2 * (lc & 3) + 16 * nt0;
     typedef short v4i16 __attribute__((ext_vector_type(4)));
     typedef v4i16 __attribute__((address_space(3))) *lds_v4i16_ptr;
 
     auto compute = [&](int t, const uint32_t *cb, auto masked_tag) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_tag)::value;
-        f32x16 s = tile_scores<DP, F32>(cb + k_ld, q);
+        f32x16 s = tile_scores<KK, F32>(cb + k_ld, q);
+        if constexpr (SHARE) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(s_share[wave][i][lane]) = make_float4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+            __syncthreads();            // (what is read here has been read by all before the next step's first barrier)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float4 x = *reinterpret_cast<const float4 *>(s_share[0][i][lane]);
+#pragma unroll
+                for (int w = 1; w < 4; ++w) {
+                    const float4 y = *reinterpret_cast<const float4 *>(s_share[w][i][lane]);
+                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                }
+                s[4 * i] = x.x; s[4 * i + 1] = x.y; s[4 * i + 2] = x.z; s[4 * i + 3] = x.w;
+            }
+        }
         const int seen = my_pos - t * KT - 4 * h;       // key_of_score(i) <= seen: row sees it
         float w[16], sum;
         auto weights = [&]() __attribute__((always_inline)) {
@@ -177,18 +205,26 @@ void chunk_attn_kernel(ChunkParams p)
 
     // Tile t is in buffer t % 2 of LDS behind the barrier of its step; t + 1 is stored and t + 3 asked for during it.
     auto step = [&](int t, auto stage) __attribute__((always_inline)) {
-        constexpr int ST = decltype(stage)::value;
+        constexpr int ST = decltype(stage)::value, BUF = SHARE ? 0 : ST;
         __syncthreads();
-        store_kv(t + 1, s_tiles + (ST ^ 1) * BUF_WORDS, ST ^ 1);
-        load_kv(t + 3, ST ^ 1);
-        if (t < t_plain) compute(t, s_tiles + ST * BUF_WORDS, std::false_type());
-        else if (t < t_seen) compute(t, s_tiles + ST * BUF_WORDS, std::true_type());
+        if constexpr (SHARE) {
+            store_kv(t, s_tiles, ST);
+            load_kv(t + 2, ST);
+            __syncthreads();
+        } else {
+            store_kv(t + 1, s_tiles + (ST ^ 1) * BUF_WORDS, ST ^ 1);
+            load_kv(t + 3, ST ^ 1);
+        }
+        if (t < t_plain) compute(t, s_tiles + BUF * BUF_WORDS, std::false_type());
+        else if (t < t_seen) compute(t, s_tiles + BUF * BUF_WORDS, std::true_type());
     };
     int t = t_begin;
     load_kv(t, 0);
     load_kv(t + 1, 1);
-    store_kv(t, s_tiles, 0);
-    load_kv(t + 2, 0);
+    if constexpr (!SHARE) {
+        store_kv(t, s_tiles, 0);
+        load_kv(t + 2, 0);
+    }
     for (; t + 1 < t_end; t += 2) {
         step(t, std::integral_constant<int, 0>());
         step(t + 1, std::integral_constant<int, 1>());
@@ -196,28 +232,28 @@ void chunk_attn_kernel(ChunkParams p)
     if (t < t_end) step(t, std::integral_constant<int, 0>());
     if (__any(bad) && lane == 0) s_bad = 1;
     __syncthreads();
-    if (!active) return;
+    if (!active || !writes) return;
 
-    // ---- epilogue: a lane holds columns 32 nt + 8 a + 4 h .. + 3 of its row
+    // ---- epilogue: a lane holds columns 32 nt + 8 a + 4 h .. + 3 of its row, nt from its wavefront's first tile on
     const float l_row = l_part + __shfl_xor(l_part, 32);
     if (row0 + l32 >= M) return;
     const int token = it.s.s0 + my_row / p.G, head = g * p.G + my_row % p.G;
     const bool direct = it.n_seg == 1;
     // row of out and lse, or of the partial results
-    const size_t at = direct ? (size_t)token * p.H_q + head : ((size_t)(it.part + wave) * p.H_kv + g) * 32 + l32;
+    const size_t at = direct ? (size_t)token * p.H_q + head : ((size_t)(it.part + (SPLIT ? 0 : wave)) * p.H_kv + g) * 32 + l32;
     const float f = direct ? 1.0f / l_row : 1.0f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            const int c = 32 * nt + 8 * a + 4 * h;
+            const int c = 32 * (nt0 + nt) + 8 * a + 4 * h;
             const float4 x = make_float4(o[nt][4 * a] * f, o[nt][4 * a + 1] * f, o[nt][4 * a + 2] * f, o[nt][4 * a + 3] * f);
             if (!direct) *reinterpret_cast<float4 *>(p.part_o + at * DP + c) = x;
             else if (c >= p.d) continue;
             else if (F32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at * p.d + c) = x;
             else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at * p.d + c) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
         }
-    if (h == 0) {
+    if (h == 0 && (!SPLIT || wave == 0)) {
         if (!direct) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(m_used, l_row);
         else if (p.lse) p.lse[at] = (m_used + __builtin_amdgcn_logf(l_row)) * LN2_F;
     }
@@ -227,7 +263,7 @@ void chunk_attn_kernel(ChunkParams p)
             const int page = p.block_table[(size_t)it.b * p.max_pages + key / p.page_size];
             if ((unsigned)page >= (unsigned)p.n_pages) continue;
             const char *v = static_cast<const char *>(p.v_pool) + (((size_t)page * p.H_kv + g) * p.page_size + key % p.page_size) * row_bytes;
-            for (int c = 4 * h; c < p.d; c += (c & 3) == 3 ? 5 : 1) {
+            for (int c = 32 * nt0 + 4 * h; c < min(p.d, 32 * (nt0 + NT)); c += (c & 3) == 3 ? 5 : 1) {
                 const float y = F32 ? reinterpret_cast<const float *>(v)[c] : bf16_bits_to_float(reinterpret_cast<const uint16_t *>(v)[c]);
                 if (fabsf(y) < INFINITY) continue;
                 if (!direct) {
@@ -374,12 +410,27 @@ __global__ __launch_bounds__(256) void kv_store_paged_kernel(StoreParams p)
     *reinterpret_cast<u32x4 *>(p.v_pool + at) = v;
 }
 
+// Where a workgroup takes 32 rows and shares out the columns, instead of 128 rows.  32 sequences on 100 to 8000 tokens, 32/8 heads, us of the
+// attention with 128 rows and with 32:
+//   bf16, d = 128, 4 rows each 133, 115; 32 rows 133, 117; 48 rows 138, 169.  d = 80, 4 rows 111, 92; d = 96, 48 rows 120, 168.
+//   d = 64, 4 rows 68, 77: two wavefronts of the four would have columns.
+//   fp32, where a wavefront's products take longer than its tiles to come: d = 128, 4 rows 735, 297; 8 prompts of 200 to 500 tokens 181, 157;
+//   d = 96, 573, 247 and 143, 135; d = 64, 259, 198 and 90, 118.
+//   d = 256, where 128 rows need more registers than there are: bf16, 4 rows 676, 233; 8 prompts of 500 to 1000 tokens 425, 374; fp32 523, 121.
+enum Split { NO_SPLIT, SPLIT_FEW, ALWAYS_SPLIT };
+constexpr Split split_rule(int DP, bool f32)
+{
+    return DP == 256 || (f32 && DP >= 96) ? ALWAYS_SPLIT : (f32 ? DP == 64 : DP >= 96) ? SPLIT_FEW : NO_SPLIT;
+}
+
 int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
 
 template <int DP, bool F32>
 void launch_shape(const ChunkParams &p, const ChunkPlan &plan, hipStream_t stream)
 {
-    launch_kernel(K_CHUNK_ATTN, chunk_attn_kernel<DP, F32>, dim3(p.H_kv * plan.max_items), dim3(256), stream, p);
+    constexpr Split rule = split_rule(DP, F32);
+    const auto kernel = plan.rows_few == ROWS_SPLIT ? chunk_attn_kernel<DP, F32, rule != NO_SPLIT> : chunk_attn_kernel<DP, F32, rule == ALWAYS_SPLIT>;
+    launch_kernel(K_CHUNK_ATTN, kernel, dim3(p.H_kv * plan.max_items), dim3(256), stream, p);
     if (plan.max_items_many) launch_chunk_wide(p, plan.max_items_many, stream);
     if (plan.max_parts + plan.max_parts_many)
         launch_kernel(K_CHUNK_MERGE, chunk_merge_kernel<DP, F32>, dim3(p.H_kv * plan.max_cut, plan.merge_y), dim3(256), stream, p);
@@ -416,6 +467,9 @@ bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
     // 32/32 heads: 158 us, 204 in one kernel).
     const bool many = d.dtype == MCSD_DTYPE_BF16 && d.d == 128 && T * G > (long)MANY * d.B;
     plan->many = many ? MANY : NEVER_MANY;
+    const Split rule = split_rule(padded_dim(d.d), d.dtype == MCSD_DTYPE_FP32);
+    const bool split = rule == ALWAYS_SPLIT || (rule == SPLIT_FEW && T * G <= (long)ROWS_SPLIT * d.B);
+    plan->rows_few = split ? ROWS_SPLIT : ROWS_FEW;
     plan->by_work = many && T * G <= (long)ROWS_MANY * d.B;
     // Segments of 8 tiles at least.  A sequence that is cut has kt / len of them, of few rows rounded up, 2 kt / len at most, of many to nearest,
     // 4/3 kt / len at most.  Two workgroups of few rows run on a compute unit, one of many.
@@ -425,7 +479,7 @@ bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
     const long target = 2L * plan->at_once, target_many = (long)(cut_at(CUTS - 1) * plan->at_once_many);
     const long n_seg = (kt + plan->min_seg - 1) / plan->min_seg;
     // (a sequence of few rows is one row tile where those of many are not here)
-    const long tiles = many && !plan->by_work ? (T < d.B ? T : d.B) : most_tiles(T, d.B, G, ROWS_FEW), tiles_many = many ? most_tiles(T, d.B, G, ROWS_MANY) : 0;
+    const long tiles = many && !plan->by_work ? (T < d.B ? T : d.B) : most_tiles(T, d.B, G, plan->rows_few), tiles_many = many ? most_tiles(T, d.B, G, ROWS_MANY) : 0;
     // a sequence of n segments has its keys cut where n >= 2
     auto parts_of = [&](long most, long row_tiles) { return n_seg < 2 ? 0 : most < row_tiles * n_seg ? most : row_tiles * n_seg; };
     auto less = [](long x, long y) { return x < y ? x : y; };
@@ -435,12 +489,12 @@ bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
     auto items_of = [&](long target, long row_tiles) { return n_seg < 2 ? row_tiles : target + row_tiles < row_tiles * n_seg ? target + row_tiles : row_tiles * n_seg; };
     const long items = items_of(target, tiles), items_many = tiles_many ? items_of(target_many, tiles_many) : 0;
     const long cut = parts / 2 < tiles ? parts / 2 : tiles, cut_many = parts_many / 2 < tiles_many ? parts_many / 2 : tiles_many;
-    const long rows = many ? ROWS_MANY : ROWS_FEW, cells = 2048 / (d.H_kv * (cut + cut_many) + 1);
+    const long rows = many ? ROWS_MANY : plan->rows_few, cells = 2048 / (d.H_kv * (cut + cut_many) + 1);
     plan->merge_y = (int)(cells < rows / 32 ? rows / 32 : cells < rows ? cells : rows);
     plan->max_items = (int)items;
     plan->max_items_many = (int)items_many;
     plan->max_cut = (int)(cut + cut_many);
-    plan->max_parts = (int)(parts * (ROWS_FEW / 32));
+    plan->max_parts = (int)(parts * (plan->rows_few / 32));
     plan->max_parts_many = (int)(parts_many * (ROWS_MANY / 32));
     const size_t rows_cut = (size_t)(plan->max_parts + plan->max_parts_many) * d.H_kv * 32;
     plan->ws_bytes = rows_cut || many ? (rows_cut * (padded_dim(d.d) + 2) * 4 + 255) / 256 * 256 + 256 : 0;
@@ -451,7 +505,7 @@ int32_t launch_chunk_attn(const mcsd_chunk_desc &d, const mcsd_chunk_bufs &b, co
 {
     ChunkParams p = chunk_params(d, kv);
     p.q = b.q; p.k_pool = b.k_pool; p.v_pool = b.v_pool; p.chunk_start = b.chunk_start; p.prefix_len = b.prefix_len; p.out = b.out; p.lse = b.lse;
-    p.min_seg = plan.min_seg; p.max_parts = plan.max_parts; p.max_parts_many = plan.max_parts_many; p.many = plan.many; p.by_work = plan.by_work;
+    p.min_seg = plan.min_seg; p.max_parts = plan.max_parts; p.max_parts_many = plan.max_parts_many; p.many = plan.many; p.by_work = plan.by_work; p.rows_few = plan.rows_few;
     p.at_once = (float)plan.at_once; p.at_once_many = (float)plan.at_once_many;
     p.part_o = static_cast<float *>(b.workspace);
     const size_t parts = (size_t)(plan.max_parts + plan.max_parts_many) * d.H_kv * 32;

@@ -36,6 +36,7 @@ struct ChunkParams {
     int B, T, H_q, H_kv, G, d, L_stride, page_size, n_pages, max_pages;
     FastDiv group;        // by G
     int many, by_work;    // rows beyond which a sequence belongs to the wide kernel; 1: where those have most of the work
+    int rows_few;         // ROWS_FEW, or ROWS_SPLIT
     int min_seg, max_parts, max_parts_many;
     float at_once, at_once_many;    // workgroups per KV head that the chip takes at once, of either kernel
     size_t q_row;         // bytes from a row of q to the next one's
@@ -113,7 +114,7 @@ __device__ __forceinline__ float wave_max(float v) { return wave_reduce<true>(v)
 // kt / length of them, rounded up (few rows: a partial result is small) or to nearest.
 // Every workgroup works out the same list, a sequence a lane; the length of segments of many rows takes longer and is left by the kernel for few
 // (worked out by all workgroups: 10 to 40 us a launch).  Partial results are numbered in blocks of 32 rows, row tile by row tile, segment by segment.
-constexpr int ROWS_FEW = 128, ROWS_MANY = 256, MANY = 64, NEVER_MANY = 0x7fffffff;
+constexpr int ROWS_SPLIT = 32, ROWS_FEW = 128, ROWS_MANY = 256, MANY = 64, NEVER_MANY = 0x7fffffff;
 // segments aimed at, times the workgroups at once
 constexpr int CUTS = 4;
 __host__ __device__ constexpr float cut_at(int j) { return j == 0 ? 1.f : j == 1 ? 1.5f : j == 2 ? 2.f : 3.f; }
@@ -134,7 +135,7 @@ struct ChunkWork {
     __device__ __forceinline__ bool has_many(const ChunkParams &p, const ChunkSeq &q) const { return q.n * p.G > many; }
     __device__ __forceinline__ int row_tiles(const ChunkParams &p, const ChunkSeq &q) const
     {
-        return has_many(p, q) ? (q.n * p.G + ROWS_MANY - 1) / ROWS_MANY : (q.n * p.G + ROWS_FEW - 1) / ROWS_FEW;
+        return has_many(p, q) ? (q.n * p.G + ROWS_MANY - 1) / ROWS_MANY : (q.n * p.G + p.rows_few - 1) / p.rows_few;
     }
     // f(many rows?, row tiles, key tiles) of every sequence
     template <class F>
@@ -217,7 +218,7 @@ struct ItemList : ChunkWork {
         const bool many = has_many(p, s);
         const int kt = (s.keys + KT - 1) / KT;
         rt = row_tiles(p, s);
-        blocks = (many ? ROWS_MANY : ROWS_FEW) / 32;
+        blocks = (many ? ROWS_MANY : p.rows_few) / 32;
         n_seg = 1;
         if (many && p.max_parts_many && KIND != FEW_ROWS) n_seg = segments<true>(kt, len_many);
         if (!many && p.max_parts && KIND != MANY_ROWS) n_seg = segments<false>(kt, len);
@@ -301,17 +302,17 @@ struct TileShape {
     static constexpr int KK = DP / (F32 ? 8 : 16);                       // 16-byte operand pieces a lane holds of a row
 };
 
-// scores of 32 keys x 32 rows: s = K Q^T, K from LDS rows at `k` (this lane's row and half), q this lane's row in registers.
+// scores of 32 keys x 32 rows, of KK 16-byte pieces of them: s = K Q^T, K from LDS rows at `k` (this lane's row and half), q this lane's row in registers.
 // Score i of a lane is key 8 (i / 4) + 4 h + i % 4 of row lane % 32, h = lane / 32.  (bf16: the pieces of a lane are the operands of
 // v_mfma_f32_32x32x16_bf16; fp32: v_mfma_f32_32x32x2_f32 takes the contraction four values of a piece after the other)
-template <int DP, bool F32>
+template <int KK, bool F32>
 __device__ __forceinline__ f32x16 tile_scores(const uint32_t *k, const u32x4 *q)
 {
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < TileShape<DP, F32>::KK; ++kk) {
+    for (int kk = 0; kk < KK; ++kk) {
         const u32x4 a = *reinterpret_cast<const u32x4 *>(k + 8 * kk);
         if constexpr (F32) {
 #pragma unroll
