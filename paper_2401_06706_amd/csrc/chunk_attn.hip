@@ -16,7 +16,7 @@ constexpr int OFF_NOWHERE = 0x7fff0000; // an offset beyond every buffer's exten
 // cheaper) and the output a quarter of the columns each: a lone token's few rows then keep four matrix units busy, and its tiles leave
 // registers for three workgroups a compute unit.
 // A decoding batch is bound by the reading of its keys and values: 32 sequences of 100 to 8000 tokens, 32/8 heads, d = 128: 116 us, 4.7 TB/s.
-template <int DP, bool F32, bool SPLIT>
+template <int DP, bool F32, bool SPLIT, bool TWO_TERMS>      // TWO_TERMS: of the weights in PV, as in tree attention
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(F32 && DP == 256 ? 1 : 2)))
 void chunk_attn_kernel(ChunkParams p)
 {
@@ -25,7 +25,6 @@ void chunk_attn_kernel(ChunkParams p)
     constexpr int NT = SPLIT ? (DP / 32 + 3) / 4 : DP / 32;             // column tiles of a wavefront
     constexpr bool SHARE = SPLIT && F32;                                // the products of the scores are shared out too
     constexpr int KK = SHARE ? S::KK / 4 : S::KK;
-    constexpr bool TWO_TERMS = !F32 && DP != 128;       // of the weights in PV, as in tree attention
     __shared__ __attribute__((aligned(16))) uint32_t s_tiles[(SHARE ? 1 : 2) * BUF_WORDS];
     __shared__ __attribute__((aligned(16))) float s_share[SHARE ? 4 : 1][4][64][4];
     __shared__ int s_bad;
@@ -429,7 +428,11 @@ template <int DP, bool F32>
 void launch_shape(const ChunkParams &p, const ChunkPlan &plan, hipStream_t stream)
 {
     constexpr Split rule = split_rule(DP, F32);
-    const auto kernel = plan.rows_few == ROWS_SPLIT ? chunk_attn_kernel<DP, F32, rule != NO_SPLIT> : chunk_attn_kernel<DP, F32, rule == ALWAYS_SPLIT>;
+    constexpr bool FEW = rule != NO_SPLIT, MORE = rule == ALWAYS_SPLIT;         // SPLIT of either number of rows
+    const bool few = plan.rows_few == ROWS_SPLIT;
+    auto kernel = few ? chunk_attn_kernel<DP, F32, FEW, !F32> : chunk_attn_kernel<DP, F32, MORE, !F32>;
+    if constexpr (!F32 && DP == 128)
+        if (p.d == DP) kernel = few ? chunk_attn_kernel<DP, F32, FEW, false> : chunk_attn_kernel<DP, F32, MORE, false>;
     launch_kernel(K_CHUNK_ATTN, kernel, dim3(p.H_kv * plan.max_items), dim3(256), stream, p);
     if (plan.max_items_many) launch_chunk_wide(p, plan.max_items_many, stream);
     if (plan.max_parts + plan.max_parts_many)

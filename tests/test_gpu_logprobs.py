@@ -122,3 +122,14 @@ def test_rows_that_start_anywhere(shift, dtype):
 def test_no_rows():
     run(torch.randn(3, 100, device=DEV), [], 5)
     run(torch.randn(3, 100, device=DEV), [], 0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,V,n_top", [(257, 515, 3), (300, 2500, 20), (700, 33, 40), (2000, 1, 1)])
+def test_more_rows_than_workgroups(rows, V, n_top, dtype):
+    """Where a row is shared by half as many threads, with row_map backwards, one row named twice and some beyond the last."""
+    logits = (3 * torch.randn(rows, V + 5, generator=gen(rows))).to(dtype).to(DEV)[:, :V]
+    row_map = [rows - 1 - i for i in range(rows)]
+    row_map[7], row_map[8], row_map[9] = row_map[6], rows, -1
+    tokens = torch.randint(0, V, (rows,), generator=gen(V)).tolist()
+    check(logits, tokens, min(n_top, V), [0.5 + (i % 5) / 2 for i in range(rows)], row_map)
