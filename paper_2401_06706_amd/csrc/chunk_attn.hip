@@ -31,32 +31,32 @@ void chunk_attn_kernel(ChunkParams p)
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, l32 = lane & 31, lj = lane >> 4, lc = lane & 15;
-    const int g = blockIdx.x % p.H_kv;          // (KV head fastest: the row tiles of one meet in one XCD's L2 where their number is a multiple of 8)
+    const int in_head = uniform(blockIdx.x / p.H_kv), g = blockIdx.x - in_head * p.H_kv;        // (KV head fastest: the row tiles of one meet in one XCD's L2 where their number is a multiple of 8)
     Item it;
     const ItemList<FEW_ROWS> list(p, lane);
     if (p.notes && blockIdx.x == gridDim.x - 1) {           // (as a rule it has no item)
         const int len_many = p.max_parts_many ? list.many_segment(p, lane) : 0;
         if (tid == 0) *p.notes = {0, list.many, list.len, len_many};
     }
-    if (!list.find(p, blockIdx.x / p.H_kv, lane, &it)) return;
+    if (!list.find(p, in_head, lane, &it)) return;
     const int M = it.s.n * p.G, row0 = it.rt * ROWS + (SPLIT ? 0 : 32 * wave);
     const int nt0 = SPLIT && NT * wave < DP / 32 ? NT * wave : 0, kk0 = SHARE ? KK * wave : 0;
     const bool writes = !SPLIT || NT * wave < DP / 32;          // (96 columns are three tiles)
-    auto position = [&](int row) { return min(it.s.L + row / p.G, it.s.keys - 1); };
-    const int kt = position(min(it.rt * ROWS + ROWS, M) - 1) / KT + 1;           // key tiles that some row of this tile sees
-    const int seg = (kt + it.n_seg - 1) / it.n_seg, t_begin = it.seg * seg, t_end = min(kt, t_begin + seg);
-    const int diagonal = (position(it.rt * ROWS) + 1) / KT;                    // from this tile on there are keys that some row does not see
+    auto position = [&](int row) { return min(it.s.L + by_group(p, row), it.s.keys - 1); };
+    const int kt = uniform(position(min(it.rt * ROWS + ROWS, M) - 1)) / KT + 1;           // key tiles that some row of this tile sees
+    const int seg = uniform((kt + it.n_seg - 1) / it.n_seg), t_begin = it.seg * seg, t_end = min(kt, t_begin + seg);
+    const int diagonal = (uniform(position(it.rt * ROWS)) + 1) / KT;                    // from this tile on there are keys that some row does not see
     const bool active = row0 < M;
     const int my_row = min(row0 + l32, M - 1), my_pos = position(my_row);
     // tiles that every row of this wavefront sees whole; tiles that any of them sees
-    const int t_plain = active ? min(t_end, (position(row0) + 1) / KT) : t_begin;
-    const int t_seen = active ? min(t_end, position(min(row0 + 32, M) - 1) / KT + 1) : t_begin;
+    const int t_plain = active ? min(t_end, (uniform(position(row0)) + 1) / KT) : t_begin;
+    const int t_seen = active ? min(t_end, uniform(position(min(row0 + 32, M) - 1)) / KT + 1) : t_begin;
     if (tid == 0) s_bad = 0;
 
     u32x4 q[KK];
     {
-        const int head = g * p.G + my_row % p.G;
-        const char *src = static_cast<const char *>(p.q) + (size_t)(it.s.s0 + my_row / p.G) * p.q_row + (size_t)head * p.d * S::ES;
+        const int token = by_group(p, my_row), head = g * p.G + my_row - token * p.G;
+        const char *src = static_cast<const char *>(p.q) + (size_t)(it.s.s0 + token) * p.q_row + (size_t)head * p.d * S::ES;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
             const int at = 32 * (kk0 + kk) + 16 * h;
@@ -80,15 +80,19 @@ void chunk_attn_kernel(ChunkParams p)
     for (int j = 0; j < S::PER_THREAD; ++j) {
         const int e = tid + 256 * j, row = e / S::GRANULES, c = e % S::GRANULES;
         load_at[j] = e < KT * S::GRANULES && 16 * c < row_bytes ? row * row_bytes + 16 * c : OFF_NOWHERE;
+        if (j && 256 % S::GRANULES == 0) load_at[j] = load_at[0] + j * (256 / S::GRANULES) * row_bytes;         // (the same column: one register holds them)
         k_st[j] = row * S::PK + 4 * c;
         v_st[j] = KT * S::PK + row * S::PV + 4 * c;
     }
     const const_i32_ptr table = (const_i32_ptr)(uintptr_t)(p.block_table + (size_t)it.b * p.max_pages);
     u32x4 kr[2][S::PER_THREAD], vr[2][S::PER_THREAD];
+    // tiles are asked for one after the other, from t_begin on
+    const int page_size = uniform(p.page_size);
+    int entry = uniform(t_begin * KT / page_size), in_page = t_begin * KT - entry * page_size;
     auto load_kv = [&](int t, int st) __attribute__((always_inline)) {
-        const int page = t < t_end ? (int)table[t * KT / p.page_size] : -1;
+        const int page = t < t_end ? (int)table[entry] : -1;
         const bool in = (unsigned)page < (unsigned)p.n_pages;
-        const size_t off = in ? (((size_t)page * p.H_kv + g) * p.page_size + t * KT % p.page_size) * row_bytes : 0;
+        const size_t off = in ? (((size_t)page * p.H_kv + g) * page_size + in_page) * row_bytes : 0;
         const uint32_t extent = in ? (uint32_t)max(0, min(KT, it.s.keys - t * KT)) * row_bytes : 0u;
         const __amdgpu_buffer_rsrc_t rk = make_rsrc(static_cast<const char *>(p.k_pool) + off, extent);
         const __amdgpu_buffer_rsrc_t rv = make_rsrc(static_cast<const char *>(p.v_pool) + off, extent);
@@ -97,6 +101,8 @@ void chunk_attn_kernel(ChunkParams p)
             kr[st][j] = __builtin_amdgcn_raw_buffer_load_b128(rk, load_at[j], 0, 0);
             vr[st][j] = __builtin_amdgcn_raw_buffer_load_b128(rv, load_at[j], 0, 0);
         }
+        in_page += KT;
+        if (in_page == page_size) { in_page = 0; ++entry; }
     };
     bool bad = false;
     auto store_kv = [&](int t, uint32_t *buf, int st) __attribute__((always_inline)) {
@@ -236,7 +242,7 @@ void chunk_attn_kernel(ChunkParams p)
     // ---- epilogue: a lane holds columns 32 nt + 8 a + 4 h .. + 3 of its row, nt from its wavefront's first tile on
     const float l_row = l_part + __shfl_xor(l_part, 32);
     if (row0 + l32 >= M) return;
-    const int token = it.s.s0 + my_row / p.G, head = g * p.G + my_row % p.G;
+    const int in_seq = by_group(p, my_row), token = it.s.s0 + in_seq, head = g * p.G + my_row - in_seq * p.G;
     const bool direct = it.n_seg == 1;
     // row of out and lse, or of the partial results
     const size_t at = direct ? (size_t)token * p.H_q + head : ((size_t)(it.part + (SPLIT ? 0 : wave)) * p.H_kv + g) * 32 + l32;
