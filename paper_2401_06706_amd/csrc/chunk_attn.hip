@@ -474,17 +474,21 @@ bool make_chunk_plan(const mcsd_chunk_desc &d, ChunkPlan *plan)
     // rows that have most of the work are bound by memory, and those of many run beside them (32 sequences, four with 200 to 512 tokens, 32/8 heads:
     // 137 us, 159 in two kernels one after the other); otherwise the kernel for many is faster (8 sequences of 128 to 256 tokens on 2000 to 4000,
     // 32/32 heads: 158 us, 204 in one kernel).
-    const bool many = d.dtype == MCSD_DTYPE_BF16 && d.d == 128 && T * G > (long)MANY * d.B;
+    // Little work of many rows stays with the kernel for few, too.  What the sizes say of the work: at least `least` (sequences of one length
+    // without cached tokens), at most all row tiles by the capacity.
+    // Two workgroups of few rows run on a compute unit, one of many.
+    plan->at_once = d.H_kv < 512 ? 512 / d.H_kv : 1;
+    plan->at_once_many = d.H_kv < 256 ? 256 / d.H_kv : 1;
+    const double small = SMALL_WORK * plan->at_once_many, least = (double)T * T * G / ((double)ROWS_MANY * KT * d.B);
+    const bool many = d.dtype == MCSD_DTYPE_BF16 && d.d == 128 && T * G > (long)MANY * d.B && (double)most_tiles(T, d.B, G, ROWS_MANY) * kt >= small;
     plan->many = many ? MANY : NEVER_MANY;
+    plan->by_work = many && (T * G <= (long)ROWS_MANY * d.B || least < small);
     const Split rule = split_rule(padded_dim(d.d), d.dtype == MCSD_DTYPE_FP32);
     const bool split = rule == ALWAYS_SPLIT || (rule == SPLIT_FEW && T * G <= (long)ROWS_SPLIT * d.B);
     plan->rows_few = split ? ROWS_SPLIT : ROWS_FEW;
-    plan->by_work = many && T * G <= (long)ROWS_MANY * d.B;
     // Segments of 8 tiles at least.  A sequence that is cut has kt / len of them, of few rows rounded up, 2 kt / len at most, of many to nearest,
-    // 4/3 kt / len at most.  Two workgroups of few rows run on a compute unit, one of many.
+    // 4/3 kt / len at most.
     plan->min_seg = 8;
-    plan->at_once = d.H_kv < 512 ? 512 / d.H_kv : 1;
-    plan->at_once_many = d.H_kv < 256 ? 256 / d.H_kv : 1;
     const long target = 2L * plan->at_once, target_many = (long)(cut_at(CUTS - 1) * plan->at_once_many);
     const long n_seg = (kt + plan->min_seg - 1) / plan->min_seg;
     // (a sequence of few rows is one row tile where those of many are not here)

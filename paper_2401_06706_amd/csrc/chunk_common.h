@@ -35,7 +35,7 @@ struct ChunkParams {
     struct ChunkNotes *notes;
     int B, T, H_q, H_kv, G, d, L_stride, page_size, n_pages, max_pages;
     FastDiv group;        // by G
-    int many, by_work;    // rows beyond which a sequence belongs to the wide kernel; 1: where those have most of the work
+    int many, by_work;    // rows beyond which a sequence belongs to the wide kernel; 1: where those have enough of the work
     int rows_few;         // ROWS_FEW, or ROWS_SPLIT
     int min_seg, max_parts, max_parts_many;
     float at_once, at_once_many;    // workgroups per KV head that the chip takes at once, of either kernel
@@ -115,6 +115,11 @@ __device__ __forceinline__ float wave_max(float v) { return wave_reduce<true>(v)
 // Every workgroup works out the same list, a sequence a lane; the length of segments of many rows takes longer and is left by the kernel for few
 // (worked out by all workgroups: 10 to 40 us a launch).  Partial results are numbered in blocks of 32 rows, row tile by row tile, segment by segment.
 constexpr int ROWS_SPLIT = 32, ROWS_FEW = 128, ROWS_MANY = 256, MANY = 64, NEVER_MANY = 0x7fffffff;
+// Key tiles of many rows a workgroup at once, below which they do not pay for a kernel of their own (each item 8 tiles' time, the launch 4 us):
+// us with the kernel for many rows and without it, work in tiles: one prompt of 512 tokens, 32/8 heads (4) 36.8, 30.2; 8 of 128 to 256, 32/32
+// heads (6) 36.5, 35.0; 32 of 32 to 64 on 0 to 512, 32/8 heads (10) 68.9, 62.7; one of 256 on 4096, 32/8 heads (17) 50, 70; 8 of 64 to 128
+// on 64 to 4096 (24) 78, 97.
+constexpr float SMALL_WORK = 12.f;
 // segments aimed at, times the workgroups at once
 constexpr int CUTS = 4;
 __host__ __device__ constexpr float cut_at(int j) { return j == 0 ? 1.f : j == 1 ? 1.5f : j == 2 ? 2.f : 3.f; }
@@ -161,7 +166,7 @@ struct ChunkWork {
             work = wave_sum(work);
         };
         sum();
-        if (p.by_work && many != NEVER_MANY && wave_sum(work_many) < work) {
+        if (p.by_work && many != NEVER_MANY && wave_sum(work_many) < fmaxf(work, SMALL_WORK * p.at_once_many)) {
             many = NEVER_MANY;
             sum();
         }

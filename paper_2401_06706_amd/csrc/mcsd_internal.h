@@ -145,7 +145,7 @@ int32_t launch_fourbit_rows(const mcsd_rows_desc &d, const mcsd_rows_bufs &b, co
 // ---- prompts in chunks over a paged cache -----------------------------------
 struct ChunkPlan {
     int many;                   // rows beyond which a sequence belongs to the wide kernel
-    int by_work;                // 1: where those have most of the work
+    int by_work;                // 1: where those have enough of the work
     int rows_few;               // of a row tile of the kernel for few rows
     int at_once, at_once_many;  // workgroups per KV head that the chip takes at once, of either kernel
     int min_seg;                // key tiles of a segment at least

@@ -166,3 +166,70 @@ def test_one_sequence_evicted_again_and_again():
         rows, s = rows[at], s[at]
         assert int(prefix) == keep and kept[0, 0, :keep].tolist() == at
         assert torch.equal(sums[0, 0, :keep], s) and torch.equal(R.rows_of(k, table[0], page, keep)[0], rows)
+
+
+WIDE = [  # enough work for the kernel that takes 256 rows a workgroup: (lens, news, H_q, H_kv, page)
+    ([0], [700], 64, 64, 64),
+    ([0], [257], 256, 256, 32),
+    ([63], [257], 256, 128, 32),
+    ([31, 500, 0], [300, 1, 513], 128, 64, 96),
+    ([5000], [100], 64, 8, 128),
+    ([5000, 40, 1], [70, 100, 60], 128, 16, 64),
+    ([1, 2, 3], [22, 129, 400], 384, 128, 32),
+    ([2000, 2016, 2017], [96, 96, 96], 56, 8, 32),
+    ([3000], [64], 256, 16, 32),
+    ([10, 0, 900], [0, 300, 65], 96, 96, 160),
+]
+
+
+@pytest.mark.parametrize("shape", WIDE)
+def test_wide(shape):
+    lens, news, H_q, H_kv, page = shape
+    check(batch(33, torch.bfloat16, lens, news, H_q, H_kv, 128, page), 1 / math.sqrt(128), torch.bfloat16)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1.0])
+def test_wide_scale(scale):
+    check(batch(34, torch.bfloat16, [100, 0], [300, 270], 128, 128, 128, 64), scale, torch.bfloat16)
+
+
+@pytest.mark.parametrize("lens,news,H_kv", [([70], [300], 128), ([2500], [280], 16)])
+def test_wide_no_number(lens, news, H_kv):
+    """Before, inside and behind the tiles that rows see in part, keys in one piece and cut; and in the keys themselves."""
+    b = batch(35, torch.bfloat16, lens, news, H_kv, H_kv, 128, 32)
+    L, n = lens[0], news[0]
+    clean, clean_lse = run(b, 0.1)
+    clean, clean_lse = clean.clone(), clean_lse.clone()
+    for pos in (30, L - 1, L + 5, L + 130, L + n - 1):
+        page, row = int(b["table"][0, pos // 32]), pos % 32
+        old = b["v_pool"][page, :, row].clone()
+        b["v_pool"][page, 0, row, 7], b["v_pool"][page, 1, row, 9] = float("nan"), -float("inf")
+        out, lse = run(b, 0.1)
+        first = max(0, pos - L)
+        want = clean.clone()
+        want[first:, 0, 7], want[first:, 1, 9] = float("nan"), -float("inf")
+        assert torch.equal(lse, clean_lse) and torch.equal(torch.nan_to_num(out.float(), nan=1e30), torch.nan_to_num(want.float(), nan=1e30))
+        b["v_pool"][page, :, row] = old
+    page, row = int(b["table"][0, (L + 50) // 32]), (L + 50) % 32
+    b["k_pool"][page, :, row] = float("nan")
+    out, lse = run(b, 0.1)
+    assert torch.equal(out[:50], clean[:50]) and torch.equal(lse[:50], clean_lse[:50]) and torch.isnan(lse[50:]).all()
+
+
+def test_wide_bad_pages():
+    b = batch(36, torch.bfloat16, [100, 64], [300, 200], 128, 64, 128, 32)
+    b["table"][0, 1], b["table"][0, 5], b["table"][1, 0], b["table"][1, 7] = -1, 2 ** 31 - 1, b["k_pool"].shape[0], -2 ** 31
+    check(b, 0.1, torch.bfloat16)
+
+
+def test_wide_lengths_beyond_the_capacity():
+    b = batch(37, torch.bfloat16, [200], [312], 64, 64, 128, 32)
+    below, bound, _, _ = R.attention(b, 0.1, torch.bfloat16)
+    b["capacity"] = 416
+    out, _ = run(b, 0.1)
+    assert ((out.double() - below).abs() <= bound)[:216].all()         # (not to the bit: fewer keys may be cut elsewhere)
+    v = R.rows_of(b["v_pool"], b["table"][0], 32, 416)
+    k = R.rows_of(b["k_pool"], b["table"][0], 32, 416)
+    want = torch.softmax(torch.einsum("thd,hkd->thk", b["q"][216:].double(), k) * 0.1, -1)
+    want = torch.einsum("thk,hkd->thd", want, v)
+    assert (out[216:].double() - want).abs().max() < 2.0 ** -7 * 4
