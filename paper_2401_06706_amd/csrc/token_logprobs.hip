@@ -1,5 +1,6 @@
 // Log probability, rank and entropy for given tokens, with the most probable alternatives.
 #include <float.h>
+#include <type_traits>
 
 #include "attn_common.h"
 #include "vocab_row.h"
@@ -312,15 +313,21 @@ int32_t launch_token_logprobs(const mcsd_logprob_desc &d, const mcsd_logprob_buf
     p.rows = d.rows; p.R = d.R; p.V = d.V; p.n_top = d.n_top; p.row_stride = (size_t)d.row_stride;
     p.logits = b.logits; p.row_map = b.row_map; p.tokens = b.tokens; p.temperature = b.temperature;
     p.logprob = b.logprob; p.entropy = b.entropy; p.rank = b.rank; p.top_tok = b.top_tok; p.top_logprob = b.top_logprob; p.flags = b.flags;
-    // Few rows, a CU each at most: 1024 threads a row.  More: 512, four rows a CU, with fewer registers for pieces under way.
-    const bool few = d.rows <= 256;
-    if (d.dtype == MCSD_DTYPE_BF16) {
-        if (few) launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<true, 1024, 4>, dim3(d.rows), dim3(1024), stream, p);
-        else launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<true, 512, 4>, dim3(d.rows), dim3(512), stream, p);
-    } else {
-        if (few) launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<false, 1024, 8>, dim3(d.rows), dim3(1024), stream, p);
-        else launch_kernel(K_TOKEN_LOGPROBS, token_logprobs_kernel<false, 512, 4>, dim3(d.rows), dim3(512), stream, p);
-    }
+    // Threads of a row, us of a call: many rows leave a CU several at a time.  3580 rows of 1 KB with 512 threads 39.0, 128 15.4; 16 KB 39.5, 23.7; 32 KB
+    // 53.1, 40.1; 64 KB 512 threads 68, 256 61.6, 128 75.9; 2000 of 100 KB 64.5 and 59.9 with 256; 4096 of 128 KB 121.9 and 125.4; 300 of 600 KB 51, 60.
+    // Up to a row a CU: 6 rows of 4 KB with 1024 threads 8.2, 128 6.6; of 8 KB 8.3, 8.8.
+    const size_t row_bytes = (size_t)d.V * (d.dtype == MCSD_DTYPE_BF16 ? 2 : 4);
+    auto launch = [&](auto bf16_tag) {
+        constexpr bool BF16 = decltype(bf16_tag)::value;
+        auto threads = [&](auto kernel, int n) { launch_kernel(K_TOKEN_LOGPROBS, kernel, dim3(d.rows), dim3(n), stream, p); };
+        const bool many = d.rows > 256;
+        if (row_bytes <= (many ? 32 << 10 : 4 << 10)) threads(token_logprobs_kernel<BF16, 128, 4>, 128);
+        else if (many && row_bytes <= 112 << 10) threads(token_logprobs_kernel<BF16, 256, 4>, 256);
+        else if (many) threads(token_logprobs_kernel<BF16, 512, 4>, 512);
+        else threads(token_logprobs_kernel<BF16, 1024, BF16 ? 4 : 8>, 1024);        // (fewer rows: registers for more pieces under way)
+    };
+    if (d.dtype == MCSD_DTYPE_BF16) launch(std::true_type());
+    else launch(std::false_type());
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("token log probabilities launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }
     return MCSD_OK;

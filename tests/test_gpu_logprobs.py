@@ -133,3 +133,12 @@ def test_more_rows_than_workgroups(rows, V, n_top, dtype):
     row_map[7], row_map[8], row_map[9] = row_map[6], rows, -1
     tokens = torch.randint(0, V, (rows,), generator=gen(V)).tolist()
     check(logits, tokens, min(n_top, V), [0.5 + (i % 5) / 2 for i in range(rows)], row_map)
+
+
+@pytest.mark.parametrize("rows,V,dtype", [(3, 2048, torch.bfloat16), (3, 2049, torch.bfloat16), (3, 1025, torch.float32), (260, 8192, torch.float32),
+                                          (260, 8193, torch.float32), (260, 57344, torch.bfloat16), (260, 57345, torch.bfloat16), (260, 28673, torch.float32)])
+def test_threads_of_a_row(rows, V, dtype):
+    """Around the sizes where a row is taken by more threads."""
+    logits = (3 * torch.randn(rows, V, generator=gen(V))).to(dtype).to(DEV)
+    ids = list(range(0, rows, max(1, rows // 9)))
+    check(logits, [(7919 * i) % V for i in range(len(ids))] + [0] * 250, 20, row_map=ids + [ids[1]] * 250) if rows > 256 else check(logits, [0, V - 1, V // 2], 20)
