@@ -181,25 +181,26 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
 
 // Rows of K or V to their new places, 8 pieces of 16 bytes a thread: kept position, page entries, row, three trips to memory behind each
 // other, so that many rows are under way at a time.
-// In place a workgroup of 1024 takes 128 bytes of all rows of a (layer, sequence, KV head), 1024 rows a step in ascending order, everything of a step read
+// In place a workgroup takes 128 bytes of all rows of a (layer, sequence, KV head), a row for each of its threads a step in ascending order, everything of a step read
 // before any of it is written: a row moves to a lower position or stays, so that a step writes only what itself and the
 // steps before it have read.  To pages of their own, a workgroup of 256 takes a step of whole rows.  grid (heads, 2 x slices, steps or 1)
-template <bool IN_PLACE>
-__global__ __launch_bounds__(IN_PLACE ? 1024 : 256) void evict_move_kernel(EvictParams p)
+template <bool IN_PLACE, int NT>
+__global__ __launch_bounds__(NT) void evict_move_kernel(EvictParams p)
 {
     constexpr int U = 8;
     const int tid = threadIdx.x, head = blockIdx.x, g = head % p.H_kv, b = head / p.H_kv % p.B, layer = head / p.H_kv / p.B;
-    const int m = min(max(0, min(p.prefix_len[b], p.L_stride)), max(0, p.keep_len[b]));
+    const int len = max(0, min(p.prefix_len[b], p.L_stride)), keep = max(0, p.keep_len[b]), m = min(len, keep);
+    const int moved = IN_PLACE && len < keep ? 0 : m;           // (all is kept where it stands)
     const bool value = blockIdx.y & 1;
     // (to other pages: as many lanes a row as it has pieces, rounded up to a power of two)
-    const int lanes = IN_PLACE ? 8 : p.row_lanes, rows = IN_PLACE ? 128 : 256 / lanes;
+    const int lanes = IN_PLACE ? 8 : p.row_lanes, rows = NT / lanes;
     const int col = IN_PLACE ? (blockIdx.y >> 1) * 128 + 16 * (tid & 7) : 16 * (tid & (lanes - 1)), my_row = IN_PLACE ? tid >> 3 : tid / lanes;
     char *pool = (value ? p.v_pool : p.k_pool) + (size_t)layer * p.pool_layer;
     const int32_t *kept = p.kept + (size_t)head * p.L_stride;
     const int32_t *from = p.block_table + (size_t)b * p.max_pages;
     const int32_t *to = IN_PLACE ? from : p.out_table + (size_t)b * p.max_pages;
     bool bad = false;
-    for (int base = blockIdx.z * rows * U; base < m; base += gridDim.z * rows * U) {
+    for (int base = blockIdx.z * rows * U; base < moved; base += gridDim.z * rows * U) {
         u32x4 x[U];
         int i[U], src[U], dst[U];
         uint32_t on = 0;
@@ -261,11 +262,15 @@ int32_t launch_kv_evict(const mcsd_evict_desc &d, const mcsd_evict_bufs &b, cons
     else if (d.L_stride <= 512 * SEL_PER) launch_kernel(K_EVICT_SELECT, evict_select_kernel<512>, dim3(heads), dim3(512), stream, p);
     else launch_kernel(K_EVICT_SELECT, evict_select_kernel<1024>, dim3(heads), dim3(1024), stream, p);
     if (!b.out_table) {
-        launch_kernel(K_EVICT_MOVE, evict_move_kernel<true>, dim3(heads, 2 * ((p.row_bytes + 127) / 128)), dim3(1024), stream, p);
+        const dim3 grid(heads, 2 * ((p.row_bytes + 127) / 128));
+        // Steps of 1024 rows where the chip has room for them, of 256 where there are more workgroups: 2304 heads with 13 of up to 375 rows of 128 bytes kept
+        // 40.7 and 10.7 us, 512 heads with 512 of 1000 rows of 256 bytes 69 and 61; 128 heads with 2048 of 4096 60 and 91.
+        if (grid.x * grid.y >= 1024) launch_kernel(K_EVICT_MOVE, evict_move_kernel<true, 256>, grid, dim3(256), stream, p);
+        else launch_kernel(K_EVICT_MOVE, evict_move_kernel<true, 1024>, grid, dim3(1024), stream, p);
     } else {
         // (workgroups that find nothing to move are many where the caches are longer than what is kept: a few per CU go through all steps)
         const unsigned step = 8 * 256 / p.row_lanes, steps = (d.L_stride + step - 1) / step, wanted = (8192 + 2 * heads - 1) / (2 * heads);
-        launch_kernel(K_EVICT_MOVE, evict_move_kernel<false>, dim3(heads, 2, steps < wanted ? steps : wanted), dim3(256), stream, p);
+        launch_kernel(K_EVICT_MOVE, evict_move_kernel<false, 256>, dim3(heads, 2, steps < wanted ? steps : wanted), dim3(256), stream, p);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("evict launch failed: %s", hipGetErrorString(e)); return MCSD_E_HIP; }

@@ -233,3 +233,22 @@ def test_wide_lengths_beyond_the_capacity():
     want = torch.softmax(torch.einsum("thd,hkd->thk", b["q"][216:].double(), k) * 0.1, -1)
     want = torch.einsum("thk,hkd->thd", want, v)
     assert (out[216:].double() - want).abs().max() < 2.0 ** -7 * 4
+
+
+@pytest.mark.parametrize("layers,keeps", [(40, [300, 150, 7]), (40, [999, 999, 999]), (3, [300, 999, 150])])
+def test_evict_many_heads(layers, keeps):
+    """More heads than workgroups at once; sequences that keep everything among others."""
+    evict_case([700, 300, 40], keeps, 4, 9, layers, 6, 128, torch.bfloat16, 32, False, some_zero)
+
+
+def test_evict_lengths_out_of_range():
+    """prefix_len below 0 counts as 0, beyond the capacity as that, and becomes what is kept."""
+    k = torch.randn(6, 1, 32, 64, generator=gen(38)).to(torch.bfloat16).to(DEV)
+    before = k.clone()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    prefix, flags, kept = i32([-5, 2 ** 31 - 1]), i32([9, 9]), torch.full((2, 1, 64), -7, dtype=torch.int32, device=DEV)
+    sums = torch.arange(128.0, device=DEV).view(2, 1, 64).contiguous()
+    M.mcsd_kv_evict_paged(M.evict_args(k, k.clone(), i32([[0, 1], [2, 3]]), sums, prefix, i32([10, 32]), kept, flags, 0, 0))
+    torch.cuda.synchronize()
+    assert prefix.tolist() == [0, 32] and flags.tolist() == [0, 0] and (kept[0] == -7).all() and kept[1, 0, :32].tolist() == list(range(32, 64))
+    assert torch.equal(k[2], before[3]) and torch.equal(k[:2], before[:2]) and torch.equal(k[3:], before[3:])
