@@ -72,15 +72,15 @@ struct Sums {
 };
 
 // A workgroup per row, which is read once: every thread keeps running sums, its largest logit and how many tokens come before the given
-// one.  For the top, the n-th largest of 64 maxima (of every eighth thread) bounds it from below: only the few threads whose
-// largest logit reaches that bound have their pieces read again, by all threads together.
+// one.  For the top, the n-th largest of 64 maxima (of groups of threads) bounds it from below: only the few threads whose
+// largest logit reaches that bound have the piece that holds it read again, or all of theirs where another reaches it too, by all threads together.
 template <bool BF16, int NT, int AHEAD>
 __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
 {
     constexpr int W = Pieces<BF16>::W, WAVES = NT / 64;
     __shared__ float s_max[NT];
     __shared__ double s_sum[2][WAVES];
-    __shared__ int s_rank[WAVES], s_hot[NT], s_n_hot, s_n_above, s_n_equal;
+    __shared__ int s_rank[WAVES], s_hot[NT], s_one[NT], s_n_hot, s_n_one, s_n_above, s_n_equal;
     __shared__ float s_val[CAP];
     __shared__ int s_id[CAP], s_eq[CAP];
     static_assert(WAVES <= CAP, "");
@@ -101,11 +101,11 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     if ((unsigned)map >= (unsigned)p.R) return refuse(MCSD_FLAG_BAD_TREE);
     const void *row = static_cast<const char *>(p.logits) + (size_t)map * p.row_stride * (BF16 ? 2 : 4);
     const Pieces<BF16> pc(row, p.V);
-    if (tid == 0) s_n_hot = s_n_above = s_n_equal = 0;
+    if (tid == 0) s_n_hot = s_n_one = s_n_above = s_n_equal = 0;
 
     Sums sums;
-    float top = -INFINITY;
-    int before = 0;
+    float top = -INFINITY, second = -INFINITY;          // the largest logit of this thread's pieces, and of all of them but that one's
+    int before = 0, top_piece = -1;
     // AHEAD pieces are under way at a time
     int piece = tid;
     u32x4 raw[AHEAD];
@@ -119,18 +119,26 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     const int x = p.tokens[i_row];
     const bool known = (unsigned)x < (unsigned)p.V;
     const float zx = known ? logit_at<BF16>(row, x) : INFINITY;
+    const float zx_next = nextafterf(zx, INFINITY);         // z > zx is z >= zx_next
     const float T = p.temperature ? p.temperature[i_row] : 1.f, c = LOG2E_F / (T > 0.f ? T : 1.f);
     auto take_piece = [&](const float *z, int piece) {
         float most = z[0];
 #pragma unroll
         for (int i = 1; i < W; ++i) most = fmaxf(most, z[i]);
         if (most > sums.m) sums.raise(most, c);
+        second = fmaxf(second, fminf(top, most));
+        top_piece = most > top ? piece : top_piece;
         top = fmaxf(top, most);
         const int d = x - (pc.head + piece * W);
+        const float least = d >= W ? zx : zx_next;          // of the logits of this piece that come before x
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             sums.add(z[i], c);
-            before += (z[i] > zx || (z[i] == zx && i < d)) ? 1 : 0;
+            before += z[i] >= least ? 1 : 0;
+        }
+        if (d > 0 && d < W) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) before += z[i] == zx && i < d ? 1 : 0;
         }
     };
     while (asked) {
@@ -150,9 +158,10 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
         pc.load(row, piece, z);
         take_piece(z, piece);
     }
+    float edge = -INFINITY;
     auto take = [&](float z, int id) {
         if (z > sums.m) sums.raise(z, c);
-        top = fmaxf(top, z);
+        edge = fmaxf(edge, z);
         sums.add(z, c);
         before += (z > zx || (z == zx && id < x)) ? 1 : 0;
     };
@@ -161,7 +170,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     if (pc.tail + tid < p.V) take(logit_at<BF16>(row, pc.tail + tid), pc.tail + tid);
 
     // ---- the row's sums
-    s_max[tid] = top;
+    s_max[tid] = fmaxf(top, edge);
     __syncthreads();
     float group = s_max[lane];
 #pragma unroll
@@ -187,7 +196,8 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
         }
         const unsigned long long at = __ballot(ahead == p.n_top - 1);
         bound = __shfl(group, at ? __ffsll((long long)at) - 1 : 0);
-        if (top >= bound) s_hot[atomicAdd(&s_n_hot, 1)] = tid;
+        if (second >= bound) s_hot[atomicAdd(&s_n_hot, 1)] = tid;
+        else if (top >= bound && top_piece >= 0) s_one[atomicAdd(&s_n_one, 1)] = top_piece;
     }
     __syncthreads();
     s = u = 0.0;
@@ -217,9 +227,9 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
             if (at < CAP) s_eq[at] = id;
         }
     };
-    const int per = (pc.n + NT - 1) / NT, n_hot = s_n_hot;
-    for (int k = tid; k < n_hot * per; k += NT) {
-        const int piece = s_hot[k / per] + k % per * NT;
+    const int per = (pc.n + NT - 1) / NT, n_one = s_n_one, n_hot = s_n_hot;
+    for (int k = tid; k < n_one + n_hot * per; k += NT) {
+        const int j = k - n_one, piece = j < 0 ? s_one[k] : s_hot[j / per] + j % per * NT;
         if (piece >= pc.n) continue;
         float z[W];
         pc.load(row, piece, z);
