@@ -22,7 +22,7 @@ HIPCC_FLAGS = [
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 # chunk_wide_kernel holds more than 256 registers: scores and accumulators that vector instructions read stay in the half of the
-# register file that these can address, instead of being copied there (chunk of 2048 tokens on 16384 cached, 64/8 heads: see its source)
+# register file that these can address, instead of being copied there
 SOURCE_FLAGS = {"chunk_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

@@ -40,6 +40,10 @@ __device__ __forceinline__ void fetch_from(uint32_t to, const void *from)
 //     there is no other workgroup on its CU that would run meanwhile.  Items are taken
 //     as workgroups come to them, the heavy row tiles of a sequence first: dealt out beforehand, forth and back, eight prompts
 //     of 1000 to 2048 tokens, 32 heads, gave the busiest workgroup 18 % more than the mean.
+// Bound by the chip's power behind a long prefix: 2048 tokens on 16384, 64/8 heads 963 to 1050 us (1.17 to 1.27 PFLOP/s; matrix instructions busy 54 % of
+// the cycles at about 2.0 GHz), 1398 with 32 rows a wavefront in the kernel for few.  Short prompts by what an item costs beside its tiles, some 8 us: 8 of 1000 to
+// 2048 tokens, 32/32 heads 250 us (0.65 PFLOP/s).  Operands are replaced in place and the loop makes one step a turn: with two sets of operand registers, or
+// scores in accumulator registers, the compiler copied them between the halves of the register file (1060 us).
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void chunk_wide_kernel(ChunkParams p)
 {

@@ -184,6 +184,7 @@ __global__ __launch_bounds__(SEL_NT) void evict_select_kernel(EvictParams p)
 // In place a workgroup takes 128 bytes of all rows of a (layer, sequence, KV head), a row for each of its threads a step in ascending order, everything of a step read
 // before any of it is written: a row moves to a lower position or stays, so that a step writes only what itself and the
 // steps before it have read.  To pages of their own, a workgroup of 256 takes a step of whole rows.  grid (heads, 2 x slices, steps or 1)
+// Bound by memory where much is kept: 1024 rows of 256 bytes of 1024 heads, keys and values, 228 us (1.07 GB read and written, 4.7 TB/s).
 template <bool IN_PLACE, int NT>
 __global__ __launch_bounds__(NT) void evict_move_kernel(EvictParams p)
 {
@@ -258,6 +259,8 @@ int32_t launch_kv_evict(const mcsd_evict_desc &d, const mcsd_evict_bufs &b, cons
     p.sums = b.sums; p.prefix_len = b.prefix_len; p.kept = b.kept; p.keep_len = b.keep_len;
     p.block_table = kv.block_table; p.out_table = b.out_table; p.flags = b.flags;
     const unsigned heads = (unsigned)(d.n_layers * d.B * d.H_kv);
+    // us of the selection with 256, 512 and 1024 threads by capacity and with 1024: 8 heads of 1200 11.2, 11.5; 512 of 1000 to 4000 19.9, 23.3; 1024 of
+    // 2048 to 8192 36.8, 58.7
     if (d.L_stride <= 256 * SEL_PER) launch_kernel(K_EVICT_SELECT, evict_select_kernel<256>, dim3(heads), dim3(256), stream, p);
     else if (d.L_stride <= 512 * SEL_PER) launch_kernel(K_EVICT_SELECT, evict_select_kernel<512>, dim3(heads), dim3(512), stream, p);
     else launch_kernel(K_EVICT_SELECT, evict_select_kernel<1024>, dim3(heads), dim3(1024), stream, p);
