@@ -510,7 +510,7 @@ int32_t mcsd_kv_store_paged(const mcsd_rows_desc *desc, const mcsd_store_bufs *b
 typedef struct {
     uint32_t struct_size;
     int32_t B;              /* sequences, <= 65535 */
-    int32_t T;              /* rows of q, out and lse, >= 0; T H_q < 2^30 */
+    int32_t T;              /* rows of q, out and lse, >= 0; T H_q < 2^30 (a launch's workgroups are limited: T H_q / 32 + min(T, B) H_kv <= 2^23 always fits) */
     int32_t H_q, H_kv;      /* query / KV heads, H_q % H_kv == 0, H_kv <= 65535 */
     int32_t d;              /* head dim <= MCSD_MAX_HEAD_DIM; d * element size a multiple of 16 bytes */
     int32_t dtype;          /* MCSD_DTYPE_* of q, the pools and out */
@@ -601,7 +601,7 @@ int32_t mcsd_kv_evict_paged(const mcsd_evict_desc *desc, const mcsd_evict_bufs *
  */
 typedef struct {
     uint32_t struct_size;
-    int32_t rows;           /* rows asked for, >= 0 */
+    int32_t rows;           /* rows asked for, 0 .. 2^22 */
     int32_t R;              /* rows of logits, >= 1 */
     int32_t V;              /* vocabulary, 1 .. 2^30 */
     int32_t dtype;          /* MCSD_DTYPE_* of logits */

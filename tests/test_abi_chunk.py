@@ -162,3 +162,14 @@ def test_binding_refuses_what_is_not_on_a_gpu():
         M.chunk_attn_args(t.bfloat16(), pool, pool, i32(1, 2), i32(2), i32(1), t, 0.1, 64)
     with pytest.raises(ValueError):
         M.logprob_desc(torch.zeros(9, 2).t(), i32(2))
+
+
+def test_chunk_sizes_that_always_fit(lib):
+    """T H_q / 32 + min(T, B) H_kv up to 2^23 has a plan, whatever the type, the head dimension and the capacity; far beyond there may be none."""
+    for B, T, H_q, H_kv in [(1, 2 ** 23, 31, 31), (65535, 65535, 64, 64), (2 ** 15, 2 ** 15, 248, 248), (8, 2 ** 18, 1016, 8), (4, 2 ** 13, 32000, 1), (1, 1, 65535, 65535), (65535, 2 ** 20, 120, 60)]:
+        assert T * H_q / 32 + min(T, B) * H_kv <= 2 ** 23 and T * H_q < 2 ** 30
+        for d in (64, 128, 256):
+            for dtype in (M.DTYPE_FP32, M.DTYPE_BF16):
+                for cap in (65536, 2 ** 22):
+                    assert M.mcsd_chunk_workspace_bytes(make(M.ChunkDesc, CHUNK, dict(B=B, T=T, H_q=H_q, H_kv=H_kv, d=d, dtype=dtype, L_stride=cap, q_stride=H_q * d))) > 0
+    assert M.mcsd_chunk_workspace_bytes(make(M.ChunkDesc, CHUNK, dict(B=65535, T=17000, H_q=60000, H_kv=60000, q_stride=60000 * 128))) == 0
