@@ -627,7 +627,7 @@ typedef struct {
     size_t workspace_bytes;
 } mcsd_logprob_bufs;
 
-size_t mcsd_logprob_workspace_bytes(const mcsd_logprob_desc *desc);     /* 0 on a bad descriptor */
+size_t mcsd_logprob_workspace_bytes(const mcsd_logprob_desc *desc);     /* 0 on a bad descriptor, and where none is needed (all but few long rows) */
 int32_t mcsd_token_logprobs(const mcsd_logprob_desc *desc, const mcsd_logprob_bufs *bufs, void *stream);
 
 /* ------------------------------------------------------- pages from lengths

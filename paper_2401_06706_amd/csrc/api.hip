@@ -35,7 +35,7 @@ const char *const g_names[K_COUNT] = {"tree_attn_mfma", "tree_attn_generic", "tr
                                       "verify_rows", "walk", "draft_rows", "tree_build", "kv_copy", "kv_finish",
                                       "kv_store_fourbit", "kv_load_fourbit", "attn_fourbit", "attn_fourbit_combine",
                                       "page_assign", "page_slots", "logits_rules",
-                                      "kv_store_paged", "chunk_attn", "chunk_merge", "weight_sums", "evict_select", "evict_move", "token_logprobs", "chunk_wide"};
+                                      "kv_store_paged", "chunk_attn", "chunk_merge", "weight_sums", "evict_select", "evict_move", "token_logprobs", "chunk_wide", "logprobs_merge"};
 }  // namespace
 
 bool timing_new_events(hipEvent_t *start, hipEvent_t *stop)

@@ -12,7 +12,7 @@ namespace mcsd {
 // Kernel ids for the optional per-kernel event timing.
 enum KernelId { K_ATTN_MFMA = 0, K_ATTN_GENERIC = 1, K_ATTN_COMBINE = 2, K_VERIFY_ROWS = 3, K_WALK = 4, K_DRAFT_ROWS = 5, K_TREE_BUILD = 6, K_KV_COPY = 7, K_KV_FINISH = 8, K_KV_STORE = 9, K_KV_LOAD = 10,
                 K_ATTN_FOURBIT = 11, K_ATTN_FOURBIT_COMBINE = 12, K_PAGE_ASSIGN = 13, K_PAGE_SLOTS = 14, K_LOGITS_RULES = 15,
-                K_KV_STORE_PAGED = 16, K_CHUNK_ATTN = 17, K_CHUNK_MERGE = 18, K_WEIGHT_SUMS = 19, K_EVICT_SELECT = 20, K_EVICT_MOVE = 21, K_TOKEN_LOGPROBS = 22, K_CHUNK_WIDE = 23, K_COUNT = 24 };
+                K_KV_STORE_PAGED = 16, K_CHUNK_ATTN = 17, K_CHUNK_MERGE = 18, K_WEIGHT_SUMS = 19, K_EVICT_SELECT = 20, K_EVICT_MOVE = 21, K_TOKEN_LOGPROBS = 22, K_CHUNK_WIDE = 23, K_LOGPROBS_MERGE = 24, K_COUNT = 25 };
 
 void set_error(const char *fmt, ...);
 

@@ -173,3 +173,15 @@ def test_chunk_sizes_that_always_fit(lib):
                 for cap in (65536, 2 ** 22):
                     assert M.mcsd_chunk_workspace_bytes(make(M.ChunkDesc, CHUNK, dict(B=B, T=T, H_q=H_q, H_kv=H_kv, d=d, dtype=dtype, L_stride=cap, q_stride=H_q * d))) > 0
     assert M.mcsd_chunk_workspace_bytes(make(M.ChunkDesc, CHUNK, dict(B=65535, T=17000, H_q=60000, H_kv=60000, q_stride=60000 * 128))) == 0
+
+
+def test_logprob_workspace(lib):
+    """Few long rows need one; it is asked for and checked."""
+    desc = dict(rows=2, R=4, V=262144, dtype=M.DTYPE_FP32, n_top=5, row_stride=262144)
+    need = M.mcsd_logprob_workspace_bytes(make(M.LogprobDesc, desc, {}))
+    assert need > 0
+    for kw in (dict(rows=129, R=200), dict(V=51199), dict(dtype=M.DTYPE_BF16, V=102399), dict(rows=0)):
+        assert M.mcsd_logprob_workspace_bytes(make(M.LogprobDesc, desc, kw)) == 0, kw
+    bufs = dict(logits=PTR, tokens=PTR, logprob=PTR, top_tok=PTR, top_logprob=PTR, flags=PTR, workspace=PTR, workspace_bytes=need)
+    for kw in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=PTR + 128)):
+        assert lib.mcsd_token_logprobs(C.byref(make(M.LogprobDesc, desc, {})), C.byref(make(M.LogprobBufs, bufs, kw)), None) == -5, kw

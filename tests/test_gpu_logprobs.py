@@ -142,3 +142,41 @@ def test_threads_of_a_row(rows, V, dtype):
     logits = (3 * torch.randn(rows, V, generator=gen(V))).to(dtype).to(DEV)
     ids = list(range(0, rows, max(1, rows // 9)))
     check(logits, [(7919 * i) % V for i in range(len(ids))] + [0] * 250, 20, row_map=ids + [ids[1]] * 250) if rows > 256 else check(logits, [0, V - 1, V // 2], 20)
+
+
+def test_temperatures_at_the_ends():
+    """The smallest numbers leave the largest logit alone, the largest make all logits equal; 0 reads as 1."""
+    logits = torch.randn(5, 300, generator=gen(3)).to(DEV)
+    best = logits.argmax(1).tolist()
+    got = run(logits, best, 2, [1e-45, 1e-38, 3e38, 0.0, 1.0], [0, 1, 2, 3, 3])
+    assert got["flags"].tolist() == [0] * 5 and got["rank"].tolist()[:4] == [0] * 4
+    for i in (0, 1):
+        assert float(got["logprob"][i]) == 0.0 and float(got["entropy"][i]) == 0.0
+        assert int(got["top_tok"][i, 0]) == best[i] and float(got["top_logprob"][i, 0]) == 0.0 and float(got["top_logprob"][i, 1]) < -1e30
+    bound = R.logprob_bound(300, math.log(300), 0)
+    assert abs(float(got["logprob"][2]) + math.log(300)) <= bound and abs(float(got["entropy"][2]) - math.log(300)) <= 2 * bound * (1 + math.log(300))
+    for k in ("entropy", "top_logprob"):
+        assert torch.equal(got[k][3], got[k][4])
+
+
+@pytest.mark.parametrize("V,dtype,shift", [(52001, torch.float32, 0), (60001, torch.float32, 3), (110003, torch.bfloat16, 5), (262144, torch.float32, 0)])
+def test_rows_in_parts(V, dtype, shift):
+    """Long rows that several workgroups share: ties across their borders, parts that a mask leaves empty or nearly so, tokens of every part, rows that start
+    anywhere, what is no number in one part alone."""
+    inf = math.inf
+    rows = [torch.randn(V, generator=gen(1)), torch.zeros(V), torch.full((V,), -inf), torch.randint(0, 3, (V,), generator=gen(2)).float(),
+            torch.full((V,), torch.finfo(dtype).min), torch.full((V,), -inf), torch.full((V,), -inf), torch.full((V,), -inf), torch.randn(V, generator=gen(3)),
+            torch.randn(V, generator=gen(4)), torch.full((V,), -inf), torch.where(torch.rand(V, generator=gen(5)) < 0.001, torch.randn(V, generator=gen(6)), torch.tensor(-inf))]
+    rows[2][V // 2] = 1.0                               # one token
+    rows[5][:30] = torch.randn(30, generator=gen(7))    # the first part alone
+    rows[6][V - 30:] = 0.5                              # the last
+    rows[7][::V // 25] = 2.0                            # a few of each, all alike
+    rows[8][V - 3], rows[9][V // 3] = float("nan"), inf
+    flat = torch.full((len(rows) * (V + 7) + shift,), float("nan"))
+    view = flat[shift:].view(len(rows), V + 7)[:, :V]
+    view.copy_(torch.stack(rows))
+    flat = flat.to(dtype).to(DEV)
+    logits = flat[shift:].view(len(rows), V + 7)[:, :V]
+    for n_top in (0, 1, 20, 64):
+        check(logits, [0, V - 1, V // 2, V // 3, 7, 29, V - 1, V // 25, 5, 5, 5, V // 2], n_top)
+    check(logits, [(V * i) // 9 for i in range(9)] + [V, -1, 3, 3], 5, [0.3 + i / 4 for i in range(13)], [0] * 11 + [len(rows), -1])
