@@ -132,54 +132,80 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     // AHEAD pieces are under way at a time
     int piece = tid;
     u32x4 raw[AHEAD];
-    auto ask = [&]() {
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) raw[k] = pc.raw(row, piece + k * NT);
+    auto ask = [&](int k, int piece) {
+        if (piece < pc.n) raw[k] = pc.raw(row, piece);
     };
-    auto whole = [&]() { return piece + (AHEAD - 1) * NT < pc.n; };
-    bool asked = whole();
-    if (asked) ask();           // (ahead of the token's logit)
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) raw[k] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) ask(k, piece + k * NT);         // (ahead of the token's logit)
     const int token = p.tokens[i_row], x = token - from;            // (in terms of the part)
     const bool known = (unsigned)token < (unsigned)p.V;
     const float zx = known ? logit_at<BF16>(whole_row, token) : INFINITY;
     const float zx_next = nextafterf(zx, INFINITY);         // z > zx is z >= zx_next
     const float T = p.temperature ? p.temperature[i_row] : 1.f, c = scale_of(T);
-    auto take_piece = [&](const float *z, int piece) {
+    auto most_of = [&](const float *z) {
         float most = z[0];
 #pragma unroll
         for (int i = 1; i < W; ++i) most = fmaxf(most, z[i]);
-        if (most > sums.m) sums.raise(most, c);
+        return most;
+    };
+    auto keep = [&](float most, int piece) {
         second = fmaxf(second, fminf(top, most));
         top_piece = most > top ? piece : top_piece;
         top = fmaxf(top, most);
+    };
+    // of a piece the logits from `least` on come before x; beside that, in the piece that holds x, those equal to it that stand before it
+    auto least_of = [&](int piece) { return x - (pc.head + piece * W) >= W ? zx : zx_next; };
+    auto own_piece = [&](const float *z, int piece) {
         const int d = x - (pc.head + piece * W);
-        const float least = d >= W ? zx : zx_next;          // of the logits of this piece that come before x
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            sums.add(z[i], c);
-            before += z[i] >= least ? 1 : 0;
-        }
         if (d > 0 && d < W) {
 #pragma unroll
             for (int i = 0; i < W; ++i) before += z[i] == zx && i < d ? 1 : 0;
         }
     };
-    while (asked) {
+    // while all lanes have AHEAD pieces: the largest of them all first, so that the sums are raised once; tokens that come before x are counted for the wavefront
+    int before_all = 0;
+    for (int first = __builtin_amdgcn_readfirstlane(piece); first + 63 + (AHEAD - 1) * NT < pc.n; first += AHEAD * NT) {
+        float z[AHEAD][W], most[AHEAD], all = -INFINITY;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            float z[W];
-            pc.values(raw[k], z);
-            // (the place of a piece that is taken is free for one of the next)
-            raw[k] = piece + (AHEAD + k) * NT < pc.n ? pc.raw(row, piece + (AHEAD + k) * NT) : raw[k];
-            take_piece(z, piece + k * NT);
+            pc.values(raw[k], z[k]);
+            ask(k, piece + (AHEAD + k) * NT);       // (the place of a piece that is taken is free for one of the next)
+            most[k] = most_of(z[k]);
+            all = fmaxf(all, most[k]);
+        }
+        if (all > sums.m) sums.raise(all, c);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int at = piece + k * NT;
+            const float least = least_of(at);
+            keep(most[k], at);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                sums.add(z[k][i], c);
+                before_all += __popcll(__ballot(z[k][i] >= least));
+            }
+            own_piece(z[k], at);
         }
         piece += AHEAD * NT;
-        asked = whole();
     }
-    for (; piece < pc.n; piece += NT) {
-        float z[W];
-        pc.load(row, piece, z);
-        take_piece(z, piece);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+        const int at = piece + k * NT;
+        if (at < pc.n) {
+            float z[W];
+            pc.values(raw[k], z);
+            const float most = most_of(z), least = least_of(at);
+            if (most > sums.m) sums.raise(most, c);
+            keep(most, at);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                sums.add(z[i], c);
+                before += z[i] >= least ? 1 : 0;
+            }
+            own_piece(z, at);
+        }
     }
     float edge = -INFINITY;
     auto take = [&](float z, int id) {
@@ -207,7 +233,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(LogprobParams p)
     before += __builtin_amdgcn_update_dpp(0, before, 0x140, 0xf, 0xf, false);
     before += __builtin_amdgcn_update_dpp(0, before, 0x142, 0xa, 0xf, false);
     before += __builtin_amdgcn_update_dpp(0, before, 0x143, 0xc, 0xf, false);
-    if (lane == 63) { s_sum[0][wave] = s; s_sum[1][wave] = u; s_rank[wave] = before; }
+    if (lane == 63) { s_sum[0][wave] = s; s_sum[1][wave] = u; s_rank[wave] = before + before_all; }
     // ---- the bound of the top: n_top-th largest of the 64 maxima
     float bound = INFINITY;
     if (p.n_top) {
