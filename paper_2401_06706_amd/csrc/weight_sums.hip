@@ -55,8 +55,7 @@ __global__ __launch_bounds__(256, DP * (F32 ? 4 : 2) <= 256 ? 3 : 1) void weight
             }
         }
         const int r = row_first + tile * KT + l32;
-        // (a row past the last one gives nothing)
-        lse_of[st] = INFINITY;
+        lse_of[st] = 0.f;
         if (r < M) {
             const int token = by_group(p, r);
             lse_of[st] = sp.lse[(size_t)(sq.s0 + token) * p.H_q + g * p.G + r - token * p.G] * LOG2E_F;
@@ -104,8 +103,10 @@ __global__ __launch_bounds__(256, DP * (F32 ? 4 : 2) <= 256 ? 3 : 1) void weight
                     }
                 }
                 const int row0 = row_first + tile * KT;
-                if (min(sq.L + by_group(p, row0), sq.keys - 1) < wkey + KT - 1) {       // some row does not see some of these keys
-                    const int seen = min(sq.L + by_group(p, min(row0 + l32, M - 1)), sq.keys - 1) - wkey - 4 * h;
+                // Some row does not see some of these keys, or stands past the last one: that sees none (its zeros times an infinity in a key would be
+                // no number).
+                if (min(sq.L + by_group(p, row0), sq.keys - 1) < wkey + KT - 1 || row0 + KT > M) {
+                    const int seen = row0 + l32 < M ? min(sq.L + by_group(p, row0 + l32), sq.keys - 1) - wkey - 4 * h : -1;
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (key_of_score(i) <= seen) part[i] += fast_exp2(fmaf(s[i], p.scale_log2, -lse));
