@@ -595,7 +595,8 @@ int32_t mcsd_kv_evict_paged(const mcsd_evict_desc *desc, const mcsd_evict_bufs *
  *   logprob[i] = z(x) - lse,  lse = ln sum_y exp z(y)        entropy[i] = -sum_y p(y) ln p(y),  p = exp(z - lse)
  *   rank[i] = tokens y that come before x: z(y) > z(x), or z(y) = z(x) and y < x  (0: x is the most probable)
  *   top_tok[i][0 .. n_top-1], top_logprob: the first n_top tokens of that order and their log probabilities
- * Tokens at -infinity (masked) have probability 0, log probability -infinity and come last, by id.  The order is that of the logits as they are, before the division.
+ * Tokens at -infinity (masked) have probability 0, log probability -infinity and come last, by id, at an infinite T too, where all others
+ * are alike.  The order is that of the logits as they are, before the division.
  * x outside [0, V): logprob NaN, rank -1, MCSD_FLAG_BAD_TOKEN, the rest as usual.  A row_map entry outside [0, R): NaN, -1, MCSD_FLAG_BAD_TREE.  A
  * row that holds NaN or +infinity, or nothing but -infinity: NaN, -1, MCSD_FLAG_NONFINITE.  Sums are taken in fp32 per lane and in fp64 across.
  */

@@ -32,8 +32,8 @@ constexpr int MAX_PARTS = 16;
 constexpr int CAP = 1024;         // candidates for the top that fit; those equal to the smallest of them
 constexpr float LOWEST = -200.0f;           // 2^-200 is 0: a bound that keeps 0 * infinity out of the entropy
 
-// log2(e) / T; finite, so that 0 times it is 0
-__device__ __forceinline__ float scale_of(float T) { return fminf(LOG2E_F / (T > 0.f ? T : 1.f), FLT_MAX); }
+// log2(e) / T; finite, so that 0 times it is 0, and not 0, so that -infinity times it is -infinity (an infinite temperature: what is not masked is alike)
+__device__ __forceinline__ float scale_of(float T) { return fmaxf(fminf(LOG2E_F / (T > 0.f ? T : 1.f), FLT_MAX), FLT_TRUE_MIN); }
 
 template <bool BF16>
 __device__ __forceinline__ float logit_at(const void *row, int i)
