@@ -74,7 +74,7 @@ def test_the_device_decides(news, wide):
     check(batch(53, [3000] * 5 + [4000], news, 32, 16, 64), wide)
 
 
-@pytest.mark.parametrize("heads,L,n,capacity", [(128, 200, 312, 416), (32, 2000, 700, 2304), (256, 300, 300, 320)])
+@pytest.mark.parametrize("heads,L,n,capacity", [(128, 200, 312, 416), (32, 2000, 700, 2304), (256, 300, 300, 576)])
 def test_lengths_beyond_the_capacity(heads, L, n, capacity):
     """Keys in one piece and cut; rows past the capacity see what lies below it."""
     b = batch(54, [L], [n], heads, heads)
