@@ -531,7 +531,7 @@ typedef struct {
     size_t workspace_bytes;
 } mcsd_chunk_bufs;
 
-size_t mcsd_chunk_workspace_bytes(const mcsd_chunk_desc *desc);     /* 0 on a bad descriptor */
+size_t mcsd_chunk_workspace_bytes(const mcsd_chunk_desc *desc);     /* 0 on a bad descriptor, and where none is needed (short capacities, few rows) */
 int32_t mcsd_chunk_attn_paged(const mcsd_chunk_desc *desc, const mcsd_chunk_bufs *bufs, const mcsd_paged_kv *paged, void *stream);
 
 /* ------------------------------------------- eviction by attention weight

@@ -115,7 +115,7 @@ __device__ __forceinline__ float wave_max(float v) { return wave_reduce<true>(v)
 // Every workgroup works out the same list, a sequence a lane; the length of segments of many rows takes longer and is left by the kernel for few
 // (worked out by all workgroups: 10 to 40 us a launch).  Partial results are numbered in blocks of 32 rows, row tile by row tile, segment by segment.
 // MANY: us with the kernel for many rows and with that for few: 32/8 heads, 80 rows of 32 sequences on 4000 tokens 151, 139, of 4 on 8000 58, 63; 128 rows 150, 153
-// and 59, 71; 192 rows of 32 162, 217.
+// and 59, 71; 192 rows of 32 162, 217.  (Between 64 and 128 rows the border loses 8 % with many sequences and gains as much with few.)
 constexpr int ROWS_SPLIT = 32, ROWS_FEW = 128, ROWS_MANY = 256, MANY = 64, NEVER_MANY = 0x7fffffff;
 // Key tiles of many rows a workgroup at once, below which they do not pay for a kernel of their own (each item 8 tiles' time, the launch 4 us):
 // us with the kernel for many rows and without it, work in tiles: one prompt of 512 tokens, 32/8 heads (4) 36.8, 30.2; 8 of 128 to 256, 32/32

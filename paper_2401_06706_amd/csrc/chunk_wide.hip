@@ -28,7 +28,8 @@ __device__ __forceinline__ void fetch_from(uint32_t to, const void *from)
 
 // A workgroup of four wavefronts, one per SIMD, owns 256 rows of a (sequence, KV head) and a segment of its key tiles; a wavefront owns
 // 64 rows in two blocks of 32, A and B, and shares every K and V operand between them.  S^T = K Q^T and O^T += V^T P^T
-// with v_mfma_f32_32x32x16_bf16 as in tree attention (a weight never leaves its lane).
+// with v_mfma_f32_32x32x16_bf16 as in tree attention (a weight never leaves its lane).  Weights are rounded to one bf16 term for PV, their sum is taken of the
+// unrounded ones: a second term would be 8 more matrix instructions on the 16 of a block and tile, and these bind.  (see launch_shape for what either costs)
 //   - One block's softmax runs beside the other's matrix instructions, tile after tile:
 //        phase A(t): weights of A from S_A(t)     beside   O_B += V(t-1) P_B(t-1),  S_B(t) = K(t) Q_B
 //        phase B(t): weights of B from S_B(t)     beside   O_A += V(t) P_A(t),      S_A(t+1) = K(t+1) Q_A
@@ -42,7 +43,7 @@ __device__ __forceinline__ void fetch_from(uint32_t to, const void *from)
 //     of 1000 to 2048 tokens, 32 heads, gave the busiest workgroup 18 % more than the mean.
 // Bound by the chip's power behind a long prefix: 2048 tokens on 16384, 64/8 heads 963 to 1050 us (1.17 to 1.27 PFLOP/s; matrix instructions busy 54 % of
 // the cycles at about 2.0 GHz), 1398 with 32 rows a wavefront in the kernel for few.  Short prompts by what an item costs beside its tiles, some 8 us: 8 of 1000 to
-// 2048 tokens, 32/32 heads 250 us (0.65 PFLOP/s).  Operands are replaced in place and the loop makes one step a turn: with two sets of operand registers, or
+// 2048 tokens, 32/32 heads 261 to 309 us, 278 on average (0.58 PFLOP/s).  Operands are replaced in place and the loop makes one step a turn: with two sets of operand registers, or
 // scores in accumulator registers, the compiler copied them between the halves of the register file (1060 us).
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void chunk_wide_kernel(ChunkParams p)

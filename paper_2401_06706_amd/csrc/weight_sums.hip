@@ -12,7 +12,9 @@ struct SumsParams { ChunkParams c; const float *lse; float *sums; int last_rows,
 // added to the whole at a time: over n tiles the error stays below (64 + n / 64) 2^-24 of the sum.
 // Few rows: a workgroup goes through `blocks` of 128 positions, the next one's keys asked for ahead, so that lengths, table and rows are
 // waited for once.  Bound by the reading of the keys: 32 sequences of 100 to 8000 tokens, 32/8 heads, d = 128, one new token 70 us (278 MB, 4.0 TB/s);
-// many rows by launch, trips to memory, exponentials and products in turn: 64 tokens on 4 x 3000 to 8000 30 us (1.1 times 10^10 products' operations).
+// many rows by launch, trips to memory, exponentials and products in turn: 64 tokens on 4 x 3000 to 8000 29 to 33 us (1.1 times 10^10 products' operations), all rows
+// of 8 prompts of 1000 to 2048 244 us.  Workgroups are those of the capacity, and find nothing behind a sequence's end: the first of these with room for 8000, 32768 and
+// 131072 tokens a sequence 69, 70, 77 us.
 template <int DP, bool F32, bool MULTI>
 __global__ __launch_bounds__(256, DP * (F32 ? 4 : 2) <= 256 ? 3 : 1) void weight_sums_kernel(SumsParams sp)
 {
@@ -195,7 +197,8 @@ int32_t launch_weight_sums(const mcsd_chunk_desc &d, const mcsd_sums_bufs &b, co
     sp.c.q = b.q; sp.c.k_pool = b.k_pool; sp.c.chunk_start = b.chunk_start; sp.c.prefix_len = b.prefix_len;
     sp.lse = b.lse; sp.sums = b.sums; sp.last_rows = b.last_rows;
     // Several blocks a workgroup where sequences bring up to two tiles of rows on average and workgroups are plenty, us with them and without: 32 sequences of
-    // 100 to 8000 tokens, one new, 32/8 heads 73.3, 75.0; 16 of 2000 to 8000 46.2, 49.2; 8 new tokens on 32 x 8000 125, 138; but 64 of 100 to 4000 78.3, 75.9.
+    // 100 to 8000 tokens, one new, 32/8 heads 73.3, 75.0; 16 of 2000 to 8000 46.2, 49.2; 8 new tokens on 32 x 8000 125, 138; 64 of 100 to 4000, which the rule
+    // takes too, 78.3, 75.9.
     const long rows = (long)d.T * (d.H_q / d.H_kv), groups = (long)d.H_kv * d.B * ((d.L_stride + 127) / 128);
     sp.blocks = rows <= 64L * d.B ? (groups >= 8192 ? 4 : groups >= 4096 ? 2 : 1) : 1;
     if (d.dtype == MCSD_DTYPE_FP32) sp.blocks > 1 ? launch_type<true, true>(sp, stream) : launch_type<true, false>(sp, stream);
